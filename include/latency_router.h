@@ -15,6 +15,8 @@
  * limits with preemption (lr_set_kv_limits), least-squares calibration of the
  * batch-time coefficients (lr_calibrate), and the baseline routers with
  * OnTimeUtility (lr_route_baseline, lr_on_time_utility).
+ * And the engine's side of a batch, whose times the batch model describes: a paged KV
+ * cache, quantised as it is written, and the attention that reads it (lr_cache_*).
  *
  * Conventions for every call:
  *  - All integers are int32 unless stated; all arrays are dense, row-major.
@@ -389,6 +391,112 @@ LR_API int lr_route_baseline(lr_ctx *ctx, int32_t policy, int32_t Q, const int32
  * in a fixed order (the same result on every run). */
 LR_API int lr_on_time_utility(lr_ctx *ctx, int32_t Q, const float *util, const float *ttft, const float *tau,
                               const float *delay, double *out, void *cuda_stream);
+
+/* ---- The engine's side of a batch: a paged KV cache and the attention over it ----
+ *
+ * The simulation counts what a serving engine does per token batch: the batch's tokens join
+ * a paged KV cache (Sec. 2; App. F) and attend over it, which is what the decode-context and
+ * prefill-attention terms of Eq. 9 cost.  These calls do it: a program that runs the
+ * scheduler's batches with them can log their times for lr_calibrate.
+ *
+ * A cache is num_blocks blocks of block_size tokens; a token has one K and one V vector of
+ * head_dim numbers per KV head.  Query head h reads KV head h / (num_q_heads / num_kv_heads).
+ * Token p of a sequence lives in block table[p / block_size] of the sequence's row of the
+ * block table, place p % block_size.  The memory is the caller's, with any strides.
+ *
+ * The calls take an lr_cache, need no lr_ctx, and follow the conventions above (device
+ * pointers, asynchronous, ordered by the caller).  Device-found errors are recorded in the
+ * cache's status word (lr_cache_status). */
+
+enum lr_dtype { LR_BF16 = 0, LR_FP16 = 1, LR_FP32 = 2 };
+
+/* How the cache holds a vector x of head_dim numbers (one token, one KV head, K or V):
+ *  16 bits: as it is, in the cache's dtype.
+ *  E4M3, INT8: 8-bit codes and one fp32 scale a vector.  With a = max(max|x|, 2^-100) and
+ *    top = 448 or 127, in fp32: scale = a / top, code = round(x * (top / a)), to the
+ *    nearest e4m3 number or integer, ties to even.  It stands for code * scale.  A vector with an
+ *    infinity or a NaN has that for its scale, and reads back as NaN throughout. */
+enum lr_cache_format { LR_CACHE_16BIT = 0, LR_CACHE_E4M3 = 1, LR_CACHE_INT8 = 2 };
+
+typedef struct {
+    int32_t num_q_heads;      /* a multiple of num_kv_heads, at most 1024 */
+    int32_t num_kv_heads;     /* >= 1 */
+    int32_t head_dim;         /* a multiple of 16 in [16, 128] */
+    int32_t dtype;            /* enum lr_dtype of the queries, new K and V, outputs: LR_BF16 or LR_FP16 */
+    int32_t format;           /* enum lr_cache_format */
+    int32_t block_size;       /* tokens a block, in [1, 4096] */
+    int32_t num_blocks;       /* >= 1 */
+    int32_t max_seqs;         /* largest number of sequences of a batch, in [1, 65536] */
+    void *k, *v;              /* DEVICE, 16-byte aligned: element d of (block, token, head) at
+                                 block * block_stride + token * token_stride + head * head_stride + d */
+    float *k_scale, *v_scale; /* DEVICE: at block * scale_block_stride + token * scale_token_stride +
+                                 head * scale_head_stride; ignored for LR_CACHE_16BIT */
+    int64_t block_stride, token_stride, head_stride; /* in elements, each a multiple of 16 bytes, >= 0 */
+    int64_t scale_block_stride, scale_token_stride, scale_head_stride; /* in floats, >= 0 */
+} lr_cache_config;
+
+/* One token batch: sequence s brings its last q_start[s+1] - q_start[s] tokens of the kv_len[s]
+ * that it has with them.  DEVICE arrays. */
+typedef struct {
+    int32_t num_seqs;           /* >= 0 */
+    int32_t max_q;              /* no sequence brings more tokens than this; >= 1 */
+    const int32_t *q_start;     /* [num_seqs + 1], from 0, non-decreasing: sequence s's rows of the
+                                   token arrays are q_start[s] .. q_start[s+1] - 1 */
+    const int32_t *kv_len;      /* [num_seqs] tokens of the sequence, the batch's own among them, at most 2^30 */
+    const int32_t *block_table; /* [num_seqs][>= max_blocks], row stride table_stride: blocks in order of position */
+    int64_t table_stride;
+    int32_t max_blocks;         /* entries of a row that may be read; those past a sequence's length are not */
+} lr_cache_batch;
+
+typedef struct lr_cache lr_cache;  /* opaque, owned by the library */
+
+/* Create a cache handle on the current CUDA device over the caller's memory (nothing of it is read
+ * or written here) and allocate the workspace the calls need.  *out is set on LR_OK. */
+LR_API int lr_cache_create(const lr_cache_config *cfg, lr_cache **out);
+
+/* Free everything lr_cache_create allocated.  Synchronizes the device first.  NULL is a no-op. */
+LR_API int lr_cache_destroy(lr_cache *c);
+
+/* Store the K and V of the batch's tokens (rows [0, T) of k and v; rows from q_start[num_seqs] on
+ * belong to no sequence and are ignored), converting to the cache's format as it is written.
+ * k, v: element d of (row, head) at row * token_stride + head * head_stride + d (elements; both
+ * strides multiples of 16 bytes, base 16-byte aligned; the same strides for k and v).
+ * Device errors: a token without a place in the cache (a sequence with more new tokens than
+ * kv_len, a position past max_blocks, a block outside [0, num_blocks), a q_start out of order) is not
+ * stored and records LR_EINVAL. */
+LR_API int lr_cache_write(lr_cache *c, const lr_cache_batch *b, int32_t T, const void *k, const void *v,
+                          int64_t token_stride, int64_t head_stride, void *cuda_stream);
+
+/* Read the batch's tokens back as values: rows as for lr_cache_write (with q_start the running sum of
+ * kv_len, whole sequences).  out_dtype: the cache's dtype or LR_FP32; 16-bit values are the
+ * fp32 product code * scale rounded to nearest.  k_out, v_out: [T][num_kv_heads][head_dim], dense, 16-byte
+ * aligned.  A token without a place reads as NaN and records LR_EINVAL; rows of no sequence are
+ * not written. */
+LR_API int lr_cache_read(lr_cache *c, const lr_cache_batch *b, int32_t T, int32_t out_dtype, void *k_out,
+                         void *v_out, void *cuda_stream);
+
+/* Attention of the batch's tokens over the cache, in which their own K and V stand already.
+ * The token at position i of its sequence (the first new one at kv_len - its number of new tokens)
+ * sees position j <= i, and with window > 0 only the last `window` of those (j > i - window) and
+ * the first `sinks` of the sequence (j < sinks).  For each query head,
+ *   out = sum_j softmax_j(scale * q . k_j) v_j   and   lse = ln sum_j exp(scale * q . k_j)
+ * over the visible j; a row that sees nothing (a negative position) gives 0 and -inf.  Products of
+ * 16-bit numbers are summed in fp32; the softmax weights are rounded to the cache's dtype for the
+ * second product (e4m3 and int8 codes are exact in it, the scales are applied in fp32).
+ * q, out: element d of (row, head) at row * token_stride + head * head_stride + d, aligned as for
+ * lr_cache_write.  lse_out: [T][num_q_heads] fp32 or NULL.  scale: finite, > 0.  window in
+ * [0, 2^30] (0: no window), sinks in [0, 2^30].  Rows of no sequence are not written.
+ * Device errors, each LR_EINVAL: a sequence whose q_start, number of new tokens (over max_q) or
+ * kv_len (over max_blocks * block_size) is out of range is left out, its rows not written;
+ * a block outside [0, num_blocks) makes the rows that would read it NaN.
+ * What a row may not see does not reach it, whatever it holds. */
+LR_API int lr_cache_attend(lr_cache *c, const lr_cache_batch *b, int32_t T, const void *q, int64_t q_token_stride,
+                           int64_t q_head_stride, float scale, int32_t window, int32_t sinks, void *out,
+                           int64_t out_token_stride, int64_t out_head_stride, float *lse_out, void *cuda_stream);
+
+/* As lr_status and lr_last_error, for a cache. */
+LR_API int lr_cache_status(lr_cache *c, void *cuda_stream);
+LR_API const char *lr_cache_last_error(const lr_cache *c);
 
 #ifdef __cplusplus
 }

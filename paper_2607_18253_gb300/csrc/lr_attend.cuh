@@ -1,0 +1,264 @@
+// What the attention kernels share: which cached tokens a tile of rows sees, the walk over a
+// batch's tiles, conversions of 8-bit codes, and the small PTX wrappers.
+#pragma once
+
+#include "lr_cache.cuh"
+
+namespace lr {
+
+// A unit: one sequence, one KV head and one tile of rows.  A row is a (new token, query head of
+// the KV head) pair, token-major, so that the query heads that share a KV head share its
+// tiles of cached tokens.  The cached tokens that some row of the unit sees are at most two ranges, the sinks
+// and the window; they are taken in tiles of TILE tokens.
+struct Unit {
+    int s, h, qt;      // sequence, KV head, tile of rows
+    int q0, ql, kv;    // first row of the token arrays, new tokens, tokens
+    int ns, wf, nt;    // tiles of sinks before the window, the window's first tile, tiles in all
+    int lo, hi;        // positions of the first and last row
+    int rows;          // rows of this tile
+};
+
+template <int TILE>
+__device__ __forceinline__ int tile_count(int lo, int hi, int window, int sinks, int &ns, int &wf) {
+    ns = wf = 0;
+    if (hi < 0) return 1;  // nothing to see: one tile, all masked, writes the zeros
+    if (window > 0) {
+        const int first = max(0, lo - window + 1);
+        wf = first / TILE;
+        ns = (min(sinks, first) + TILE - 1) / TILE;
+        if (ns >= wf) ns = wf = 0;  // the sinks reach the window's first tile
+    }
+    return ns + hi / TILE - wf + 1;
+}
+
+// Sequence s as the batch gives it, false if it is not this launch's: no rows, a number of rows
+// outside [row_lo, row_hi], or values out of range (recorded).
+__device__ __forceinline__ bool load_seq(const AttendLaunch &a, int s, int &q0, int &ql, int &kv) {
+    q0 = __ldg(a.b.q_start + s);
+    ql = __ldg(a.b.q_start + s + 1) - q0;
+    kv = __ldg(a.b.kv_len + s);
+    if (ql == 0) return false;
+    if (q0 < 0 || ql < 0 || ql > a.b.max_q || ql > a.b.T - q0 || kv < 0 || kv > kMaxTokens ||
+        (long long)kv > (long long)a.b.max_blocks * a.c.b) {
+        report(a.c.status, kEInval);
+        return false;
+    }
+    const int rows = ql * a.c.G;
+    return rows >= a.row_lo && rows <= a.row_hi;
+}
+
+template <int ROWS, int TILE>
+__device__ __forceinline__ void set_tile(const AttendLaunch &a, Unit &u) {
+    const int r0 = u.qt * ROWS;
+    u.rows = min(ROWS, u.ql * a.c.G - r0);
+    u.lo = u.kv - u.ql + quot(r0, a.c.div_g);
+    u.hi = u.kv - u.ql + quot(r0 + u.rows - 1, a.c.div_g);
+    u.nt = tile_count<TILE>(u.lo, u.hi, a.window, a.sinks, u.ns, u.wf);
+}
+
+// Tiles of a sequence for one KV head.
+template <int ROWS, int TILE>
+__device__ __forceinline__ long long seq_tiles(const AttendLaunch &a, int s) {
+    Unit u;
+    u.s = s;
+    if (!load_seq(a, s, u.q0, u.ql, u.kv)) return 0;
+    const int nq = (u.ql * a.c.G + ROWS - 1) / ROWS;
+    long long n = 0;
+    for (u.qt = 0; u.qt < nq; ++u.qt) {
+        set_tile<ROWS, TILE>(a, u);
+        n += u.nt;
+    }
+    return n;
+}
+
+// A position in the batch's sequence of tiles: units in order of sequence, KV head, tile of rows.
+template <int ROWS, int TILE>
+struct Cursor {
+    Unit u;
+    int j;  // tile of the unit
+    __device__ __forceinline__ int base() const { return (j < u.ns ? j : u.wf + j - u.ns) * TILE; }
+    __device__ __forceinline__ void next(const AttendLaunch &a) {  // there is a next tile
+        if (++j < u.nt) return;
+        j = 0;
+        if ((++u.qt) * ROWS >= u.ql * a.c.G) {
+            u.qt = 0;
+            if (++u.h == a.c.H) {
+                u.h = 0;
+                do ++u.s;
+                while (u.s < a.b.n && !load_seq(a, u.s, u.q0, u.ql, u.kv));
+            }
+        }
+        set_tile<ROWS, TILE>(a, u);
+    }
+};
+
+// Inclusive sum over a CTA of THREADS threads (all take part); `total` is the sum of all.
+template <int THREADS>
+__device__ __forceinline__ long long block_sum(long long v, long long *sh, long long &total) {
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long x = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += x;
+    }
+    __syncthreads();
+    if (lane == 31) sh[w] = v;
+    __syncthreads();
+    total = 0;
+#pragma unroll
+    for (int i = 0; i < THREADS / 32; ++i) {
+        if (i < w) v += sh[i];
+        total += sh[i];
+    }
+    return v;
+}
+
+// Splits the batch's tiles evenly over the CTAs: this CTA takes [x0, x1) of the `all` tiles, by
+// `ctas` CTAs (the others have none), and `cur` stands at x0.
+struct Share {
+    long long x0, x1, all;
+    int ctas;
+};
+template <int ROWS, int TILE, int THREADS>
+__device__ __forceinline__ bool take_share(const AttendLaunch &a, Cursor<ROWS, TILE> &cur, Share &sh) {
+    __shared__ long long s_sum[THREADS / 32];
+    __shared__ long long s_rest;
+    __shared__ int s_seq;
+    const int n = a.b.n, tid = threadIdx.x;
+    long long all = 0, first = 0, incl = 0, mine = 0;
+    for (int base = 0; base < n; base += THREADS) {
+        mine = base + tid < n ? a.c.H * seq_tiles<ROWS, TILE>(a, base + tid) : 0;
+        long long t;
+        incl = block_sum<THREADS>(mine, s_sum, t);
+        all += t;
+    }
+    if (all == 0) return false;
+    sh.all = all;
+    sh.ctas = (int)min((long long)gridDim.x, all);
+    const int c = blockIdx.x;
+    if (c >= sh.ctas) return false;
+    sh.x0 = all * c / sh.ctas;
+    sh.x1 = all * (c + 1) / sh.ctas;
+    for (int base = 0; base < n; base += THREADS) {
+        long long t;
+        if (n > THREADS) {
+            mine = base + tid < n ? a.c.H * seq_tiles<ROWS, TILE>(a, base + tid) : 0;
+            incl = block_sum<THREADS>(mine, s_sum, t);
+        } else {
+            t = all;
+        }
+        const long long x = sh.x0 - first;
+        if (x < incl && x >= incl - mine) {
+            s_seq = base + tid;
+            s_rest = x - (incl - mine);
+        }
+        first += t;
+        if (first > sh.x0) break;
+    }
+    __syncthreads();
+    Unit &u = cur.u;
+    u.s = s_seq;
+    load_seq(a, u.s, u.q0, u.ql, u.kv);
+    long long r = s_rest;
+    const long long per = seq_tiles<ROWS, TILE>(a, u.s);
+    u.h = (int)(r / per);
+    r -= u.h * per;
+    for (u.qt = 0;; ++u.qt) {
+        set_tile<ROWS, TILE>(a, u);
+        if (r < u.nt) break;
+        r -= u.nt;
+    }
+    cur.j = (int)r;
+    return true;
+}
+
+// The CTAs c0 .. c1 that share the unit of tiles [u0, u1), and where CTA c's part of it lies: its
+// first unit in slot 2c, a later one in slot 2c + 1.
+__device__ __forceinline__ int cta_of(const Share &s, long long x) { return (int)(((x + 1) * s.ctas - 1) / s.all); }
+__device__ __forceinline__ int slot_of(const Share &s, int c, long long u0) {
+    return 2 * c + (s.all * c / s.ctas < u0 ? 1 : 0);
+}
+
+__device__ __forceinline__ bool visible(int pos, int j, int window, int sinks) {
+    return j <= pos && (window == 0 || j > pos - window || j < sinks);
+}
+
+// Two 8-bit codes to two 16-bit numbers, exactly.  e4m3: sign, four exponent and three mantissa bits
+// moved to their places, then a product with the power of two between the biases (subnormal codes
+// become subnormal 16-bit numbers first, which the product turns right as well).
+// int8 to bf16: 128 + the low seven bits, less 128 or, for a negative code, 256.  To fp16: 1024 +
+// (code + 128), less 1152.
+// `t` holds the codes in the high bytes of its halves.
+template <bool BF16>
+__device__ __forceinline__ uint32_t from_e4m3(uint32_t t) {
+    if constexpr (BF16) {
+        const uint32_t r = (t & 0x80008000u) | ((t >> 4) & 0x07f007f0u);
+        const uint32_t k = 0x7b807b80u;  // 2^120
+        uint32_t d;
+        asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(r), "r"(k));
+        return d;
+    } else {
+        const uint32_t r = (t & 0x80008000u) | ((t >> 1) & 0x3f803f80u);
+        const uint32_t k = 0x5c005c00u;  // 2^8
+        uint32_t d;
+        asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(r), "r"(k));
+        return d;
+    }
+}
+// `t` holds the codes in the low bytes of its halves.
+template <bool BF16>
+__device__ __forceinline__ uint32_t from_int8(uint32_t t) {
+    uint32_t d;
+    if constexpr (BF16) {
+        const uint32_t x = (t & 0x007f007fu) | 0x43004300u, y = (t & 0x00800080u) | 0x43004300u;
+        asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(x), "r"(y));
+    } else {
+        const uint32_t x = ((t & 0x00ff00ffu) ^ 0x00800080u) | 0x64006400u;
+        asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(x), "r"(0x64806480u));
+    }
+    return d;
+}
+// Bytes i and j of w as two 16-bit numbers (i in the low half).
+template <bool BF16, int FMT>
+__device__ __forceinline__ uint32_t from_codes(uint32_t w, int i, int j) {
+    if constexpr (FMT == kFmtE4M3) return from_e4m3<BF16>(__byte_perm(w, 0, 0x0404u | i << 4 | j << 12));
+    else return from_int8<BF16>(__byte_perm(w, 0, 0x4040u | i | j << 8));
+}
+
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack16(float lo, float hi) {
+    uint32_t r;
+    if constexpr (BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+template <bool BF16>
+__device__ __forceinline__ float2 unpack16(uint32_t x) {
+    if constexpr (BF16) return make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
+    else return __half22float2(*reinterpret_cast<__half2 *>(&x));
+}
+// An infinity or a NaN among the two 16-bit numbers.
+template <bool BF16>
+__device__ __forceinline__ bool not_finite(uint32_t x) {
+    constexpr uint32_t e = BF16 ? 0x7f80u : 0x7c00u;
+    return (x & e) == e || (x >> 16 & e) == e;
+}
+
+__device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// 16 bytes of global memory to shared memory, zeros if `ok` is false.
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool ok) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t dst, const void *src, bool ok) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(ok ? 4 : 0) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+}  // namespace lr

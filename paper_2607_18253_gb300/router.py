@@ -27,7 +27,8 @@ EXPORTED_SYMBOLS = ("lr_create", "lr_destroy", "lr_load_state", "lr_estimate_ttf
                     "lr_route", "lr_route_frontier_static", "lr_advance", "lr_read_state", "lr_status",
                     "lr_set_queue_params", "lr_set_ttft_source", "lr_calibrate", "lr_route_baseline",
                     "lr_on_time_utility", "lr_set_kv_limits", "lr_strerror", "lr_last_error",
-                    "lr_track_first_tokens", "lr_advance_tracked")
+                    "lr_track_first_tokens", "lr_advance_tracked", "lr_cache_create", "lr_cache_destroy",
+                    "lr_cache_write", "lr_cache_read", "lr_cache_attend", "lr_cache_status", "lr_cache_last_error")
 
 _P = ctypes.c_void_p
 _I32 = ctypes.c_int32
@@ -48,6 +49,19 @@ class _QueueParams(ctypes.Structure):
 class _StateView(ctypes.Structure):
     _fields_ = [("n_run", _P), ("run_ctx", _P), ("run_pre", _P), ("run_dec", _P), ("n_wait", _P),
                 ("wait_pre", _P), ("wait_dec", _P)]
+
+
+class _CacheConfig(ctypes.Structure):
+    _fields_ = [("num_q_heads", _I32), ("num_kv_heads", _I32), ("head_dim", _I32), ("dtype", _I32), ("format", _I32),
+                ("block_size", _I32), ("num_blocks", _I32), ("max_seqs", _I32), ("k", _P), ("v", _P), ("k_scale", _P),
+                ("v_scale", _P)] + [(n, ctypes.c_int64) for n in (
+                    "block_stride", "token_stride", "head_stride", "scale_block_stride", "scale_token_stride",
+                    "scale_head_stride")]
+
+
+class _CacheBatch(ctypes.Structure):
+    _fields_ = [("num_seqs", _I32), ("max_q", _I32), ("q_start", _P), ("kv_len", _P), ("block_table", _P),
+                ("table_stride", ctypes.c_int64), ("max_blocks", _I32)]
 
 
 _lib = None
@@ -78,6 +92,15 @@ def load_library(path: str = LIB_PATH):
     lib.lr_on_time_utility.argtypes = [_P, _I32, _P, _P, _P, _P, _P, _P]
     lib.lr_set_kv_limits.argtypes = [_P, _P, _P, _P, _I32]
     lib.lr_read_state.argtypes = [_P, _P, _P, _P, _P, _P, _P, _P, _P, _P]
+    lib.lr_cache_create.argtypes = [ctypes.POINTER(_CacheConfig), ctypes.POINTER(_P)]
+    lib.lr_cache_destroy.argtypes = [_P]
+    lib.lr_cache_write.argtypes = [_P, ctypes.POINTER(_CacheBatch), _I32, _P, _P, ctypes.c_int64, ctypes.c_int64, _P]
+    lib.lr_cache_read.argtypes = [_P, ctypes.POINTER(_CacheBatch), _I32, _I32, _P, _P, _P]
+    lib.lr_cache_attend.argtypes = [_P, ctypes.POINTER(_CacheBatch), _I32, _P, ctypes.c_int64, ctypes.c_int64,
+                                    ctypes.c_float, _I32, _I32, _P, ctypes.c_int64, ctypes.c_int64, _P, _P]
+    lib.lr_cache_status.argtypes = [_P, _P]
+    lib.lr_cache_last_error.argtypes = [_P]
+    lib.lr_cache_last_error.restype = ctypes.c_char_p
     lib.lr_status.argtypes = [_P, _P]
     lib.lr_strerror.argtypes = [ctypes.c_int]
     lib.lr_strerror.restype = ctypes.c_char_p
@@ -86,7 +109,9 @@ def load_library(path: str = LIB_PATH):
     for name in ("lr_create", "lr_destroy", "lr_load_state", "lr_estimate_ttft", "lr_estimate_features",
                  "lr_route", "lr_route_frontier_static", "lr_advance", "lr_read_state", "lr_status",
                  "lr_set_queue_params", "lr_set_ttft_source", "lr_calibrate", "lr_route_baseline",
-                 "lr_on_time_utility", "lr_set_kv_limits", "lr_advance_tracked", "lr_track_first_tokens"):
+                 "lr_on_time_utility", "lr_set_kv_limits", "lr_advance_tracked", "lr_track_first_tokens",
+                 "lr_cache_create", "lr_cache_destroy", "lr_cache_write", "lr_cache_read", "lr_cache_attend",
+                 "lr_cache_status"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
