@@ -17,7 +17,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIBDIR = os.path.join(PKG, "_lib")
 LIB = os.path.join(LIBDIR, "liblr.so")
 SOURCES = ["lr_api.cu", "lr_trajectory.cu", "lr_estimate.cu", "lr_advance.cu", "lr_calibrate.cu", "lr_kv.cu",
-           "lr_cache_api.cu", "lr_cache_rw.cu", "lr_attend_step.cu"]
+           "lr_cache_api.cu", "lr_cache_rw.cu", "lr_attend_step.cu", "lr_attend_chunk.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-std=c++17", "-O3", "-lineinfo", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",
               "--expt-relaxed-constexpr"]

@@ -119,11 +119,10 @@ struct Share {
     long long x0, x1, all;
     int ctas;
 };
+// (scratch: THREADS / 32 + 2 words of shared memory)
 template <int ROWS, int TILE, int THREADS>
-__device__ __forceinline__ bool take_share(const AttendLaunch &a, Cursor<ROWS, TILE> &cur, Share &sh) {
-    __shared__ long long s_sum[THREADS / 32];
-    __shared__ long long s_rest;
-    __shared__ int s_seq;
+__device__ __forceinline__ bool take_share(const AttendLaunch &a, Cursor<ROWS, TILE> &cur, Share &sh, long long *scratch) {
+    long long *const s_sum = scratch, &s_rest = scratch[THREADS / 32], &s_seq = scratch[THREADS / 32 + 1];
     const int n = a.b.n, tid = threadIdx.x;
     long long all = 0, first = 0, incl = 0, mine = 0;
     for (int base = 0; base < n; base += THREADS) {
@@ -157,7 +156,7 @@ __device__ __forceinline__ bool take_share(const AttendLaunch &a, Cursor<ROWS, T
     }
     __syncthreads();
     Unit &u = cur.u;
-    u.s = s_seq;
+    u.s = (int)s_seq;
     load_seq(a, u.s, u.q0, u.ql, u.kv);
     long long r = s_rest;
     const long long per = seq_tiles<ROWS, TILE>(a, u.s);

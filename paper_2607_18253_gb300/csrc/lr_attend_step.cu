@@ -81,6 +81,7 @@ __global__ void __launch_bounds__(kThreads) k_attend_step(const __grid_constant_
     float4 *const s_ml = reinterpret_cast<float4 *>(reinterpret_cast<char *>(places) + S::kPlaces);  // [warp][lane]
     int *const s_bad = reinterpret_cast<int *>(s_ml + 4 * 32);  // [8][2]
     __shared__ int s_last;
+    __shared__ long long s_scratch[kThreads / 32 + 2];
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, g = lane / 4, i4 = lane % 4;
     const int wm = warp / WN, wn = warp % WN;
     const CacheDev &c = a.c;
@@ -88,7 +89,7 @@ __global__ void __launch_bounds__(kThreads) k_attend_step(const __grid_constant_
     chain_wait();
     Cursor<kRows, kTok> cu, lk;
     Share sh;
-    if (!take_share<kRows, kTok, kThreads>(a, cu, sh)) {
+    if (!take_share<kRows, kTok, kThreads>(a, cu, sh, s_scratch)) {
         chain_next();
         return;
     }

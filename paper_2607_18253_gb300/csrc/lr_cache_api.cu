@@ -1,5 +1,6 @@
 // Host side of the paged-cache calls declared in include/latency_router.h: validation,
 // workspace, launch shapes and the status word.
+#include <algorithm>
 #include <cmath>
 #include <cstdio>
 #include <cstring>
@@ -15,13 +16,18 @@ struct lr_cache {
     lr_cache_config cfg{};
     lr::CacheDev dev{};
     bool bf16 = true;
-    float *part_o = nullptr;
-    float2 *part_ml = nullptr;
-    uint32_t *done = nullptr;
+    struct Parts {  // workspace of an attention kernel
+        float *o = nullptr;
+        float2 *ml = nullptr;
+        uint32_t *done = nullptr;
+    } step, chunk;
     std::string err;
 };
 
 namespace {
+
+// Rows (new tokens x query heads a KV head) from which a sequence is the chunk kernel's.
+constexpr int kLeastChunk = 65;
 
 int fail(lr_cache *c, int code, const char *msg) {
     try {
@@ -41,9 +47,20 @@ int cuda_fail(lr_cache *c, cudaError_t e, const char *what) {
 
 void free_all(lr_cache *c) {
     cudaFree(c->dev.status);
-    cudaFree(c->part_o);
-    cudaFree(c->part_ml);
-    cudaFree(c->done);
+    for (lr_cache::Parts *p : {&c->step, &c->chunk}) {
+        cudaFree(p->o);
+        cudaFree(p->ml);
+        cudaFree(p->done);
+    }
+}
+
+// Two slots of partial rows a CTA and a counter, at zero.
+cudaError_t alloc_parts(lr_cache::Parts &p, size_t ctas, size_t rows) {
+    cudaError_t e = cudaMalloc(&p.o, 2 * ctas * rows * 128 * sizeof(float));
+    if (e == cudaSuccess) e = cudaMalloc(&p.ml, 2 * ctas * rows * sizeof(float2));
+    if (e == cudaSuccess) e = cudaMalloc(&p.done, ctas * sizeof(uint32_t));
+    if (e == cudaSuccess) e = cudaMemset(p.done, 0, ctas * sizeof(uint32_t));
+    return e;
 }
 
 bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
@@ -105,6 +122,7 @@ int lr_cache_create(const lr_cache_config *cfg, lr_cache **out) {
     cudaError_t e = cudaGetDevice(&c->device);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&c->sms, cudaDevAttrMultiProcessorCount, c->device);
     if (e == cudaSuccess) e = lr::attend_step_init();
+    if (e == cudaSuccess) e = lr::attend_chunk_init();
     if (e != cudaSuccess) return bail(LR_ECUDA, cudaGetErrorString(e));
     lr::CacheDev &d = c->dev;
     d.k = static_cast<char *>(cfg->k);
@@ -125,14 +143,10 @@ int lr_cache_create(const lr_cache_config *cfg, lr_cache **out) {
     d.b = cfg->block_size;
     d.div_b = lr::fast_div(d.b);
     d.div_g = lr::fast_div(d.G);
-    // workspace: two slots of partial rows a CTA, a counter a CTA, the status word
-    const size_t ctas = lr::attend_step_ctas(c->sms), rows = 2 * ctas * lr::kStepRows;
     e = cudaMalloc(&d.status, 16);
     if (e == cudaSuccess) e = cudaMemset(d.status, 0, 16);
-    if (e == cudaSuccess) e = cudaMalloc(&c->part_o, rows * 128 * sizeof(float));
-    if (e == cudaSuccess) e = cudaMalloc(&c->part_ml, rows * sizeof(float2));
-    if (e == cudaSuccess) e = cudaMalloc(&c->done, ctas * sizeof(uint32_t));
-    if (e == cudaSuccess) e = cudaMemset(c->done, 0, ctas * sizeof(uint32_t));
+    if (e == cudaSuccess) e = alloc_parts(c->step, lr::attend_step_ctas(c->sms), lr::kStepRows);
+    if (e == cudaSuccess) e = alloc_parts(c->chunk, c->sms, lr::kChunkRows);
     if (e != cudaSuccess) return bail(LR_ENOMEM, cudaGetErrorString(e));
     *out = c;
     return LR_OK;
@@ -216,14 +230,28 @@ int lr_cache_attend(lr_cache *c, const lr_cache_batch *b, int32_t T, const void 
     a.scale_log2 = (float)((double)scale * 1.4426950408889634);
     a.window = window;
     a.sinks = window ? sinks : 0;
-    a.part_o = c->part_o;
-    a.part_ml = c->part_ml;
-    a.done = c->done;
+    // Sequences of few rows go to the step kernel, of many to the chunk kernel; a batch whose sequences
+    // have many on average is the chunk kernel's whole.
+    const int most = (int)std::min<long long>((long long)b->max_q * c->dev.G, 0x7fffffff);
+    const bool all = (long long)T * c->dev.G >= (long long)kLeastChunk * b->num_seqs;
+    cudaStream_t st = (cudaStream_t)stream;
+    if (most >= kLeastChunk) {
+        a.row_lo = all ? 1 : kLeastChunk;
+        a.row_hi = 0x7fffffff;
+        a.part_o = c->chunk.o;
+        a.part_ml = c->chunk.ml;
+        a.done = c->chunk.done;
+        cudaError_t e = lr::launch_attend_chunk(a, c->bf16, c->cfg.format, c->sms, st);
+        if (e != cudaSuccess) return cuda_fail(c, e, "attention launch");
+        if (all) return LR_OK;
+    }
     a.row_lo = 1;
-    a.row_hi = 0x7fffffff;
-    const long long rows = (long long)b->max_q * c->dev.G;
-    const int tile = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
-    cudaError_t e = lr::launch_attend_step(a, c->bf16, c->cfg.format, tile, lr::attend_step_ctas(c->sms), (cudaStream_t)stream);
+    a.row_hi = std::min(most, kLeastChunk - 1);
+    a.part_o = c->step.o;
+    a.part_ml = c->step.ml;
+    a.done = c->step.done;
+    const int rows = a.row_hi <= 16 ? 16 : a.row_hi <= 32 ? 32 : 64;
+    cudaError_t e = lr::launch_attend_step(a, c->bf16, c->cfg.format, rows, lr::attend_step_ctas(c->sms), st);
     return e == cudaSuccess ? LR_OK : cuda_fail(c, e, "attention launch");
 }
 
