@@ -56,7 +56,7 @@ __device__ __forceinline__ void set_tile(const AttendLaunch &a, Unit &u) {
     u.nt = tile_count<TILE>(u.lo, u.hi, a.window, a.sinks, u.ns, u.wf);
 }
 
-// Tiles of a sequence for one KV head.
+// Tiles of a sequence for one KV head, a warp's lanes taking its tiles of rows in turn (all call).
 template <int ROWS, int TILE>
 __device__ __forceinline__ long long seq_tiles(const AttendLaunch &a, int s) {
     Unit u;
@@ -64,10 +64,12 @@ __device__ __forceinline__ long long seq_tiles(const AttendLaunch &a, int s) {
     if (!load_seq(a, s, u.q0, u.ql, u.kv)) return 0;
     const int nq = (u.ql * a.c.G + ROWS - 1) / ROWS;
     long long n = 0;
-    for (u.qt = 0; u.qt < nq; ++u.qt) {
+    for (u.qt = threadIdx.x & 31; u.qt < nq; u.qt += 32) {
         set_tile<ROWS, TILE>(a, u);
         n += u.nt;
     }
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
     return n;
 }
 
@@ -123,10 +125,30 @@ struct Share {
 template <int ROWS, int TILE, int THREADS>
 __device__ __forceinline__ bool take_share(const AttendLaunch &a, Cursor<ROWS, TILE> &cur, Share &sh, long long *scratch) {
     long long *const s_sum = scratch, &s_rest = scratch[THREADS / 32], &s_seq = scratch[THREADS / 32 + 1];
-    const int n = a.b.n, tid = threadIdx.x;
+    const int n = a.b.n, tid = threadIdx.x, lane = tid & 31;
+    // tiles of sequence base + tid: a thread's own look where no sequence has more than one tile of rows,
+    // else a warp together for each of its threads
+    const bool single = (long long)a.b.max_q * a.c.G <= ROWS;
+    auto tiles_of = [&](int base) -> long long {
+        if (single) {
+            Unit u;
+            u.s = base + tid;
+            u.qt = 0;
+            if (u.s >= n || !load_seq(a, u.s, u.q0, u.ql, u.kv)) return 0;
+            set_tile<ROWS, TILE>(a, u);
+            return (long long)a.c.H * u.nt;
+        }
+        long long mine = 0;
+        const int w0 = base + tid - lane;
+        for (int i = 0; i < 32 && w0 + i < n; ++i) {
+            const long long t = a.c.H * seq_tiles<ROWS, TILE>(a, w0 + i);
+            if (i == lane) mine = t;
+        }
+        return mine;
+    };
     long long all = 0, first = 0, incl = 0, mine = 0;
     for (int base = 0; base < n; base += THREADS) {
-        mine = base + tid < n ? a.c.H * seq_tiles<ROWS, TILE>(a, base + tid) : 0;
+        mine = tiles_of(base);
         long long t;
         incl = block_sum<THREADS>(mine, s_sum, t);
         all += t;
@@ -141,7 +163,7 @@ __device__ __forceinline__ bool take_share(const AttendLaunch &a, Cursor<ROWS, T
     for (int base = 0; base < n; base += THREADS) {
         long long t;
         if (n > THREADS) {
-            mine = base + tid < n ? a.c.H * seq_tiles<ROWS, TILE>(a, base + tid) : 0;
+            mine = tiles_of(base);
             incl = block_sum<THREADS>(mine, s_sum, t);
         } else {
             t = all;
@@ -162,11 +184,27 @@ __device__ __forceinline__ bool take_share(const AttendLaunch &a, Cursor<ROWS, T
     const long long per = seq_tiles<ROWS, TILE>(a, u.s);
     u.h = (int)(r / per);
     r -= u.h * per;
-    for (u.qt = 0;; ++u.qt) {
+    const int nq = (u.ql * a.c.G + ROWS - 1) / ROWS;
+    for (int q0 = 0;; q0 += 32) {  // 32 tiles of rows at a time
+        u.qt = min(q0 + lane, nq - 1);
         set_tile<ROWS, TILE>(a, u);
-        if (r < u.nt) break;
-        r -= u.nt;
+        const long long own = q0 + lane < nq ? u.nt : 0;
+        long long upto = own;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long y = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += y;
+        }
+        const unsigned hit = __ballot_sync(0xffffffffu, r < upto);
+        if (hit) {
+            const int at = __ffs(hit) - 1;
+            r -= __shfl_sync(0xffffffffu, upto - own, at);
+            u.qt = q0 + at;
+            break;
+        }
+        r -= __shfl_sync(0xffffffffu, upto, 31);
     }
+    set_tile<ROWS, TILE>(a, u);
     cur.j = (int)r;
     return true;
 }

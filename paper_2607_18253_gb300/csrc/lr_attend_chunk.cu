@@ -23,10 +23,33 @@ namespace {
 
 constexpr int kTok = 128;     // tokens of a tile
 constexpr int kThreads = 512;
-constexpr uint32_t kSpin = 1u << 22;  // polls before a wait gives up
+// registers a thread of the softmax warps and of the others: together the 512 x 128 of the launch
+constexpr int kSoftRegs = 192, kOtherRegs = 64;
+constexpr uint32_t kSpin = 1u << 28;  // polls before a wait gives up
 
-template <int DP, int FMT>
+// How K and V reach shared memory.
+enum : int {
+    kTma = 0,     // 16-bit cache: the tensor copy engine, one box of tokens of a block at a time
+    kGather = 1,  // 16-bit cache of odd blocks: 16 bytes a thread (cp.async)
+    kConvert = 2  // 8-bit cache: 16 codes a thread, converted on the way
+};
+
+// What the CTA does for one unit, written by the warps that bring its queries: the walk over the batch is
+// theirs and the loaders', so that the softmax warps' registers are left to the softmax.
+struct Job {
+    Unit u;
+    int j0, n;          // the CTA's tiles of the unit, from the first
+    int whole, last;    // all of the unit's; the CTA's last job
+    int c0, c1;         // the CTAs that share the unit
+    int slot, slot0;    // where this CTA's and the first one's parts go
+};
+constexpr int kJobs = 4;
+
+template <int DP, int FMT, int LOAD>
 struct Shape {
+    // Warps 0-7 softmax, 8 products.  By the copy engine: 9 K, 10 V, 12-15 queries; else 12-15 K and V, 10
+    // and 11 queries.
+    static constexpr int kQueryWarp = LOAD == kTma ? 12 : 10, kQueryWarps = LOAD == kTma ? 4 : 2;
     static constexpr int kPanel = kTok * 128;                   // 128 rows of 64 16-bit elements
     static constexpr int kTile = kTok * DP * 2;                 // a tile of K or V, or half of Q, in 16 bits
     static constexpr int kStages = FMT == kFmt16 ? 5 : 4;
@@ -36,8 +59,9 @@ struct Shape {
     static constexpr int kRaw = FMT == kFmt16 ? 0 : kSlots * 128 * 16;
     static constexpr int kQ = 2 * kTile;
     static constexpr int kBytes = kQ + kStages * kTile + kRaw;
+    static constexpr int kBars = 2 + 2 * kStages + 10 + 4 + 1 + 2 * kJobs + 2;
     static constexpr int kScales = FMT == kFmt16 ? 0 : 4 * 2 * kTok * 4;
-    static constexpr int kSmem = kBytes + kScales + 2 * kTok * 8 + 32 * 8 + (kThreads / 32 + 2) * 8 + 8 * 4;
+    static constexpr int kSmem = kBytes + kScales + 2 * kTok * 8 + kBars * 8 + (kThreads / 32 + 2) * 8 + 12 * 4 + kJobs * sizeof(Job);
     static_assert(kSmem <= 227 * 1024, "shared memory");
 };
 
@@ -48,24 +72,37 @@ __device__ __forceinline__ void bar_init(uint32_t bar, int count) {
 __device__ __forceinline__ void bar_arrive(uint32_t bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
+// One arrival for the warp, after all its lanes have come.
+__device__ __forceinline__ void bar_arrive_warp(uint32_t bar) {
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) bar_arrive(bar);
+}
 __device__ __forceinline__ bool bar_test(uint32_t bar, uint32_t parity) {
     uint32_t done;
     asm volatile("{\n .reg .pred P;\n mbarrier.test_wait.parity.shared::cta.b64 P, [%1], %2;\n selp.u32 %0, 1, 0, P;\n}"
                  : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     return done;
 }
-// Waits until the phase of the given parity is over; false if it gives up, or another thread has.
+// Waits until the phase of the given parity is over; false if it gives up, or another thread has.  All lanes
+// of a warp come together and go on together (`distant`: the wait is long, its tests sleep between).
+template <bool DISTANT = false>
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *dead) {
-    for (uint32_t i = 0; i < kSpin; ++i) {
+    for (uint32_t i = 1; i < kSpin; ++i) {
         uint32_t done;
         asm volatile(
             "{\n .reg .pred P;\n mbarrier.try_wait.parity.shared::cta.b64 P, [%1], %2;\n selp.u32 %0, 1, 0, P;\n}"
             : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-        if (done) return true;
-        if ((i & 1023) == 1023 && *dead) return false;
+        if (__all_sync(0xffffffffu, done)) return true;
+        if (DISTANT) __nanosleep(200);
+        if (i % 1024 == 0 && __any_sync(0xffffffffu, *dead)) return false;
     }
     *dead = 1;
     return false;
+}
+__device__ __forceinline__ bool elect() {
+    uint32_t r;
+    asm volatile("{\n .reg .pred P;\n elect.sync _|P, 0xffffffff;\n selp.u32 %0, 1, 0, P;\n}" : "=r"(r));
+    return r;
 }
 
 // ---- tensor cores ----
@@ -108,14 +145,23 @@ __device__ __forceinline__ void tm_load(float *r, uint32_t addr) {
           "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
         : "r"(addr));
 }
-__device__ __forceinline__ void tm_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// (the registers pass through, so that nothing reads them earlier)
+__device__ __forceinline__ void tm_load_wait(float *r) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+    uint32_t *u = reinterpret_cast<uint32_t *>(r);
+    asm volatile(""
+                 : "+r"(u[0]), "+r"(u[1]), "+r"(u[2]), "+r"(u[3]), "+r"(u[4]), "+r"(u[5]), "+r"(u[6]), "+r"(u[7]), "+r"(u[8]), "+r"(u[9]),
+                   "+r"(u[10]), "+r"(u[11]), "+r"(u[12]), "+r"(u[13]), "+r"(u[14]), "+r"(u[15]));
+    asm volatile(""
+                 : "+r"(u[16]), "+r"(u[17]), "+r"(u[18]), "+r"(u[19]), "+r"(u[20]), "+r"(u[21]), "+r"(u[22]), "+r"(u[23]), "+r"(u[24]),
+                   "+r"(u[25]), "+r"(u[26]), "+r"(u[27]), "+r"(u[28]), "+r"(u[29]), "+r"(u[30]), "+r"(u[31]));
+}
+// 16 columns, a lane a thread.
 __device__ __forceinline__ void tm_store(uint32_t addr, const uint32_t *u) {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
-        "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::"r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]),
-        "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]), "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15]),
-        "r"(u[16]), "r"(u[17]), "r"(u[18]), "r"(u[19]), "r"(u[20]), "r"(u[21]), "r"(u[22]), "r"(u[23]), "r"(u[24]), "r"(u[25]),
-        "r"(u[26]), "r"(u[27]), "r"(u[28]), "r"(u[29]), "r"(u[30]), "r"(u[31]), "r"(addr)
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::"r"(u[0]), "r"(u[1]),
+        "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]), "r"(u[10]), "r"(u[11]), "r"(u[12]),
+        "r"(u[13]), "r"(u[14]), "r"(u[15]), "r"(addr)
         : "memory");
 }
 __device__ __forceinline__ void tm_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -152,52 +198,63 @@ __device__ __forceinline__ uint32_t swizzled(int row, int chunk) {  // byte offs
     return (chunk >> 3) * (kTok * 128) + row * 128 + ((chunk ^ row) & 7) * 16;
 }
 
-// A row of O in which 32 columns from `col` came out with infinities or NaN (`bad`: which): tokens that the row
-// does not see have weight zero, but zero times a value that is not finite is not zero.  The columns
-// in which the row sees such a value itself get the sum of those; the others are summed again over what
-// it sees.  16-bit caches only (8-bit codes are finite, and their scales are kept from hidden weights).
+// Tokens that a row does not see have weight zero, but zero times an infinity or a NaN in V is not
+// zero.  In a tile that is hidden from some of its rows, such elements of V are therefore set to zero in
+// shared memory (clear_row), and the rows that do see them add them at the end (add_lost).  16-bit caches
+// only: 8-bit codes are finite, and their scales are kept from hidden weights.
 template <bool BF16>
-__device__ __noinline__ void mend(const AttendLaunch &a, const Unit &u, int j0, int j1, int row, int pos, float mref, int col, float *o) {
+__device__ __forceinline__ const char *v_row(const AttendLaunch &a, const Unit &u, int t) {
     const CacheDev &c = a.c;
-    const int gr = u.qt * 256 + row, t = quot(gr, c.div_g), hd = u.h * c.G + gr - t * c.G;
-    const uint32_t *const q = reinterpret_cast<const uint32_t *>(a.q + (int64_t)(u.q0 + t) * a.q_t + (int64_t)hd * a.q_h);
-    for (int d = 0; d < 32; ++d) {
-        if (fabsf(o[d]) < INFINITY || col + d >= c.D) continue;
-        float seen = 0.0f, sum = 0.0f;
-        for (int pass = 0; pass < 2; ++pass) {  // first only the values that are not finite
-            if (pass == 1 && seen != 0.0f) break;
-            for (int j = j0; j < j1; ++j) {
-                const int base = (j < u.ns ? j : u.wf + j - u.ns) * kTok;
-                for (int i = base; i < base + kTok; ++i) {
-                    if (!visible(pos, i, a.window, a.sinks)) continue;
-                    int place;
-                    const int64_t blk = block_of(c, a.b, u.s, i, place);
-                    if (blk < 0) continue;
-                    const int64_t at = blk * c.sb + place * c.st + u.h * c.sh;
-                    const uint32_t w = *reinterpret_cast<const uint16_t *>(c.v + at + (col + d) * 2);
-                    const float v = unpack16<BF16>(w).x;
-                    if (pass == 0) {
-                        if (!(fabsf(v) < INFINITY)) seen += v;
-                        continue;
-                    }
-                    const uint32_t *const k = reinterpret_cast<const uint32_t *>(c.k + at);
-                    float s = 0.0f;
-                    for (int e = 0; e < c.D / 2; ++e) {
-                        const float2 x = unpack16<BF16>(q[e]), y = unpack16<BF16>(k[e]);
-                        s = fmaf(x.x, y.x, fmaf(x.y, y.y, s));
-                    }
-                    const float p = exp2_fast(s * a.scale_log2 - mref);
-                    sum = fmaf(unpack16<BF16>(pack16<BF16>(p, 0.0f)).x, v, sum);
-                }
+    if (t > u.hi || (a.window > 0 && t <= u.lo - a.window && t >= a.sinks)) return nullptr;  // not read: zeros
+    int place;
+    const int64_t blk = block_of(c, a.b, u.s, t, place);
+    return blk < 0 ? nullptr : c.v + blk * c.sb + place * c.st + u.h * c.sh;
+}
+template <bool BF16>
+__device__ __forceinline__ bool lost_in(const uint4 &w) {
+    return not_finite<BF16>(w.x) || not_finite<BF16>(w.y) || not_finite<BF16>(w.z) || not_finite<BF16>(w.w);
+}
+// The elements that are not finite, or all.
+template <bool BF16, int DP>
+__device__ __noinline__ void clear_row(uint32_t tile, int row, bool all) {
+    constexpr uint32_t e = BF16 ? 0x7f80u : 0x7c00u;
+    for (int ch = 0; ch < DP / 8; ++ch) {
+        const uint32_t at = tile + (ch >> 3) * (kTok * 128) + row * 128 + ((ch ^ row) & 7) * 16;
+        uint32_t w[4];
+        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
+        for (int k = 0; k < 4; ++k) {
+            if (all || (w[k] & e) == e) w[k] &= 0xffff0000u;
+            if (all || (w[k] >> 16 & e) == e) w[k] &= 0xffffu;
+        }
+        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+    }
+}
+template <bool BF16>
+__device__ __noinline__ void add_lost(const AttendLaunch &a, const Unit &u, int tile0, int tile1, int pos, int col, float *o) {
+    for (int tile = tile0; tile < tile1; ++tile) {
+        const int base = (tile < u.ns ? tile : u.wf + tile - u.ns) * kTok;
+        if (!(base + kTok - 1 > u.lo || (a.window > 0 && base <= u.hi - a.window && base + kTok > a.sinks))) continue;
+        for (int t = base; t < base + kTok; ++t) {
+            if (!visible(pos, t, a.window, a.sinks)) continue;
+            const char *const p = v_row<BF16>(a, u, t);
+            for (int d = 0; p && d < 32 && col + d < a.c.D; ++d) {
+                const float v = unpack16<BF16>(*reinterpret_cast<const uint16_t *>(p + (col + d) * 2)).x;
+                if (!(fabsf(v) < INFINITY)) o[d] += v;
             }
         }
-        o[d] = seen != 0.0f ? seen : sum;
     }
 }
 
-template <bool BF16, int FMT, int DP>
-__global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_constant__ AttendLaunch a) {
-    using S = Shape<DP, FMT>;
+struct ChunkLaunch {
+    AttendLaunch a;
+    CacheMaps m;
+};
+
+template <bool BF16, int FMT, int DP, int LOAD>
+__global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_constant__ ChunkLaunch in) {
+    using S = Shape<DP, FMT, LOAD>;
+    const AttendLaunch &a = in.a;
+    constexpr int kKvArrive = LOAD == kTma ? 1 : 4;  // arrivals that hand over a tile: one a warp
     constexpr int kStages = S::kStages;
     constexpr float kLag = BF16 ? 8.0f : 4.0f;
     // fp16 weights that carry 8-bit scales: lifted from fp16's subnormal numbers (scales are at most
@@ -210,15 +267,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
     float *const scales = reinterpret_cast<float *>(smem + S::kBytes);                                    // [4][K, V][token]
     int64_t *const places = reinterpret_cast<int64_t *>(smem + S::kBytes + S::kScales);                   // [2][token]
     uint64_t *const bars = reinterpret_cast<uint64_t *>(places + 2 * kTok);
-    long long *const scratch = reinterpret_cast<long long *>(bars + 32);
-    int *const s_bad = reinterpret_cast<int *>(scratch + kThreads / 32 + 2);                              // [4]
-    int *const s_last = s_bad + 4, &s_dead = s_bad[6];                                                    // [2], one
-    uint32_t &s_tmem = *reinterpret_cast<uint32_t *>(s_bad + 7);
+    long long *const scratch = reinterpret_cast<long long *>(bars + S::kBars);
+    Job *const jobs = reinterpret_cast<Job *>(scratch + kThreads / 32 + 2);
+    int *const s_bad = reinterpret_cast<int *>(jobs + kJobs);  // [4] a block of the tile is out of range
+    int *const s_lost = s_bad + 4;                             // [half][2] the last scan that found V not finite
+    int &s_dead = s_bad[8];
+    uint32_t &s_tmem = *reinterpret_cast<uint32_t *>(s_bad + 9);
     const uint32_t b0 = smem_addr(bars);
-    // (the barriers: how many arrive, who)
     const uint32_t q_full = b0, q_free = b0 + 8, kv_full = b0 + 16, kv_free = kv_full + 8 * kStages, s_full = kv_free + 8 * kStages,
-                   p_full = s_full + 16, o_full = p_full + 16, o_free = o_full + 16, sc_full = o_free + 16, ended = sc_full + 32;
-    static_assert(2 + 2 * kStages + 8 + 4 + 1 <= 32, "barriers");
+                   p_half = s_full + 16, p_full = p_half + 16, o_full = p_full + 16, o_free = o_full + 16, sc_full = o_free + 16,
+                   ended = sc_full + 32, job_full = ended + 8, job_free = job_full + 8 * kJobs, scanned = job_free + 8 * kJobs;
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     const CacheDev &c = a.c;
 
@@ -231,25 +289,33 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
     }
     const int count = (int)(sh.x1 - sh.x0);
     if (tid == 0) {
-        bar_init(q_full, 128);
+        bar_init(q_full, S::kQueryWarps);
         bar_init(q_free, 1);
         for (int i = 0; i < kStages; ++i) {
-            bar_init(kv_full + 8 * i, 128);
+            bar_init(kv_full + 8 * i, kKvArrive);
             bar_init(kv_free + 8 * i, 1);
         }
         for (int i = 0; i < 2; ++i) {
             bar_init(s_full + 8 * i, 1);
-            bar_init(p_full + 8 * i, 128);
+            bar_init(p_full + 8 * i, 4);
+            bar_init(p_half + 8 * i, 4);
             bar_init(o_full + 8 * i, 1);
-            bar_init(o_free + 8 * i, 128);
+            bar_init(o_free + 8 * i, 4);
         }
-        for (int i = 0; i < 4; ++i) bar_init(sc_full + 8 * i, 128);
+        for (int i = 0; i < 4; ++i) bar_init(sc_full + 8 * i, kKvArrive);
         bar_init(ended, 1);
+        for (int i = 0; i < kJobs; ++i) {
+            bar_init(job_full + 8 * i, 1);
+            bar_init(job_free + 8 * i, 8);
+        }
+        bar_init(scanned, 4);
+        bar_init(scanned + 8, 4);
+        for (int i = 0; i < 4; ++i) s_lost[i] = -1;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         shared_to_async();
         s_dead = 0;
     }
-    if (warp == 12) {
+    if (warp == 8) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&s_tmem)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
@@ -261,23 +327,24 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
 
     if (warp < 8) {
         // ================= softmax: a thread a row =================
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
         const int half = warp / 4, r = tid;  // row of the unit
         const uint32_t lanes = (uint32_t)(warp % 4) << 21;
         const uint32_t ts = tm + half * 128 + lanes, to = tm + 256 + half * 128 + lanes;
-        uint32_t n_s = 0, n_o = 0;
+        uint32_t n_s = 0, n_o = 0, n_scan = 0;
+        int x = 0;  // the CTA's tile
         bool ok = true;
-        // (a wait that gave up leaves `ok` false: the rest is walked through without waiting, the barriers between
-        // the threads of the CTA kept)
-        for (int x = 0, frag = 0; x < count; ++frag) {
-            const Unit &u = cu.u;
-            const int n = min(u.nt - cu.j, count - x);
+        for (int frag = 0;; ++frag) {
+            const Job &job = jobs[frag % kJobs];
+            const Unit &u = job.u;
+            ok = bar_wait(job_full + 8 * (frag % kJobs), frag / kJobs & 1, dead);
+            if (!ok) break;
+            const int n = job.n;
+            const bool last_job = job.last;
             if (half == 1 && u.rows <= 128) {
                 x += n;
-                if (x < count) {
-                    cu.j += n - 1;
-                    cu.next(a);
-                }
+                bar_arrive_warp(job_free + 8 * (frag % kJobs));
+                if (last_job) break;
                 continue;
             }
             const int gr = u.qt * 256 + r, t = quot(gr, c.div_g);
@@ -288,43 +355,86 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
             const int lo = u.kv - u.ql + quot(f0, c.div_g), hi = u.kv - u.ql + quot(f1, c.div_g);
             float mref = -INFINITY;  // the maximum that the weights refer to, times scale * log2(e)
             float2 l2 = make_float2(0.0f, 0.0f);
-            const int j0 = cu.j;
-            for (int j = 0; j < n; ++j) {
-                const int tile = j0 + j, base = (tile < u.ns ? tile : u.wf + tile - u.ns) * kTok;
-                const int slot = (x + j) & 3;
+            bool lost = false;  // values of V that were set to zero
+            const int ulo = u.lo, uhi = u.hi, ns = u.ns, skip = u.wf - u.ns;
+            for (int j = 0, tile = job.j0; j < n; ++j, ++tile, ++x) {
+                const int base = (tile < ns ? tile : tile + skip) * kTok;
+                const int slot = x & 3;
                 // (the scores first: a half that skips units may be ahead of the scales' barrier by a phase)
-                ok = ok && bar_wait(s_full + 8 * half, n_s & 1, dead) && bar_wait(sc_full + 8 * slot, (x + j) >> 2 & 1, dead);
-                ok = __all_sync(0xffffffffu, ok);
+                ok = bar_wait(s_full + 8 * half, n_s & 1, dead) && (FMT == kFmt16 || bar_wait(sc_full + 8 * slot, x >> 2 & 1, dead));
                 if (!ok) break;
                 ++n_s;
-                after_sync();
-                float s[kTok];
-#pragma unroll
-                for (int k = 0; k < kTok; k += 32) tm_load(s + k, ts + k);
-                tm_load_wait();
                 const float *const ks = scales + slot * 2 * kTok, *const vs = ks + kTok;
-                if constexpr (FMT != kFmt16) {
-#pragma unroll
-                    for (int k = 0; k < kTok; k += 4) {
-                        const float4 f = *reinterpret_cast<const float4 *>(ks + k);
-                        s[k] *= f.x;
-                        s[k + 1] *= f.y;
-                        s[k + 2] *= f.z;
-                        s[k + 3] *= f.w;
+                const bool masked = base + kTok - 1 > lo || (a.window > 0 && base <= hi - a.window && base + kTok > a.sinks);
+                if constexpr (FMT == kFmt16) {
+                    // (hidden from a row of either half: they share V)
+                    if (base + kTok - 1 > ulo || (a.window > 0 && base <= uhi - a.window && base + kTok > a.sinks)) {
+                        // a thread a token: is all of its V finite?
+                        bool bad = false;
+                        const char *const p = v_row<BF16>(a, u, base + (tid & 127));
+                        for (int d = 0; p && d < c.D; d += 8) bad |= lost_in<BF16>(__ldg(reinterpret_cast<const uint4 *>(p + d * 2)));
+                        const bool gone = LOAD == kTma && !p;  // no token of the unit: whatever was copied, or nothing
+                        int *const found = s_lost + half * 2 + (n_scan & 1);
+                        if (bad) *found = x;
+                        bar_arrive_warp(scanned + 8 * half);
+                        ok = bar_wait(scanned + 8 * half, n_scan & 1, dead);
+                        ++n_scan;
+                        lost |= *reinterpret_cast<volatile int *>(found) == x;
+                        if (__any_sync(0xffffffffu, bad || gone)) {
+                            const uint32_t v = 2 * x + 1;
+                            ok = ok && bar_wait(kv_full + 8 * (v % kStages), v / kStages & 1, dead);
+                            if (ok && (bad || gone)) clear_row<BF16, DP>(smem_addr(tiles + v % kStages * S::kTile), tid & 127, gone);
+                            shared_to_async();
+                            __syncwarp();
+                        }
+                        if (!ok) break;
                     }
                 }
-                const bool masked = base + kTok - 1 > lo || (a.window > 0 && base <= hi - a.window && base + kTok > a.sinks);
-                if (masked) {
-                    const int top = pos - base, low = a.window > 0 ? pos - a.window - base : -1, sink = a.sinks - base;
+                after_sync();
+                const int last = pos - base, low = a.window > 0 ? pos - a.window - base : -1, sink = a.sinks - base;
+                // 32 scores from tensor memory as they enter the softmax: times the scales of K, hidden ones -inf
+                auto enter = [&](float *s, int k0) {
+                    if constexpr (FMT != kFmt16) {
 #pragma unroll
-                    for (int k = 0; k < kTok; ++k)
-                        if (!(k <= top && (k > low || k < sink))) s[k] = -INFINITY;
-                }
-                float mx[4] = {s[0], s[1], s[2], s[3]};
+                        for (int k = 0; k < 32; k += 4) {
+                            const float4 f = *reinterpret_cast<const float4 *>(ks + k0 + k);
+                            s[k] *= f.x;
+                            s[k + 1] *= f.y;
+                            s[k + 2] *= f.z;
+                            s[k + 3] *= f.w;
+                        }
+                    }
+                    if (masked) {
 #pragma unroll
-                for (int k = 4; k < kTok; k += 4)
+                        for (int k = 0; k < 32; ++k)
+                            if (!(k0 + k <= last && (k0 + k > low || k0 + k < sink))) s[k] = -INFINITY;
+                    }
+                };
+                // The first 64 scores are read again for their weights: 128 would not fit the registers.
+                float sa[32], sb[64];
+                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                auto most = [&](const float *s) {
 #pragma unroll
-                    for (int z = 0; z < 4; ++z) mx[z] = fmaxf(mx[z], s[k + z]);
+                    for (int k = 0; k < 32; k += 8)
+#pragma unroll
+                        for (int z = 0; z < 4; ++z) mx[z] = fmaxf(fmaxf(mx[z], s[k + z]), s[k + 4 + z]);
+                };
+                tm_load(sb, ts);
+                tm_load(sb + 32, ts + 32);
+                tm_load_wait(sb);
+                tm_load_wait(sb + 32);
+                enter(sb, 0);
+                most(sb);
+                enter(sb + 32, 32);
+                most(sb + 32);
+                tm_load(sb, ts + 64);
+                tm_load(sb + 32, ts + 96);
+                tm_load_wait(sb);
+                tm_load_wait(sb + 32);
+                enter(sb, 64);
+                most(sb);
+                enter(sb + 32, 96);
+                most(sb + 32);
                 const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2;
                 const bool raise = top > mref + kLag;  // (from -inf: any number)
                 if (__any_sync(0xffffffffu, raise)) {
@@ -335,75 +445,86 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
                         // the sums that the products so far have left: they are done, since this tile's scores come after them
 #pragma unroll
                         for (int k = 0; k < DP; k += 32) {
-                            float o[32];
-                            tm_load(o, to + k);
-                            tm_load_wait();
+                            tm_load(sa, to + k);
+                            tm_load_wait(sa);
 #pragma unroll
-                            for (int z = 0; z < 32; ++z) o[z] *= f;
-                            tm_store(to + k, reinterpret_cast<uint32_t *>(o));
+                            for (int z = 0; z < 32; ++z) sa[z] *= f;
+                            tm_store(to + k, reinterpret_cast<uint32_t *>(sa));
+                            tm_store(to + k + 16, reinterpret_cast<uint32_t *>(sa) + 16);
                         }
                     }
                 }
                 const float neg = mref == -INFINITY ? 0.0f : -mref;
                 const float2 sc2 = make_float2(a.scale_log2, a.scale_log2), neg2 = make_float2(neg, neg);
-                uint32_t p[kTok / 2];
+                // the weights of 32 tokens, to the upper half of the scores' columns
+                auto weigh = [&](const float *s, int k0) {
+                    uint32_t p[16];
 #pragma unroll
-                for (int k = 0; k < kTok; k += 4) {
-                    float2 e = fma2(make_float2(s[k], s[k + 1]), sc2, neg2), g = fma2(make_float2(s[k + 2], s[k + 3]), sc2, neg2);
-                    e.x = exp2_fast(e.x);
-                    e.y = exp2_fast(e.y);
-                    g.x = exp2_fast(g.x);
-                    g.y = exp2_fast(g.y);
-                    l2 = add2(l2, add2(e, g));
-                    if constexpr (FMT != kFmt16) {
-                        const float4 f = *reinterpret_cast<const float4 *>(vs + k);
-                        e = mul2(e, make_float2(f.x * kLift, f.y * kLift));
-                        g = mul2(g, make_float2(f.z * kLift, f.w * kLift));
-                        if (masked) {  // a scale that is not finite stays away from a weight that the mask takes
-                            if (s[k] == -INFINITY) e.x = 0.0f;
-                            if (s[k + 1] == -INFINITY) e.y = 0.0f;
-                            if (s[k + 2] == -INFINITY) g.x = 0.0f;
-                            if (s[k + 3] == -INFINITY) g.y = 0.0f;
+                    for (int k = 0; k < 32; k += 4) {
+                        float2 e = fma2(make_float2(s[k], s[k + 1]), sc2, neg2), g = fma2(make_float2(s[k + 2], s[k + 3]), sc2, neg2);
+                        e.x = exp2_fast(e.x);
+                        e.y = exp2_fast(e.y);
+                        g.x = exp2_fast(g.x);
+                        g.y = exp2_fast(g.y);
+                        l2 = add2(l2, add2(e, g));
+                        if constexpr (FMT != kFmt16) {
+                            const float4 f = *reinterpret_cast<const float4 *>(vs + k0 + k);
+                            e = mul2(e, make_float2(f.x * kLift, f.y * kLift));
+                            g = mul2(g, make_float2(f.z * kLift, f.w * kLift));
+                            if (masked) {  // a scale that is not finite stays away from a weight that the mask takes
+                                if (s[k] == -INFINITY) e.x = 0.0f;
+                                if (s[k + 1] == -INFINITY) e.y = 0.0f;
+                                if (s[k + 2] == -INFINITY) g.x = 0.0f;
+                                if (s[k + 3] == -INFINITY) g.y = 0.0f;
+                            }
                         }
+                        p[k / 2] = pack16<BF16>(e.x, e.y);
+                        p[k / 2 + 1] = pack16<BF16>(g.x, g.y);
                     }
-                    p[k / 2] = pack16<BF16>(e.x, e.y);
-                    p[k / 2 + 1] = pack16<BF16>(g.x, g.y);
-                }
-                tm_store(ts, p);
-                tm_store(ts + 32, p + 32);
+                    tm_store(ts + 64 + k0 / 2, p);
+                };
+                tm_load(sa, ts);
+                weigh(sb, 64);
+                weigh(sb + 32, 96);
+                tm_store_wait();
+                before_sync();
+                bar_arrive_warp(p_half + 8 * half);  // the products of these may begin
+                tm_load_wait(sa);
+                tm_load(sb, ts + 32);
+                enter(sa, 0);
+                weigh(sa, 0);
+                tm_load_wait(sb);
+                enter(sb, 32);
+                weigh(sb, 32);
                 tm_store_wait();
                 if (s_bad[slot]) l2.x = __uint_as_float(0x7fffffffu);
                 before_sync();
-                bar_arrive(p_full + 8 * half);
+                bar_arrive_warp(p_full + 8 * half);
             }
             // ---- the unit ends here, for this CTA ----
-            ok = __all_sync(0xffffffffu, ok && bar_wait(o_full + 8 * half, n_o & 1, dead));
+            ok = ok && bar_wait(o_full + 8 * half, n_o & 1, dead);
+            if (!ok) break;
             ++n_o;
             after_sync();
             const float l = l2.x + l2.y;
-            const long long u0 = sh.x0 + x - j0, u1 = u0 + u.nt;
-            const bool whole = u0 >= sh.x0 && u1 <= sh.x1;
+            const bool whole = job.whole;
             const int hd = u.h * c.G + gr - t * c.G;
-            const int64_t slot = whole ? 0 : slot_of(sh, blockIdx.x, u0);
+            const int64_t slot = job.slot;
             char *const po = a.out + (int64_t)(u.q0 + t) * a.o_t + (int64_t)hd * a.o_h;
             float *const pw = a.part_o + (slot * 256 + r) * 128;
             const float inv = l == 0.0f ? 0.0f : 1.0f / (l * kLift);
 #pragma unroll
             for (int k = 0; k < DP; k += 32) {
-                if (!ok) break;
                 float o[32];
                 __syncwarp();
                 tm_load(o, to + k);
-                tm_load_wait();
+                tm_load_wait(o);
                 if constexpr (FMT == kFmt16) {
-                    bool bad = false;
-#pragma unroll
-                    for (int z = 0; z < 32; ++z) bad |= !(fabsf(o[z]) < INFINITY);
-                    if (bad && real && l == l) {
+                    if (lost && real) {
                         float y[32];
 #pragma unroll
                         for (int z = 0; z < 32; ++z) y[z] = o[z];
-                        mend<BF16>(a, u, j0, j0 + n, r, pos, mref == -INFINITY ? 0.0f : mref, k, y);
+                        add_lost<BF16>(a, u, job.j0, job.j0 + n, pos, k, y);
 #pragma unroll
                         for (int z = 0; z < 32; ++z) o[z] = y[z];
                     }
@@ -422,36 +543,38 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
             }
             __syncwarp();
             before_sync();
-            bar_arrive(o_free + 8 * half);
-            if (real && ok) {
+            bar_arrive_warp(o_free + 8 * half);
+            if (real) {
                 if (!whole) a.part_ml[slot * 256 + r] = make_float2(mref, l);
                 else if (a.lse) a.lse[(int64_t)(u.q0 + t) * c.Hq + hd] = l == 0.0f ? -INFINITY : (mref + log2f(l)) * 0.69314718f;
             }
             if (!whole) {
-                // both halves, or the one that has rows
-                const int threads = u.rows > 128 ? 256 : 128;
-                const int c0 = cta_of(sh, u0), c1 = cta_of(sh, u1 - 1);
+                // The warps that have the same rows of the unit, one a CTA: the last of them joins the parts, in the
+                // order of the CTAs whichever came last.
+                const int c0 = job.c0, c1 = job.c1;
+                uint32_t before = 0;
                 __threadfence();
-                named_sync(2, threads);
-                if (tid == 0) {
-                    const bool last = atomicAdd(a.done + c0, 1u) == (uint32_t)(c1 - c0);
-                    if (last) a.done[c0] = 0;
-                    s_last[frag != 0] = last;  // (only a CTA's first and last units are shared)
+                __syncwarp();
+                if (lane == 0) {
+                    before = atomicAdd(a.done + c0 * 8 + warp, 1u);
+                    if (before == (uint32_t)(c1 - c0)) a.done[c0 * 8 + warp] = 0;
                 }
-                named_sync(2, threads);
-                if (s_last[frag != 0]) {  // join the parts, in the order of the CTAs whichever came last: a warp a row
+                before = __shfl_sync(0xffffffffu, before, 0);
+                if (before == (uint32_t)(c1 - c0)) {
                     __threadfence();
-                    constexpr int kLanes = DP / 4;
-                    for (int q = tid / kLanes; q < u.rows; q += threads / kLanes) {
-                        const int d = tid % kLanes * 4;
+                    constexpr int kLanes = DP / 4;  // four elements a thread
+                    const int64_t s0 = job.slot0;
+                    const int end = min(u.rows, warp * 32 + 32);
+                    for (int q = warp * 32 + lane / kLanes; q < end; q += 32 / kLanes) {
+                        const int d = lane % kLanes * 4;
+                        auto at = [&](int k) { return (k == c0 ? s0 : 2 * (int64_t)k) * 256 + q; };
                         float mm = -INFINITY, ll = 0.0f;
-                        for (int k = c0; k <= c1; ++k) mm = fmaxf(mm, __ldcg(&a.part_ml[(int64_t)slot_of(sh, k, u0) * 256 + q].x));
+                        for (int k = c0; k <= c1; ++k) mm = fmaxf(mm, __ldcg(&a.part_ml[at(k)].x));
                         float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                         for (int k = c0; k <= c1; ++k) {
-                            const int64_t at = (int64_t)slot_of(sh, k, u0) * 256 + q;
-                            const float2 ml = __ldcg(a.part_ml + at);
+                            const float2 ml = __ldcg(a.part_ml + at(k));
                             const float f = ml.x == -INFINITY ? 0.0f : exp2_fast(ml.x - mm);
-                            const float4 w = __ldcg(reinterpret_cast<const float4 *>(a.part_o + at * 128 + d));
+                            const float4 w = __ldcg(reinterpret_cast<const float4 *>(a.part_o + at(k) * 128 + d));
                             ll += ml.y == 0.0f ? 0.0f : ml.y * f;
                             if (ml.x == -INFINITY && ml.y == 0.0f) continue;  // saw nothing
                             acc.x += w.x * f;
@@ -467,19 +590,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
                         if (a.lse && d == 0)
                             a.lse[(int64_t)(u.q0 + t2) * c.Hq + h2] = ll == 0.0f ? -INFINITY : (mm + log2f(ll)) * 0.69314718f;
                     }
+                    __syncwarp();
                 }
             }
-            x += n;
-            if (x < count) {
-                cu.j += n - 1;
-                cu.next(a);
-            }
+            bar_arrive_warp(job_free + 8 * (frag % kJobs));
+            if (last_job) break;
         }
-    } else if (warp < 12) {
-        // ================= K, V and Q to shared memory =================
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-        const int i = tid - 256;
-        uint32_t item = 0, frag = 0;
+    } else if (LOAD != kTma && warp >= 12) {
+        // ================= K and V to shared memory, by threads =================
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        const int i = tid - 384;
+        uint32_t item = 0;
         bool ok = true;
         // 16-bit copies complete in order: the barriers of the last two groups wait for theirs
         uint32_t w0 = 0, w1 = 0;
@@ -488,7 +609,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
             if (w1) {
                 copy_wait<2>();
                 shared_to_async();
-                bar_arrive(w1);
+                bar_arrive_warp(w1);
             }
             w1 = w0;
             w0 = bar;
@@ -496,8 +617,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
         auto drain = [&]() {
             copy_wait<0>();
             shared_to_async();
-            if (w1) bar_arrive(w1);
-            if (w0) bar_arrive(w0);
+            if (w1) bar_arrive_warp(w1);
+            if (w0) bar_arrive_warp(w0);
             w0 = w1 = 0;
         };
         // where token i of the tile at cursor p is, with its scales
@@ -529,16 +650,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
         constexpr int CH = FMT == kFmt16 ? DP / 8 : DP / 16, kStep = 128 / CH, kIts = kTok / kStep;
         const int ch = i % CH, r0 = i / CH;
         const bool in = ch * (FMT == kFmt16 ? 8 : 16) < c.D;
-        auto queries = [&](const Unit &u) {
-            constexpr int QC = DP / 8, QS = 128 / QC;
-            const int qc = i % QC;
-            for (int r = i / QC; r < 256; r += QS) {
-                const int gr = u.qt * 256 + r, t = quot(gr, c.div_g), hd = u.h * c.G + gr - t * c.G;
-                const bool real = r < u.rows && qc * 8 < c.D;
-                const int64_t at = real ? (int64_t)(u.q0 + t) * a.q_t + (int64_t)hd * a.q_h + qc * 16 : 0;
-                copy16(smem_addr(smem + r / 128 * S::kTile) + swizzled<DP>(r % 128, qc), a.q + at, real);
-            }
-        };
         auto put = [&](int x, const Found &f) {
             places[(x & 1) * kTok + i] = f.off;
             if constexpr (FMT != kFmt16) {
@@ -551,12 +662,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
         // stage of the next item, free to be written
         auto stage = [&]() {
             const uint32_t st = item % kStages, round = item / kStages;
-            if (round > 0 && ok) {
+            if (round > 0) {
                 if constexpr (FMT == kFmt16) {
-                    // a thread that has to wait hands over what it has copied first
-                    if (!bar_test(kv_free + 8 * st, (round - 1) & 1)) drain();
+                    // a warp that has to wait hands over what it has copied first
+                    if (!__all_sync(0xffffffffu, bar_test(kv_free + 8 * st, (round - 1) & 1))) drain();
                 }
-                ok = bar_wait(kv_free + 8 * st, (round - 1) & 1, dead);
+                ok = ok && bar_wait(kv_free + 8 * st, (round - 1) & 1, dead);
             }
             return st;
         };
@@ -581,21 +692,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
             for (int k = 0; k < S::kSlots; ++k) request(true);
         }
         for (int x = 0; x < count; ++x) {  // (cu stands at tile x, then at x + 1)
-            bar_arrive(sc_full + 8 * (x & 3));  // the tile's scales and flag
-            if (x == 0 || cu.j == 0) {
-                if constexpr (FMT == kFmt16) drain();
-                if (frag > 0 && ok) ok = bar_wait(q_free, (frag - 1) & 1, dead);
-                queries(cu.u);
-                if constexpr (FMT == kFmt16) {
-                    landed(q_full);
-                } else {
-                    copy_commit();
-                    copy_wait<0>();
-                    shared_to_async();
-                    bar_arrive(q_full);
-                }
-                ++frag;
-            }
+            bar_arrive_warp(sc_full + 8 * (x & 3));  // the tile's scales and flag
             const bool more = x + 1 < count;
             Found f{-1, 0.0f, 0.0f, false};
             if (more) {
@@ -608,11 +705,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
                     const uint32_t to = smem_addr(tiles + st * S::kTile);
                     const char *const from = y ? c.v : c.k;
 #pragma unroll
-                    for (int k = 0; k < kIts; ++k) {
-                        const int r = r0 + k * kStep;
-                        const int64_t off = places[(x & 1) * kTok + r];
-                        const bool have = in && off >= 0;
-                        copy16(to + swizzled<DP>(r, ch), from + (have ? off + ch * 16 : 0), have);
+                    for (int k0 = 0; k0 < kIts; k0 += 8) {
+                        int64_t off[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) off[k] = places[(x & 1) * kTok + r0 + (k0 + k) * kStep];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            const bool have = in && off[k] >= 0;
+                            copy16(to + swizzled<DP>(r0 + (k0 + k) * kStep, ch), from + (have ? off[k] + ch * 16 : 0), have);
+                        }
                     }
                     landed(kv_full + 8 * st);
                 }
@@ -644,66 +745,107 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
                         request(ahead / (2 * kIts) <= (uint32_t)x + (more ? 1 : 0));
                     }
                     shared_to_async();
-                    bar_arrive(kv_full + 8 * st);
+                    bar_arrive_warp(kv_full + 8 * st);
                 }
             }
         }
         if constexpr (FMT == kFmt16) drain();
         copy_wait<0>();
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-        if (warp == 12 && lane == 0) {
-            // ================= products =================
-            constexpr uint32_t kQK = shape_of<BF16, kTok, false>(), kPV = shape_of<BF16, DP, true>();
-            const uint32_t sq = smem_addr(smem), sk = smem_addr(tiles);
-            uint32_t item = 0, n_p[2] = {0, 0}, n_o[2] = {0, 0};
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        if (LOAD == kTma && (warp == 9 || warp == 10)) {
+            // ================= K and V to shared memory, by the copy engine =================
+            // lane i: box i of the tile; warp 9 takes K, warp 10 V
+            const int box = in.m.box;
+            const bool is_v = warp == 10;
+            const CUtensorMap *const map = is_v ? &in.m.v : &in.m.k;
+            uint32_t item = is_v;
             bool ok = true;
-            auto scores = [&](int h, uint32_t st) {
-#pragma unroll
-                for (int k = 0; k < DP / 16; ++k) {
-                    const uint32_t at = (k / 4) * S::kPanel + (k % 4) * 32;
-                    mma_ss(tm + h * 128, operand(sq + h * S::kTile + at, 16), operand(sk + st * S::kTile + at, 16), kQK, k > 0);
+            auto look = [&](int &place, bool &bad) {
+                const int t = cu.base() + lane * box;
+                bad = false;
+                if (lane * box >= kTok || t > cu.u.hi || (a.window > 0 && t + box - 1 <= cu.u.lo - a.window && t >= a.sinks)) return -1;
+                const int blk = (int)block_of(c, a.b, cu.u.s, t, place);
+                if (blk < 0) {
+                    bad = true;
+                    report(c.status, kEInval);
                 }
-                commit(s_full + 8 * h);
+                return blk;
             };
-            auto full = [&](uint32_t it) { return bar_wait(kv_full + 8 * (it % kStages), it / kStages & 1, dead); };
-            for (int x = 0, frag = 0; x < count && ok; ++frag) {
-                const int n = min(cu.u.nt - cu.j, count - x), nh = cu.u.rows > 128 ? 2 : 1;
-                ok = bar_wait(q_full, frag & 1, dead) && full(item);
-                if (!ok) break;
-                after_sync();
-                for (int h = 0; h < nh; ++h) scores(h, item % kStages);
-                commit(kv_free + 8 * (item % kStages));
-                if (n == 1) commit(q_free);
-                ++item;
-                for (int j = 0; j < n && ok; ++j) {
-                    const bool more = j + 1 < n;
-                    const uint32_t sv = item % kStages, sk1 = (item + 1) % kStages;
-                    ok = full(item) && (!more || full(item + 1));
-                    for (int h = 0; h < nh && ok; ++h) {
-                        ok = bar_wait(p_full + 8 * h, n_p[h] & 1, dead) &&
-                             (j > 0 || n_o[h] == 0 || bar_wait(o_free + 8 * h, (n_o[h] - 1) & 1, dead));
-                        if (!ok) break;
-                        ++n_p[h];
-                        after_sync();
+            int place = 0;
+            bool bad = false;
+            int blk = look(place, bad);
+            for (int x = 0; x < count; ++x) {
+                const bool more = x + 1 < count;
+                const int h = cu.u.h, now = blk, at = place;
+                const unsigned any = __ballot_sync(0xffffffffu, bad), boxes = __popc(__ballot_sync(0xffffffffu, now >= 0));
+                if (more) {
+                    cu.next(a);
+                    blk = look(place, bad);
+                }
+                if (!is_v && lane == 0) {
+                    s_bad[x & 3] = any != 0;
+                    bar_arrive(sc_full + 8 * (x & 3));
+                }
+                const uint32_t st = item % kStages, round = item / kStages;
+                item += 2;
+                if (round > 0) ok = ok && bar_wait(kv_free + 8 * st, (round - 1) & 1, dead);
+                if (!ok) continue;
+                const uint32_t bar = kv_full + 8 * st, to = smem_addr(tiles + st * S::kTile) + lane * box * 128;
+                if (lane == 0)
+                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(boxes * box * 2 * DP) : "memory");
+                __syncwarp();
+                if (now >= 0) {
 #pragma unroll
-                        for (int k = 0; k < kTok / 16; ++k)
-                            mma_ts(tm + 256 + h * 128, tm + h * 128 + k * 8, operand(sk + sv * S::kTile + k * 2048, S::kPanel), kPV,
-                                   j > 0 || k > 0);
-                        if (more) {
-                            scores(h, sk1);
-                        } else {
-                            commit(o_full + 8 * h);
-                            ++n_o[h];
+                    for (int p = 0; p < DP / 64; ++p)
+                        asm volatile(
+                            "cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(
+                                to + p * S::kPanel), "l"(map), "r"(bar), "r"(p * 64), "r"(at), "r"(h), "r"(now)
+                            : "memory");
+                }
+            }
+        } else if (warp >= S::kQueryWarp && warp < S::kQueryWarp + S::kQueryWarps) {
+            // ================= queries to shared memory =================
+            constexpr int QC = DP / 8, QS = S::kQueryWarps * 32 / QC;
+            const int i = tid - S::kQueryWarp * 32, qc = i % QC;
+            bool ok = true;
+            for (int x = 0, frag = 0; x < count; ++frag) {
+                const Unit &u = cu.u;
+                const int n = min(u.nt - cu.j, count - x);
+                if (i < 32) {
+                    if (frag >= kJobs) ok = ok && bar_wait<true>(job_free + 8 * (frag % kJobs), (frag / kJobs - 1) & 1, dead);
+                    if (ok && i == 0) {
+                        Job &job = jobs[frag % kJobs];
+                        const long long u0 = sh.x0 + x - cu.j, u1 = u0 + u.nt;
+                        job.u = u;
+                        job.j0 = cu.j;
+                        job.n = n;
+                        job.whole = u0 >= sh.x0 && u1 <= sh.x1;
+                        job.last = x + n >= count;
+                        job.c0 = job.c1 = job.slot = job.slot0 = 0;
+                        if (!job.whole) {
+                            job.c0 = cta_of(sh, u0);
+                            job.c1 = cta_of(sh, u1 - 1);
+                            job.slot = slot_of(sh, blockIdx.x, u0);
+                            job.slot0 = slot_of(sh, job.c0, u0);
                         }
+                        bar_arrive(job_full + 8 * (frag % kJobs));
                     }
-                    if (!ok) break;
-                    commit(kv_free + 8 * sv);
-                    if (more) {
-                        commit(kv_free + 8 * sk1);
-                        if (j + 2 == n) commit(q_free);
+                }
+                __syncwarp();
+                if (frag > 0) ok = ok && bar_wait<true>(q_free, (frag - 1) & 1, dead);
+                if (ok) {
+#pragma unroll 4
+                    for (int r = i / QC; r < 256; r += QS) {
+                        const int gr = u.qt * 256 + r, t = quot(gr, c.div_g), hd = u.h * c.G + gr - t * c.G;
+                        const bool real = r < u.rows && qc * 8 < c.D;
+                        const int64_t at = real ? (int64_t)(u.q0 + t) * a.q_t + (int64_t)hd * a.q_h + qc * 16 : 0;
+                        copy16(smem_addr(smem + r / 128 * S::kTile) + swizzled<DP>(r % 128, qc), a.q + at, real);
                     }
-                    item += more ? 2 : 1;
+                    copy_commit();
+                    copy_wait<0>();
+                    shared_to_async();
+                    bar_arrive_warp(q_full);
                 }
                 x += n;
                 if (x < count) {
@@ -711,8 +853,89 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
                     cu.next(a);
                 }
             }
+        } else if (warp == 8) {
+            // ================= products: the warp waits, one thread issues =================
+            const bool one = elect();
+            constexpr uint32_t kQK = shape_of<BF16, kTok, false>(), kPV = shape_of<BF16, DP, true>();
+            const uint32_t sq = smem_addr(smem), sk = smem_addr(tiles);
+            uint32_t item = 0, n_p0 = 0, n_p1 = 0, n_o0 = 0, n_o1 = 0;
+            bool ok = true;
+            auto scores = [&](int h, uint32_t st) {
+                if (!one) return;
+                const uint64_t dq = operand(sq + h * S::kTile, 16), dk = operand(sk + st * S::kTile, 16);
+#pragma unroll
+                for (int k = 0; k < DP / 16; ++k) {
+                    constexpr uint32_t kStep16 = 32 >> 4, kPanel16 = S::kPanel >> 4;  // addresses in the descriptor count 16 bytes
+                    const uint32_t at = (k / 4) * kPanel16 + (k % 4) * kStep16;
+                    mma_ss(tm + h * 128, dq + at, dk + at, kQK, k > 0);
+                }
+                commit(s_full + 8 * h);
+            };
+            auto full = [&](uint32_t it) { return bar_wait(kv_full + 8 * (it % kStages), it / kStages & 1, dead); };
+            // one half's products of tile j: its sums, then its scores of the next tile
+            auto half_tile = [&](int h, uint32_t &n_p, uint32_t &n_o, bool first, bool more, uint64_t dv, uint32_t st) {
+                ok = bar_wait(p_half + 8 * h, n_p & 1, dead) && (!first || n_o == 0 || bar_wait(o_free + 8 * h, (n_o - 1) & 1, dead));
+                if (!ok) return;
+                after_sync();
+                const uint32_t o = tm + 256 + h * 128, p = tm + h * 128 + 64;
+                // the later half of the tokens first, as their weights come
+                if (one)
+#pragma unroll
+                    for (int k = kTok / 32; k < kTok / 16; ++k) mma_ts(o, p + k * 8, dv + k * (2048 >> 4), kPV, !first || k > kTok / 32);
+                __syncwarp();
+                ok = bar_wait(p_full + 8 * h, n_p & 1, dead);
+                if (!ok) return;
+                after_sync();
+                if (one) {
+#pragma unroll
+                    for (int k = 0; k < kTok / 32; ++k) mma_ts(o, p + k * 8, dv + k * (2048 >> 4), kPV, true);
+                }
+                if (more) scores(h, st);
+                else if (one) commit(o_full + 8 * h);
+                __syncwarp();
+                ++n_p;
+                n_o += !more;
+            };
+            for (int frag = 0; ok; ++frag) {
+                ok = bar_wait(q_full, frag & 1, dead);
+                if (!ok) break;
+                const Job &job = jobs[frag % kJobs];
+                const int n = job.n;
+                const bool two = job.u.rows > 128, last = job.last;
+                ok = full(item);
+                if (!ok) break;
+                after_sync();
+                scores(0, item % kStages);
+                if (two) scores(1, item % kStages);
+                if (one) {
+                    commit(kv_free + 8 * (item % kStages));
+                    if (n == 1) commit(q_free);
+                }
+                __syncwarp();
+                ++item;
+                for (int j = 0; j < n && ok; ++j) {
+                    const bool more = j + 1 < n;
+                    const uint32_t sv = item % kStages, sk1 = (item + 1) % kStages;
+                    ok = full(item) && (!more || full(item + 1));
+                    if (!ok) break;
+                    const uint64_t dv = operand(sk + sv * S::kTile, S::kPanel);
+                    half_tile(0, n_p0, n_o0, j == 0, more, dv, sk1);
+                    if (two && ok) half_tile(1, n_p1, n_o1, j == 0, more, dv, sk1);
+                    if (!ok) break;
+                    if (one) {
+                        commit(kv_free + 8 * sv);
+                        if (more) {
+                            commit(kv_free + 8 * sk1);
+                            if (j + 2 == n) commit(q_free);
+                        }
+                    }
+                    __syncwarp();
+                    item += more ? 2 : 1;
+                }
+                if (last) break;
+            }
             if (!ok) {  // what was issued ends before its memory is given back
-                commit(ended);
+                if (one) commit(ended);
                 for (uint32_t i = 0; i < kSpin && !bar_test(ended, 0); ++i) {
                 }
             }
@@ -720,46 +943,79 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
         __syncwarp();
     }
     __syncthreads();
-    if (warp == 12) {
+    if (warp == 8) {
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tm));
         if (lane == 0 && *dead) report(c.status, kECuda);
     }
     chain_next();
 }
 
-using Kernel = void (*)(const AttendLaunch);
+using Kernel = void (*)(const ChunkLaunch);
+struct Pick {
+    Kernel k;
+    size_t smem;
+};
 
-template <int FMT, int DP>
-Kernel pick_type(bool bf16, size_t &smem) {
-    smem = Shape<DP, FMT>::kSmem;
-    return bf16 ? k_attend_chunk<true, FMT, DP> : k_attend_chunk<false, FMT, DP>;
+template <int FMT, int DP, int LOAD>
+Pick pick_type(bool bf16) {
+    using S = Shape<DP, FMT, LOAD>;
+    return {bf16 ? k_attend_chunk<true, FMT, DP, LOAD> : k_attend_chunk<false, FMT, DP, LOAD>, S::kSmem};
 }
-Kernel pick_kernel(bool bf16, int fmt, int D, size_t &smem) {
-    if (D <= 64)
-        return fmt == kFmt16 ? pick_type<kFmt16, 64>(bf16, smem)
-             : fmt == kFmtE4M3 ? pick_type<kFmtE4M3, 64>(bf16, smem) : pick_type<kFmtInt8, 64>(bf16, smem);
-    return fmt == kFmt16 ? pick_type<kFmt16, 128>(bf16, smem)
-         : fmt == kFmtE4M3 ? pick_type<kFmtE4M3, 128>(bf16, smem) : pick_type<kFmtInt8, 128>(bf16, smem);
+template <int DP>
+Pick pick_load(bool bf16, int fmt, bool tma) {
+    return fmt == kFmtE4M3 ? pick_type<kFmtE4M3, DP, kConvert>(bf16)
+         : fmt == kFmtInt8 ? pick_type<kFmtInt8, DP, kConvert>(bf16)
+         : tma             ? pick_type<kFmt16, DP, kTma>(bf16)
+                           : pick_type<kFmt16, DP, kGather>(bf16);
 }
+Pick pick(bool bf16, int fmt, int D, bool tma) { return D <= 64 ? pick_load<64>(bf16, fmt, tma) : pick_load<128>(bf16, fmt, tma); }
 
 }  // namespace
 
+int encode_maps(const CacheDev &c, bool bf16, CacheMaps &m) {
+    m.box = 0;
+    const int box = c.b & -c.b;  // the largest power of two in a block
+    if (box < 8) return 0;
+    void *fn = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+        found != cudaDriverEntryPointSuccess || !fn) {
+        cudaGetLastError();
+        return 0;
+    }
+    using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    const cuuint32_t tokens = (cuuint32_t)(box < kTok ? box : kTok);
+    const cuuint64_t dims[4] = {(cuuint64_t)c.D, (cuuint64_t)c.b, (cuuint64_t)c.H, (cuuint64_t)c.nb};
+    // (the stride of a dimension of one element is never used, but has to be one)
+    const cuuint64_t strides[3] = {(cuuint64_t)(c.b > 1 ? c.st : 256), (cuuint64_t)(c.H > 1 ? c.sh : 256), (cuuint64_t)(c.nb > 1 ? c.sb : 256)};
+    const cuuint32_t boxes[4] = {64, tokens, 1, 1}, steps[4] = {1, 1, 1, 1};
+    for (cuuint64_t s : strides)
+        if (s == 0 || s >= (1ull << 40)) return 0;
+    for (int y = 0; y < 2; ++y)
+        if (reinterpret_cast<Encode>(fn)(y ? &m.v : &m.k, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4,
+                                         y ? c.v : c.k, dims, strides, boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+            return 0;
+    return m.box = (int)tokens;
+}
+
 cudaError_t attend_chunk_init() {
     for (int bf16 = 0; bf16 < 2; ++bf16)
-        for (int fmt = 0; fmt < 3; ++fmt)
+        for (int load = 0; load < 4; ++load)
             for (int D = 64; D <= 128; D += 64) {
-                size_t smem;
-                const Kernel k = pick_kernel(bf16, fmt, D, smem);
-                const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+                const Pick p = pick(bf16, load == 3 ? (int)kFmt16 : load, D, load == 3);
+                const cudaError_t e = cudaFuncSetAttribute(p.k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)p.smem);
                 if (e != cudaSuccess) return e;
             }
     return cudaSuccess;
 }
 
-cudaError_t launch_attend_chunk(const AttendLaunch &a, bool bf16, int fmt, int ctas, cudaStream_t st) {
-    size_t smem;
-    const Kernel k = pick_kernel(bf16, fmt, a.c.D, smem);
-    return launch_chained(k, ctas, kThreads, smem, st, a);
+cudaError_t launch_attend_chunk(const AttendLaunch &a, const CacheMaps &m, bool bf16, int fmt, int ctas, cudaStream_t st) {
+    const Pick p = pick(bf16, fmt, a.c.D, m.box > 0);
+    return launch_chained(p.k, ctas, kThreads, p.smem, st, ChunkLaunch{a, m});
 }
 
 }  // namespace lr

@@ -3,6 +3,7 @@
 #pragma once
 
 #include <cstdint>
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -84,14 +85,22 @@ struct AttendLaunch {
     int32_t row_lo, row_hi;      // sequences with this many rows (tokens x query heads a KV head) are this launch's
     float *part_o;               // [slots][rows][DP] sums of weighted V
     float2 *part_ml;             // [slots][rows] running maximum (log2) and sum
-    uint32_t *done;              // [CTAs] fragments finished of the unit that began in the CTA; zero between calls
+    uint32_t *done;              // parts finished of the unit that began in a CTA ([CTAs]; chunk kernel [CTAs][8 warps]); zero
+                                 // between calls
 };
 constexpr int kStepRows = 64;   // rows of a unit of the step kernel, at most
 cudaError_t launch_attend_step(const AttendLaunch &a, bool bf16, int fmt, int rows, int ctas, cudaStream_t st);
 cudaError_t attend_step_init();
 int attend_step_ctas(int sms);  // CTAs of a launch, at most
 constexpr int kChunkRows = 256;  // rows of a unit of the chunk kernel; one CTA an SM
-cudaError_t launch_attend_chunk(const AttendLaunch &a, bool bf16, int fmt, int ctas, cudaStream_t st);
+// Tensor maps of a 16-bit cache's K and V: boxes of 64 elements of `box` tokens, the largest number that
+// divides a block and the chunk kernel's tiles; box 0: none (blocks that are no multiple of 8 tokens).
+struct CacheMaps {
+    CUtensorMap k, v;
+    int32_t box;
+};
+int encode_maps(const CacheDev &c, bool bf16, CacheMaps &m);  // the box, 0 if there can be none
+cudaError_t launch_attend_chunk(const AttendLaunch &a, const CacheMaps &m, bool bf16, int fmt, int ctas, cudaStream_t st);
 cudaError_t attend_chunk_init();
 
 }  // namespace lr

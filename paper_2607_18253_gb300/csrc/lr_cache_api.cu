@@ -16,6 +16,7 @@ struct lr_cache {
     lr_cache_config cfg{};
     lr::CacheDev dev{};
     bool bf16 = true;
+    lr::CacheMaps maps{};
     struct Parts {  // workspace of an attention kernel
         float *o = nullptr;
         float2 *ml = nullptr;
@@ -54,12 +55,12 @@ void free_all(lr_cache *c) {
     }
 }
 
-// Two slots of partial rows a CTA and a counter, at zero.
-cudaError_t alloc_parts(lr_cache::Parts &p, size_t ctas, size_t rows) {
+// Two slots of partial rows a CTA, and counters at zero.
+cudaError_t alloc_parts(lr_cache::Parts &p, size_t ctas, size_t rows, size_t counters) {
     cudaError_t e = cudaMalloc(&p.o, 2 * ctas * rows * 128 * sizeof(float));
     if (e == cudaSuccess) e = cudaMalloc(&p.ml, 2 * ctas * rows * sizeof(float2));
-    if (e == cudaSuccess) e = cudaMalloc(&p.done, ctas * sizeof(uint32_t));
-    if (e == cudaSuccess) e = cudaMemset(p.done, 0, ctas * sizeof(uint32_t));
+    if (e == cudaSuccess) e = cudaMalloc(&p.done, counters * sizeof(uint32_t));
+    if (e == cudaSuccess) e = cudaMemset(p.done, 0, counters * sizeof(uint32_t));
     return e;
 }
 
@@ -143,10 +144,11 @@ int lr_cache_create(const lr_cache_config *cfg, lr_cache **out) {
     d.b = cfg->block_size;
     d.div_b = lr::fast_div(d.b);
     d.div_g = lr::fast_div(d.G);
+    if (cfg->format == LR_CACHE_16BIT) lr::encode_maps(d, c->bf16, c->maps);
     e = cudaMalloc(&d.status, 16);
     if (e == cudaSuccess) e = cudaMemset(d.status, 0, 16);
-    if (e == cudaSuccess) e = alloc_parts(c->step, lr::attend_step_ctas(c->sms), lr::kStepRows);
-    if (e == cudaSuccess) e = alloc_parts(c->chunk, c->sms, lr::kChunkRows);
+    if (e == cudaSuccess) e = alloc_parts(c->step, lr::attend_step_ctas(c->sms), lr::kStepRows, lr::attend_step_ctas(c->sms));
+    if (e == cudaSuccess) e = alloc_parts(c->chunk, c->sms, lr::kChunkRows, 8 * (size_t)c->sms);
     if (e != cudaSuccess) return bail(LR_ENOMEM, cudaGetErrorString(e));
     *out = c;
     return LR_OK;
@@ -241,7 +243,7 @@ int lr_cache_attend(lr_cache *c, const lr_cache_batch *b, int32_t T, const void 
         a.part_o = c->chunk.o;
         a.part_ml = c->chunk.ml;
         a.done = c->chunk.done;
-        cudaError_t e = lr::launch_attend_chunk(a, c->bf16, c->cfg.format, c->sms, st);
+        cudaError_t e = lr::launch_attend_chunk(a, c->maps, c->bf16, c->cfg.format, c->sms, st);
         if (e != cudaSuccess) return cuda_fail(c, e, "attention launch");
         if (all) return LR_OK;
     }
@@ -263,6 +265,10 @@ int lr_cache_status(lr_cache *c, void *stream) {
     if (e == cudaSuccess) e = cudaStreamSynchronize(st);
     if (e == cudaSuccess) e = cudaMemsetAsync(c->dev.status, 0, sizeof(int32_t), st);
     if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+    if (e == cudaSuccess && h == LR_ECUDA) {  // a kernel gave up: its counts of finished parts start again
+        e = cudaMemsetAsync(c->chunk.done, 0, 8 * (size_t)c->sms * sizeof(uint32_t), st);
+        if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+    }
     if (e != cudaSuccess) return cuda_fail(c, e, "status");
     return h;
 }
