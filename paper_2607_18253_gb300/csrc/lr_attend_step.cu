@@ -68,7 +68,7 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint3
 
 // BF16: the type of q and of the products.  WM: warps by rows (16 each); the others split the tokens.
 template <bool BF16, int FMT, int DP, int WM>
-__global__ void __launch_bounds__(kThreads) k_attend_step(const __grid_constant__ AttendLaunch a) {
+__global__ void __launch_bounds__(kThreads) k_attend_rows(const __grid_constant__ AttendLaunch a) {
     using S = Shape<DP, FMT>;
     constexpr int kRows = 16 * WM, WN = 4 / WM, kMine = kTok / WN, NB = kMine / 8, KS = DP / 16;
     // with 8-bit V the weights carry its scales: in fp16 they are kept away from its subnormal
@@ -124,11 +124,14 @@ __global__ void __launch_bounds__(kThreads) k_attend_step(const __grid_constant_
         constexpr int kStep = kThreads / S::kChunks;
         const int ch = tid % S::kChunks, r0 = tid / S::kChunks;
         const bool in = ch * 16 < c.D * (FMT == kFmt16 ? 2 : 1);
+        int64_t offs[kTok / kStep];  // (all read before the first copy, which the compiler would not move them past)
 #pragma unroll
-        for (int r = r0; r < kTok; r += kStep) {
-            const int64_t off = pl[r].x;
-            const bool ok = in && off >= 0;
-            const int64_t at = ok ? off + ch * 16 : 0;
+        for (int k = 0; k < kTok / kStep; ++k) offs[k] = pl[r0 + k * kStep].x;
+#pragma unroll
+        for (int k = 0; k < kTok / kStep; ++k) {
+            const int r = r0 + k * kStep;
+            const bool ok = in && offs[k] >= 0;
+            const int64_t at = ok ? offs[k] + ch * 16 : 0;
             copy16(smem_addr(st + r * S::kRow + swizzle<DP, FMT, false>(r, ch) * 16), c.k + at, ok);
             copy16(smem_addr(st + S::kHalf + r * S::kRow + swizzle<DP, FMT, true>(r, ch) * 16), c.v + at, ok);
         }
@@ -462,14 +465,16 @@ __global__ void __launch_bounds__(kThreads) k_attend_step(const __grid_constant_
             if (s_last) {  // join the parts, in the order of the CTAs whichever came last
                 __threadfence();
                 constexpr int kLanes = DP / 4;  // four elements a thread
+                const int64_t s0 = slot_of(sh, c0, u0);  // (a unit is the first of every later CTA)
+                auto at_of = [&](int k, int r) { return (k == c0 ? s0 : 2 * (int64_t)k) * kStepRows + r; };
                 for (int r = tid / kLanes; r < u.rows; r += kThreads / kLanes) {
                     const int d = tid % kLanes * 4;
                     float mm = -INFINITY;
-                    for (int k = c0; k <= c1; ++k) mm = fmaxf(mm, __ldcg(&a.part_ml[(int64_t)slot_of(sh, k, u0) * kStepRows + r].x));
+                    for (int k = c0; k <= c1; ++k) mm = fmaxf(mm, __ldcg(&a.part_ml[at_of(k, r)].x));
                     float ll = 0.0f;
                     float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                     for (int k = c0; k <= c1; ++k) {
-                        const int64_t at = (int64_t)slot_of(sh, k, u0) * kStepRows + r;
+                        const int64_t at = at_of(k, r);
                         const float2 ml = __ldcg(a.part_ml + at);
                         const float f = ml.x == -INFINITY ? 0.0f : exp2_fast(ml.x - mm);
                         const float4 w = __ldcg(reinterpret_cast<const float4 *>(a.part_o + at * 128 + d));
@@ -496,11 +501,423 @@ __global__ void __launch_bounds__(kThreads) k_attend_step(const __grid_constant_
     chain_next();
 }
 
+// ---- up to 16 rows: every warp on its own ----
+//
+// A tile's tokens are divided over the four warps, and a warp copies, waits for and multiplies its own:
+// nothing is exchanged until the unit ends (the warps then join their sums through the stages just used), so
+// no warp waits for another's copies.
+template <int DP, int FMT>
+struct Solo {
+    static constexpr int kRow = DP * (FMT == kFmt16 ? 2 : 1);
+    static constexpr int kChunks = kRow / 16;
+    static constexpr int kMine = FMT == kFmt16 ? 16 : 32;  // tokens of a warp: its stage also takes 16 rows of sums
+    static constexpr int kTile = 4 * kMine;
+    static constexpr int kHalf = kMine * kRow;
+    static constexpr int kStage = 2 * kHalf;
+    static constexpr int kStages = 3;
+    static constexpr int kScales = FMT == kFmt16 ? 0 : kStages * 2 * kMine * 4;
+    static constexpr int kWarp = kStages * kStage + kScales;
+    static constexpr int kSmem = 4 * kWarp + 4 * 16 * 8;
+    static_assert(kStage >= 16 * DP * 4, "room for a warp's sums");
+};
+
+template <bool BF16, int FMT, int DP>
+__global__ void __launch_bounds__(kThreads, 2) k_attend_step(const __grid_constant__ AttendLaunch a) {
+    using S = Solo<DP, FMT>;
+    constexpr int kRows = 16, kMine = S::kMine, NB = kMine / 8, KS = DP / 16;
+    constexpr float kLift = FMT != kFmt16 && !BF16 ? 64.0f : 1.0f;  // as above
+    extern __shared__ __align__(128) char smem[];
+    __shared__ int s_last, s_bad;  // (s_bad: 1 + the last tile of the unit in which a block was out of range)
+    __shared__ long long s_scratch[kThreads / 32 + 2];
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, g = lane / 4, i4 = lane % 4;
+    char *const stages = smem + warp * S::kWarp;
+    float *const scales = reinterpret_cast<float *>(stages + S::kStages * S::kStage);  // [stage][K, V][token]
+    float2 *const s_ml = reinterpret_cast<float2 *>(smem + 4 * S::kWarp);              // [warp][row]
+    const CacheDev &c = a.c;
+
+    chain_wait();
+    if (tid == 0) s_bad = 0;
+    Cursor<kRows, S::kTile> cu, lk;
+    Share sh;
+    if (!take_share<kRows, S::kTile, kThreads>(a, cu, sh, s_scratch)) {
+        chain_next();
+        return;
+    }
+    const int count = (int)(sh.x1 - sh.x0);
+    lk = cu;
+
+    // where lane l's token of the tile at lk is (in bytes from the cache's start; the scales in floats)
+    int64_t off = -1, soff = 0;
+    bool bad = false, bad_next = false;
+    auto look = [&]() {
+        const int t = lk.base() + warp * kMine + lane;
+        off = -1;
+        soff = 0;
+        // what no row of the unit sees is not looked up (its block may be gone): zeros
+        if (lane >= kMine || t > lk.u.hi || (a.window > 0 && t <= lk.u.lo - a.window && t >= a.sinks)) return;
+        int place;
+        const int64_t blk = block_of(c, a.b, lk.u.s, t, place);
+        if (blk < 0) {
+            bad_next = true;
+            report(c.status, kEInval);
+            return;
+        }
+        off = blk * c.sb + place * c.st + lk.u.h * c.sh;
+        soff = blk * c.ssb + place * c.sst + lk.u.h * c.ssh;
+    };
+    auto issue = [&](int tile) {
+        char *const st = stages + tile % S::kStages * S::kStage;
+        constexpr int kStep = 32 / S::kChunks;
+        const int ch = lane % S::kChunks, r0 = lane / S::kChunks;
+        const bool in = ch * 16 < c.D * (FMT == kFmt16 ? 2 : 1);
+#pragma unroll
+        for (int r1 = 0; r1 < kMine; r1 += kStep) {
+            const int r = r1 + r0;
+            const int64_t o = __shfl_sync(0xffffffffu, off, r);
+            const bool ok = in && o >= 0;
+            const int64_t at = ok ? o + ch * 16 : 0;
+            copy16(smem_addr(st + r * S::kRow + swizzle<DP, FMT, false>(r, ch) * 16), c.k + at, ok);
+            copy16(smem_addr(st + S::kHalf + r * S::kRow + swizzle<DP, FMT, true>(r, ch) * 16), c.v + at, ok);
+        }
+        if constexpr (FMT != kFmt16) {
+            float *const to = scales + tile % S::kStages * 2 * kMine + lane;
+            copy4(smem_addr(to), c.ks + soff, off >= 0);
+            copy4(smem_addr(to + kMine), c.vs + soff, off >= 0);
+        }
+    };
+    // (bad tiles: a bit for each tile on its way)
+    unsigned bad_tiles = 0;
+    for (int t = 0; t < S::kStages - 1; ++t) {
+        if (t < count) {
+            bad_next = false;
+            look();
+            if (__any_sync(0xffffffffu, bad_next)) bad_tiles |= 1u << t;
+            issue(t);
+            if (t + 1 < count) lk.next(a);
+        }
+        copy_commit();
+    }
+    if (S::kStages - 1 < count) {
+        bad_next = false;
+        look();
+    }
+
+    uint32_t q[KS][4];
+    float o[2 * KS][4], m[2], l[2];
+    int pos[2];
+    for (int x = 0; x < count; ++x) {
+        const Unit &u = cu.u;
+        if (x == 0 || cu.j == 0) {  // a new unit: its queries, straight to the registers that multiply them
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                const int r = g + y * 8;
+                const int t = quot(r, c.div_g), hd = r - t * c.G;
+                const bool ok = r < u.rows;
+                pos[y] = ok ? u.kv - u.ql + t : -1;
+                const char *const p = a.q + (int64_t)(u.q0 + t) * a.q_t + (int64_t)(u.h * c.G + hd) * a.q_h;
+#pragma unroll
+                for (int k = 0; k < KS; ++k) {
+                    if constexpr (FMT == kFmt16) {
+#pragma unroll
+                        for (int z = 0; z < 2; ++z) {
+                            const int d = k * 16 + z * 8 + 2 * i4;
+                            q[k][y + 2 * z] = ok && d < c.D ? __ldg(reinterpret_cast<const uint32_t *>(p + d * 2)) : 0u;
+                        }
+                    } else {  // four neighbouring elements, the order in which the codes lie in a register
+                        const int d = (k / 4) * 64 + i4 * 16 + (k % 4) * 4;
+                        const uint2 w = ok && d < c.D ? __ldg(reinterpret_cast<const uint2 *>(p + d * 2)) : make_uint2(0, 0);
+                        q[k][y] = w.x;
+                        q[k][y + 2] = w.y;
+                    }
+                }
+                m[y] = -INFINITY;
+                l[y] = 0.0f;
+            }
+#pragma unroll
+            for (int k = 0; k < 2 * KS; ++k)
+#pragma unroll
+                for (int z = 0; z < 4; ++z) o[k][z] = 0.0f;
+            bad = false;
+        }
+        // the copies of the tile two ahead, then the places of the one after it (their latency is the tile's work)
+        if (x + S::kStages - 1 < count) {
+            if (__any_sync(0xffffffffu, bad_next)) bad_tiles |= 1u << ((x + S::kStages - 1) & 31);
+            issue(x + S::kStages - 1);
+            if (x + S::kStages < count) {
+                lk.next(a);
+                bad_next = false;
+                look();
+            }
+        }
+        copy_commit();
+        copy_wait<S::kStages - 1>();
+        __syncwarp();
+        bad |= bad_tiles >> (x & 31) & 1;
+        bad_tiles &= ~(1u << (x & 31));
+
+        // ---- scores ----
+        char *const st = stages + x % S::kStages * S::kStage;
+        const uint32_t sk = smem_addr(st), sv = sk + S::kHalf;
+        const int base = cu.base() + warp * kMine;
+        float s[NB][4];
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int z = 0; z < 4; ++z) s[n][z] = 0.0f;
+        if constexpr (FMT == kFmt16) {
+#pragma unroll
+            for (int k = 0; k < KS; ++k)
+#pragma unroll
+                for (int n = 0; n < NB; n += 2) {
+                    uint32_t b[4];
+                    const int mi = lane / 8, row = n * 8 + (mi >> 1) * 8 + lane % 8;
+                    ldsm4(b, sk + row * S::kRow + swizzle<DP, FMT, false>(row, k * 2 + (mi & 1)) * 16);
+                    mma<BF16>(s[n], q[k], b[0], b[1]);
+                    mma<BF16>(s[n + 1], q[k], b[2], b[3]);
+                }
+        } else {
+#pragma unroll
+            for (int hf = 0; hf < DP / 64; ++hf)
+#pragma unroll
+                for (int n = 0; n < NB; ++n) {
+                    const int row = n * 8 + g;
+                    const uint4 w = lds16(sk + row * S::kRow + swizzle<DP, FMT, false>(row, hf * 4 + i4) * 16);
+                    const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        mma<BF16>(s[n], q[hf * 4 + k], from_codes<BF16, FMT>(ww[k], 0, 1), from_codes<BF16, FMT>(ww[k], 2, 3));
+                }
+        }
+        // ---- softmax ----
+        const float *const ks = scales + x % S::kStages * 2 * kMine, *const vs = ks + kMine;
+        const bool masked = base + kMine - 1 > u.lo || (a.window > 0 && base <= u.hi - a.window && base + kMine > a.sinks);
+        float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int z = 0; z < 4; ++z) {
+                float f = a.scale_log2;
+                if constexpr (FMT != kFmt16) f *= ks[n * 8 + 2 * i4 + (z & 1)];
+                s[n][z] *= f;
+            }
+        if (masked) {
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int z = 0; z < 4; ++z)
+                    if (!visible(pos[z >> 1], base + n * 8 + 2 * i4 + (z & 1), a.window, a.sinks)) s[n][z] = -INFINITY;
+        }
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int z = 0; z < 4; ++z) mx[z >> 1] = fmaxf(mx[z >> 1], s[n][z]);
+        float al[2];
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+            mx[y] = fmaxf(mx[y], __shfl_xor_sync(0xffffffffu, mx[y], 1));
+            mx[y] = fmaxf(mx[y], __shfl_xor_sync(0xffffffffu, mx[y], 2));
+            const float mn = fmaxf(m[y], mx[y]);
+            al[y] = mn == -INFINITY ? 1.0f : exp2_fast(m[y] - mn);
+            m[y] = mn;
+            mx[y] = mn == -INFINITY ? 0.0f : mn;
+            l[y] *= al[y];
+        }
+        if (__any_sync(0xffffffffu, al[0] != 1.0f || al[1] != 1.0f)) {
+#pragma unroll
+            for (int k = 0; k < 2 * KS; ++k)
+#pragma unroll
+                for (int z = 0; z < 4; ++z) o[k][z] *= al[z >> 1];
+        }
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int z = 0; z < 4; ++z) {
+                const float p = exp2_fast(s[n][z] - mx[z >> 1]);
+                l[z >> 1] += p;
+                if constexpr (FMT != kFmt16) {
+                    // (a scale that is not finite stays away from a weight that the mask takes)
+                    const float w = p * (kLift * vs[n * 8 + 2 * i4 + (z & 1)]);
+                    s[n][z] = masked && s[n][z] == -INFINITY ? 0.0f : w;
+                } else {
+                    s[n][z] = p;
+                }
+            }
+
+        // ---- weighted sum ----
+        bool slow = false;
+        if constexpr (FMT == kFmt16) {
+            if (masked) {  // V that is not finite: as above
+                bool z = false;
+                for (int k = lane; k < kMine * S::kChunks; k += 32) {
+                    const uint4 w = lds16(sv + k * 16);
+                    z |= not_finite<BF16>(w.x) || not_finite<BF16>(w.y) || not_finite<BF16>(w.z) || not_finite<BF16>(w.w);
+                }
+                slow = __any_sync(0xffffffffu, z);
+            }
+        }
+        if (!slow) {
+#pragma unroll
+            for (int kk = 0; kk < kMine / 16; ++kk) {
+                const uint32_t p[4] = {pack16<BF16>(s[2 * kk][0], s[2 * kk][1]), pack16<BF16>(s[2 * kk][2], s[2 * kk][3]),
+                                       pack16<BF16>(s[2 * kk + 1][0], s[2 * kk + 1][1]),
+                                       pack16<BF16>(s[2 * kk + 1][2], s[2 * kk + 1][3])};
+                const int mi = lane / 8, row = kk * 16 + (mi & 1) * 8 + lane % 8;
+                if constexpr (FMT == kFmt16) {
+#pragma unroll
+                    for (int d = 0; d < KS; ++d) {
+                        uint32_t b[4];
+                        ldsm4t(b, sv + row * S::kRow + swizzle<DP, FMT, true>(row, d * 2 + (mi >> 1)) * 16);
+                        mma<BF16>(o[2 * d], p, b[0], b[1]);
+                        mma<BF16>(o[2 * d + 1], p, b[2], b[3]);
+                    }
+                } else {
+#pragma unroll
+                    for (int d = 0; d < KS; d += 2) {  // even and odd elements: as above
+                        uint32_t b[4];
+                        ldsm4t(b, sv + row * S::kRow + swizzle<DP, FMT, true>(row, d + (mi >> 1)) * 16);
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            mma<BF16>(o[2 * (d + e)], p, from_codes<BF16, FMT>(b[2 * e], 0, 2), from_codes<BF16, FMT>(b[2 * e + 1], 0, 2));
+                            mma<BF16>(o[2 * (d + e) + 1], p, from_codes<BF16, FMT>(b[2 * e], 1, 3), from_codes<BF16, FMT>(b[2 * e + 1], 1, 3));
+                        }
+                    }
+                }
+            }
+        } else if constexpr (FMT == kFmt16) {
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+                for (int t8 = 0; t8 < 8; ++t8) {
+                    const int row = n * 8 + t8;
+                    const int src = (lane & ~3) | t8 >> 1;
+                    float w[2];
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const float e0 = __shfl_sync(0xffffffffu, s[n][2 * y], src), e1 = __shfl_sync(0xffffffffu, s[n][2 * y + 1], src);
+                        w[y] = unpack16<BF16>(pack16<BF16>(t8 & 1 ? e1 : e0, 0.0f)).x;
+                    }
+                    const bool v0 = visible(pos[0], base + row, a.window, a.sinks), v1 = visible(pos[1], base + row, a.window, a.sinks);
+#pragma unroll
+                    for (int d = 0; d < 2 * KS; ++d) {
+                        const float2 v = unpack16<BF16>(*reinterpret_cast<const uint32_t *>(
+                            st + S::kHalf + row * S::kRow + swizzle<DP, FMT, true>(row, d) * 16 + i4 * 4));
+                        if (v0) {
+                            o[d][0] += w[0] * v.x;
+                            o[d][1] += w[0] * v.y;
+                        }
+                        if (v1) {
+                            o[d][2] += w[1] * v.x;
+                            o[d][3] += w[1] * v.y;
+                        }
+                    }
+                }
+        }
+        if (cu.j + 1 < u.nt && x + 1 < count) {
+            ++cu.j;
+            __syncwarp();
+            continue;
+        }
+
+        // ---- the unit ends here, for this CTA: the warps' sums to their stages just used, [row][element] ----
+        __syncwarp();
+        float *const xo = reinterpret_cast<float *>(st);
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+            l[y] += __shfl_xor_sync(0xffffffffu, l[y], 1);
+            l[y] += __shfl_xor_sync(0xffffffffu, l[y], 2);
+            const int r = g + y * 8;
+            if (r >= u.rows) continue;
+            if (i4 == 0) s_ml[warp * 16 + r] = make_float2(m[y], l[y]);
+            // a lane's elements: of 16-bit V 8d + 2i, +1 in o[d]; of 8-bit V 16d + 4i .. + 3 in o[2d], o[2d + 1]
+            if constexpr (FMT == kFmt16) {
+#pragma unroll
+                for (int d = 0; d < 2 * KS; ++d)
+                    *reinterpret_cast<float2 *>(xo + r * DP + d * 8 + 2 * i4) = make_float2(o[d][2 * y], o[d][2 * y + 1]);
+            } else {
+#pragma unroll
+                for (int d = 0; d < KS; ++d)
+                    *reinterpret_cast<float4 *>(xo + r * DP + d * 16 + 4 * i4) =
+                        make_float4(o[2 * d][2 * y], o[2 * d + 1][2 * y], o[2 * d][2 * y + 1], o[2 * d + 1][2 * y + 1]);
+            }
+        }
+        if (__any_sync(0xffffffffu, bad) && lane == 0) s_bad = x + 1;
+        __syncthreads();
+        const long long u0 = sh.x0 + x - cu.j, u1 = u0 + u.nt;
+        const bool whole = u0 >= sh.x0 && u1 <= sh.x1;
+        constexpr int kLanes = DP / 4;  // four elements a thread
+        const int d = tid % kLanes * 4;
+        const bool lost = s_bad == x + 1;
+        int64_t slot = 0;
+        if (!whole) slot = slot_of(sh, blockIdx.x, u0);
+        auto write = [&](int r, float mm, float ll, float4 w) {
+            const int t = quot(r, c.div_g), hd = u.h * c.G + r - t * c.G;
+            const float inv = ll == 0.0f ? 0.0f : 1.0f / (ll * kLift);
+            if (d < c.D)
+                *reinterpret_cast<uint2 *>(a.out + (int64_t)(u.q0 + t) * a.o_t + (int64_t)hd * a.o_h + d * 2) =
+                    make_uint2(pack16<BF16>(w.x * inv, w.y * inv), pack16<BF16>(w.z * inv, w.w * inv));
+            if (a.lse && d == 0) a.lse[(int64_t)(u.q0 + t) * c.Hq + hd] = ll == 0.0f ? -INFINITY : (mm + log2f(ll)) * 0.69314718f;
+        };
+        // a join of parts (m, l, sums), in a fixed order
+        auto join = [&](float2 ml, const float4 &w, float mm, float &ll, float4 &acc) {
+            if (ml.x == -INFINITY && ml.y == 0.0f) return;  // saw nothing
+            const float f = ml.x == -INFINITY ? 0.0f : exp2_fast(ml.x - mm);
+            ll += ml.y == 0.0f ? 0.0f : ml.y * f;
+            acc.x += w.x * f;
+            acc.y += w.y * f;
+            acc.z += w.z * f;
+            acc.w += w.w * f;
+        };
+        for (int r = tid / kLanes; r < u.rows; r += kThreads / kLanes) {
+            float mm = -INFINITY, ll = 0.0f;
+            float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) mm = fmaxf(mm, s_ml[w * 16 + r].x);
+#pragma unroll
+            for (int w = 0; w < 4; ++w)
+                join(s_ml[w * 16 + r], *reinterpret_cast<const float4 *>(smem + w * S::kWarp + x % S::kStages * S::kStage + (r * DP + d) * 4), mm, ll, acc);
+            if (lost) ll = __uint_as_float(0x7fffffffu);
+            if (whole) {
+                write(r, mm, ll, acc);
+            } else {
+                if (d == 0) a.part_ml[slot * kStepRows + r] = make_float2(mm, ll);
+                *reinterpret_cast<float4 *>(a.part_o + (slot * kStepRows + r) * 128 + d) = acc;
+            }
+        }
+        if (!whole) {
+            const int c0 = cta_of(sh, u0), c1 = cta_of(sh, u1 - 1);
+            __threadfence();
+            __syncthreads();
+            if (tid == 0) {
+                const bool last = atomicAdd(a.done + c0, 1u) == (uint32_t)(c1 - c0);
+                if (last) a.done[c0] = 0;
+                s_last = last;
+            }
+            __syncthreads();
+            if (s_last) {  // join the parts, in the order of the CTAs whichever came last
+                __threadfence();
+                const int64_t s0 = slot_of(sh, c0, u0);  // (a unit is the first of every later CTA)
+                for (int r = tid / kLanes; r < u.rows; r += kThreads / kLanes) {
+                    auto at = [&](int k) { return (k == c0 ? s0 : 2 * (int64_t)k) * kStepRows + r; };
+                    float mm = -INFINITY, ll = 0.0f;
+                    for (int k = c0; k <= c1; ++k) mm = fmaxf(mm, __ldcg(&a.part_ml[at(k)].x));
+                    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+                    for (int k = c0; k <= c1; ++k)
+                        join(__ldcg(a.part_ml + at(k)), __ldcg(reinterpret_cast<const float4 *>(a.part_o + at(k) * 128 + d)), mm, ll, acc);
+                    write(r, mm, ll, acc);
+                }
+            }
+        }
+        __syncthreads();  // the stages are free again
+        if (x + 1 < count) cu.next(a);
+    }
+    chain_next();
+}
+
 using Kernel = void (*)(const AttendLaunch);
 
 template <bool BF16, int FMT, int DP>
 Kernel pick_rows(int rows) {
-    return rows <= 16 ? k_attend_step<BF16, FMT, DP, 1> : rows <= 32 ? k_attend_step<BF16, FMT, DP, 2> : k_attend_step<BF16, FMT, DP, 4>;
+    return rows <= 16 ? k_attend_step<BF16, FMT, DP> : rows <= 32 ? k_attend_rows<BF16, FMT, DP, 2> : k_attend_rows<BF16, FMT, DP, 4>;
 }
 template <int FMT, int DP>
 Kernel pick_type(bool bf16, int rows) {
@@ -508,7 +925,8 @@ Kernel pick_type(bool bf16, int rows) {
 }
 template <int FMT>
 Kernel pick(bool bf16, int D, int rows, size_t &smem) {
-    smem = D <= 64 ? Shape<64, FMT>::kSmem : Shape<128, FMT>::kSmem;
+    smem = rows <= 16 ? (D <= 64 ? Solo<64, FMT>::kSmem : Solo<128, FMT>::kSmem)
+                      : (D <= 64 ? Shape<64, FMT>::kSmem : Shape<128, FMT>::kSmem);
     return D <= 64 ? pick_type<FMT, 64>(bf16, rows) : pick_type<FMT, 128>(bf16, rows);
 }
 Kernel pick_kernel(bool bf16, int fmt, int D, int rows, size_t &smem) {
