@@ -415,7 +415,8 @@ enum lr_dtype { LR_BF16 = 0, LR_FP16 = 1, LR_FP32 = 2 };
  *  E4M3, INT8: 8-bit codes and one fp32 scale a vector.  With a = max(max|x|, 2^-100) and
  *    top = 448 or 127, in fp32: scale = a / top, code = round(x * (top / a)), to the
  *    nearest e4m3 number or integer, ties to even.  It stands for code * scale.  A vector with an
- *    infinity or a NaN has that for its scale, and reads back as NaN throughout. */
+ *    infinity or a NaN has that for its scale and codes of zero, and reads back as NaN
+ *    throughout. */
 enum lr_cache_format { LR_CACHE_16BIT = 0, LR_CACHE_E4M3 = 1, LR_CACHE_INT8 = 2 };
 
 typedef struct {

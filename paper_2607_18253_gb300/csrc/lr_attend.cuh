@@ -121,6 +121,10 @@ struct Share {
     long long x0, x1, all;
     int ctas;
 };
+// The first tile of CTA c's share (32-bit divisions where they do, as nearly always).
+__device__ __forceinline__ long long share_start(const Share &s, int c) {
+    return s.all < 1 << 20 ? (long long)((uint32_t)s.all * (uint32_t)c / (uint32_t)s.ctas) : s.all * c / s.ctas;
+}
 // (scratch: THREADS / 32 + 2 words of shared memory)
 template <int ROWS, int TILE, int THREADS>
 __device__ __forceinline__ bool take_share(const AttendLaunch &a, Cursor<ROWS, TILE> &cur, Share &sh, long long *scratch) {
@@ -158,8 +162,8 @@ __device__ __forceinline__ bool take_share(const AttendLaunch &a, Cursor<ROWS, T
     sh.ctas = (int)min((long long)gridDim.x, all);
     const int c = blockIdx.x;
     if (c >= sh.ctas) return false;
-    sh.x0 = all * c / sh.ctas;
-    sh.x1 = all * (c + 1) / sh.ctas;
+    sh.x0 = share_start(sh, c);
+    sh.x1 = share_start(sh, c + 1);
     for (int base = 0; base < n; base += THREADS) {
         long long t;
         if (n > THREADS) {
@@ -211,10 +215,10 @@ __device__ __forceinline__ bool take_share(const AttendLaunch &a, Cursor<ROWS, T
 
 // The CTAs c0 .. c1 that share the unit of tiles [u0, u1), and where CTA c's part of it lies: its
 // first unit in slot 2c, a later one in slot 2c + 1.
-__device__ __forceinline__ int cta_of(const Share &s, long long x) { return (int)(((x + 1) * s.ctas - 1) / s.all); }
-__device__ __forceinline__ int slot_of(const Share &s, int c, long long u0) {
-    return 2 * c + (s.all * c / s.ctas < u0 ? 1 : 0);
+__device__ __forceinline__ int cta_of(const Share &s, long long x) {
+    return s.all < 1 << 20 ? (int)((((uint32_t)x + 1) * (uint32_t)s.ctas - 1) / (uint32_t)s.all) : (int)(((x + 1) * s.ctas - 1) / s.all);
 }
+__device__ __forceinline__ int slot_of(const Share &s, int c, long long u0) { return 2 * c + (share_start(s, c) < u0 ? 1 : 0); }
 
 __device__ __forceinline__ bool visible(int pos, int j, int window, int sinks) {
     return j <= pos && (window == 0 || j > pos - window || j < sinks);
@@ -260,6 +264,27 @@ template <bool BF16, int FMT>
 __device__ __forceinline__ uint32_t from_codes(uint32_t w, int i, int j) {
     if constexpr (FMT == kFmtE4M3) return from_e4m3<BF16>(__byte_perm(w, 0, 0x0404u | i << 4 | j << 12));
     else return from_int8<BF16>(__byte_perm(w, 0, 0x4040u | i | j << 8));
+}
+
+// Four 8-bit codes to fp16 numbers, exactly, as two pairs: codes (0, 1) and (2, 3), or with SPLIT (0, 2) and
+// (1, 3).  e4m3 by the conversion instruction.  int8: 1024 + (code + 128), less 1152.
+template <int FMT, bool SPLIT>
+__device__ __forceinline__ void to_half(uint32_t w, uint32_t &a, uint32_t &b) {
+    if constexpr (FMT == kFmtE4M3) {
+        if constexpr (SPLIT) w = __byte_perm(w, 0, 0x3120);
+        asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %2;\n cvt.rn.f16x2.e4m3x2 %0, l;\n cvt.rn.f16x2.e4m3x2 %1, h;\n}" : "=r"(a), "=r"(b) : "r"(w));
+    } else {
+        w ^= 0x80808080u;
+        a = __byte_perm(w, 0x64646464u, SPLIT ? 0x4240 : 0x4140);
+        b = __byte_perm(w, 0x64646464u, SPLIT ? 0x4341 : 0x4342);
+        asm("sub.rn.f16x2 %0, %0, %1;" : "+r"(a) : "r"(0x64806480u));
+        asm("sub.rn.f16x2 %0, %0, %1;" : "+r"(b) : "r"(0x64806480u));
+    }
+}
+// e4m3's codes for NaN set to zero.
+__device__ __forceinline__ uint32_t without_nan(uint32_t w) {
+    const uint32_t x = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;  // the high bit of each such byte
+    return w & ~(x | (x - (x >> 7)));
 }
 
 template <bool BF16>

@@ -505,27 +505,39 @@ __global__ void __launch_bounds__(kThreads) k_attend_rows(const __grid_constant_
 //
 // A tile's tokens are divided over the four warps, and a warp copies, waits for and multiplies its own:
 // nothing is exchanged until the unit ends (the warps then join their sums through the stages just used), so
-// no warp waits for another's copies.
-template <int DP, int FMT>
+// no warp waits for another's copies.  The products are the other way round here, S^T = K Q^T and
+// O^T += V^T P^T: the 16-row operand is the cache and the 8-column one the queries, so up to eight rows (NR = 1)
+// cost half of what they would as half of a 16-row operand, in instructions and registers, and
+// four CTAs fit an SM.  That counts because a tile is a chain of dependent steps: with two CTAs of the other
+// form an SM, 64 sequences over an e4m3 cache took 91 us, 78 of them without any copies.
+template <int DP, int FMT, int NR>
 struct Solo {
     static constexpr int kRow = DP * (FMT == kFmt16 ? 2 : 1);
     static constexpr int kChunks = kRow / 16;
-    static constexpr int kMine = FMT == kFmt16 ? 16 : 32;  // tokens of a warp: its stage also takes 16 rows of sums
+    static constexpr int kMine = FMT == kFmt16 || NR == 1 ? 16 : 32;  // tokens of a warp
     static constexpr int kTile = 4 * kMine;
     static constexpr int kHalf = kMine * kRow;
     static constexpr int kStage = 2 * kHalf;
-    static constexpr int kStages = 3;
+    static constexpr int kStages = FMT == kFmt16 && DP == 128 ? 2 : 3;
+    static constexpr int kCtas = NR == 1 ? (FMT == kFmt16 && DP == 128 ? 3 : 4) : 2;  // of an SM
     static constexpr int kScales = FMT == kFmt16 ? 0 : kStages * 2 * kMine * 4;
     static constexpr int kWarp = kStages * kStage + kScales;
-    static constexpr int kSmem = 4 * kWarp + 4 * 16 * 8;
-    static_assert(kStage >= 16 * DP * 4, "room for a warp's sums");
+    static constexpr int kSmem = 4 * kWarp + 4 * 8 * NR * 8;
+    static_assert(kStage >= 8 * NR * DP * 4, "room for a warp's sums");
 };
 
-template <bool BF16, int FMT, int DP>
-__global__ void __launch_bounds__(kThreads, 2) k_attend_step(const __grid_constant__ AttendLaunch a) {
-    using S = Solo<DP, FMT>;
-    constexpr int kRows = 16, kMine = S::kMine, NB = kMine / 8, KS = DP / 16;
-    constexpr float kLift = FMT != kFmt16 && !BF16 ? 64.0f : 1.0f;  // as above
+template <bool BF16, int FMT, int DP, int NR>
+__global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_step(const __grid_constant__ AttendLaunch a) {
+    using S = Solo<DP, FMT, NR>;
+    constexpr int kRows = 8 * NR, kMine = S::kMine, NB = kMine / 16, KS = DP / 16;
+    // 8-bit codes are multiplied in fp16, which holds them exactly and converts them in the fewest
+    // instructions.  The queries come to fp16 as they are, or from bf16 divided by a power of two
+    // a row that brings the largest to [1, 2): what fp16 then rounds is below 2^-24 of it.  The weights
+    // carry V's scales divided by the largest so far.
+    constexpr bool MB = FMT == kFmt16 ? BF16 : false;  // type of the products
+    // The maximum that the weights refer to is left behind until a score exceeds it by this (log2): any
+    // reference gives the same quotient, and a tile that raises none needs no exchange between lanes.
+    constexpr float kLag = MB ? 8.0f : 4.0f;
     extern __shared__ __align__(128) char smem[];
     __shared__ int s_last, s_bad;  // (s_bad: 1 + the last tile of the unit in which a block was out of range)
     __shared__ long long s_scratch[kThreads / 32 + 2];
@@ -580,13 +592,14 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_step(const __grid_consta
             copy16(smem_addr(st + S::kHalf + r * S::kRow + swizzle<DP, FMT, true>(r, ch) * 16), c.v + at, ok);
         }
         if constexpr (FMT != kFmt16) {
-            float *const to = scales + tile % S::kStages * 2 * kMine + lane;
-            copy4(smem_addr(to), c.ks + soff, off >= 0);
-            copy4(smem_addr(to + kMine), c.vs + soff, off >= 0);
+            if (lane < kMine) {
+                float *const to = scales + tile % S::kStages * 2 * kMine + lane;
+                copy4(smem_addr(to), c.ks + soff, off >= 0);
+                copy4(smem_addr(to + kMine), c.vs + soff, off >= 0);
+            }
         }
     };
-    // (bad tiles: a bit for each tile on its way)
-    unsigned bad_tiles = 0;
+    unsigned bad_tiles = 0;  // a bit for each tile on its way
     for (int t = 0; t < S::kStages - 1; ++t) {
         if (t < count) {
             bad_next = false;
@@ -602,18 +615,18 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_step(const __grid_consta
         look();
     }
 
-    uint32_t q[KS][4];
-    float o[2 * KS][4], m[2], l[2];
-    int pos[2];
+    // a lane's columns are the rows n * 8 + 2 * i4, + 1 of the unit
+    uint32_t q[KS][NR][2];
+    float o[KS][NR][4], m[NR][2], l[NR][2], qf[NR][2], vmax = 0.0f;
+    int pos[NR][2];
     for (int x = 0; x < count; ++x) {
         const Unit &u = cu.u;
         if (x == 0 || cu.j == 0) {  // a new unit: its queries, straight to the registers that multiply them
 #pragma unroll
-            for (int y = 0; y < 2; ++y) {
-                const int r = g + y * 8;
+            for (int n = 0; n < NR; ++n) {
+                const int r = n * 8 + g;  // (the row whose elements the lane holds)
                 const int t = quot(r, c.div_g), hd = r - t * c.G;
                 const bool ok = r < u.rows;
-                pos[y] = ok ? u.kv - u.ql + t : -1;
                 const char *const p = a.q + (int64_t)(u.q0 + t) * a.q_t + (int64_t)(u.h * c.G + hd) * a.q_h;
 #pragma unroll
                 for (int k = 0; k < KS; ++k) {
@@ -621,25 +634,50 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_step(const __grid_consta
 #pragma unroll
                         for (int z = 0; z < 2; ++z) {
                             const int d = k * 16 + z * 8 + 2 * i4;
-                            q[k][y + 2 * z] = ok && d < c.D ? __ldg(reinterpret_cast<const uint32_t *>(p + d * 2)) : 0u;
+                            q[k][n][z] = ok && d < c.D ? __ldg(reinterpret_cast<const uint32_t *>(p + d * 2)) : 0u;
                         }
                     } else {  // four neighbouring elements, the order in which the codes lie in a register
                         const int d = (k / 4) * 64 + i4 * 16 + (k % 4) * 4;
                         const uint2 w = ok && d < c.D ? __ldg(reinterpret_cast<const uint2 *>(p + d * 2)) : make_uint2(0, 0);
-                        q[k][y] = w.x;
-                        q[k][y + 2] = w.y;
+                        q[k][n][0] = w.x;
+                        q[k][n][1] = w.y;
+                    }
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) o[k][n][z] = 0.0f;
+                }
+                float pow2 = 1.0f;
+                if constexpr (FMT != kFmt16 && BF16) {
+                    float top = 0.0f;
+#pragma unroll
+                    for (int k = 0; k < 2 * KS; ++k) {
+                        const float2 f = unpack16<true>(q[k / 2][n][k % 2]);
+                        top = fmaxf(top, fmaxf(fabsf(f.x), fabsf(f.y)));
+                    }
+                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                    // (not below 2^-100, whose reciprocal is a number; infinities stay what they are)
+                    const uint32_t e = min(max(__float_as_uint(top) & 0x7f800000u, 27u << 23), 253u << 23);
+                    const float inv = __uint_as_float((254u << 23) - e);
+                    pow2 = __uint_as_float(e);
+#pragma unroll
+                    for (int k = 0; k < 2 * KS; ++k) {
+                        const float2 f = unpack16<true>(q[k / 2][n][k % 2]);
+                        q[k / 2][n][k % 2] = pack16<false>(f.x * inv, f.y * inv);
                     }
                 }
-                m[y] = -INFINITY;
-                l[y] = 0.0f;
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const int row = n * 8 + 2 * i4 + y;
+                    pos[n][y] = row < u.rows ? u.kv - u.ql + quot(row, c.div_g) : -1;
+                    qf[n][y] = a.scale_log2 * __shfl_sync(0xffffffffu, pow2, (2 * i4 + y) * 4);
+                    m[n][y] = -INFINITY;
+                    l[n][y] = 0.0f;
+                }
             }
-#pragma unroll
-            for (int k = 0; k < 2 * KS; ++k)
-#pragma unroll
-                for (int z = 0; z < 4; ++z) o[k][z] = 0.0f;
+            vmax = 0.0f;
             bad = false;
         }
-        // the copies of the tile two ahead, then the places of the one after it (their latency is the tile's work)
+        // the copies of the tile ahead, then the places of the one after it (their latency is the tile's work)
         if (x + S::kStages - 1 < count) {
             if (__any_sync(0xffffffffu, bad_next)) bad_tiles |= 1u << ((x + S::kStages - 1) & 31);
             issue(x + S::kStages - 1);
@@ -655,93 +693,124 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_step(const __grid_consta
         bad |= bad_tiles >> (x & 31) & 1;
         bad_tiles &= ~(1u << (x & 31));
 
-        // ---- scores ----
+        // ---- scores: tokens g, g + 8 of each 16 ----
         char *const st = stages + x % S::kStages * S::kStage;
         const uint32_t sk = smem_addr(st), sv = sk + S::kHalf;
         const int base = cu.base() + warp * kMine;
-        float s[NB][4];
+        float s[NB][NR][4];
 #pragma unroll
-        for (int n = 0; n < NB; ++n)
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int z = 0; z < 4; ++z) s[n][z] = 0.0f;
-        if constexpr (FMT == kFmt16) {
+            for (int n = 0; n < NR; ++n)
 #pragma unroll
-            for (int k = 0; k < KS; ++k)
+                for (int z = 0; z < 4; ++z) s[b][n][z] = 0.0f;
 #pragma unroll
-                for (int n = 0; n < NB; n += 2) {
-                    uint32_t b[4];
-                    const int mi = lane / 8, row = n * 8 + (mi >> 1) * 8 + lane % 8;
-                    ldsm4(b, sk + row * S::kRow + swizzle<DP, FMT, false>(row, k * 2 + (mi & 1)) * 16);
-                    mma<BF16>(s[n], q[k], b[0], b[1]);
-                    mma<BF16>(s[n + 1], q[k], b[2], b[3]);
+        for (int b = 0; b < NB; ++b) {
+            if constexpr (FMT == kFmt16) {
+#pragma unroll
+                for (int k = 0; k < KS; ++k) {
+                    uint32_t w[4];
+                    const int row = b * 16 + lane % 16;
+                    ldsm4(w, sk + row * S::kRow + swizzle<DP, FMT, false>(row, k * 2 + lane / 16) * 16);
+#pragma unroll
+                    for (int n = 0; n < NR; ++n) mma<MB>(s[b][n], w, q[k][n][0], q[k][n][1]);
                 }
-        } else {
+            } else {
 #pragma unroll
-            for (int hf = 0; hf < DP / 64; ++hf)
-#pragma unroll
-                for (int n = 0; n < NB; ++n) {
-                    const int row = n * 8 + g;
+                for (int hf = 0; hf < DP / 64; ++hf) {
+                    const int row = b * 16 + g;
                     const uint4 w = lds16(sk + row * S::kRow + swizzle<DP, FMT, false>(row, hf * 4 + i4) * 16);
-                    const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+                    const uint4 v = lds16(sk + (row + 8) * S::kRow + swizzle<DP, FMT, false>(row + 8, hf * 4 + i4) * 16);
+                    const uint32_t ww[4] = {w.x, w.y, w.z, w.w}, vv[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        mma<BF16>(s[n], q[hf * 4 + k], from_codes<BF16, FMT>(ww[k], 0, 1), from_codes<BF16, FMT>(ww[k], 2, 3));
+                    for (int k = 0; k < 4; ++k) {
+                        uint32_t f[4];
+                        to_half<FMT, false>(ww[k], f[0], f[2]);
+                        to_half<FMT, false>(vv[k], f[1], f[3]);
+#pragma unroll
+                        for (int n = 0; n < NR; ++n) mma<MB>(s[b][n], f, q[hf * 4 + k][n][0], q[hf * 4 + k][n][1]);
+                    }
                 }
+            }
         }
         // ---- softmax ----
         const float *const ks = scales + x % S::kStages * 2 * kMine, *const vs = ks + kMine;
         const bool masked = base + kMine - 1 > u.lo || (a.window > 0 && base <= u.hi - a.window && base + kMine > a.sinks);
-        float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-        for (int n = 0; n < NB; ++n)
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int z = 0; z < 4; ++z) {
-                float f = a.scale_log2;
-                if constexpr (FMT != kFmt16) f *= ks[n * 8 + 2 * i4 + (z & 1)];
-                s[n][z] *= f;
-            }
+            for (int n = 0; n < NR; ++n)
+#pragma unroll
+                for (int z = 0; z < 4; ++z) {
+                    float f = qf[n][z & 1];
+                    if constexpr (FMT != kFmt16) f *= ks[b * 16 + g + (z >> 1) * 8];
+                    s[b][n][z] *= f;
+                }
         if (masked) {
 #pragma unroll
-            for (int n = 0; n < NB; ++n)
+            for (int b = 0; b < NB; ++b)
 #pragma unroll
-                for (int z = 0; z < 4; ++z)
-                    if (!visible(pos[z >> 1], base + n * 8 + 2 * i4 + (z & 1), a.window, a.sinks)) s[n][z] = -INFINITY;
+                for (int n = 0; n < NR; ++n)
+#pragma unroll
+                    for (int z = 0; z < 4; ++z)
+                        if (!visible(pos[n][z & 1], base + b * 16 + g + (z >> 1) * 8, a.window, a.sinks)) s[b][n][z] = -INFINITY;
         }
+        float mx[NR][2];
+        bool raise = false;
 #pragma unroll
-        for (int n = 0; n < NB; ++n)
+        for (int n = 0; n < NR; ++n)
 #pragma unroll
-            for (int z = 0; z < 4; ++z) mx[z >> 1] = fmaxf(mx[z >> 1], s[n][z]);
-        float al[2];
+            for (int y = 0; y < 2; ++y) {
+                mx[n][y] = fmaxf(s[0][n][y], s[0][n][y + 2]);
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
-            mx[y] = fmaxf(mx[y], __shfl_xor_sync(0xffffffffu, mx[y], 1));
-            mx[y] = fmaxf(mx[y], __shfl_xor_sync(0xffffffffu, mx[y], 2));
-            const float mn = fmaxf(m[y], mx[y]);
-            al[y] = mn == -INFINITY ? 1.0f : exp2_fast(m[y] - mn);
-            m[y] = mn;
-            mx[y] = mn == -INFINITY ? 0.0f : mn;
-            l[y] *= al[y];
-        }
-        if (__any_sync(0xffffffffu, al[0] != 1.0f || al[1] != 1.0f)) {
-#pragma unroll
-            for (int k = 0; k < 2 * KS; ++k)
-#pragma unroll
-                for (int z = 0; z < 4; ++z) o[k][z] *= al[z >> 1];
-        }
-#pragma unroll
-        for (int n = 0; n < NB; ++n)
-#pragma unroll
-            for (int z = 0; z < 4; ++z) {
-                const float p = exp2_fast(s[n][z] - mx[z >> 1]);
-                l[z >> 1] += p;
-                if constexpr (FMT != kFmt16) {
-                    // (a scale that is not finite stays away from a weight that the mask takes)
-                    const float w = p * (kLift * vs[n * 8 + 2 * i4 + (z & 1)]);
-                    s[n][z] = masked && s[n][z] == -INFINITY ? 0.0f : w;
-                } else {
-                    s[n][z] = p;
-                }
+                for (int b = 1; b < NB; ++b) mx[n][y] = fmaxf(mx[n][y], fmaxf(s[b][n][y], s[b][n][y + 2]));
+                raise |= mx[n][y] > m[n][y] + kLag;
             }
+        float vnew = vmax;
+        if constexpr (FMT != kFmt16) {
+            // the largest scale of V so far (positive numbers compare as integers; one that is not finite does not count)
+            const uint32_t bits = __float_as_uint(vs[lane % kMine]);
+            vnew = fmaxf(vmax, __uint_as_float(__reduce_max_sync(0xffffffffu, bits < 0x7f800000u ? bits : 0u)));
+            raise |= vnew > vmax;
+        }
+        if (__any_sync(0xffffffffu, raise)) {
+            const float fv = FMT != kFmt16 && vnew > vmax ? vmax / vnew : 1.0f;  // 0 at first
+            vmax = vnew;
+#pragma unroll
+            for (int n = 0; n < NR; ++n)
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    float w = mx[n][y];
+                    w = fmaxf(w, __shfl_xor_sync(0xffffffffu, w, 4));
+                    w = fmaxf(w, __shfl_xor_sync(0xffffffffu, w, 8));
+                    w = fmaxf(w, __shfl_xor_sync(0xffffffffu, w, 16));
+                    const float mn = fmaxf(m[n][y], w), f = mn == -INFINITY ? 1.0f : exp2_fast(m[n][y] - mn);
+                    m[n][y] = mn;
+                    l[n][y] *= f;
+#pragma unroll
+                    for (int k = 0; k < KS; ++k) {
+                        o[k][n][y] *= f * fv;
+                        o[k][n][y + 2] *= f * fv;
+                    }
+                }
+        }
+        const float vinv = FMT != kFmt16 && vmax > 0.0f ? 1.0f / vmax : 0.0f;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int n = 0; n < NR; ++n)
+#pragma unroll
+                for (int z = 0; z < 4; ++z) {
+                    const float p = exp2_fast(s[b][n][z] - (m[n][z & 1] == -INFINITY ? 0.0f : m[n][z & 1]));
+                    l[n][z & 1] += p;
+                    if constexpr (FMT != kFmt16) {
+                        // (a scale that is not finite stays away from a weight that the mask takes)
+                        const float w = p * (vinv * vs[b * 16 + g + (z >> 1) * 8]);
+                        s[b][n][z] = masked && s[b][n][z] == -INFINITY ? 0.0f : w;
+                    } else {
+                        s[b][n][z] = p;
+                    }
+                }
 
         // ---- weighted sum ----
         bool slow = false;
@@ -757,59 +826,70 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_step(const __grid_consta
         }
         if (!slow) {
 #pragma unroll
-            for (int kk = 0; kk < kMine / 16; ++kk) {
-                const uint32_t p[4] = {pack16<BF16>(s[2 * kk][0], s[2 * kk][1]), pack16<BF16>(s[2 * kk][2], s[2 * kk][3]),
-                                       pack16<BF16>(s[2 * kk + 1][0], s[2 * kk + 1][1]),
-                                       pack16<BF16>(s[2 * kk + 1][2], s[2 * kk + 1][3])};
-                const int mi = lane / 8, row = kk * 16 + (mi & 1) * 8 + lane % 8;
+            for (int b = 0; b < NB; ++b) {
+                // the weights turned, from a lane's token to a lane's row
+                uint32_t p[NR][2];
+#pragma unroll
+                for (int n = 0; n < NR; ++n)
+#pragma unroll
+                    for (int y = 0; y < 2; ++y)
+                        asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(p[n][y]) : "r"(pack16<MB>(s[b][n][2 * y], s[b][n][2 * y + 1])));
+                const int mi = lane / 8;
                 if constexpr (FMT == kFmt16) {
 #pragma unroll
-                    for (int d = 0; d < KS; ++d) {
-                        uint32_t b[4];
-                        ldsm4t(b, sv + row * S::kRow + swizzle<DP, FMT, true>(row, d * 2 + (mi >> 1)) * 16);
-                        mma<BF16>(o[2 * d], p, b[0], b[1]);
-                        mma<BF16>(o[2 * d + 1], p, b[2], b[3]);
+                    for (int k = 0; k < KS; ++k) {
+                        uint32_t w[4];
+                        const int row = b * 16 + (mi >> 1) * 8 + lane % 8;
+                        ldsm4t(w, sv + row * S::kRow + swizzle<DP, FMT, true>(row, k * 2 + (mi & 1)) * 16);
+#pragma unroll
+                        for (int n = 0; n < NR; ++n) mma<MB>(o[k][n], w, p[n][0], p[n][1]);
                     }
                 } else {
+                    // pairs of neighbouring elements move as one: rows g of the product are the even ones of 16, rows
+                    // g + 8 the odd ones
 #pragma unroll
-                    for (int d = 0; d < KS; d += 2) {  // even and odd elements: as above
-                        uint32_t b[4];
-                        ldsm4t(b, sv + row * S::kRow + swizzle<DP, FMT, true>(row, d + (mi >> 1)) * 16);
+                    for (int k = 0; k < KS; k += 2) {
+                        uint32_t w[4];
+                        const int row = b * 16 + (mi & 1) * 8 + lane % 8;
+                        ldsm4t(w, sv + row * S::kRow + swizzle<DP, FMT, true>(row, k + (mi >> 1)) * 16);
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            mma<BF16>(o[2 * (d + e)], p, from_codes<BF16, FMT>(b[2 * e], 0, 2), from_codes<BF16, FMT>(b[2 * e + 1], 0, 2));
-                            mma<BF16>(o[2 * (d + e) + 1], p, from_codes<BF16, FMT>(b[2 * e], 1, 3), from_codes<BF16, FMT>(b[2 * e + 1], 1, 3));
+                            if (FMT == kFmtE4M3 && masked) {  // codes of NaN stay away from weights that the mask takes
+                                w[2 * e] = without_nan(w[2 * e]);
+                                w[2 * e + 1] = without_nan(w[2 * e + 1]);
+                            }
+                            uint32_t f[4];
+                            to_half<FMT, true>(w[2 * e], f[0], f[1]);
+                            to_half<FMT, true>(w[2 * e + 1], f[2], f[3]);
+#pragma unroll
+                            for (int n = 0; n < NR; ++n) mma<MB>(o[k + e][n], f, p[n][0], p[n][1]);
                         }
                     }
                 }
             }
         } else if constexpr (FMT == kFmt16) {
+            for (int t = 0; t < kMine; ++t) {
+                const int src = (t & 7) * 4 + i4;
 #pragma unroll
-            for (int n = 0; n < NB; ++n)
-                for (int t8 = 0; t8 < 8; ++t8) {
-                    const int row = n * 8 + t8;
-                    const int src = (lane & ~3) | t8 >> 1;
+                for (int n = 0; n < NR; ++n) {
                     float w[2];
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
-                        const float e0 = __shfl_sync(0xffffffffu, s[n][2 * y], src), e1 = __shfl_sync(0xffffffffu, s[n][2 * y + 1], src);
-                        w[y] = unpack16<BF16>(pack16<BF16>(t8 & 1 ? e1 : e0, 0.0f)).x;
+                        const float e0 = __shfl_sync(0xffffffffu, s[0][n][y], src), e1 = __shfl_sync(0xffffffffu, s[0][n][y + 2], src);
+                        w[y] = unpack16<BF16>(pack16<BF16>(t & 8 ? e1 : e0, 0.0f)).x;
                     }
-                    const bool v0 = visible(pos[0], base + row, a.window, a.sinks), v1 = visible(pos[1], base + row, a.window, a.sinks);
+                    const bool v0 = visible(pos[n][0], base + t, a.window, a.sinks), v1 = visible(pos[n][1], base + t, a.window, a.sinks);
 #pragma unroll
-                    for (int d = 0; d < 2 * KS; ++d) {
-                        const float2 v = unpack16<BF16>(*reinterpret_cast<const uint32_t *>(
-                            st + S::kHalf + row * S::kRow + swizzle<DP, FMT, true>(row, d) * 16 + i4 * 4));
-                        if (v0) {
-                            o[d][0] += w[0] * v.x;
-                            o[d][1] += w[0] * v.y;
+                    for (int k = 0; k < KS; ++k)
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            const float v = unpack16<BF16>(*reinterpret_cast<const uint16_t *>(
+                                st + S::kHalf + t * S::kRow + swizzle<DP, FMT, true>(t, k * 2 + y) * 16 + g * 2)).x;
+                            if (v0) o[k][n][2 * y] += w[0] * v;
+                            if (v1) o[k][n][2 * y + 1] += w[1] * v;
                         }
-                        if (v1) {
-                            o[d][2] += w[1] * v.x;
-                            o[d][3] += w[1] * v.y;
-                        }
-                    }
                 }
+            }
         }
         if (cu.j + 1 < u.nt && x + 1 < count) {
             ++cu.j;
@@ -821,24 +901,27 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_step(const __grid_consta
         __syncwarp();
         float *const xo = reinterpret_cast<float *>(st);
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
-            l[y] += __shfl_xor_sync(0xffffffffu, l[y], 1);
-            l[y] += __shfl_xor_sync(0xffffffffu, l[y], 2);
-            const int r = g + y * 8;
-            if (r >= u.rows) continue;
-            if (i4 == 0) s_ml[warp * 16 + r] = make_float2(m[y], l[y]);
-            // a lane's elements: of 16-bit V 8d + 2i, +1 in o[d]; of 8-bit V 16d + 4i .. + 3 in o[2d], o[2d + 1]
-            if constexpr (FMT == kFmt16) {
+        for (int n = 0; n < NR; ++n)
 #pragma unroll
-                for (int d = 0; d < 2 * KS; ++d)
-                    *reinterpret_cast<float2 *>(xo + r * DP + d * 8 + 2 * i4) = make_float2(o[d][2 * y], o[d][2 * y + 1]);
-            } else {
+            for (int y = 0; y < 2; ++y) {
+                float w = l[n][y];
+                w += __shfl_xor_sync(0xffffffffu, w, 4);
+                w += __shfl_xor_sync(0xffffffffu, w, 8);
+                w += __shfl_xor_sync(0xffffffffu, w, 16);
+                const int r = n * 8 + 2 * i4 + y;
+                if (r >= u.rows) continue;
+                if (g == 0) s_ml[warp * kRows + r] = make_float2(m[n][y], w);
+                const float f = FMT == kFmt16 ? 1.0f : vmax;
 #pragma unroll
-                for (int d = 0; d < KS; ++d)
-                    *reinterpret_cast<float4 *>(xo + r * DP + d * 16 + 4 * i4) =
-                        make_float4(o[2 * d][2 * y], o[2 * d + 1][2 * y], o[2 * d][2 * y + 1], o[2 * d + 1][2 * y + 1]);
+                for (int k = 0; k < KS; ++k) {
+                    if constexpr (FMT == kFmt16) {
+                        xo[r * DP + k * 16 + g] = o[k][n][y];
+                        xo[r * DP + k * 16 + g + 8] = o[k][n][y + 2];
+                    } else {
+                        *reinterpret_cast<float2 *>(xo + r * DP + k * 16 + 2 * g) = make_float2(o[k][n][y] * f, o[k][n][y + 2] * f);
+                    }
+                }
             }
-        }
         if (__any_sync(0xffffffffu, bad) && lane == 0) s_bad = x + 1;
         __syncthreads();
         const long long u0 = sh.x0 + x - cu.j, u1 = u0 + u.nt;
@@ -850,7 +933,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_step(const __grid_consta
         if (!whole) slot = slot_of(sh, blockIdx.x, u0);
         auto write = [&](int r, float mm, float ll, float4 w) {
             const int t = quot(r, c.div_g), hd = u.h * c.G + r - t * c.G;
-            const float inv = ll == 0.0f ? 0.0f : 1.0f / (ll * kLift);
+            const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
             if (d < c.D)
                 *reinterpret_cast<uint2 *>(a.out + (int64_t)(u.q0 + t) * a.o_t + (int64_t)hd * a.o_h + d * 2) =
                     make_uint2(pack16<BF16>(w.x * inv, w.y * inv), pack16<BF16>(w.z * inv, w.w * inv));
@@ -870,10 +953,10 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_step(const __grid_consta
             float mm = -INFINITY, ll = 0.0f;
             float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-            for (int w = 0; w < 4; ++w) mm = fmaxf(mm, s_ml[w * 16 + r].x);
+            for (int w = 0; w < 4; ++w) mm = fmaxf(mm, s_ml[w * kRows + r].x);
 #pragma unroll
             for (int w = 0; w < 4; ++w)
-                join(s_ml[w * 16 + r], *reinterpret_cast<const float4 *>(smem + w * S::kWarp + x % S::kStages * S::kStage + (r * DP + d) * 4), mm, ll, acc);
+                join(s_ml[w * kRows + r], *reinterpret_cast<const float4 *>(smem + w * S::kWarp + x % S::kStages * S::kStage + (r * DP + d) * 4), mm, ll, acc);
             if (lost) ll = __uint_as_float(0x7fffffffu);
             if (whole) {
                 write(r, mm, ll, acc);
@@ -898,9 +981,10 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_step(const __grid_consta
                 for (int r = tid / kLanes; r < u.rows; r += kThreads / kLanes) {
                     auto at = [&](int k) { return (k == c0 ? s0 : 2 * (int64_t)k) * kStepRows + r; };
                     float mm = -INFINITY, ll = 0.0f;
+#pragma unroll 8
                     for (int k = c0; k <= c1; ++k) mm = fmaxf(mm, __ldcg(&a.part_ml[at(k)].x));
                     float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
+#pragma unroll 8
                     for (int k = c0; k <= c1; ++k)
                         join(__ldcg(a.part_ml + at(k)), __ldcg(reinterpret_cast<const float4 *>(a.part_o + at(k) * 128 + d)), mm, ll, acc);
                     write(r, mm, ll, acc);
@@ -914,48 +998,48 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_step(const __grid_consta
 }
 
 using Kernel = void (*)(const AttendLaunch);
+struct Pick {
+    Kernel k;
+    size_t smem;
+    int ctas;  // of an SM
+};
 
 template <bool BF16, int FMT, int DP>
-Kernel pick_rows(int rows) {
-    return rows <= 16 ? k_attend_step<BF16, FMT, DP> : rows <= 32 ? k_attend_rows<BF16, FMT, DP, 2> : k_attend_rows<BF16, FMT, DP, 4>;
-}
-template <int FMT, int DP>
-Kernel pick_type(bool bf16, int rows) {
-    return bf16 ? pick_rows<true, FMT, DP>(rows) : pick_rows<false, FMT, DP>(rows);
+Pick pick_rows(int rows) {
+    if (rows <= 8) return {k_attend_step<BF16, FMT, DP, 1>, Solo<DP, FMT, 1>::kSmem, Solo<DP, FMT, 1>::kCtas};
+    if (rows <= 16) return {k_attend_step<BF16, FMT, DP, 2>, Solo<DP, FMT, 2>::kSmem, Solo<DP, FMT, 2>::kCtas};
+    return {rows <= 32 ? k_attend_rows<BF16, FMT, DP, 2> : k_attend_rows<BF16, FMT, DP, 4>, Shape<DP, FMT>::kSmem, 2};
 }
 template <int FMT>
-Kernel pick(bool bf16, int D, int rows, size_t &smem) {
-    smem = rows <= 16 ? (D <= 64 ? Solo<64, FMT>::kSmem : Solo<128, FMT>::kSmem)
-                      : (D <= 64 ? Shape<64, FMT>::kSmem : Shape<128, FMT>::kSmem);
-    return D <= 64 ? pick_type<FMT, 64>(bf16, rows) : pick_type<FMT, 128>(bf16, rows);
+Pick pick_type(bool bf16, int D, int rows) {
+    return D <= 64 ? (bf16 ? pick_rows<true, FMT, 64>(rows) : pick_rows<false, FMT, 64>(rows))
+                   : (bf16 ? pick_rows<true, FMT, 128>(rows) : pick_rows<false, FMT, 128>(rows));
 }
-Kernel pick_kernel(bool bf16, int fmt, int D, int rows, size_t &smem) {
-    return fmt == kFmt16 ? pick<kFmt16>(bf16, D, rows, smem)
-         : fmt == kFmtE4M3 ? pick<kFmtE4M3>(bf16, D, rows, smem)
-                           : pick<kFmtInt8>(bf16, D, rows, smem);
+Pick pick(bool bf16, int fmt, int D, int rows) {
+    return fmt == kFmt16 ? pick_type<kFmt16>(bf16, D, rows)
+         : fmt == kFmtE4M3 ? pick_type<kFmtE4M3>(bf16, D, rows)
+                           : pick_type<kFmtInt8>(bf16, D, rows);
 }
 
 }  // namespace
 
-int attend_step_ctas(int sms) { return 2 * sms; }
+int attend_step_ctas(int sms) { return 4 * sms; }
 
 cudaError_t attend_step_init() {
     for (int bf16 = 0; bf16 < 2; ++bf16)
         for (int fmt = 0; fmt < 3; ++fmt)
             for (int D = 64; D <= 128; D += 64)
-                for (int rows = 16; rows <= 64; rows *= 2) {
-                    size_t smem;
-                    const Kernel k = pick_kernel(bf16, fmt, D, rows, smem);
-                    const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+                for (int rows = 8; rows <= 64; rows *= 2) {
+                    const Pick p = pick(bf16, fmt, D, rows);
+                    const cudaError_t e = cudaFuncSetAttribute(p.k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)p.smem);
                     if (e != cudaSuccess) return e;
                 }
     return cudaSuccess;
 }
 
-cudaError_t launch_attend_step(const AttendLaunch &a, bool bf16, int fmt, int rows, int ctas, cudaStream_t st) {
-    size_t smem;
-    const Kernel k = pick_kernel(bf16, fmt, a.c.D, rows, smem);
-    return launch_chained(k, ctas, kThreads, smem, st, a);
+cudaError_t launch_attend_step(const AttendLaunch &a, bool bf16, int fmt, int rows, int sms, cudaStream_t st) {
+    const Pick p = pick(bf16, fmt, a.c.D, rows);
+    return launch_chained(p.k, p.ctas * sms, kThreads, p.smem, st, a);
 }
 
 }  // namespace lr

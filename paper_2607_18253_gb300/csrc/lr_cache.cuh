@@ -89,7 +89,7 @@ struct AttendLaunch {
                                  // between calls
 };
 constexpr int kStepRows = 64;   // rows of a unit of the step kernel, at most
-cudaError_t launch_attend_step(const AttendLaunch &a, bool bf16, int fmt, int rows, int ctas, cudaStream_t st);
+cudaError_t launch_attend_step(const AttendLaunch &a, bool bf16, int fmt, int rows, int sms, cudaStream_t st);
 cudaError_t attend_step_init();
 int attend_step_ctas(int sms);  // CTAs of a launch, at most
 constexpr int kChunkRows = 256;  // rows of a unit of the chunk kernel; one CTA an SM

@@ -252,8 +252,7 @@ int lr_cache_attend(lr_cache *c, const lr_cache_batch *b, int32_t T, const void 
     a.part_o = c->step.o;
     a.part_ml = c->step.ml;
     a.done = c->step.done;
-    const int rows = a.row_hi <= 16 ? 16 : a.row_hi <= 32 ? 32 : 64;
-    cudaError_t e = lr::launch_attend_step(a, c->bf16, c->cfg.format, rows, lr::attend_step_ctas(c->sms), st);
+    cudaError_t e = lr::launch_attend_step(a, c->bf16, c->cfg.format, a.row_hi, c->sms, st);
     return e == cudaSuccess ? LR_OK : cuda_fail(c, e, "attention launch");
 }
 

@@ -93,6 +93,7 @@ __device__ __forceinline__ uint2 quantise(const uint4 &w, float &scale) {
     constexpr float kTop = FMT == kFmtE4M3 ? 448.0f : 127.0f;
     const float a = __uint_as_float(top), inv = __fdiv_rn(kTop, a);
     scale = __fdiv_rn(a, kTop);
+    if (top >= 0x7f800000u) return make_uint2(0, 0);  // the scale says it all
     uint2 r;
     if constexpr (FMT == kFmtE4M3) {
         uint32_t h[4];
