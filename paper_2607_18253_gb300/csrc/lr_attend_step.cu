@@ -526,6 +526,69 @@ struct Solo {
     static_assert(kStage >= 8 * NR * DP * 4, "room for a warp's sums");
 };
 
+// A part (m, l, sums) added to others whose common maximum is mm.
+__device__ __forceinline__ void add_part(float2 ml, const float4 &w, float mm, float &ll, float4 &acc) {
+    if (ml.x == -INFINITY && ml.y == 0.0f) return;  // saw nothing
+    const float f = ml.x == -INFINITY ? 0.0f : exp2_fast(ml.x - mm);
+    ll += ml.y == 0.0f ? 0.0f : ml.y * f;
+    acc.x += w.x * f;
+    acc.y += w.y * f;
+    acc.z += w.z * f;
+    acc.w += w.w * f;
+}
+
+// Elements d .. d + 3 of a finished row of a unit whose only tile of rows it is.
+template <bool BF16>
+__device__ __forceinline__ void write_row(const AttendLaunch &a, int r, int d, int q0, int h, float mm, float ll, float4 w) {
+    const CacheDev &c = a.c;
+    const int t = quot(r, c.div_g), hd = h * c.G + r - t * c.G;
+    const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
+    if (d < c.D)
+        *reinterpret_cast<uint2 *>(a.out + (int64_t)(q0 + t) * a.o_t + (int64_t)hd * a.o_h + d * 2) =
+            make_uint2(pack16<BF16>(w.x * inv, w.y * inv), pack16<BF16>(w.z * inv, w.w * inv));
+    if (a.lse && d == 0) a.lse[(int64_t)(q0 + t) * c.Hq + hd] = ll == 0.0f ? -INFINITY : (mm + log2f(ll)) * 0.69314718f;
+}
+
+// Joins the parts of a unit, in the order of the CTAs whichever came last: a warp a row, its lanes first the
+// parts' maxima and sums, then four elements each of 16 parts at a time (of 2 x 16 with 64 elements).  The
+// first part is in slot0, the others each the first of their CTAs.  (Not inlined: its registers are not the loop's.)
+template <bool BF16, int DP>
+__device__ __noinline__ void join_parts(const AttendLaunch &a, int c0, int parts, int slot0, int rows, int q0, int h) {
+    constexpr int kLanes = DP / 4, kTwo = 32 / kLanes;
+    const int lane = threadIdx.x % 32, part0 = lane / kLanes, e = lane % kLanes * 4;
+    for (int r = threadIdx.x / 32; r < rows; r += kThreads / 32) {
+        auto at = [&](int k) { return (int64_t)(k == 0 ? slot0 : 2 * (c0 + k)) * kStepRows + r; };
+        float mm = -INFINITY, ll = 0.0f;
+        for (int k = lane; k < parts; k += 32) mm = fmaxf(mm, __ldcg(&a.part_ml[at(k)].x));
+#pragma unroll
+        for (int z = 16; z >= 1; z /= 2) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, z));
+        float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int k0 = 0; k0 < parts; k0 += 16 * kTwo) {
+            float2 ml = make_float2(-INFINITY, 0.0f);
+            if (k0 + lane < parts && lane < 16 * kTwo) ml = __ldcg(a.part_ml + at(k0 + lane));
+            float4 w[16];
+#pragma unroll
+            for (int z = 0; z < 16; ++z) {
+                const int k = k0 + z * kTwo + part0;
+                w[z] = k < parts ? __ldcg(reinterpret_cast<const float4 *>(a.part_o + at(k) * 128 + e)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            }
+#pragma unroll
+            for (int z = 0; z < 16; ++z) {
+                const int src = z * kTwo + part0;
+                add_part(make_float2(__shfl_sync(0xffffffffu, ml.x, src), __shfl_sync(0xffffffffu, ml.y, src)), w[z], mm, ll, acc);
+            }
+        }
+        if constexpr (kTwo == 2) {
+            ll += __shfl_xor_sync(0xffffffffu, ll, 16);
+            acc.x += __shfl_xor_sync(0xffffffffu, acc.x, 16);
+            acc.y += __shfl_xor_sync(0xffffffffu, acc.y, 16);
+            acc.z += __shfl_xor_sync(0xffffffffu, acc.z, 16);
+            acc.w += __shfl_xor_sync(0xffffffffu, acc.w, 16);
+        }
+        if (part0 == 0) write_row<BF16>(a, r, e, q0, h, mm, ll, acc);
+    }
+}
+
 template <bool BF16, int FMT, int DP, int NR>
 __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_step(const __grid_constant__ AttendLaunch a) {
     using S = Solo<DP, FMT, NR>;
@@ -558,27 +621,29 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
     const int count = (int)(sh.x1 - sh.x0);
     lk = cu;
 
-    // where lane l's token of the tile at lk is (in bytes from the cache's start; the scales in floats)
-    int64_t off = -1, soff = 0;
-    bool bad = false, bad_next = false;
+    // Lane l's token of the tile at lk: its block as the table has it -- a load that nothing waits for until the
+    // tile's copies are issued, a tile later --, its place and KV head.  seen: some row of the unit sees it (what
+    // none sees is not looked up, its block may be gone: zeros).
+    int blk = -1, place = 0, head = 0;
+    bool seen = false, bad = false;
     auto look = [&]() {
         const int t = lk.base() + warp * kMine + lane;
-        off = -1;
-        soff = 0;
-        // what no row of the unit sees is not looked up (its block may be gone): zeros
-        if (lane >= kMine || t > lk.u.hi || (a.window > 0 && t <= lk.u.lo - a.window && t >= a.sinks)) return;
-        int place;
-        const int64_t blk = block_of(c, a.b, lk.u.s, t, place);
-        if (blk < 0) {
-            bad_next = true;
-            report(c.status, kEInval);
-            return;
-        }
-        off = blk * c.sb + place * c.st + lk.u.h * c.sh;
-        soff = blk * c.ssb + place * c.sst + lk.u.h * c.ssh;
+        seen = lane < kMine && t <= lk.u.hi && !(a.window > 0 && t <= lk.u.lo - a.window && t >= a.sinks);
+        const int i = quot(max(t, 0), c.div_b);
+        place = t - i * c.b;
+        head = lk.u.h;
+        blk = -1;
+        if (seen && i < a.b.max_blocks) blk = __ldg(a.b.table + (int64_t)lk.u.s * a.b.table_stride + i);
     };
+    unsigned bad_tiles = 0;  // a bit for each tile on its way that has a block out of range
     auto issue = [&](int tile) {
         char *const st = stages + tile % S::kStages * S::kStage;
+        const bool there = seen && (uint32_t)blk < (uint32_t)c.nb;
+        if (__any_sync(0xffffffffu, seen && !there)) {
+            bad_tiles |= 1u << (tile & 31);
+            report(c.status, kEInval);
+        }
+        const int64_t off = there ? (int64_t)blk * c.sb + place * c.st + head * c.sh : -1;
         constexpr int kStep = 32 / S::kChunks;
         const int ch = lane % S::kChunks, r0 = lane / S::kChunks;
         const bool in = ch * 16 < c.D * (FMT == kFmt16 ? 2 : 1);
@@ -593,35 +658,31 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
         }
         if constexpr (FMT != kFmt16) {
             if (lane < kMine) {
+                const int64_t so = there ? (int64_t)blk * c.ssb + place * c.sst + head * c.ssh : 0;
                 float *const to = scales + tile % S::kStages * 2 * kMine + lane;
-                copy4(smem_addr(to), c.ks + soff, off >= 0);
-                copy4(smem_addr(to + kMine), c.vs + soff, off >= 0);
+                copy4(smem_addr(to), c.ks + so, there);
+                copy4(smem_addr(to + kMine), c.vs + so, there);
             }
         }
     };
-    unsigned bad_tiles = 0;  // a bit for each tile on its way
+    look();
     for (int t = 0; t < S::kStages - 1; ++t) {
-        if (t < count) {
-            bad_next = false;
+        if (t < count) issue(t);
+        if (t + 1 < count) {
+            lk.next(a);
             look();
-            if (__any_sync(0xffffffffu, bad_next)) bad_tiles |= 1u << t;
-            issue(t);
-            if (t + 1 < count) lk.next(a);
         }
         copy_commit();
-    }
-    if (S::kStages - 1 < count) {
-        bad_next = false;
-        look();
     }
 
     // a lane's columns are the rows n * 8 + 2 * i4, + 1 of the unit
     uint32_t q[KS][NR][2];
-    float o[KS][NR][4], m[NR][2], l[NR][2], qf[NR][2], vmax = 0.0f;
+    float o[KS][NR][4], m[NR][2], l[NR][2], qf[NR][2], less[NR][2], vmax = 0.0f, vinv = 0.0f;  // less: m, 0 where it is -inf
     int pos[NR][2];
-    for (int x = 0; x < count; ++x) {
+    for (int x = 0; x < count;) {
         const Unit &u = cu.u;
-        if (x == 0 || cu.j == 0) {  // a new unit: its queries, straight to the registers that multiply them
+        const long long u0 = sh.x0 + x - cu.j, u1 = u0 + u.nt;  // the unit's tiles
+        {  // its queries, straight to the registers that multiply them
 #pragma unroll
             for (int n = 0; n < NR; ++n) {
                 const int r = n * 8 + g;  // (the row whose elements the lane holds)
@@ -671,19 +732,19 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
                     pos[n][y] = row < u.rows ? u.kv - u.ql + quot(row, c.div_g) : -1;
                     qf[n][y] = a.scale_log2 * __shfl_sync(0xffffffffu, pow2, (2 * i4 + y) * 4);
                     m[n][y] = -INFINITY;
+                    less[n][y] = 0.0f;
                     l[n][y] = 0.0f;
                 }
             }
-            vmax = 0.0f;
+            vmax = vinv = 0.0f;
             bad = false;
         }
+        for (const int end = x + min(u.nt - cu.j, count - x); x < end; ++x, ++cu.j) {
         // the copies of the tile ahead, then the places of the one after it (their latency is the tile's work)
         if (x + S::kStages - 1 < count) {
-            if (__any_sync(0xffffffffu, bad_next)) bad_tiles |= 1u << ((x + S::kStages - 1) & 31);
             issue(x + S::kStages - 1);
             if (x + S::kStages < count) {
                 lk.next(a);
-                bad_next = false;
                 look();
             }
         }
@@ -776,6 +837,7 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
         if (__any_sync(0xffffffffu, raise)) {
             const float fv = FMT != kFmt16 && vnew > vmax ? vmax / vnew : 1.0f;  // 0 at first
             vmax = vnew;
+            if (FMT != kFmt16 && vmax > 0.0f) vinv = 1.0f / vmax;
 #pragma unroll
             for (int n = 0; n < NR; ++n)
 #pragma unroll
@@ -786,6 +848,7 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
                     w = fmaxf(w, __shfl_xor_sync(0xffffffffu, w, 16));
                     const float mn = fmaxf(m[n][y], w), f = mn == -INFINITY ? 1.0f : exp2_fast(m[n][y] - mn);
                     m[n][y] = mn;
+                    less[n][y] = mn == -INFINITY ? 0.0f : mn;
                     l[n][y] *= f;
 #pragma unroll
                     for (int k = 0; k < KS; ++k) {
@@ -794,14 +857,13 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
                     }
                 }
         }
-        const float vinv = FMT != kFmt16 && vmax > 0.0f ? 1.0f / vmax : 0.0f;
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int n = 0; n < NR; ++n)
 #pragma unroll
                 for (int z = 0; z < 4; ++z) {
-                    const float p = exp2_fast(s[b][n][z] - (m[n][z & 1] == -INFINITY ? 0.0f : m[n][z & 1]));
+                    const float p = exp2_fast(s[b][n][z] - less[n][z & 1]);
                     l[n][z & 1] += p;
                     if constexpr (FMT != kFmt16) {
                         // (a scale that is not finite stays away from a weight that the mask takes)
@@ -891,15 +953,12 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
                 }
             }
         }
-        if (cu.j + 1 < u.nt && x + 1 < count) {
-            ++cu.j;
-            __syncwarp();
-            continue;
+        __syncwarp();
         }
 
         // ---- the unit ends here, for this CTA: the warps' sums to their stages just used, [row][element] ----
-        __syncwarp();
-        float *const xo = reinterpret_cast<float *>(st);
+        const int used = (x - 1) % S::kStages * S::kStage;
+        float *const xo = reinterpret_cast<float *>(stages + used);
 #pragma unroll
         for (int n = 0; n < NR; ++n)
 #pragma unroll
@@ -922,33 +981,14 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
                     }
                 }
             }
-        if (__any_sync(0xffffffffu, bad) && lane == 0) s_bad = x + 1;
+        if (__any_sync(0xffffffffu, bad) && lane == 0) s_bad = x;
         __syncthreads();
-        const long long u0 = sh.x0 + x - cu.j, u1 = u0 + u.nt;
         const bool whole = u0 >= sh.x0 && u1 <= sh.x1;
         constexpr int kLanes = DP / 4;  // four elements a thread
         const int d = tid % kLanes * 4;
-        const bool lost = s_bad == x + 1;
+        const bool lost = s_bad == x;
         int64_t slot = 0;
         if (!whole) slot = slot_of(sh, blockIdx.x, u0);
-        auto write = [&](int r, float mm, float ll, float4 w) {
-            const int t = quot(r, c.div_g), hd = u.h * c.G + r - t * c.G;
-            const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
-            if (d < c.D)
-                *reinterpret_cast<uint2 *>(a.out + (int64_t)(u.q0 + t) * a.o_t + (int64_t)hd * a.o_h + d * 2) =
-                    make_uint2(pack16<BF16>(w.x * inv, w.y * inv), pack16<BF16>(w.z * inv, w.w * inv));
-            if (a.lse && d == 0) a.lse[(int64_t)(u.q0 + t) * c.Hq + hd] = ll == 0.0f ? -INFINITY : (mm + log2f(ll)) * 0.69314718f;
-        };
-        // a join of parts (m, l, sums), in a fixed order
-        auto join = [&](float2 ml, const float4 &w, float mm, float &ll, float4 &acc) {
-            if (ml.x == -INFINITY && ml.y == 0.0f) return;  // saw nothing
-            const float f = ml.x == -INFINITY ? 0.0f : exp2_fast(ml.x - mm);
-            ll += ml.y == 0.0f ? 0.0f : ml.y * f;
-            acc.x += w.x * f;
-            acc.y += w.y * f;
-            acc.z += w.z * f;
-            acc.w += w.w * f;
-        };
         for (int r = tid / kLanes; r < u.rows; r += kThreads / kLanes) {
             float mm = -INFINITY, ll = 0.0f;
             float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -956,10 +996,10 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
             for (int w = 0; w < 4; ++w) mm = fmaxf(mm, s_ml[w * kRows + r].x);
 #pragma unroll
             for (int w = 0; w < 4; ++w)
-                join(s_ml[w * kRows + r], *reinterpret_cast<const float4 *>(smem + w * S::kWarp + x % S::kStages * S::kStage + (r * DP + d) * 4), mm, ll, acc);
+                add_part(s_ml[w * kRows + r], *reinterpret_cast<const float4 *>(smem + w * S::kWarp + used + (r * DP + d) * 4), mm, ll, acc);
             if (lost) ll = __uint_as_float(0x7fffffffu);
             if (whole) {
-                write(r, mm, ll, acc);
+                write_row<BF16>(a, r, d, u.q0, u.h, mm, ll, acc);
             } else {
                 if (d == 0) a.part_ml[slot * kStepRows + r] = make_float2(mm, ll);
                 *reinterpret_cast<float4 *>(a.part_o + (slot * kStepRows + r) * 128 + d) = acc;
@@ -975,24 +1015,16 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
                 s_last = last;
             }
             __syncthreads();
-            if (s_last) {  // join the parts, in the order of the CTAs whichever came last
+            if (s_last) {
                 __threadfence();
-                const int64_t s0 = slot_of(sh, c0, u0);  // (a unit is the first of every later CTA)
-                for (int r = tid / kLanes; r < u.rows; r += kThreads / kLanes) {
-                    auto at = [&](int k) { return (k == c0 ? s0 : 2 * (int64_t)k) * kStepRows + r; };
-                    float mm = -INFINITY, ll = 0.0f;
-#pragma unroll 8
-                    for (int k = c0; k <= c1; ++k) mm = fmaxf(mm, __ldcg(&a.part_ml[at(k)].x));
-                    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 8
-                    for (int k = c0; k <= c1; ++k)
-                        join(__ldcg(a.part_ml + at(k)), __ldcg(reinterpret_cast<const float4 *>(a.part_o + at(k) * 128 + d)), mm, ll, acc);
-                    write(r, mm, ll, acc);
-                }
+                join_parts<BF16, DP>(a, c0, c1 - c0 + 1, slot_of(sh, c0, u0), u.rows, u.q0, u.h);
             }
         }
         __syncthreads();  // the stages are free again
-        if (x + 1 < count) cu.next(a);
+        if (x < count) {
+            --cu.j;  // (the last tile that was taken)
+            cu.next(a);
+        }
     }
     chain_next();
 }
