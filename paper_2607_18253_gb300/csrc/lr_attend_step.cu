@@ -514,12 +514,15 @@ template <int DP, int FMT, int NR>
 struct Solo {
     static constexpr int kRow = DP * (FMT == kFmt16 ? 2 : 1);
     static constexpr int kChunks = kRow / 16;
-    static constexpr int kMine = FMT == kFmt16 || NR == 1 ? 16 : 32;  // tokens of a warp
+    static constexpr int kMine = FMT == kFmt16 ? 16 : 32;  // tokens of a warp
     static constexpr int kTile = 4 * kMine;
     static constexpr int kHalf = kMine * kRow;
     static constexpr int kStage = 2 * kHalf;
-    static constexpr int kStages = FMT == kFmt16 && DP == 128 ? 2 : 3;
-    static constexpr int kCtas = NR == 1 ? (FMT == kFmt16 && DP == 128 ? 3 : 4) : 2;  // of an SM
+    // stages, and CTAs of an SM.  64 elements of 16 tokens in 4 CTAs; else by what the room takes, measured: 8-bit
+    // 2 x 3 CTAs (256 sequences with a window over int8 131 us; 3 x 2: 150; 16 tokens, 3 x 4: 151), 16-bit
+    // 3 x 2 (a context of 200,001 tokens 86 us; 2 x 3: 98).
+    static constexpr int kStages = FMT == kFmt16 || DP == 64 ? 3 : 2;
+    static constexpr int kCtas = NR == 2 ? 2 : DP == 64 ? (FMT == kFmt16 ? 4 : 3) : FMT == kFmt16 ? 2 : 3;
     static constexpr int kScales = FMT == kFmt16 ? 0 : kStages * 2 * kMine * 4;
     static constexpr int kWarp = kStages * kStage + kScales;
     static constexpr int kSmem = 4 * kWarp + 4 * 8 * NR * 8;
@@ -621,44 +624,67 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
     const int count = (int)(sh.x1 - sh.x0);
     lk = cu;
 
-    // Lane l's token of the tile at lk: its block as the table has it -- a load that nothing waits for until the
-    // tile's copies are issued, a tile later --, its place and KV head.  seen: some row of the unit sees it (what
-    // none sees is not looked up, its block may be gone: zeros).
-    int blk = -1, place = 0, head = 0;
-    bool seen = false, bad = false;
+    // The block of lane l's token of the tile at lk, as the table has it: a load that nothing waits for until the
+    // tile's copies are issued, a tile later.  Where blocks are multiples of 16 tokens, 16 neighbouring tokens
+    // share one, and their addresses follow from the first's: 16 lanes have one look (fewer instructions,
+    // which bound an 8-bit step: XX with a look a token).  What no row of the unit sees is not looked
+    // up (its block may be gone) and reads as zeros.
+    const bool even = c.b % 16 == 0;
+    int blk = -1, place = 0;
+    auto seen = [&](int t) { return t <= lk.u.hi && !(a.window > 0 && t <= lk.u.lo - a.window && t >= a.sinks); };
     auto look = [&]() {
-        const int t = lk.base() + warp * kMine + lane;
-        seen = lane < kMine && t <= lk.u.hi && !(a.window > 0 && t <= lk.u.lo - a.window && t >= a.sinks);
-        const int i = quot(max(t, 0), c.div_b);
+        const int t0 = lk.base() + warp * kMine, t = t0 + (even ? lane & ~15 : lane);
+        const int i = quot(t, c.div_b);
         place = t - i * c.b;
-        head = lk.u.h;
         blk = -1;
-        if (seen && i < a.b.max_blocks) blk = __ldg(a.b.table + (int64_t)lk.u.s * a.b.table_stride + i);
+        const int last = min(even ? t + 15 : t, lk.u.hi);
+        const bool any = t <= lk.u.hi && (a.window == 0 || last > lk.u.lo - a.window || t < a.sinks);
+        if (lane < kMine && any && i < a.b.max_blocks) blk = __ldg(a.b.table + (int64_t)lk.u.s * a.b.table_stride + i);
     };
     unsigned bad_tiles = 0;  // a bit for each tile on its way that has a block out of range
+    bool bad = false;
     auto issue = [&](int tile) {
         char *const st = stages + tile % S::kStages * S::kStage;
-        const bool there = seen && (uint32_t)blk < (uint32_t)c.nb;
-        if (__any_sync(0xffffffffu, seen && !there)) {
+        constexpr int kStep = 32 / S::kChunks;
+        const int ch = lane % S::kChunks, r0 = lane / S::kChunks, t0 = lk.base() + warp * kMine;
+        const bool in = ch * 16 < c.D * (FMT == kFmt16 ? 2 : 1), mine = lane < kMine && seen(t0 + lane);
+        const int myblk = even ? __shfl_sync(0xffffffffu, blk, lane & 16) : blk;
+        const bool there = mine && (uint32_t)myblk < (uint32_t)c.nb;
+        const unsigned have = __ballot_sync(0xffffffffu, there);  // a bit a token
+        if (__any_sync(0xffffffffu, mine && !there)) {
             bad_tiles |= 1u << (tile & 31);
             report(c.status, kEInval);
         }
-        const int64_t off = there ? (int64_t)blk * c.sb + place * c.st + head * c.sh : -1;
-        constexpr int kStep = 32 / S::kChunks;
-        const int ch = lane % S::kChunks, r0 = lane / S::kChunks;
-        const bool in = ch * 16 < c.D * (FMT == kFmt16 ? 2 : 1);
+        if (even) {
 #pragma unroll
-        for (int r1 = 0; r1 < kMine; r1 += kStep) {
-            const int r = r1 + r0;
-            const int64_t o = __shfl_sync(0xffffffffu, off, r);
-            const bool ok = in && o >= 0;
-            const int64_t at = ok ? o + ch * 16 : 0;
-            copy16(smem_addr(st + r * S::kRow + swizzle<DP, FMT, false>(r, ch) * 16), c.k + at, ok);
-            copy16(smem_addr(st + S::kHalf + r * S::kRow + swizzle<DP, FMT, true>(r, ch) * 16), c.v + at, ok);
+            for (int r2 = 0; r2 < kMine; r2 += 16) {
+                const int bk = __shfl_sync(0xffffffffu, blk, r2), pl = __shfl_sync(0xffffffffu, place, r2);
+                int64_t at = (int64_t)bk * c.sb + (int64_t)(pl + r0) * c.st + lk.u.h * c.sh + ch * 16;
+                const int64_t step = kStep * c.st;
+#pragma unroll
+                for (int r1 = r2; r1 < r2 + 16; r1 += kStep, at += step) {
+                    const int r = r1 | r0;
+                    const bool ok = in && (have >> r & 1);
+                    const char *const k = ok ? c.k + at : c.k, *const v = ok ? c.v + at : c.v;
+                    copy16(smem_addr(st + r * S::kRow + swizzle<DP, FMT, false>(r, ch) * 16), k, ok);
+                    copy16(smem_addr(st + S::kHalf + r * S::kRow + swizzle<DP, FMT, true>(r, ch) * 16), v, ok);
+                }
+            }
+        } else {
+            const int64_t off = (int64_t)blk * c.sb + place * c.st + lk.u.h * c.sh + ch * 16;
+#pragma unroll
+            for (int r1 = 0; r1 < kMine; r1 += kStep) {
+                const int r = r1 | r0;
+                const int64_t o = __shfl_sync(0xffffffffu, off - ch * 16, r) + ch * 16;
+                const bool ok = in && (have >> r & 1);
+                const char *const k = ok ? c.k + o : c.k, *const v = ok ? c.v + o : c.v;
+                copy16(smem_addr(st + r * S::kRow + swizzle<DP, FMT, false>(r, ch) * 16), k, ok);
+                copy16(smem_addr(st + S::kHalf + r * S::kRow + swizzle<DP, FMT, true>(r, ch) * 16), v, ok);
+            }
         }
         if constexpr (FMT != kFmt16) {
             if (lane < kMine) {
-                const int64_t so = there ? (int64_t)blk * c.ssb + place * c.sst + head * c.ssh : 0;
+                const int64_t so = there ? (int64_t)myblk * c.ssb + (place + (even ? lane & 15 : 0)) * c.sst + lk.u.h * c.ssh : 0;
                 float *const to = scales + tile % S::kStages * 2 * kMine + lane;
                 copy4(smem_addr(to), c.ks + so, there);
                 copy4(smem_addr(to + kMine), c.vs + so, there);
@@ -832,7 +858,7 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
             // the largest scale of V so far (positive numbers compare as integers; one that is not finite does not count)
             const uint32_t bits = __float_as_uint(vs[lane % kMine]);
             vnew = fmaxf(vmax, __uint_as_float(__reduce_max_sync(0xffffffffu, bits < 0x7f800000u ? bits : 0u)));
-            raise |= vnew > vmax;
+            raise |= vnew > 2.0f * vmax;  // (weights up to twice as large do no harm)
         }
         if (__any_sync(0xffffffffu, raise)) {
             const float fv = FMT != kFmt16 && vnew > vmax ? vmax / vnew : 1.0f;  // 0 at first
