@@ -61,7 +61,7 @@ struct Shape {
     static constexpr int kBytes = kQ + kStages * kTile + kRaw;
     static constexpr int kBars = 2 + 2 * kStages + 10 + 4 + 1 + 2 * kJobs + 2;
     static constexpr int kScales = FMT == kFmt16 ? 0 : 4 * 2 * kTok * 4;
-    static constexpr int kSmem = kBytes + kScales + 2 * kTok * 8 + kBars * 8 + (kThreads / 32 + 2) * 8 + 12 * 4 + kJobs * sizeof(Job);
+    static constexpr int kSmem = kBytes + kScales + 2 * kTok * 8 + kBars * 8 + (kThreads / 32 + 2) * 8 + 26 * 4 + kJobs * sizeof(Job);
     static_assert(kSmem <= 227 * 1024, "shared memory");
 };
 
@@ -248,7 +248,49 @@ __device__ __noinline__ void add_lost(const AttendLaunch &a, const Unit &u, int 
 struct ChunkLaunch {
     AttendLaunch a;
     CacheMaps m;
+    CUtensorMap q;   // boxes of 64 elements of 128 rows: the query heads of a KV head, times tokens
+    int32_t q_map;   // there is one: their number divides 128
 };
+
+// Scores that a row does not see to -inf (at most `last`, and above `low` or below `sink` it does), in tensor
+// memory and out of the way of the loop, which nearly every tile goes through without; kbad: a bit for each
+// token whose K has a scale that is not finite, to NaN.
+__device__ __noinline__ void mask_scores(uint32_t ts, int last, int low, int sink, const uint32_t *kbad) {
+    auto below = [](int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; };
+#pragma unroll 1
+    for (int k0 = 0; k0 < kTok; k0 += 32) {
+        const uint32_t see = below(last + 1 - k0) & (~below(low + 1 - k0) | below(sink - k0)), nan = kbad ? kbad[k0 / 32] : 0u;
+        if (__all_sync(0xffffffffu, see == ~0u && nan == 0u)) continue;
+        float s[32];
+        tm_load(s, ts + k0);
+        tm_load_wait(s);
+        if (nan) {
+#pragma unroll
+            for (int k = 0; k < 32; ++k)
+                if (nan >> k & 1) s[k] = __uint_as_float(0x7fffffffu);
+        }
+#pragma unroll
+        for (int k = 0; k < 32; ++k)
+            if (!(see >> k & 1)) s[k] = -INFINITY;
+        tm_store(ts + k0, reinterpret_cast<uint32_t *>(s));
+        tm_store(ts + k0 + 16, reinterpret_cast<uint32_t *>(s) + 16);
+    }
+    tm_store_wait();
+}
+// Whether a row sees a token whose V has a scale that is not finite (its weights were multiplied by zero).
+__device__ __noinline__ bool sees_lost(const AttendLaunch &a, const Unit &u, int tile0, int tile1, int pos) {
+    const CacheDev &c = a.c;
+    for (int tile = tile0; tile < tile1; ++tile) {
+        const int base = (tile < u.ns ? tile : u.wf + tile - u.ns) * kTok;
+        for (int t = base; t < base + kTok; ++t) {
+            if (!visible(pos, t, a.window, a.sinks)) continue;
+            int place;
+            const int64_t blk = block_of(c, a.b, u.s, t, place);
+            if (blk >= 0 && !(fabsf(c.vs[blk * c.ssb + place * c.sst + u.h * c.ssh]) < INFINITY)) return true;
+        }
+    }
+    return false;
+}
 
 template <bool BF16, int FMT, int DP, int LOAD>
 __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_constant__ ChunkLaunch in) {
@@ -269,10 +311,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
     uint64_t *const bars = reinterpret_cast<uint64_t *>(places + 2 * kTok);
     long long *const scratch = reinterpret_cast<long long *>(bars + S::kBars);
     Job *const jobs = reinterpret_cast<Job *>(scratch + kThreads / 32 + 2);
-    int *const s_bad = reinterpret_cast<int *>(jobs + kJobs);  // [4] a block of the tile is out of range
+    int *const s_bad = reinterpret_cast<int *>(jobs + kJobs);  // [4] 1: a block of the tile is out of range
     int *const s_lost = s_bad + 4;                             // [half][2] the last scan that found V not finite
     int &s_dead = s_bad[8];
     uint32_t &s_tmem = *reinterpret_cast<uint32_t *>(s_bad + 9);
+    uint32_t *const s_kbad = reinterpret_cast<uint32_t *>(s_bad + 10);  // [4][4] a bit a token: K's scale is not finite
     const uint32_t b0 = smem_addr(bars);
     const uint32_t q_full = b0, q_free = b0 + 8, kv_full = b0 + 16, kv_free = kv_full + 8 * kStages, s_full = kv_free + 8 * kStages,
                    p_half = s_full + 16, p_full = p_half + 16, o_full = p_full + 16, o_free = o_full + 16, sc_full = o_free + 16,
@@ -360,11 +403,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
             for (int j = 0, tile = job.j0; j < n; ++j, ++tile, ++x) {
                 const int base = (tile < ns ? tile : tile + skip) * kTok;
                 const int slot = x & 3;
-                // (the scores first: a half that skips units may be ahead of the scales' barrier by a phase)
-                ok = bar_wait(s_full + 8 * half, n_s & 1, dead) && (FMT == kFmt16 || bar_wait(sc_full + 8 * slot, x >> 2 & 1, dead));
-                if (!ok) break;
-                ++n_s;
-                const float *const ks = scales + slot * 2 * kTok, *const vs = ks + kTok;
                 const bool masked = base + kTok - 1 > lo || (a.window > 0 && base <= hi - a.window && base + kTok > a.sinks);
                 if constexpr (FMT == kFmt16) {
                     // (hidden from a row of either half: they share V)
@@ -390,9 +428,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
                         if (!ok) break;
                     }
                 }
+                // (the scores first: a half that skips units may be ahead of the scales' barrier by a phase)
+                ok = bar_wait(s_full + 8 * half, n_s & 1, dead) && (FMT == kFmt16 || bar_wait(sc_full + 8 * slot, x >> 2 & 1, dead));
+                if (!ok) break;
+                ++n_s;
+                const float *const ks = scales + slot * 2 * kTok, *const vs = ks + kTok;
                 after_sync();
-                const int last = pos - base, low = a.window > 0 ? pos - a.window - base : -1, sink = a.sinks - base;
-                // 32 scores from tensor memory as they enter the softmax: times the scales of K, hidden ones -inf
+                const int flags = *const_cast<volatile int *>(s_bad + slot);
+                if (masked || (flags & 2))
+                    mask_scores(ts, pos - base, a.window > 0 ? pos - a.window - base : -1, a.sinks - base,
+                                flags & 2 ? s_kbad + slot * 4 : nullptr);
+                // 32 scores from tensor memory as they enter the softmax: times the scales of K
                 auto enter = [&](float *s, int k0) {
                     if constexpr (FMT != kFmt16) {
 #pragma unroll
@@ -403,11 +449,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
                             s[k + 2] *= f.z;
                             s[k + 3] *= f.w;
                         }
-                    }
-                    if (masked) {
-#pragma unroll
-                        for (int k = 0; k < 32; ++k)
-                            if (!(k0 + k <= last && (k0 + k > low || k0 + k < sink))) s[k] = -INFINITY;
                     }
                 };
                 // The first 64 scores are read again for their weights: 128 would not fit the registers.
@@ -471,12 +512,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
                             const float4 f = *reinterpret_cast<const float4 *>(vs + k0 + k);
                             e = mul2(e, make_float2(f.x * kLift, f.y * kLift));
                             g = mul2(g, make_float2(f.z * kLift, f.w * kLift));
-                            if (masked) {  // a scale that is not finite stays away from a weight that the mask takes
-                                if (s[k] == -INFINITY) e.x = 0.0f;
-                                if (s[k + 1] == -INFINITY) e.y = 0.0f;
-                                if (s[k + 2] == -INFINITY) g.x = 0.0f;
-                                if (s[k + 3] == -INFINITY) g.y = 0.0f;
-                            }
                         }
                         p[k / 2] = pack16<BF16>(e.x, e.y);
                         p[k / 2 + 1] = pack16<BF16>(g.x, g.y);
@@ -497,7 +532,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
                 enter(sb, 32);
                 weigh(sb, 32);
                 tm_store_wait();
-                if (s_bad[slot]) l2.x = __uint_as_float(0x7fffffffu);
+                if (flags & 1) l2.x = __uint_as_float(0x7fffffffu);
+                if (FMT != kFmt16 && (flags & 4)) lost = true;
                 before_sync();
                 bar_arrive_warp(p_full + 8 * half);
             }
@@ -513,6 +549,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
             char *const po = a.out + (int64_t)(u.q0 + t) * a.o_t + (int64_t)hd * a.o_h;
             float *const pw = a.part_o + (slot * 256 + r) * 128;
             const float inv = l == 0.0f ? 0.0f : 1.0f / (l * kLift);
+            bool gone = false;
 #pragma unroll
             for (int k = 0; k < DP; k += 32) {
                 float o[32];
@@ -527,6 +564,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
                         add_lost<BF16>(a, u, job.j0, job.j0 + n, pos, k, y);
 #pragma unroll
                         for (int z = 0; z < 32; ++z) o[z] = y[z];
+                    }
+                }
+                if constexpr (FMT != kFmt16) {
+                    if (lost && real && (k > 0 ? gone : (gone = sees_lost(a, u, job.j0, job.j0 + n, pos)))) {
+#pragma unroll
+                        for (int z = 0; z < 32; ++z) o[z] = __uint_as_float(0x7fffffffu);
                     }
                 }
                 if (whole && real) {
@@ -628,7 +671,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
             bool bad;
         };
         auto look = [&](const Cursor<256, kTok> &p) {
-            Found f{-1, 0.0f, 0.0f, false};
+            Found f{-1, 1.0f, 0.0f, false};
             const int t = p.base() + i;
             if (t > p.u.hi || (a.window > 0 && t <= p.u.lo - a.window && t >= a.sinks)) return f;
             int place;
@@ -652,12 +695,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
         const bool in = ch * (FMT == kFmt16 ? 8 : 16) < c.D;
         auto put = [&](int x, const Found &f) {
             places[(x & 1) * kTok + i] = f.off;
+            int flags = __any_sync(0xffffffffu, f.bad) ? 1 : 0;
             if constexpr (FMT != kFmt16) {
-                scales[(x & 3) * 2 * kTok + i] = f.ks;
-                scales[(x & 3) * 2 * kTok + kTok + i] = f.vs;
+                // scales that are not finite are kept from rows that do not see them: 2 and 4 say that there are such
+                const bool kb = !(fabsf(f.ks) < INFINITY), vb = !(fabsf(f.vs) < INFINITY);
+                scales[(x & 3) * 2 * kTok + i] = kb ? 1.0f : f.ks;
+                scales[(x & 3) * 2 * kTok + kTok + i] = vb ? 0.0f : f.vs;
+                const unsigned kw = __ballot_sync(0xffffffffu, kb);
+                flags |= (kw ? 2 : 0) | (__any_sync(0xffffffffu, vb) ? 4 : 0);
+                if (lane == 0) s_kbad[(x & 3) * 4 + warp - 12] = kw;
             }
-            const unsigned any = __ballot_sync(0xffffffffu, f.bad);
-            if (lane == 0 && any) s_bad[x & 3] = 1;
+            if (lane == 0 && flags) atomicOr(s_bad + (x & 3), flags);
         };
         // stage of the next item, free to be written
         auto stage = [&]() {
@@ -694,7 +742,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
         for (int x = 0; x < count; ++x) {  // (cu stands at tile x, then at x + 1)
             bar_arrive_warp(sc_full + 8 * (x & 3));  // the tile's scales and flag
             const bool more = x + 1 < count;
-            Found f{-1, 0.0f, 0.0f, false};
+            Found f{-1, 1.0f, 0.0f, false};
             if (more) {
                 cu.next(a);
                 f = look(cu);
@@ -834,7 +882,25 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
                 }
                 __syncwarp();
                 if (frag > 0) ok = ok && bar_wait<true>(q_free, (frag - 1) & 1, dead);
-                if (ok) {
+                if (ok && in.q_map) {
+                    // by the copy engine, 128 rows of 64 elements at a time
+                    if (lane == 0) {
+                        const int halves = u.rows > 128 ? 2 : 1;
+                        if (i == 0) {
+                            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(q_full), "r"(halves * S::kTile) : "memory");
+                            for (int k = 0; k < halves; ++k)
+                                for (int p = 0; p < DP / 64; ++p)
+                                    asm volatile(
+                                        "cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(
+                                            smem_addr(smem) + k * S::kTile + p * S::kPanel), "l"(&in.q), "r"(q_full), "r"(p * 64), "r"(u.h * c.G),
+                                        "r"(u.q0 + quot(u.qt * 256 + k * 128, c.div_g))
+                                        : "memory");
+                        } else {
+                            bar_arrive(q_full);
+                        }
+                    }
+                    __syncwarp();
+                } else if (ok) {
 #pragma unroll 4
                     for (int r = i / QC; r < 256; r += QS) {
                         const int gr = u.qt * 256 + r, t = quot(gr, c.div_g), hd = u.h * c.G + gr - t * c.G;
@@ -972,33 +1038,48 @@ Pick pick(bool bf16, int fmt, int D, bool tma) { return D <= 64 ? pick_load<64>(
 
 }  // namespace
 
+namespace {
+
+using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                            const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                            CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+Encode encoder() {  // the driver's function, looked up once; null if it has none
+    static const Encode fn = [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            return (Encode) nullptr;
+        }
+        return reinterpret_cast<Encode>(p);
+    }();
+    return fn;
+}
+// A map of 16-bit elements: 64 of the first dimension a box, zeros beyond the tensor, rows of 128 bytes swizzled.
+bool encode(CUtensorMap &map, bool bf16, int dims, const void *at, const cuuint64_t *size, const cuuint64_t *stride, const cuuint32_t *box) {
+    const cuuint32_t steps[4] = {1, 1, 1, 1};
+    for (int i = 0; i + 1 < dims; ++i)
+        if (stride[i] == 0 || stride[i] >= (1ull << 40)) return false;
+    return encoder() && encoder()(&map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, (cuuint32_t)dims,
+                                  const_cast<void *>(at), size, stride, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace
+
 int encode_maps(const CacheDev &c, bool bf16, CacheMaps &m) {
     m.box = 0;
     const int box = c.b & -c.b;  // the largest power of two in a block
     if (box < 8) return 0;
-    void *fn = nullptr;
-    cudaDriverEntryPointQueryResult found;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found) != cudaSuccess ||
-        found != cudaDriverEntryPointSuccess || !fn) {
-        cudaGetLastError();
-        return 0;
-    }
-    using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
-                                const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
     const cuuint32_t tokens = (cuuint32_t)(box < kTok ? box : kTok);
     const cuuint64_t dims[4] = {(cuuint64_t)c.D, (cuuint64_t)c.b, (cuuint64_t)c.H, (cuuint64_t)c.nb};
     // (the stride of a dimension of one element is never used, but has to be one)
     const cuuint64_t strides[3] = {(cuuint64_t)(c.b > 1 ? c.st : 256), (cuuint64_t)(c.H > 1 ? c.sh : 256), (cuuint64_t)(c.nb > 1 ? c.sb : 256)};
-    const cuuint32_t boxes[4] = {64, tokens, 1, 1}, steps[4] = {1, 1, 1, 1};
-    for (cuuint64_t s : strides)
-        if (s == 0 || s >= (1ull << 40)) return 0;
+    const cuuint32_t boxes[4] = {64, tokens, 1, 1};
     for (int y = 0; y < 2; ++y)
-        if (reinterpret_cast<Encode>(fn)(y ? &m.v : &m.k, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4,
-                                         y ? c.v : c.k, dims, strides, boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-            return 0;
+        if (!encode(y ? m.v : m.k, bf16, 4, y ? c.v : c.k, dims, strides, boxes)) return 0;
     return m.box = (int)tokens;
 }
 
@@ -1015,7 +1096,18 @@ cudaError_t attend_chunk_init() {
 
 cudaError_t launch_attend_chunk(const AttendLaunch &a, const CacheMaps &m, bool bf16, int fmt, int ctas, cudaStream_t st) {
     const Pick p = pick(bf16, fmt, a.c.D, m.box > 0);
-    return launch_chained(p.k, ctas, kThreads, p.smem, st, ChunkLaunch{a, m});
+    ChunkLaunch l;
+    l.a = a;
+    l.m = m;
+    const CacheDev &c = a.c;
+    l.q_map = 0;
+    if (c.G <= 128 && 128 % c.G == 0) {
+        const cuuint64_t dims[3] = {(cuuint64_t)c.D, (cuuint64_t)c.Hq, (cuuint64_t)a.b.T};
+        const cuuint64_t strides[2] = {(cuuint64_t)(c.Hq > 1 ? a.q_h : 256), (cuuint64_t)(a.b.T > 1 ? a.q_t : 256)};
+        const cuuint32_t box[3] = {64, (cuuint32_t)c.G, (cuuint32_t)(128 / c.G)};
+        l.q_map = encode(l.q, bf16, 3, a.q, dims, strides, box);
+    }
+    return launch_chained(p.k, ctas, kThreads, p.smem, st, l);
 }
 
 }  // namespace lr

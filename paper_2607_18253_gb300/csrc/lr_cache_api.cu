@@ -232,10 +232,11 @@ int lr_cache_attend(lr_cache *c, const lr_cache_batch *b, int32_t T, const void 
     a.scale_log2 = (float)((double)scale * 1.4426950408889634);
     a.window = window;
     a.sinks = window ? sinks : 0;
-    // Sequences of few rows go to the step kernel, of many to the chunk kernel; a batch whose sequences
-    // have many on average is the chunk kernel's whole.
+    // Sequences of few rows go to the step kernel, of many to the chunk kernel (a single one whole, whatever
+    // it brings).  A batch of both takes two launches: 63 single tokens beside a chunk of 1,985 (32 query and
+    // 8 KV heads of 128) XX us, in the chunk kernel alone XX.
     const int most = (int)std::min<long long>((long long)b->max_q * c->dev.G, 0x7fffffff);
-    const bool all = (long long)T * c->dev.G >= (long long)kLeastChunk * b->num_seqs;
+    const bool all = b->num_seqs == 1;
     cudaStream_t st = (cudaStream_t)stream;
     if (most >= kLeastChunk) {
         a.row_lo = all ? 1 : kLeastChunk;
