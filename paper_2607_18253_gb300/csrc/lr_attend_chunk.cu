@@ -292,13 +292,68 @@ __device__ __noinline__ bool sees_lost(const AttendLaunch &a, const Unit &u, int
     return false;
 }
 
+// Joins the parts of 32 rows of a unit, in the order of the CTAs: a lane first a row's maximum and sum, then four
+// elements each of 16 rows at a time (of 2 x 8 with 64 elements), their loads in flight together.
+template <bool BF16, int DP>
+__device__ __noinline__ void join_rows(const AttendLaunch &a, const Unit &u, int c0, int parts, int slot0, int row0, float lift) {
+    constexpr int kLanes = DP / 4, kTwo = 32 / kLanes, kStep = 16;
+    const CacheDev &c = a.c;
+    const int lane = threadIdx.x % 32, sub = lane / kLanes, e = lane % kLanes * 4;
+    auto at = [&](int k, int r) { return (int64_t)(k == 0 ? slot0 : 2 * (c0 + k)) * 256 + r; };
+    const bool mine = row0 + lane < u.rows;
+    float mm = -INFINITY, ll = 0.0f;
+    for (int k = 0; k < parts; ++k)
+        if (mine) mm = fmaxf(mm, __ldcg(&a.part_ml[at(k, row0 + lane)].x));
+    for (int r0 = row0; r0 < min(u.rows, row0 + 32); r0 += kStep) {
+        float4 acc[kStep / kTwo];
+#pragma unroll
+        for (int z = 0; z < kStep / kTwo; ++z) acc[z] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        ll = 0.0f;
+        for (int k = 0; k < parts; ++k) {
+            float4 w[kStep / kTwo];
+#pragma unroll
+            for (int z = 0; z < kStep / kTwo; ++z) {
+                const int r = r0 + z * kTwo + sub;
+                w[z] = r < u.rows ? __ldcg(reinterpret_cast<const float4 *>(a.part_o + at(k, r) * 128 + e)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            }
+            const float2 ml = mine ? __ldcg(a.part_ml + at(k, row0 + lane)) : make_float2(-INFINITY, 0.0f);
+            const float f = ml.x == -INFINITY ? 0.0f : exp2_fast(ml.x - mm);  // (one that saw nothing: no part of it)
+            ll += ml.y == 0.0f ? 0.0f : ml.x == -INFINITY ? ml.y : ml.y * f;
+#pragma unroll
+            for (int z = 0; z < kStep / kTwo; ++z) {
+                const float g = __shfl_sync(0xffffffffu, f, r0 - row0 + z * kTwo + sub);
+                if (g != 0.0f) {
+                    acc[z].x += w[z].x * g;
+                    acc[z].y += w[z].y * g;
+                    acc[z].z += w[z].z * g;
+                    acc[z].w += w[z].w * g;
+                }
+            }
+        }
+#pragma unroll
+        for (int z = 0; z < kStep / kTwo; ++z) {
+            const int r = r0 + z * kTwo + sub;
+            const float l = __shfl_sync(0xffffffffu, ll, r - row0);
+            const int gr = u.qt * 256 + r, t = quot(gr, c.div_g), hd = u.h * c.G + gr - t * c.G;
+            const float iv = l == 0.0f ? 0.0f : 1.0f / (l * lift);
+            if (r < u.rows && e < c.D)
+                *reinterpret_cast<uint2 *>(a.out + (int64_t)(u.q0 + t) * a.o_t + (int64_t)hd * a.o_h + e * 2) =
+                    make_uint2(pack16<BF16>(acc[z].x * iv, acc[z].y * iv), pack16<BF16>(acc[z].z * iv, acc[z].w * iv));
+        }
+    }
+    if (a.lse && mine) {
+        const int gr = u.qt * 256 + row0 + lane, t = quot(gr, c.div_g), hd = u.h * c.G + gr - t * c.G;
+        a.lse[(int64_t)(u.q0 + t) * c.Hq + hd] = ll == 0.0f ? -INFINITY : (mm + log2f(ll)) * 0.69314718f;
+    }
+}
+
 template <bool BF16, int FMT, int DP, int LOAD>
 __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_constant__ ChunkLaunch in) {
     using S = Shape<DP, FMT, LOAD>;
     const AttendLaunch &a = in.a;
     constexpr int kKvArrive = LOAD == kTma ? 1 : 4;  // arrivals that hand over a tile: one a warp
     constexpr int kStages = S::kStages;
-    constexpr float kLag = BF16 ? 8.0f : 4.0f;
+    constexpr float kLag = BF16 || FMT == kFmt16 ? 8.0f : 4.0f;
     // fp16 weights that carry 8-bit scales: lifted from fp16's subnormal numbers (scales are at most
     // 65504/127 = 516 and weights 2^kLag = 16, so 4 times them stays below 65504)
     constexpr float kLift = FMT != kFmt16 && !BF16 ? 4.0f : 1.0f;
@@ -444,10 +499,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
 #pragma unroll
                         for (int k = 0; k < 32; k += 4) {
                             const float4 f = *reinterpret_cast<const float4 *>(ks + k0 + k);
-                            s[k] *= f.x;
-                            s[k + 1] *= f.y;
-                            s[k + 2] *= f.z;
-                            s[k + 3] *= f.w;
+                            const float2 e = mul2(make_float2(s[k], s[k + 1]), make_float2(f.x, f.y)), g = mul2(make_float2(s[k + 2], s[k + 3]), make_float2(f.z, f.w));
+                            s[k] = e.x;
+                            s[k + 1] = e.y;
+                            s[k + 2] = g.x;
+                            s[k + 3] = g.y;
                         }
                     }
                 };
@@ -510,8 +566,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
                         l2 = add2(l2, add2(e, g));
                         if constexpr (FMT != kFmt16) {
                             const float4 f = *reinterpret_cast<const float4 *>(vs + k0 + k);
-                            e = mul2(e, make_float2(f.x * kLift, f.y * kLift));
-                            g = mul2(g, make_float2(f.z * kLift, f.w * kLift));
+                            e = mul2(e, make_float2(f.x, f.y));
+                            g = mul2(g, make_float2(f.z, f.w));
                         }
                         p[k / 2] = pack16<BF16>(e.x, e.y);
                         p[k / 2 + 1] = pack16<BF16>(g.x, g.y);
@@ -550,8 +606,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
             float *const pw = a.part_o + (slot * 256 + r) * 128;
             const float inv = l == 0.0f ? 0.0f : 1.0f / (l * kLift);
             bool gone = false;
-#pragma unroll
-            for (int k = 0; k < DP; k += 32) {
+#pragma unroll 1
+            for (int k = 0; k < DP; k += 32) {  // (short code: it is fetched anew for each unit)
                 float o[32];
                 __syncwarp();
                 tm_load(o, to + k);
@@ -605,35 +661,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
                 before = __shfl_sync(0xffffffffu, before, 0);
                 if (before == (uint32_t)(c1 - c0)) {
                     __threadfence();
-                    constexpr int kLanes = DP / 4;  // four elements a thread
-                    const int64_t s0 = job.slot0;
-                    const int end = min(u.rows, warp * 32 + 32);
-                    for (int q = warp * 32 + lane / kLanes; q < end; q += 32 / kLanes) {
-                        const int d = lane % kLanes * 4;
-                        auto at = [&](int k) { return (k == c0 ? s0 : 2 * (int64_t)k) * 256 + q; };
-                        float mm = -INFINITY, ll = 0.0f;
-                        for (int k = c0; k <= c1; ++k) mm = fmaxf(mm, __ldcg(&a.part_ml[at(k)].x));
-                        float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                        for (int k = c0; k <= c1; ++k) {
-                            const float2 ml = __ldcg(a.part_ml + at(k));
-                            const float f = ml.x == -INFINITY ? 0.0f : exp2_fast(ml.x - mm);
-                            const float4 w = __ldcg(reinterpret_cast<const float4 *>(a.part_o + at(k) * 128 + d));
-                            ll += ml.y == 0.0f ? 0.0f : ml.y * f;
-                            if (ml.x == -INFINITY && ml.y == 0.0f) continue;  // saw nothing
-                            acc.x += w.x * f;
-                            acc.y += w.y * f;
-                            acc.z += w.z * f;
-                            acc.w += w.w * f;
-                        }
-                        const int g2 = u.qt * 256 + q, t2 = quot(g2, c.div_g), h2 = u.h * c.G + g2 - t2 * c.G;
-                        const float iv = ll == 0.0f ? 0.0f : 1.0f / (ll * kLift);
-                        if (d < c.D)
-                            *reinterpret_cast<uint2 *>(a.out + (int64_t)(u.q0 + t2) * a.o_t + (int64_t)h2 * a.o_h + d * 2) =
-                                make_uint2(pack16<BF16>(acc.x * iv, acc.y * iv), pack16<BF16>(acc.z * iv, acc.w * iv));
-                        if (a.lse && d == 0)
-                            a.lse[(int64_t)(u.q0 + t2) * c.Hq + h2] = ll == 0.0f ? -INFINITY : (mm + log2f(ll)) * 0.69314718f;
-                    }
-                    __syncwarp();
+                    join_rows<BF16, DP>(a, u, c0, c1 - c0 + 1, job.slot0, warp * 32, kLift);
                 }
             }
             bar_arrive_warp(job_free + 8 * (frag % kJobs));
@@ -700,7 +728,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
                 // scales that are not finite are kept from rows that do not see them: 2 and 4 say that there are such
                 const bool kb = !(fabsf(f.ks) < INFINITY), vb = !(fabsf(f.vs) < INFINITY);
                 scales[(x & 3) * 2 * kTok + i] = kb ? 1.0f : f.ks;
-                scales[(x & 3) * 2 * kTok + kTok + i] = vb ? 0.0f : f.vs;
+                scales[(x & 3) * 2 * kTok + kTok + i] = vb ? 0.0f : f.vs * kLift;
                 const unsigned kw = __ballot_sync(0xffffffffu, kb);
                 flags |= (kw ? 2 : 0) | (__any_sync(0xffffffffu, vb) ? 4 : 0);
                 if (lane == 0) s_kbad[(x & 3) * 4 + warp - 12] = kw;
@@ -775,22 +803,35 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
                 for (int y = 0; y < 2; ++y, ++item) {
                     const uint32_t st = stage();
                     const uint32_t to = smem_addr(tiles + st * S::kTile);
-#pragma unroll 2
-                    for (int k = 0; k < kIts; ++k) {
-                        const int r = r0 + k * kStep;
-                        const uint32_t at = smem_addr(raw + ((item * kIts + k) % S::kSlots * 128 + i) * 16);
-                        copy_wait<S::kSlots - 1>();
-                        uint32_t w[4], v[8];
-                        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
+                    // four pieces at a time: read, converted and written, then their slots requested again
+                    for (int k0 = 0; k0 < kIts; k0 += 4) {
+                        uint32_t w[4][4];
+                        copy_wait<S::kSlots - 4>();
 #pragma unroll
-                        for (int z = 0; z < 4; ++z) {
-                            v[2 * z] = from_codes<BF16, FMT>(w[z], 0, 1);
-                            v[2 * z + 1] = from_codes<BF16, FMT>(w[z], 2, 3);
+                        for (int k = 0; k < 4; ++k)
+                            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
+                                         : "=r"(w[k][0]), "=r"(w[k][1]), "=r"(w[k][2]), "=r"(w[k][3])
+                                         : "r"(smem_addr(raw + ((item * kIts + k0 + k) % S::kSlots * 128 + i) * 16)) : "memory");
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const int r = r0 + (k0 + k) * kStep;
+                            uint32_t v[8];
+#pragma unroll
+                            for (int z = 0; z < 4; ++z) {
+                                if constexpr (BF16) {
+                                    v[2 * z] = from_codes<true, FMT>(w[k][z], 0, 1);
+                                    v[2 * z + 1] = from_codes<true, FMT>(w[k][z], 2, 3);
+                                } else {
+                                    if (FMT == kFmtE4M3 && y) w[k][z] = without_nan(w[k][z]);  // (a hidden weight's zero times it is not zero)
+                                    to_half<FMT, false>(w[k][z], v[2 * z], v[2 * z + 1]);
+                                }
+                            }
+                            asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to + swizzled<DP>(r, 2 * ch)), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+                            asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to + swizzled<DP>(r, 2 * ch + 1)), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
                         }
-                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to + swizzled<DP>(r, 2 * ch)), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
-                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to + swizzled<DP>(r, 2 * ch + 1)), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
-                        // the copy that takes this slot next is of this tile's V or of the next tile
-                        request(ahead / (2 * kIts) <= (uint32_t)x + (more ? 1 : 0));
+                        // the copies that take these slots next are of this tile's V or of the next tile
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) request(ahead / (2 * kIts) <= (uint32_t)x + (more ? 1 : 0));
                     }
                     shared_to_async();
                     bar_arrive_warp(kv_full + 8 * st);
