@@ -115,8 +115,8 @@ __device__ __forceinline__ long long block_sum(long long v, long long *sh, long 
     return v;
 }
 
-// Splits the batch's tiles evenly over the CTAs: this CTA takes [x0, x1) of the `all` tiles, by
-// `ctas` CTAs (the others have none), and `cur` stands at x0.
+// Splits the batch's tiles evenly over the CTAs, LEAST of them or more to each: this CTA takes [x0, x1) of the `all`
+// tiles, by `ctas` CTAs (the others have none), and `cur` stands at x0.
 struct Share {
     long long x0, x1, all;
     int ctas;
@@ -126,7 +126,7 @@ __device__ __forceinline__ long long share_start(const Share &s, int c) {
     return s.all < 1 << 20 ? (long long)((uint32_t)s.all * (uint32_t)c / (uint32_t)s.ctas) : s.all * c / s.ctas;
 }
 // (scratch: THREADS / 32 + 2 words of shared memory)
-template <int ROWS, int TILE, int THREADS>
+template <int ROWS, int TILE, int THREADS, int LEAST>
 __device__ __forceinline__ bool take_share(const AttendLaunch &a, Cursor<ROWS, TILE> &cur, Share &sh, long long *scratch) {
     long long *const s_sum = scratch, &s_rest = scratch[THREADS / 32], &s_seq = scratch[THREADS / 32 + 1];
     const int n = a.b.n, tid = threadIdx.x, lane = tid & 31;
@@ -159,7 +159,7 @@ __device__ __forceinline__ bool take_share(const AttendLaunch &a, Cursor<ROWS, T
     }
     if (all == 0) return false;
     sh.all = all;
-    sh.ctas = (int)min((long long)gridDim.x, all);
+    sh.ctas = (int)min((long long)gridDim.x, max(all / LEAST, 1ll));
     const int c = blockIdx.x;
     if (c >= sh.ctas) return false;
     sh.x0 = share_start(sh, c);

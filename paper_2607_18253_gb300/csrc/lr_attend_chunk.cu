@@ -302,8 +302,8 @@ __device__ __noinline__ void join_rows(const AttendLaunch &a, const Unit &u, int
     auto at = [&](int k, int r) { return (int64_t)(k == 0 ? slot0 : 2 * (c0 + k)) * 256 + r; };
     const bool mine = row0 + lane < u.rows;
     float mm = -INFINITY, ll = 0.0f;
-    for (int k = 0; k < parts; ++k)
-        if (mine) mm = fmaxf(mm, __ldcg(&a.part_ml[at(k, row0 + lane)].x));
+#pragma unroll 4
+    for (int k = 0; k < parts; ++k) mm = fmaxf(mm, mine ? __ldcg(&a.part_ml[at(k, row0 + lane)].x) : 0.0f);
     for (int r0 = row0; r0 < min(u.rows, row0 + 32); r0 += kStep) {
         float4 acc[kStep / kTwo];
 #pragma unroll
@@ -381,7 +381,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
     chain_wait();
     Cursor<256, kTok> cu;
     Share sh;
-    if (!take_share<256, kTok, kThreads>(a, cu, sh, scratch)) {
+    if (!take_share<256, kTok, kThreads, 4>(a, cu, sh, scratch)) {
         chain_next();
         return;
     }

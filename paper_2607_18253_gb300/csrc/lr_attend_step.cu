@@ -20,18 +20,6 @@ namespace {
 constexpr int kTok = 64;      // tokens of a tile
 constexpr int kThreads = 128;
 
-template <int DP, int FMT>
-struct Shape {
-    static constexpr int kRow = DP * (FMT == kFmt16 ? 2 : 1);  // bytes of a cached vector, padded
-    static constexpr int kChunks = kRow / 16;
-    static constexpr int kHalf = kTok * kRow;                  // bytes of a tile's K
-    static constexpr int kStage = 2 * kHalf;
-    static constexpr int kStages = FMT == kFmt16 ? 3 : 4;
-    static constexpr int kScales = FMT == kFmt16 ? 0 : kStages * 2 * kTok * 4;
-    static constexpr int kPlaces = 2 * kTok * 16;
-    static constexpr int kSmem = kStages * kStage + kScales + kPlaces + 4 * 32 * 16 + 128;
-};
-
 // Where a 16-byte chunk of a cached vector lies in its shared-memory row, so that the eight rows that
 // one instruction reads at a time are in different banks.
 template <int DP, int FMT, bool V>
@@ -64,441 +52,6 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint3
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-
-// BF16: the type of q and of the products.  WM: warps by rows (16 each); the others split the tokens.
-template <bool BF16, int FMT, int DP, int WM>
-__global__ void __launch_bounds__(kThreads) k_attend_rows(const __grid_constant__ AttendLaunch a) {
-    using S = Shape<DP, FMT>;
-    constexpr int kRows = 16 * WM, WN = 4 / WM, kMine = kTok / WN, NB = kMine / 8, KS = DP / 16;
-    // with 8-bit V the weights carry its scales: in fp16 they are kept away from its subnormal
-    // numbers by 2^6 (scales of fp16 data are at most 65504/127, so 2^6 of one stays in range)
-    constexpr float kLift = FMT != kFmt16 && !BF16 ? 64.0f : 1.0f;
-    extern __shared__ __align__(128) char smem[];
-    char *const stages = smem;
-    float *const scales = reinterpret_cast<float *>(smem + S::kStages * S::kStage);  // [stage][K, V][token]
-    longlong2 *const places = reinterpret_cast<longlong2 *>(smem + S::kStages * S::kStage + S::kScales);  // [2][token]
-    float4 *const s_ml = reinterpret_cast<float4 *>(reinterpret_cast<char *>(places) + S::kPlaces);  // [warp][lane]
-    int *const s_bad = reinterpret_cast<int *>(s_ml + 4 * 32);  // [8][2]
-    __shared__ int s_last;
-    __shared__ long long s_scratch[kThreads / 32 + 2];
-    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, g = lane / 4, i4 = lane % 4;
-    const int wm = warp / WN, wn = warp % WN;
-    const CacheDev &c = a.c;
-
-    chain_wait();
-    Cursor<kRows, kTok> cu, lk;
-    Share sh;
-    if (!take_share<kRows, kTok, kThreads>(a, cu, sh, s_scratch)) {
-        chain_next();
-        return;
-    }
-    const int count = (int)(sh.x1 - sh.x0);
-    lk = cu;
-
-    // the place of one token (thread t < 64: token t) of the tile at lk
-    auto look = [&](longlong2 &p, bool &bad) {
-        const int t = lk.base() + tid;
-        p.x = p.y = -1;
-        bad = false;
-        // what no row of the unit sees is not looked up (its block may be gone): zeros
-        if (t > lk.u.hi || (a.window > 0 && t <= lk.u.lo - a.window && t >= a.sinks)) return;
-        int place;
-        const int64_t blk = block_of(c, a.b, lk.u.s, t, place);
-        if (blk < 0) {
-            bad = true;
-            report(c.status, kEInval);
-            return;
-        }
-        p.x = blk * c.sb + place * c.st + lk.u.h * c.sh;
-        p.y = blk * c.ssb + place * c.sst + lk.u.h * c.ssh;
-    };
-    auto put = [&](int tile, const longlong2 &p, bool bad) {
-        places[(tile & 1) * kTok + tid] = p;
-        const unsigned any = __ballot_sync(0xffffffffu, bad);
-        if (lane == 0) s_bad[(tile & 7) * 2 + warp] = any != 0;
-    };
-    auto issue = [&](int tile) {
-        char *const st = stages + tile % S::kStages * S::kStage;
-        const longlong2 *const pl = places + (tile & 1) * kTok;
-        constexpr int kStep = kThreads / S::kChunks;
-        const int ch = tid % S::kChunks, r0 = tid / S::kChunks;
-        const bool in = ch * 16 < c.D * (FMT == kFmt16 ? 2 : 1);
-        int64_t offs[kTok / kStep];  // (all read before the first copy, which the compiler would not move them past)
-#pragma unroll
-        for (int k = 0; k < kTok / kStep; ++k) offs[k] = pl[r0 + k * kStep].x;
-#pragma unroll
-        for (int k = 0; k < kTok / kStep; ++k) {
-            const int r = r0 + k * kStep;
-            const bool ok = in && offs[k] >= 0;
-            const int64_t at = ok ? offs[k] + ch * 16 : 0;
-            copy16(smem_addr(st + r * S::kRow + swizzle<DP, FMT, false>(r, ch) * 16), c.k + at, ok);
-            copy16(smem_addr(st + S::kHalf + r * S::kRow + swizzle<DP, FMT, true>(r, ch) * 16), c.v + at, ok);
-        }
-        if constexpr (FMT != kFmt16) {
-            const int64_t off = pl[tid % kTok].y;
-            copy4(smem_addr(scales + tile % S::kStages * 2 * kTok + tid), (tid < kTok ? c.ks : c.vs) + max(off, (int64_t)0), off >= 0);
-        }
-    };
-
-    longlong2 pl;
-    bool bad = false;
-    // the first tiles, each looked up and requested at once
-    for (int t = 0; t < S::kStages; ++t) {
-        if (t < count) {
-            if (tid < kTok) {
-                look(pl, bad);
-                put(t, pl, bad);
-            }
-            if (t + 1 < count) lk.next(a);
-        }
-        __syncthreads();
-        if (t < S::kStages - 1) {
-            if (t < count) issue(t);
-            copy_commit();
-        }
-        // (tile kStages - 1's places wait in their slot for the loop)
-    }
-
-    uint32_t q[KS][4];
-    float o[2 * KS][4], m[2], l[2];
-    int pos[2];
-    for (int x = 0; x < count; ++x) {
-        const Unit &u = cu.u;
-        if (x == 0 || cu.j == 0) {  // a new unit: its queries, straight to the registers that multiply them
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-                const int r = wm * 16 + g + y * 8;
-                const int gr = u.qt * kRows + r, t = quot(gr, c.div_g), hd = gr - t * c.G;
-                const bool ok = r < u.rows;
-                pos[y] = ok ? u.kv - u.ql + t : -1;
-                const char *const p = a.q + (int64_t)(u.q0 + t) * a.q_t + (int64_t)(u.h * c.G + hd) * a.q_h;
-#pragma unroll
-                for (int k = 0; k < KS; ++k) {
-                    if constexpr (FMT == kFmt16) {
-#pragma unroll
-                        for (int z = 0; z < 2; ++z) {
-                            const int d = k * 16 + z * 8 + 2 * i4;
-                            q[k][y + 2 * z] = ok && d < c.D ? __ldg(reinterpret_cast<const uint32_t *>(p + d * 2)) : 0u;
-                        }
-                    } else {  // four neighbouring elements, the order in which the codes lie in a register
-                        const int d = (k / 4) * 64 + i4 * 16 + (k % 4) * 4;
-                        const uint2 w = ok && d < c.D ? __ldg(reinterpret_cast<const uint2 *>(p + d * 2)) : make_uint2(0, 0);
-                        q[k][y] = w.x;
-                        q[k][y + 2] = w.y;
-                    }
-                }
-                m[y] = -INFINITY;
-                l[y] = 0.0f;
-            }
-#pragma unroll
-            for (int k = 0; k < 2 * KS; ++k)
-#pragma unroll
-                for (int z = 0; z < 4; ++z) o[k][z] = 0.0f;
-        }
-        copy_wait<S::kStages - 2>();
-        __syncthreads();
-        if (x + S::kStages - 1 < count) issue(x + S::kStages - 1);
-        copy_commit();
-        const bool more = x + S::kStages < count;
-        if (more && tid < kTok) look(pl, bad);
-
-        // ---- scores ----
-        char *const st = stages + x % S::kStages * S::kStage;
-        const uint32_t sk = smem_addr(st), sv = sk + S::kHalf;
-        const int first = wn * kMine, base = cu.base();
-        float s[NB][4];
-#pragma unroll
-        for (int n = 0; n < NB; ++n)
-#pragma unroll
-            for (int z = 0; z < 4; ++z) s[n][z] = 0.0f;
-        if constexpr (FMT == kFmt16) {
-#pragma unroll
-            for (int k = 0; k < KS; ++k)
-#pragma unroll
-                for (int n = 0; n < NB; n += 2) {
-                    uint32_t b[4];
-                    const int mi = lane / 8, row = first + n * 8 + (mi >> 1) * 8 + lane % 8;
-                    ldsm4(b, sk + row * S::kRow + swizzle<DP, FMT, false>(row, k * 2 + (mi & 1)) * 16);
-                    mma<BF16>(s[n], q[k], b[0], b[1]);
-                    mma<BF16>(s[n + 1], q[k], b[2], b[3]);
-                }
-        } else {
-#pragma unroll
-            for (int n = 0; n < NB; ++n)
-#pragma unroll
-                for (int hf = 0; hf < DP / 64; ++hf) {
-                    const int row = first + n * 8 + g;
-                    const uint4 w = lds16(sk + row * S::kRow + swizzle<DP, FMT, false>(row, hf * 4 + i4) * 16);
-                    const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        mma<BF16>(s[n], q[hf * 4 + k], from_codes<BF16, FMT>(ww[k], 0, 1), from_codes<BF16, FMT>(ww[k], 2, 3));
-                }
-        }
-        // ---- softmax ----
-        const float *const ks = scales + x % S::kStages * 2 * kTok + first, *const vs = ks + kTok;
-        const bool masked = base + first + kMine - 1 > u.lo ||
-                            (a.window > 0 && base + first <= u.hi - a.window && base + first + kMine > a.sinks);
-        float mx[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-        for (int n = 0; n < NB; ++n)
-#pragma unroll
-            for (int z = 0; z < 4; ++z) {
-                float f = a.scale_log2;
-                if constexpr (FMT != kFmt16) f *= ks[n * 8 + 2 * i4 + (z & 1)];
-                s[n][z] *= f;
-                if (masked && !visible(pos[z >> 1], base + first + n * 8 + 2 * i4 + (z & 1), a.window, a.sinks)) s[n][z] = -INFINITY;
-                mx[z >> 1] = fmaxf(mx[z >> 1], s[n][z]);
-            }
-        float al[2];
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-            mx[y] = fmaxf(mx[y], __shfl_xor_sync(0xffffffffu, mx[y], 1));
-            mx[y] = fmaxf(mx[y], __shfl_xor_sync(0xffffffffu, mx[y], 2));
-            const float mn = fmaxf(m[y], mx[y]);
-            al[y] = mn == -INFINITY ? 1.0f : exp2_fast(m[y] - mn);
-            m[y] = mn;
-            mx[y] = mn == -INFINITY ? 0.0f : mn;
-            l[y] *= al[y];
-        }
-        if (__any_sync(0xffffffffu, al[0] != 1.0f || al[1] != 1.0f)) {
-#pragma unroll
-            for (int k = 0; k < 2 * KS; ++k)
-#pragma unroll
-                for (int z = 0; z < 4; ++z) o[k][z] *= al[z >> 1];
-        }
-#pragma unroll
-        for (int n = 0; n < NB; ++n)
-#pragma unroll
-            for (int z = 0; z < 4; ++z) {
-                const float p = exp2_fast(s[n][z] - mx[z >> 1]);
-                l[z >> 1] += p;
-                if constexpr (FMT != kFmt16) {
-                    // (a scale that is not finite stays away from a weight that the mask takes)
-                    const float w = p * (kLift * vs[n * 8 + 2 * i4 + (z & 1)]);
-                    s[n][z] = masked && s[n][z] == -INFINITY ? 0.0f : w;
-                } else {
-                    s[n][z] = p;
-                }
-            }
-        if (s_bad[(x & 7) * 2] | s_bad[(x & 7) * 2 + 1]) l[0] = l[1] = __uint_as_float(0x7fffffffu);
-
-        // ---- weighted sum ----
-        bool slow = false;
-        if constexpr (FMT == kFmt16) {
-            // an infinity or a NaN in V that some row may not see: 0 times it is not 0, so such a tile is
-            // summed without the tensor cores, skipping what a row does not see
-            if (masked) {
-                bool x = false;
-                for (int k = lane; k < kMine * S::kChunks; k += 32) {
-                    const uint4 w = lds16(sv + (first + k / S::kChunks) * S::kRow + k % S::kChunks * 16);
-                    x |= not_finite<BF16>(w.x) || not_finite<BF16>(w.y) || not_finite<BF16>(w.z) || not_finite<BF16>(w.w);
-                }
-                slow = __any_sync(0xffffffffu, x);
-            }
-        }
-        if (!slow) {
-#pragma unroll
-            for (int kk = 0; kk < kMine / 16; ++kk) {
-                const uint32_t p[4] = {pack16<BF16>(s[2 * kk][0], s[2 * kk][1]), pack16<BF16>(s[2 * kk][2], s[2 * kk][3]),
-                                       pack16<BF16>(s[2 * kk + 1][0], s[2 * kk + 1][1]),
-                                       pack16<BF16>(s[2 * kk + 1][2], s[2 * kk + 1][3])};
-                const int mi = lane / 8, row = first + kk * 16 + (mi & 1) * 8 + lane % 8;
-                if constexpr (FMT == kFmt16) {
-#pragma unroll
-                    for (int d = 0; d < KS; ++d) {
-                        uint32_t b[4];
-                        ldsm4t(b, sv + row * S::kRow + swizzle<DP, FMT, true>(row, d * 2 + (mi >> 1)) * 16);
-                        mma<BF16>(o[2 * d], p, b[0], b[1]);
-                        mma<BF16>(o[2 * d + 1], p, b[2], b[3]);
-                    }
-                } else {
-                    // pairs of neighbouring elements move as one: of each 16 elements, the even ones make one
-                    // product and the odd ones the next
-#pragma unroll
-                    for (int d = 0; d < KS; d += 2) {
-                        uint32_t b[4];
-                        ldsm4t(b, sv + row * S::kRow + swizzle<DP, FMT, true>(row, d + (mi >> 1)) * 16);
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            mma<BF16>(o[2 * (d + e)], p, from_codes<BF16, FMT>(b[2 * e], 0, 2), from_codes<BF16, FMT>(b[2 * e + 1], 0, 2));
-                            mma<BF16>(o[2 * (d + e) + 1], p, from_codes<BF16, FMT>(b[2 * e], 1, 3), from_codes<BF16, FMT>(b[2 * e + 1], 1, 3));
-                        }
-                    }
-                }
-            }
-        } else if constexpr (FMT == kFmt16) {
-#pragma unroll
-            for (int n = 0; n < NB; ++n)
-                for (int t8 = 0; t8 < 8; ++t8) {
-                    const int row = first + n * 8 + t8;
-                    const int src = (lane & ~3) | t8 >> 1;
-                    float w[2];
-#pragma unroll
-                    for (int y = 0; y < 2; ++y) {
-                        const float e0 = __shfl_sync(0xffffffffu, s[n][2 * y], src), e1 = __shfl_sync(0xffffffffu, s[n][2 * y + 1], src);
-                        w[y] = unpack16<BF16>(pack16<BF16>(t8 & 1 ? e1 : e0, 0.0f)).x;
-                    }
-                    const bool v0 = visible(pos[0], base + row, a.window, a.sinks), v1 = visible(pos[1], base + row, a.window, a.sinks);
-#pragma unroll
-                    for (int d = 0; d < 2 * KS; ++d) {
-                        const float2 v = unpack16<BF16>(*reinterpret_cast<const uint32_t *>(
-                            st + S::kHalf + row * S::kRow + swizzle<DP, FMT, true>(row, d) * 16 + i4 * 4));
-                        if (v0) {
-                            o[d][0] += w[0] * v.x;
-                            o[d][1] += w[0] * v.y;
-                        }
-                        if (v1) {
-                            o[d][2] += w[1] * v.x;
-                            o[d][3] += w[1] * v.y;
-                        }
-                    }
-                }
-        }
-
-        if (more) {  // (the slot's earlier places were taken before this tile's barrier)
-            if (tid < kTok) put(x + S::kStages, pl, bad);
-            if (x + S::kStages + 1 < count) lk.next(a);
-        }
-        if (cu.j + 1 < u.nt && x + 1 < count) {
-            ++cu.j;
-            continue;
-        }
-
-        // ---- the unit ends here, for this CTA ----
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-            l[y] += __shfl_xor_sync(0xffffffffu, l[y], 1);
-            l[y] += __shfl_xor_sync(0xffffffffu, l[y], 2);
-        }
-        if constexpr (WN > 1) {  // the warps that split the tokens, through the stage just used
-            float *const xo = reinterpret_cast<float *>(st);
-            constexpr int kRegs = 8 * KS;
-#pragma unroll
-            for (int half = WN / 2; half >= 1; half /= 2) {
-                __syncthreads();
-                if (wn >= half && wn < 2 * half) {
-                    float *const to = xo + (wm * half + wn - half) * kRegs * 32 + lane;
-#pragma unroll
-                    for (int k = 0; k < kRegs; ++k) to[k * 32] = o[k / 4][k % 4];
-                    s_ml[warp * 32 + lane] = make_float4(m[0], m[1], l[0], l[1]);
-                }
-                __syncthreads();
-                if (wn < half) {
-                    const float4 w = s_ml[(warp + half) * 32 + lane];
-                    const float *const from = xo + (wm * half + wn) * kRegs * 32 + lane;
-                    const float mo[2] = {w.x, w.y}, lo[2] = {w.z, w.w};
-                    float f0[2], f1[2];
-#pragma unroll
-                    for (int y = 0; y < 2; ++y) {
-                        const float mn = fmaxf(m[y], mo[y]);
-                        f0[y] = m[y] == -INFINITY ? 0.0f : exp2_fast(m[y] - mn);
-                        f1[y] = mo[y] == -INFINITY ? 0.0f : exp2_fast(mo[y] - mn);
-                        l[y] = (l[y] == 0.0f ? 0.0f : l[y] * f0[y]) + (lo[y] == 0.0f ? 0.0f : lo[y] * f1[y]);
-                        m[y] = mn;
-                    }
-#pragma unroll
-                    for (int k = 0; k < kRegs; ++k) o[k / 4][k % 4] = o[k / 4][k % 4] * f0[k % 4 >> 1] + from[k * 32] * f1[k % 4 >> 1];
-                }
-            }
-        }
-        const long long u0 = sh.x0 + x - cu.j, u1 = u0 + u.nt;
-        const bool whole = u0 >= sh.x0 && u1 <= sh.x1;
-        // a lane's elements: of 16-bit V 8d + 2i, +1 in o[d]; of 8-bit V 16d + 4i .. + 3 in o[2d], o[2d + 1]
-        if (whole) {
-            if (wn == 0) {
-#pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    const int r = wm * 16 + g + y * 8;
-                    if (r >= u.rows) continue;
-                    const int gr = u.qt * kRows + r, t = quot(gr, c.div_g), hd = u.h * c.G + gr - t * c.G;
-                    const float inv = l[y] == 0.0f ? 0.0f : 1.0f / (l[y] * kLift);
-                    char *const p = a.out + (int64_t)(u.q0 + t) * a.o_t + (int64_t)hd * a.o_h;
-                    if (a.lse && i4 == 0)
-                        a.lse[(int64_t)(u.q0 + t) * c.Hq + hd] = l[y] == 0.0f ? -INFINITY : (m[y] + log2f(l[y])) * 0.69314718f;
-                    if constexpr (FMT == kFmt16) {
-#pragma unroll
-                        for (int d = 0; d < 2 * KS; ++d)
-                            if (d * 8 < c.D)
-                                *reinterpret_cast<uint32_t *>(p + (d * 8 + 2 * i4) * 2) = pack16<BF16>(o[d][2 * y] * inv, o[d][2 * y + 1] * inv);
-                    } else {
-#pragma unroll
-                        for (int d = 0; d < KS; ++d)
-                            if (d * 16 < c.D)
-                                *reinterpret_cast<uint2 *>(p + (d * 16 + 4 * i4) * 2) =
-                                    make_uint2(pack16<BF16>(o[2 * d][2 * y] * inv, o[2 * d + 1][2 * y] * inv),
-                                               pack16<BF16>(o[2 * d][2 * y + 1] * inv, o[2 * d + 1][2 * y + 1] * inv));
-                    }
-                }
-            }
-        } else {
-            const int c0 = cta_of(sh, u0), c1 = cta_of(sh, u1 - 1);
-            const int64_t slot = slot_of(sh, blockIdx.x, u0);
-            if (wn == 0) {
-#pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    const int r = wm * 16 + g + y * 8;
-                    if (r >= u.rows) continue;
-                    float *const p = a.part_o + (slot * kStepRows + r) * 128;
-                    if (i4 == 0) a.part_ml[slot * kStepRows + r] = make_float2(m[y], l[y]);
-                    if constexpr (FMT == kFmt16) {
-#pragma unroll
-                        for (int d = 0; d < 2 * KS; ++d)
-                            *reinterpret_cast<float2 *>(p + d * 8 + 2 * i4) = make_float2(o[d][2 * y], o[d][2 * y + 1]);
-                    } else {
-#pragma unroll
-                        for (int d = 0; d < KS; ++d)
-                            *reinterpret_cast<float4 *>(p + d * 16 + 4 * i4) =
-                                make_float4(o[2 * d][2 * y], o[2 * d + 1][2 * y], o[2 * d][2 * y + 1], o[2 * d + 1][2 * y + 1]);
-                    }
-                }
-            }
-            __threadfence();
-            __syncthreads();
-            if (tid == 0) {
-                const bool last = atomicAdd(a.done + c0, 1u) == (uint32_t)(c1 - c0);
-                if (last) a.done[c0] = 0;
-                s_last = last;
-            }
-            __syncthreads();
-            if (s_last) {  // join the parts, in the order of the CTAs whichever came last
-                __threadfence();
-                constexpr int kLanes = DP / 4;  // four elements a thread
-                const int64_t s0 = slot_of(sh, c0, u0);  // (a unit is the first of every later CTA)
-                auto at_of = [&](int k, int r) { return (k == c0 ? s0 : 2 * (int64_t)k) * kStepRows + r; };
-                for (int r = tid / kLanes; r < u.rows; r += kThreads / kLanes) {
-                    const int d = tid % kLanes * 4;
-                    float mm = -INFINITY;
-                    for (int k = c0; k <= c1; ++k) mm = fmaxf(mm, __ldcg(&a.part_ml[at_of(k, r)].x));
-                    float ll = 0.0f;
-                    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                    for (int k = c0; k <= c1; ++k) {
-                        const int64_t at = at_of(k, r);
-                        const float2 ml = __ldcg(a.part_ml + at);
-                        const float f = ml.x == -INFINITY ? 0.0f : exp2_fast(ml.x - mm);
-                        const float4 w = __ldcg(reinterpret_cast<const float4 *>(a.part_o + at * 128 + d));
-                        ll += ml.y == 0.0f ? 0.0f : ml.y * f;
-                        if (ml.x == -INFINITY && ml.y == 0.0f) continue;  // saw nothing
-                        acc.x += w.x * f;
-                        acc.y += w.y * f;
-                        acc.z += w.z * f;
-                        acc.w += w.w * f;
-                    }
-                    const int gr = u.qt * kRows + r, t = quot(gr, c.div_g), hd = u.h * c.G + gr - t * c.G;
-                    const float inv = ll == 0.0f ? 0.0f : 1.0f / (ll * kLift);
-                    if (d < c.D)
-                        *reinterpret_cast<uint2 *>(a.out + (int64_t)(u.q0 + t) * a.o_t + (int64_t)hd * a.o_h + d * 2) =
-                            make_uint2(pack16<BF16>(acc.x * inv, acc.y * inv), pack16<BF16>(acc.z * inv, acc.w * inv));
-                    if (a.lse && d == 0)
-                        a.lse[(int64_t)(u.q0 + t) * c.Hq + hd] = ll == 0.0f ? -INFINITY : (mm + log2f(ll)) * 0.69314718f;
-                }
-            }
-        }
-        if (x + 1 < count) cu.next(a);
-        if constexpr (WN > 1) __syncthreads();  // the exchanged stage is free again
-    }
-    chain_next();
 }
 
 // ---- up to 16 rows: every warp on its own ----
@@ -617,7 +170,7 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
     if (tid == 0) s_bad = 0;
     Cursor<kRows, S::kTile> cu, lk;
     Share sh;
-    if (!take_share<kRows, S::kTile, kThreads>(a, cu, sh, s_scratch)) {
+    if (!take_share<kRows, S::kTile, kThreads, 1>(a, cu, sh, s_scratch)) {
         chain_next();
         return;
     }
@@ -1065,8 +618,7 @@ struct Pick {
 template <bool BF16, int FMT, int DP>
 Pick pick_rows(int rows) {
     if (rows <= 8) return {k_attend_step<BF16, FMT, DP, 1>, Solo<DP, FMT, 1>::kSmem, Solo<DP, FMT, 1>::kCtas};
-    if (rows <= 16) return {k_attend_step<BF16, FMT, DP, 2>, Solo<DP, FMT, 2>::kSmem, Solo<DP, FMT, 2>::kCtas};
-    return {rows <= 32 ? k_attend_rows<BF16, FMT, DP, 2> : k_attend_rows<BF16, FMT, DP, 4>, Shape<DP, FMT>::kSmem, 2};
+    return {k_attend_step<BF16, FMT, DP, 2>, Solo<DP, FMT, 2>::kSmem, Solo<DP, FMT, 2>::kCtas};
 }
 template <int FMT>
 Pick pick_type(bool bf16, int D, int rows) {
@@ -1087,7 +639,7 @@ cudaError_t attend_step_init() {
     for (int bf16 = 0; bf16 < 2; ++bf16)
         for (int fmt = 0; fmt < 3; ++fmt)
             for (int D = 64; D <= 128; D += 64)
-                for (int rows = 8; rows <= 64; rows *= 2) {
+                for (int rows = 8; rows <= 16; rows *= 2) {
                     const Pick p = pick(bf16, fmt, D, rows);
                     const cudaError_t e = cudaFuncSetAttribute(p.k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)p.smem);
                     if (e != cudaSuccess) return e;

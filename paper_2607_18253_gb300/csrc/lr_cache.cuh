@@ -88,7 +88,7 @@ struct AttendLaunch {
     uint32_t *done;              // parts finished of the unit that began in a CTA ([CTAs]; chunk kernel [CTAs][8 warps]); zero
                                  // between calls
 };
-constexpr int kStepRows = 64;   // rows of a unit of the step kernel, at most
+constexpr int kStepRows = 16;   // rows of a unit of the step kernel, at most
 cudaError_t launch_attend_step(const AttendLaunch &a, bool bf16, int fmt, int rows, int sms, cudaStream_t st);
 cudaError_t attend_step_init();
 int attend_step_ctas(int sms);  // CTAs of a launch, at most

@@ -27,9 +27,6 @@ struct lr_cache {
 
 namespace {
 
-// Rows (new tokens x query heads a KV head) from which a sequence is the chunk kernel's.
-constexpr int kLeastChunk = 65;
-
 int fail(lr_cache *c, int code, const char *msg) {
     try {
         c->err = msg;
@@ -232,24 +229,26 @@ int lr_cache_attend(lr_cache *c, const lr_cache_batch *b, int32_t T, const void 
     a.scale_log2 = (float)((double)scale * 1.4426950408889634);
     a.window = window;
     a.sinks = window ? sinks : 0;
-    // Sequences of few rows go to the step kernel, of many to the chunk kernel (a single one whole, whatever
-    // it brings).  A batch of both takes two launches: 63 single tokens beside a chunk of 1,985 (32 query and
-    // 8 KV heads of 128) XX us, in the chunk kernel alone XX.
-    const int most = (int)std::min<long long>((long long)b->max_q * c->dev.G, 0x7fffffff);
-    const bool all = b->num_seqs == 1;
+    // Rows of a sequence: its new tokens x the query heads of a KV head.  Up to 8, or up to 16 if a batch has no more,
+    // are the step kernel's, more the chunk kernel's (a single sequence whole, whatever it brings).  A batch of both takes two
+    // launches: 63 single tokens beside a chunk of 1,985 (32 query and 8 KV heads of 128) XX us, in the chunk
+    // kernel alone XX.
+    const long long most = (long long)b->max_q * c->dev.G;
+    const int few = most <= 16 || c->dev.G > 8 ? 16 : 8;
     cudaStream_t st = (cudaStream_t)stream;
-    if (most >= kLeastChunk) {
-        a.row_lo = all ? 1 : kLeastChunk;
+    if (most > few) {
+        const bool all = b->num_seqs == 1;
+        a.row_lo = all ? 1 : few + 1;
         a.row_hi = 0x7fffffff;
         a.part_o = c->chunk.o;
         a.part_ml = c->chunk.ml;
         a.done = c->chunk.done;
         cudaError_t e = lr::launch_attend_chunk(a, c->maps, c->bf16, c->cfg.format, c->sms, st);
         if (e != cudaSuccess) return cuda_fail(c, e, "attention launch");
-        if (all) return LR_OK;
+        if (all || c->dev.G > few) return LR_OK;
     }
     a.row_lo = 1;
-    a.row_hi = std::min(most, kLeastChunk - 1);
+    a.row_hi = (int)std::min<long long>(most, few);
     a.part_o = c->step.o;
     a.part_ml = c->step.ml;
     a.done = c->step.done;
