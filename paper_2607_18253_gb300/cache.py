@@ -39,19 +39,21 @@ class CacheBatch:
         self._ref = ctypes.byref(self._c)
 
 
-def _strides(t: torch.Tensor, name: str, heads: int, dim: int, dtype: torch.dtype) -> Tuple[int, int]:
-    """(token, head) strides of a [T, heads, dim] CUDA tensor whose last dimension is dense."""
+def _strides(t: torch.Tensor, name: str, heads: int, dim: int, dtype: torch.dtype) -> Tuple[int, int, int]:
+    """(T, token stride, head stride) of a [T, heads, dim] CUDA tensor whose last dimension is dense."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim:
-        raise ValueError(f"{name} must be [T, {heads}, {dim}], got {tuple(t.shape)}")
+    shape = t.shape
+    if len(shape) != 3 or shape[1] != heads or shape[2] != dim:
+        raise ValueError(f"{name} must be [T, {heads}, {dim}], got {tuple(shape)}")
     st, sh, sd = t.stride()
     if sd != 1:
         raise ValueError(f"{name} must be dense along its last dimension")
     # (a dimension of one element is never stepped along: its stride says nothing)
-    return (st if t.shape[0] > 1 else heads * dim), (sh if heads > 1 else dim)
+    T = shape[0]
+    return T, (st if T > 1 else heads * dim), (sh if heads > 1 else dim)
 
 
 class PagedCache:
@@ -88,6 +90,7 @@ class PagedCache:
         cfg = _CacheConfig(self.num_q_heads, H, D, _DTYPES[dtype], fmt, bs, nb, int(max_seqs), k.data_ptr(), v.data_ptr(),
                            k_scale.data_ptr() if fmt else None, v_scale.data_ptr() if fmt else None, *st, *ss)
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self._scale = 1.0 / math.sqrt(self.head_dim)
         torch.cuda.init()
         h = _P()
         rc = self._lib.lr_cache_create(ctypes.byref(cfg), ctypes.byref(h))
@@ -113,21 +116,27 @@ class PagedCache:
     def write(self, k: torch.Tensor, v: torch.Tensor, batch: CacheBatch, stream=None):
         """Store the batch's K and V, [T, num_kv_heads, head_dim] of equal strides (slices of a fused projection too)."""
         s = _strides(k, "k", self.num_kv_heads, self.head_dim, self.dtype)
-        if _strides(v, "v", self.num_kv_heads, self.head_dim, self.dtype) != s or v.shape != k.shape:
+        if _strides(v, "v", self.num_kv_heads, self.head_dim, self.dtype) != s:
             raise ValueError("k and v must have one shape and strides")
-        self._check(self._lib.lr_cache_write(self._h, batch._ref, k.shape[0], k.data_ptr(), v.data_ptr(), s[0], s[1],
-                                             _stream(stream)), "lr_cache_write")
+        rc = self._lib.lr_cache_write(self._h, batch._ref, s[0], k.data_ptr(), v.data_ptr(), s[1], s[2], _stream(stream))
+        if rc:
+            self._check(rc, "lr_cache_write")
 
     def read(self, batch: CacheBatch, tokens: int, dtype: Optional[torch.dtype] = None,
              out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
         """The batch's `tokens` tokens as values, (k, v) [tokens, num_kv_heads, head_dim] of the cache's dtype or float32."""
         dt = self.dtype if dtype is None else dtype
-        shape = (int(tokens), self.num_kv_heads, self.head_dim)
-        k, v = out if out is not None else (torch.empty(shape, dtype=dt, device=self.k.device),
-                                            torch.empty(shape, dtype=dt, device=self.k.device))
-        n = shape[0] * shape[1] * shape[2]
-        self._check(self._lib.lr_cache_read(self._h, batch._ref, shape[0], _DTYPES.get(dt, -1), _dev(k, dt, "k_out", n),
-                                            _dev(v, dt, "v_out", n), _stream(stream)), "lr_cache_read")
+        T, H, D = int(tokens), self.num_kv_heads, self.head_dim
+        if out is None:
+            k = torch.empty((T, H, D), dtype=dt, device=self.k.device)
+            v = torch.empty_like(k)
+            kp, vp = k.data_ptr(), v.data_ptr()
+        else:
+            k, v = out
+            kp, vp = _dev(k, dt, "k_out", T * H * D), _dev(v, dt, "v_out", T * H * D)
+        rc = self._lib.lr_cache_read(self._h, batch._ref, T, _DTYPES.get(dt, -1), kp, vp, _stream(stream))
+        if rc:
+            self._check(rc, "lr_cache_read")
         return k, v
 
     def attend(self, q: torch.Tensor, batch: CacheBatch, scale: Optional[float] = None, window: int = 0, sinks: int = 0,
@@ -136,22 +145,24 @@ class PagedCache:
 
         scale: head_dim ** -0.5 if not given.  window, sinks: see lr_cache_attend.  lse: True, or the tensor to write."""
         Hq, D = self.num_q_heads, self.head_dim
-        qs = _strides(q, "q", Hq, D, self.dtype)
-        T = q.shape[0]
+        T, qt, qh = _strides(q, "q", Hq, D, self.dtype)
         if out is None:
             out = torch.empty((T, Hq, D), dtype=self.dtype, device=q.device)
-        os_ = _strides(out, "out", Hq, D, self.dtype)
-        if out.shape[0] != T:
-            raise ValueError("out must have q's shape")
+            ot, oh = Hq * D, D
+        else:
+            To, ot, oh = _strides(out, "out", Hq, D, self.dtype)
+            if To != T:
+                raise ValueError("out must have q's shape")
         if lse is True:
             lse = torch.empty((T, Hq), dtype=torch.float32, device=q.device)
-        elif lse is False:
-            lse = None
-        rc = self._lib.lr_cache_attend(self._h, batch._ref, T, q.data_ptr(), qs[0], qs[1],
-                                       1.0 / math.sqrt(D) if scale is None else float(scale), int(window), int(sinks),
-                                       out.data_ptr(), os_[0], os_[1], _dev(lse, torch.float32, "lse_out", T * Hq),
-                                       _stream(stream))
-        self._check(rc, "lr_cache_attend")
+            lp = lse.data_ptr()
+        else:
+            lse = None if lse is False else lse
+            lp = _dev(lse, torch.float32, "lse_out", T * Hq)
+        rc = self._lib.lr_cache_attend(self._h, batch._ref, T, q.data_ptr(), qt, qh, self._scale if scale is None else scale,
+                                       window, sinks, out.data_ptr(), ot, oh, lp, _stream(stream))
+        if rc:
+            self._check(rc, "lr_cache_attend")
         return out, lse
 
     def status(self, stream=None) -> int:

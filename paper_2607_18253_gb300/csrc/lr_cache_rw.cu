@@ -4,7 +4,7 @@
 // Sixteen lanes hold one vector, eight elements each (the largest magnitude of a vector
 // is four shuffles); a CTA takes 64 consecutive (token, head) pairs, four a group of lanes with
 // their loads issued together, K and V of a pair by the same lanes.  The CTA's tokens are looked up once
-// (sequence by binary search over q_start, then block table) and kept in shared memory.
+// (sequence, then block table) and kept in shared memory.
 #include <cuda_fp8.h>
 
 #include "lr_cache.cuh"
@@ -20,23 +20,9 @@ struct Place {
     int64_t soff; // the same in the scales
 };
 
-__device__ __forceinline__ Place find_place(const CacheDev &c, const BatchDev &b, int t) {
-    Place p{-2, 0};
-    // the last sequence that begins at or before t
-    int lo = 0, hi = b.n;
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (__ldg(b.q_start + mid) <= t) lo = mid + 1;
-        else hi = mid;
-    }
-    const int s = lo - 1;
-    if (s < 0) return p;
-    const int end = __ldg(b.q_start + s + 1);
-    if (t >= end) {
-        if (s + 1 < b.n) report(c.status, kEInval);  // q_start out of order
-        return p;
-    }
-    p.off = -1;
+// The place of token t, which is token t - begin of sequence s's [begin, end).
+__device__ __forceinline__ Place find_place(const CacheDev &c, const BatchDev &b, int s, int end, int t) {
+    Place p{-1, 0};
     const int kv = __ldg(b.kv_len + s), pos = kv - (end - t);
     if (pos < 0 || kv > kMaxTokens) return p;
     int place;
@@ -47,12 +33,42 @@ __device__ __forceinline__ Place find_place(const CacheDev &c, const BatchDev &b
     return p;
 }
 
-// The places of the CTA's tokens t0 .. (at most kPairs of them), in shared memory.
-__device__ __forceinline__ void find_places(Place *sp, const CacheDev &c, const BatchDev &b, int t0, int t1) {
-    for (int t = t0 + threadIdx.x; t < t1; t += kThreads) {
-        const Place p = find_place(c, b, t);
+// The places of the CTA's tokens t0 .. t1 - 1 (at most kPairs + 1 of them), in shared memory.  The sequences that have
+// them are found by all threads together, a sequence each: one round of loads for 256 sequences, where a
+// search takes one a halving (budget of 8,192 tokens, 63 sequences, stored and read back: XX).  More than
+// kScan sequences are searched for.
+constexpr int kScan = 1024;
+__device__ __forceinline__ void find_places(Place *sp, int2 *seq, const CacheDev &c, const BatchDev &b, int t0, int t1) {
+    const int mine = t0 + (int)threadIdx.x;
+    if (mine < t1) seq[threadIdx.x] = make_int2(-1, 0);
+    __syncthreads();
+    if (b.n <= kScan) {
+        for (int s = threadIdx.x; s < b.n; s += kThreads) {
+            const int begin = __ldg(b.q_start + s), end = __ldg(b.q_start + s + 1);
+            if (begin > end) report(c.status, kEInval);  // out of order
+            for (int t = max(begin, t0); t < min(end, t1); ++t) seq[t - t0] = make_int2(s, end);
+        }
+    } else if (mine < t1) {
+        // the last sequence that begins at or before the token
+        int lo = 0, hi = b.n;
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (__ldg(b.q_start + mid) <= mine) lo = mid + 1;
+            else hi = mid;
+        }
+        if (lo > 0) {
+            const int end = __ldg(b.q_start + lo);
+            if (mine < end) seq[threadIdx.x] = make_int2(lo - 1, end);
+            else if (lo < b.n) report(c.status, kEInval);
+        }
+    }
+    __syncthreads();
+    if (mine < t1) {
+        const int2 e = seq[threadIdx.x];
+        Place p{-2, 0};
+        if (e.x >= 0) p = find_place(c, b, e.x, e.y, mine);
         if (p.off == -1) report(c.status, kEInval);
-        sp[t - t0] = p;
+        sp[threadIdx.x] = p;
     }
     __syncthreads();
 }
@@ -119,6 +135,7 @@ __device__ __forceinline__ uint2 quantise(const uint4 &w, float &scale) {
 template <bool BF16, int FMT>
 __global__ void __launch_bounds__(kThreads) k_cache_write(const __grid_constant__ RwLaunch a) {
     __shared__ Place sp[kPairs + 1];
+    __shared__ int2 seq[kPairs + 1];
     chain_wait();
     const CacheDev &c = a.c;
     const int64_t first = (int64_t)blockIdx.x * kPairs, total = (int64_t)a.b.T * c.H;
@@ -141,7 +158,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_write(const __grid_constant_
         k[u] = __ldcs(reinterpret_cast<const uint4 *>(a.k_in + at));
         v[u] = __ldcs(reinterpret_cast<const uint4 *>(a.v_in + at));
     }
-    find_places(sp, c, a.b, t0, t1);
+    find_places(sp, seq, c, a.b, t0, t1);
 #pragma unroll
     for (int u = 0; u < kItems; ++u) {
         const Place p = tok[u] < 0 ? Place{-2, 0} : sp[tok[u] - t0];
@@ -195,6 +212,7 @@ __device__ __forceinline__ void values(const uint4 &w, float scale, float *f) {
 template <bool BF16, int FMT, bool F32>
 __global__ void __launch_bounds__(kThreads) k_cache_read(const __grid_constant__ RwLaunch a) {
     __shared__ Place sp[kPairs + 1];
+    __shared__ int2 seq[kPairs + 1];
     chain_wait();
     const CacheDev &c = a.c;
     const int64_t first = (int64_t)blockIdx.x * kPairs, total = (int64_t)a.b.T * c.H;
@@ -202,7 +220,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_read(const __grid_constant__
     const int t0 = (int)(first / c.H), t1 = (int)(last / c.H) + 1;
     const int g = threadIdx.x / 16, l = threadIdx.x % 16;
     const bool on = l * 8 < c.D;
-    find_places(sp, c, a.b, t0, t1);
+    find_places(sp, seq, c, a.b, t0, t1);
     uint4 k[kItems], v[kItems];
     float sk[kItems], sv[kItems];
     bool write[kItems];
