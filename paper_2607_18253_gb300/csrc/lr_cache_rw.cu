@@ -13,7 +13,12 @@ namespace lr {
 
 namespace {
 
-constexpr int kThreads = 256, kGroups = kThreads / 16, kItems = 4, kPairs = kGroups * kItems;
+constexpr int kThreads = 256, kGroups = kThreads / 16;
+// (token, head) pairs a group of lanes: four where their bytes are only moved (6.9 TB/s), two where they are
+// converted as they are stored, which takes registers (8,192 tokens to int8: XX and XX us)
+template <int FMT>
+constexpr int kStoreItems = FMT == kFmt16 ? 4 : 2;
+constexpr int kLoadItems = 4, kMostTokens = kGroups * 4 + 1;
 
 struct Place {
     int64_t off;  // byte offset of the token's place for head 0, -1: none, -2: of no sequence
@@ -33,7 +38,7 @@ __device__ __forceinline__ Place find_place(const CacheDev &c, const BatchDev &b
     return p;
 }
 
-// The places of the CTA's tokens t0 .. t1 - 1 (at most kPairs + 1 of them), in shared memory.  The sequences that have
+// The places of the CTA's tokens t0 .. t1 - 1 (at most kMostTokens of them), in shared memory.  The sequences that have
 // them are found by all threads together, a sequence each: one round of loads for 256 sequences, where a
 // search takes one a halving (budget of 8,192 tokens, 63 sequences, stored and read back: XX).  More than
 // kScan sequences are searched for.
@@ -120,22 +125,23 @@ __device__ __forceinline__ uint2 quantise(const uint4 &w, float &scale) {
         r.x = h[0] | h[1] << 16;
         r.y = h[2] | h[3] << 16;
     } else {
+        // 1.5 * 2^23 added: the sum's last bit is one, so it is rounded to an integer (ties to even), which its low bits
+        // hold.  The products are at most 127 and a rounding.
         uint32_t q[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int v = __float2int_rn(__fmul_rn(f[i], inv));
-            q[i] = (uint32_t)max(-127, min(127, v)) & 0xffu;
-        }
-        r.x = q[0] | q[1] << 8 | q[2] << 16 | q[3] << 24;
-        r.y = q[4] | q[5] << 8 | q[6] << 16 | q[7] << 24;
+        for (int i = 0; i < 8; ++i) q[i] = __float_as_uint(__fadd_rn(__fmul_rn(f[i], inv), 12582912.0f));
+        auto four = [&](int i) { return __byte_perm(__byte_perm(q[i], q[i + 1], 0x0040), __byte_perm(q[i + 2], q[i + 3], 0x0040), 0x5410); };
+        r.x = four(0);
+        r.y = four(4);
     }
     return r;
 }
 
 template <bool BF16, int FMT>
 __global__ void __launch_bounds__(kThreads) k_cache_write(const __grid_constant__ RwLaunch a) {
-    __shared__ Place sp[kPairs + 1];
-    __shared__ int2 seq[kPairs + 1];
+    __shared__ Place sp[kMostTokens];
+    __shared__ int2 seq[kMostTokens];
+    constexpr int kItems = kStoreItems<FMT>, kPairs = kGroups * kItems;
     chain_wait();
     const CacheDev &c = a.c;
     const int64_t first = (int64_t)blockIdx.x * kPairs, total = (int64_t)a.b.T * c.H;
@@ -211,8 +217,9 @@ __device__ __forceinline__ void values(const uint4 &w, float scale, float *f) {
 
 template <bool BF16, int FMT, bool F32>
 __global__ void __launch_bounds__(kThreads) k_cache_read(const __grid_constant__ RwLaunch a) {
-    __shared__ Place sp[kPairs + 1];
-    __shared__ int2 seq[kPairs + 1];
+    __shared__ Place sp[kMostTokens];
+    __shared__ int2 seq[kMostTokens];
+    constexpr int kItems = kLoadItems, kPairs = kGroups * kItems;
     chain_wait();
     const CacheDev &c = a.c;
     const int64_t first = (int64_t)blockIdx.x * kPairs, total = (int64_t)a.b.T * c.H;
@@ -278,12 +285,15 @@ __global__ void __launch_bounds__(kThreads) k_cache_read(const __grid_constant__
     chain_next();
 }
 
-int grid_of(const RwLaunch &a) { return (int)(((int64_t)a.b.T * a.c.H + kPairs - 1) / kPairs); }
+int grid_of(const RwLaunch &a, int items) {
+    const int pairs = kGroups * items;
+    return (int)(((int64_t)a.b.T * a.c.H + pairs - 1) / pairs);
+}
 
 }  // namespace
 
 cudaError_t launch_cache_write(const RwLaunch &a, bool bf16, int fmt, int, cudaStream_t st) {
-    auto go = [&](void (*k)(const RwLaunch)) { return launch_chained(k, grid_of(a), kThreads, 0, st, a); };
+    auto go = [&](void (*k)(const RwLaunch)) { return launch_chained(k, grid_of(a, fmt == kFmt16 ? kStoreItems<kFmt16> : kStoreItems<kFmtInt8>), kThreads, 0, st, a); };
     switch (fmt) {
         case kFmtE4M3: return go(bf16 ? k_cache_write<true, kFmtE4M3> : k_cache_write<false, kFmtE4M3>);
         case kFmtInt8: return go(bf16 ? k_cache_write<true, kFmtInt8> : k_cache_write<false, kFmtInt8>);
@@ -292,7 +302,7 @@ cudaError_t launch_cache_write(const RwLaunch &a, bool bf16, int fmt, int, cudaS
 }
 
 cudaError_t launch_cache_read(const RwLaunch &a, bool bf16, int fmt, bool f32, int, cudaStream_t st) {
-    auto go = [&](void (*k)(const RwLaunch)) { return launch_chained(k, grid_of(a), kThreads, 0, st, a); };
+    auto go = [&](void (*k)(const RwLaunch)) { return launch_chained(k, grid_of(a, kLoadItems), kThreads, 0, st, a); };
     switch (fmt) {
         case kFmtE4M3:
             return f32 ? go(k_cache_read<true, kFmtE4M3, true>)
