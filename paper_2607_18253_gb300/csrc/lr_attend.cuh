@@ -56,8 +56,9 @@ __device__ __forceinline__ void set_tile(const AttendLaunch &a, Unit &u) {
     u.nt = tile_count<TILE>(u.lo, u.hi, a.window, a.sinks, u.ns, u.wf);
 }
 
-// Tiles of a sequence for one KV head, a warp's lanes taking its tiles of rows in turn (all call).
-template <int ROWS, int TILE>
+// Tiles of a sequence for one KV head, with the units' weights, a warp's lanes taking its tiles of rows in
+// turn (all call).
+template <int ROWS, int TILE, int WEIGHT>
 __device__ __forceinline__ long long seq_tiles(const AttendLaunch &a, int s) {
     Unit u;
     u.s = s;
@@ -66,22 +67,40 @@ __device__ __forceinline__ long long seq_tiles(const AttendLaunch &a, int s) {
     long long n = 0;
     for (u.qt = threadIdx.x & 31; u.qt < nq; u.qt += 32) {
         set_tile<ROWS, TILE>(a, u);
-        n += u.nt;
+        n += u.nt + WEIGHT;
     }
 #pragma unroll
     for (int o = 16; o >= 1; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
     return n;
 }
 
-// A position in the batch's sequence of tiles: units in order of sequence, KV head, tile of rows.
-template <int ROWS, int TILE>
+// The batch's tiles in one line, units in order of sequence, KV head, tile of rows, cut into equal shares for the
+// CTAs.  A unit counts WEIGHT more than its tiles, at its front, for what it costs to begin and end one: a cut
+// that falls there takes the unit whole.
+struct Share {
+    long long x0, x1, all;  // this CTA's share, of the whole
+    int ctas;               // by so many CTAs (the others have none)
+};
+
+// A position in the line, within a CTA's share.
+template <int ROWS, int TILE, int WEIGHT>
 struct Cursor {
     Unit u;
-    int j;  // tile of the unit
+    int j, end;    // tile of the unit; the CTA's tiles of it end there
+    bool last;     // its last unit
+    long long at;  // where the unit begins
     __device__ __forceinline__ int base() const { return (j < u.ns ? j : u.wf + j - u.ns) * TILE; }
-    __device__ __forceinline__ void next(const AttendLaunch &a) {  // there is a next tile
-        if (++j < u.nt) return;
+    __device__ __forceinline__ bool more() const { return j + 1 < end || !last; }
+    __device__ __forceinline__ bool whole() const { return j == 0 && end == u.nt; }  // (at the unit's first tile)
+    __device__ __forceinline__ void enter(const AttendLaunch &a, const Share &s) {
+        set_tile<ROWS, TILE>(a, u);
+        end = (int)min((long long)u.nt, s.x1 - at - WEIGHT);
+        last = at + u.nt + 2 * WEIGHT >= s.x1;
+    }
+    __device__ __forceinline__ void next(const AttendLaunch &a, const Share &s) {  // there is more
+        if (++j < end) return;
         j = 0;
+        at += u.nt + WEIGHT;
         if ((++u.qt) * ROWS >= u.ql * a.c.G) {
             u.qt = 0;
             if (++u.h == a.c.H) {
@@ -90,7 +109,7 @@ struct Cursor {
                 while (u.s < a.b.n && !load_seq(a, u.s, u.q0, u.ql, u.kv));
             }
         }
-        set_tile<ROWS, TILE>(a, u);
+        enter(a, s);
     }
 };
 
@@ -115,19 +134,14 @@ __device__ __forceinline__ long long block_sum(long long v, long long *sh, long 
     return v;
 }
 
-// Splits the batch's tiles evenly over the CTAs, LEAST of them or more to each: this CTA takes [x0, x1) of the `all`
-// tiles, by `ctas` CTAs (the others have none), and `cur` stands at x0.
-struct Share {
-    long long x0, x1, all;
-    int ctas;
-};
-// The first tile of CTA c's share (32-bit divisions where they do, as nearly always).
+// The start of CTA c's share (32-bit divisions where they do, as nearly always).
 __device__ __forceinline__ long long share_start(const Share &s, int c) {
     return s.all < 1 << 20 ? (long long)((uint32_t)s.all * (uint32_t)c / (uint32_t)s.ctas) : s.all * c / s.ctas;
 }
 // (scratch: THREADS / 32 + 2 words of shared memory)
-template <int ROWS, int TILE, int THREADS, int LEAST>
-__device__ __forceinline__ bool take_share(const AttendLaunch &a, Cursor<ROWS, TILE> &cur, Share &sh, long long *scratch) {
+// This CTA's share, LEAST or more long, with `cur` at its first tile; false if it has none.
+template <int ROWS, int TILE, int WEIGHT, int THREADS, int LEAST>
+__device__ __forceinline__ bool take_share(const AttendLaunch &a, Cursor<ROWS, TILE, WEIGHT> &cur, Share &sh, long long *scratch) {
     long long *const s_sum = scratch, &s_rest = scratch[THREADS / 32], &s_seq = scratch[THREADS / 32 + 1];
     const int n = a.b.n, tid = threadIdx.x, lane = tid & 31;
     // tiles of sequence base + tid: a thread's own look where no sequence has more than one tile of rows,
@@ -140,12 +154,12 @@ __device__ __forceinline__ bool take_share(const AttendLaunch &a, Cursor<ROWS, T
             u.qt = 0;
             if (u.s >= n || !load_seq(a, u.s, u.q0, u.ql, u.kv)) return 0;
             set_tile<ROWS, TILE>(a, u);
-            return (long long)a.c.H * u.nt;
+            return (long long)a.c.H * (u.nt + WEIGHT);
         }
         long long mine = 0;
         const int w0 = base + tid - lane;
         for (int i = 0; i < 32 && w0 + i < n; ++i) {
-            const long long t = a.c.H * seq_tiles<ROWS, TILE>(a, w0 + i);
+            const long long t = a.c.H * seq_tiles<ROWS, TILE, WEIGHT>(a, w0 + i);
             if (i == lane) mine = t;
         }
         return mine;
@@ -185,14 +199,14 @@ __device__ __forceinline__ bool take_share(const AttendLaunch &a, Cursor<ROWS, T
     u.s = (int)s_seq;
     load_seq(a, u.s, u.q0, u.ql, u.kv);
     long long r = s_rest;
-    const long long per = seq_tiles<ROWS, TILE>(a, u.s);
+    const long long per = seq_tiles<ROWS, TILE, WEIGHT>(a, u.s);
     u.h = (int)(r / per);
     r -= u.h * per;
     const int nq = (u.ql * a.c.G + ROWS - 1) / ROWS;
     for (int q0 = 0;; q0 += 32) {  // 32 tiles of rows at a time
         u.qt = min(q0 + lane, nq - 1);
         set_tile<ROWS, TILE>(a, u);
-        const long long own = q0 + lane < nq ? u.nt : 0;
+        const long long own = q0 + lane < nq ? u.nt + WEIGHT : 0;
         long long upto = own;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -208,17 +222,18 @@ __device__ __forceinline__ bool take_share(const AttendLaunch &a, Cursor<ROWS, T
         }
         r -= __shfl_sync(0xffffffffu, upto, 31);
     }
-    set_tile<ROWS, TILE>(a, u);
-    cur.j = (int)r;
-    return true;
+    cur.at = sh.x0 - r;
+    cur.enter(a, sh);
+    cur.j = max(0, (int)r - WEIGHT);
+    return cur.j < cur.end;  // (a share may end in a unit's weight)
 }
 
-// The CTAs c0 .. c1 that share the unit of tiles [u0, u1), and where CTA c's part of it lies: its
-// first unit in slot 2c, a later one in slot 2c + 1.
+// The CTA that has position x, and where CTA c's part of the unit that begins at `at` lies: its first unit in slot
+// 2c, a later one in slot 2c + 1.
 __device__ __forceinline__ int cta_of(const Share &s, long long x) {
     return s.all < 1 << 20 ? (int)((((uint32_t)x + 1) * (uint32_t)s.ctas - 1) / (uint32_t)s.all) : (int)(((x + 1) * s.ctas - 1) / s.all);
 }
-__device__ __forceinline__ int slot_of(const Share &s, int c, long long u0) { return 2 * c + (share_start(s, c) < u0 ? 1 : 0); }
+__device__ __forceinline__ int slot_of(const Share &s, int c, long long at) { return 2 * c + (share_start(s, c) < at ? 1 : 0); }
 
 __device__ __forceinline__ bool visible(int pos, int j, int window, int sinks) {
     return j <= pos && (window == 0 || j > pos - window || j < sinks);

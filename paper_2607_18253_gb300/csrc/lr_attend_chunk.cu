@@ -22,6 +22,7 @@ namespace lr {
 namespace {
 
 constexpr int kTok = 128;     // tokens of a tile
+constexpr int kWeight = 4;    // tiles that a unit's beginning and end take the time of
 constexpr int kThreads = 512;
 // registers a thread of the softmax warps and of the others: together the 512 x 128 of the launch
 constexpr int kSoftRegs = 192, kOtherRegs = 64;
@@ -379,13 +380,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
     const CacheDev &c = a.c;
 
     chain_wait();
-    Cursor<256, kTok> cu;
+    Cursor<256, kTok, kWeight> cu;
     Share sh;
-    if (!take_share<256, kTok, kThreads, 4>(a, cu, sh, scratch)) {
+    if (!take_share<256, kTok, kWeight, kThreads, 4>(a, cu, sh, scratch)) {
         chain_next();
         return;
     }
-    const int count = (int)(sh.x1 - sh.x0);
     if (tid == 0) {
         bar_init(q_full, S::kQueryWarps);
         bar_init(q_free, 1);
@@ -698,7 +698,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
             float ks, vs;
             bool bad;
         };
-        auto look = [&](const Cursor<256, kTok> &p) {
+        auto look = [&](const Cursor<256, kTok, kWeight> &p) {
             Found f{-1, 1.0f, 0.0f, false};
             const int t = p.base() + i;
             if (t > p.u.hi || (a.window > 0 && t <= p.u.lo - a.window && t >= a.sinks)) return f;
@@ -767,12 +767,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
             static_assert(FMT == kFmt16 || S::kSlots <= 2 * kIts, "the first requests are the first tile's");
             for (int k = 0; k < S::kSlots; ++k) request(true);
         }
-        for (int x = 0; x < count; ++x) {  // (cu stands at tile x, then at x + 1)
+        for (int x = 0, more = 1; more; ++x) {  // (cu stands at tile x, then at x + 1)
             bar_arrive_warp(sc_full + 8 * (x & 3));  // the tile's scales and flag
-            const bool more = x + 1 < count;
+            more = cu.more();
             Found f{-1, 1.0f, 0.0f, false};
             if (more) {
-                cu.next(a);
+                cu.next(a, sh);
                 f = look(cu);
             }
             if constexpr (FMT == kFmt16) {
@@ -864,12 +864,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
             int place = 0;
             bool bad = false;
             int blk = look(place, bad);
-            for (int x = 0; x < count; ++x) {
-                const bool more = x + 1 < count;
+            for (int x = 0, more = 1; more; ++x) {
+                more = cu.more();
                 const int h = cu.u.h, now = blk, at = place;
                 const unsigned any = __ballot_sync(0xffffffffu, bad), boxes = __popc(__ballot_sync(0xffffffffu, now >= 0));
                 if (more) {
-                    cu.next(a);
+                    cu.next(a, sh);
                     blk = look(place, bad);
                 }
                 if (!is_v && lane == 0) {
@@ -898,25 +898,23 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
             constexpr int QC = DP / 8, QS = S::kQueryWarps * 32 / QC;
             const int i = tid - S::kQueryWarp * 32, qc = i % QC;
             bool ok = true;
-            for (int x = 0, frag = 0; x < count; ++frag) {
+            for (int frag = 0;; ++frag) {
                 const Unit &u = cu.u;
-                const int n = min(u.nt - cu.j, count - x);
                 if (i < 32) {
                     if (frag >= kJobs) ok = ok && bar_wait<true>(job_free + 8 * (frag % kJobs), (frag / kJobs - 1) & 1, dead);
                     if (ok && i == 0) {
                         Job &job = jobs[frag % kJobs];
-                        const long long u0 = sh.x0 + x - cu.j, u1 = u0 + u.nt;
                         job.u = u;
                         job.j0 = cu.j;
-                        job.n = n;
-                        job.whole = u0 >= sh.x0 && u1 <= sh.x1;
-                        job.last = x + n >= count;
+                        job.n = cu.end - cu.j;
+                        job.whole = cu.whole();
+                        job.last = cu.last;
                         job.c0 = job.c1 = job.slot = job.slot0 = 0;
                         if (!job.whole) {
-                            job.c0 = cta_of(sh, u0);
-                            job.c1 = cta_of(sh, u1 - 1);
-                            job.slot = slot_of(sh, blockIdx.x, u0);
-                            job.slot0 = slot_of(sh, job.c0, u0);
+                            job.c0 = cta_of(sh, cu.at + kWeight);
+                            job.c1 = cta_of(sh, cu.at + kWeight + u.nt - 1);
+                            job.slot = slot_of(sh, blockIdx.x, cu.at);
+                            job.slot0 = slot_of(sh, job.c0, cu.at);
                         }
                         bar_arrive(job_full + 8 * (frag % kJobs));
                     }
@@ -954,11 +952,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
                     shared_to_async();
                     bar_arrive_warp(q_full);
                 }
-                x += n;
-                if (x < count) {
-                    cu.j += n - 1;
-                    cu.next(a);
-                }
+                if (cu.last) break;
+                cu.j = cu.end - 1;
+                cu.next(a, sh);
             }
         } else if (warp == 8) {
             // ================= products: the warp waits, one thread issues =================

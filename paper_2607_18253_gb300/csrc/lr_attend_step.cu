@@ -19,6 +19,7 @@ namespace {
 
 constexpr int kTok = 64;      // tokens of a tile
 constexpr int kThreads = 128;
+constexpr int kStepWeight = 2;  // tiles that a unit's beginning and end take the time of
 
 // Where a 16-byte chunk of a cached vector lies in its shared-memory row, so that the eight rows that
 // one instruction reads at a time are in different banks.
@@ -168,14 +169,14 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
 
     chain_wait();
     if (tid == 0) s_bad = 0;
-    Cursor<kRows, S::kTile> cu, lk;
+    Cursor<kRows, S::kTile, kStepWeight> cu, lk;
     Share sh;
-    if (!take_share<kRows, S::kTile, kThreads, 1>(a, cu, sh, s_scratch)) {
+    if (!take_share<kRows, S::kTile, kStepWeight, kThreads, 1>(a, cu, sh, s_scratch)) {
         chain_next();
         return;
     }
-    const int count = (int)(sh.x1 - sh.x0);
     lk = cu;
+    bool ahead = true;  // lk stands at a tile that is to be requested
 
     // The block of lane l's token of the tile at lk, as the table has it: a load that nothing waits for until the
     // tile's copies are issued, a tile later.  Where blocks are multiples of 16 tokens, 16 neighbouring tokens
@@ -246,10 +247,13 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
     };
     look();
     for (int t = 0; t < S::kStages - 1; ++t) {
-        if (t < count) issue(t);
-        if (t + 1 < count) {
-            lk.next(a);
-            look();
+        if (ahead) {
+            issue(t);
+            ahead = lk.more();
+            if (ahead) {
+                lk.next(a, sh);
+                look();
+            }
         }
         copy_commit();
     }
@@ -258,9 +262,9 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
     uint32_t q[KS][NR][2];
     float o[KS][NR][4], m[NR][2], l[NR][2], qf[NR][2], less[NR][2], vmax = 0.0f, vinv = 0.0f;  // less: m, 0 where it is -inf
     int pos[NR][2];
-    for (int x = 0; x < count;) {
+    for (int x = 0;;) {
         const Unit &u = cu.u;
-        const long long u0 = sh.x0 + x - cu.j, u1 = u0 + u.nt;  // the unit's tiles
+        const bool whole = cu.whole(), last_unit = cu.last;
         {  // its queries, straight to the registers that multiply them
 #pragma unroll
             for (int n = 0; n < NR; ++n) {
@@ -318,12 +322,13 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
             vmax = vinv = 0.0f;
             bad = false;
         }
-        for (const int end = x + min(u.nt - cu.j, count - x); x < end; ++x, ++cu.j) {
+        for (; cu.j < cu.end; ++x, ++cu.j) {
         // the copies of the tile ahead, then the places of the one after it (their latency is the tile's work)
-        if (x + S::kStages - 1 < count) {
+        if (ahead) {
             issue(x + S::kStages - 1);
-            if (x + S::kStages < count) {
-                lk.next(a);
+            ahead = lk.more();
+            if (ahead) {
+                lk.next(a, sh);
                 look();
             }
         }
@@ -562,12 +567,11 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
             }
         if (__any_sync(0xffffffffu, bad) && lane == 0) s_bad = x;
         __syncthreads();
-        const bool whole = u0 >= sh.x0 && u1 <= sh.x1;
         constexpr int kLanes = DP / 4;  // four elements a thread
         const int d = tid % kLanes * 4;
         const bool lost = s_bad == x;
         int64_t slot = 0;
-        if (!whole) slot = slot_of(sh, blockIdx.x, u0);
+        if (!whole) slot = slot_of(sh, blockIdx.x, cu.at);
         for (int r = tid / kLanes; r < u.rows; r += kThreads / kLanes) {
             float mm = -INFINITY, ll = 0.0f;
             float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -585,7 +589,7 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
             }
         }
         if (!whole) {
-            const int c0 = cta_of(sh, u0), c1 = cta_of(sh, u1 - 1);
+            const int c0 = cta_of(sh, cu.at + kStepWeight), c1 = cta_of(sh, cu.at + kStepWeight + u.nt - 1);
             __threadfence();
             __syncthreads();
             if (tid == 0) {
@@ -596,14 +600,13 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
             __syncthreads();
             if (s_last) {
                 __threadfence();
-                join_parts<BF16, DP>(a, c0, c1 - c0 + 1, slot_of(sh, c0, u0), u.rows, u.q0, u.h);
+                join_parts<BF16, DP>(a, c0, c1 - c0 + 1, slot_of(sh, c0, cu.at), u.rows, u.q0, u.h);
             }
         }
         __syncthreads();  // the stages are free again
-        if (x < count) {
-            --cu.j;  // (the last tile that was taken)
-            cu.next(a);
-        }
+        if (last_unit) break;
+        --cu.j;  // (the last tile that was taken)
+        cu.next(a, sh);
     }
     chain_next();
 }
