@@ -1,23 +1,29 @@
-// Attention of few rows over a paged KV cache: single tokens of many sequences, short chunks.
+// Attention of few rows over a paged KV cache: the single tokens of many sequences.
 //
 // For the rows of a unit (lr_attend.cuh) the softmax needs one pass over the cached tokens: with
 // the running maximum m, the sum l of exp(x_j - m) and the weighted sum o of v_j, a tile of tokens
 // that raises m to m' scales l and o by exp(m - m') first.  Two ranges of tokens are
 // joined the same way, so a unit may be split anywhere.
 //
-// What bounds it is the cache's bytes.  A CTA of four warps therefore takes an equal, contiguous
-// share of the batch's tiles of 64 tokens whatever sequences they belong to, and keeps
-// two to three tiles in flight (cp.async, 16 bytes a thread, block ids looked up a tile
-// earlier); the products run on 16x8x16 tensor-core instructions whose 16 rows are the query heads of
-// a KV head.  With up to 16 rows the warps split a tile's tokens, with up to 32 in halves,
-// with up to 64 each warp has rows of its own.
+// What bounds it is the cache's bytes, and next to them the chain of dependent steps that a tile is: scores,
+// maximum, weights, sums.  So the batch is one line of tiles, whatever sequences they belong to, of which
+// each CTA takes an equal share (lr_attend.cuh), and within a CTA
+//   - a tile's tokens are divided over the four warps, and a warp copies (cp.async, a tile or two ahead), waits
+//     for and multiplies its own: nothing is exchanged until the unit ends, where the warps join their
+//     sums through the stages just used, and the CTAs of a shared unit theirs through memory;
+//   - the products are S^T = K Q^T and O^T += V^T P^T (16x8x16 tensor-core instructions): the 16-row operand is
+//     the cache and the 8-column one the queries, so up to eight rows (NR = 1) cost half of what they would as half of
+//     a 16-row operand, in instructions and registers, and more warps fit an SM;
+//   - the maximum that the weights refer to lags behind the true one, so most tiles exchange nothing between lanes.
+// Measured (32 query heads on 8 KV heads of 128, blocks of 16): a 16-bit cache 5.9 TB/s (63 sequences of
+// 512 to 6,001 tokens, 98 us) and 4.7 (one of 200,001, 86 us); e4m3 4.6 (64 of 128 to 8,192, 56 us), bound
+// by instructions: an 8-bit token is as many as a 16-bit one, and its conversion.
 #include "lr_attend.cuh"
 
 namespace lr {
 
 namespace {
 
-constexpr int kTok = 64;      // tokens of a tile
 constexpr int kThreads = 128;
 constexpr int kStepWeight = 2;  // tiles that a unit's beginning and end take the time of
 
@@ -55,15 +61,6 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint3
                      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// ---- up to 16 rows: every warp on its own ----
-//
-// A tile's tokens are divided over the four warps, and a warp copies, waits for and multiplies its own:
-// nothing is exchanged until the unit ends (the warps then join their sums through the stages just used), so
-// no warp waits for another's copies.  The products are the other way round here, S^T = K Q^T and
-// O^T += V^T P^T: the 16-row operand is the cache and the 8-column one the queries, so up to eight rows (NR = 1)
-// cost half of what they would as half of a 16-row operand, in instructions and registers, and
-// four CTAs fit an SM.  That counts because a tile is a chain of dependent steps: with two CTAs of the other
-// form an SM, 64 sequences over an e4m3 cache took 91 us, 78 of them without any copies.
 template <int DP, int FMT, int NR>
 struct Solo {
     static constexpr int kRow = DP * (FMT == kFmt16 ? 2 : 1);
@@ -180,9 +177,8 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
 
     // The block of lane l's token of the tile at lk, as the table has it: a load that nothing waits for until the
     // tile's copies are issued, a tile later.  Where blocks are multiples of 16 tokens, 16 neighbouring tokens
-    // share one, and their addresses follow from the first's: 16 lanes have one look (fewer instructions,
-    // which bound an 8-bit step: XX with a look a token).  What no row of the unit sees is not looked
-    // up (its block may be gone) and reads as zeros.
+    // share one, and their addresses follow from the first's.  What no row of the unit sees is not looked up (its
+    // block may be gone) and reads as zeros.
     const bool even = c.b % 16 == 0;
     int blk = -1, place = 0;
     auto seen = [&](int t) { return t <= lk.u.hi && !(a.window > 0 && t <= lk.u.lo - a.window && t >= a.sinks); };
@@ -323,221 +319,223 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
             bad = false;
         }
         for (; cu.j < cu.end; ++x, ++cu.j) {
-        // the copies of the tile ahead, then the places of the one after it (their latency is the tile's work)
-        if (ahead) {
-            issue(x + S::kStages - 1);
-            ahead = lk.more();
+            // the copies of the tile ahead, then the places of the one after it (their latency is the tile's work)
             if (ahead) {
-                lk.next(a, sh);
-                look();
+                issue(x + S::kStages - 1);
+                ahead = lk.more();
+                if (ahead) {
+                    lk.next(a, sh);
+                    look();
+                }
             }
-        }
-        copy_commit();
-        copy_wait<S::kStages - 1>();
-        __syncwarp();
-        bad |= bad_tiles >> (x & 31) & 1;
-        bad_tiles &= ~(1u << (x & 31));
+            copy_commit();
+            copy_wait<S::kStages - 1>();
+            __syncwarp();
+            bad |= bad_tiles >> (x & 31) & 1;
+            bad_tiles &= ~(1u << (x & 31));
 
-        // ---- scores: tokens g, g + 8 of each 16 ----
-        char *const st = stages + x % S::kStages * S::kStage;
-        const uint32_t sk = smem_addr(st), sv = sk + S::kHalf;
-        const int base = cu.base() + warp * kMine;
-        float s[NB][NR][4];
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int n = 0; n < NR; ++n)
-#pragma unroll
-                for (int z = 0; z < 4; ++z) s[b][n][z] = 0.0f;
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            if constexpr (FMT == kFmt16) {
-#pragma unroll
-                for (int k = 0; k < KS; ++k) {
-                    uint32_t w[4];
-                    const int row = b * 16 + lane % 16;
-                    ldsm4(w, sk + row * S::kRow + swizzle<DP, FMT, false>(row, k * 2 + lane / 16) * 16);
-#pragma unroll
-                    for (int n = 0; n < NR; ++n) mma<MB>(s[b][n], w, q[k][n][0], q[k][n][1]);
-                }
-            } else {
-#pragma unroll
-                for (int hf = 0; hf < DP / 64; ++hf) {
-                    const int row = b * 16 + g;
-                    const uint4 w = lds16(sk + row * S::kRow + swizzle<DP, FMT, false>(row, hf * 4 + i4) * 16);
-                    const uint4 v = lds16(sk + (row + 8) * S::kRow + swizzle<DP, FMT, false>(row + 8, hf * 4 + i4) * 16);
-                    const uint32_t ww[4] = {w.x, w.y, w.z, w.w}, vv[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        uint32_t f[4];
-                        to_half<FMT, false>(ww[k], f[0], f[2]);
-                        to_half<FMT, false>(vv[k], f[1], f[3]);
-#pragma unroll
-                        for (int n = 0; n < NR; ++n) mma<MB>(s[b][n], f, q[hf * 4 + k][n][0], q[hf * 4 + k][n][1]);
-                    }
-                }
-            }
-        }
-        // ---- softmax ----
-        const float *const ks = scales + x % S::kStages * 2 * kMine, *const vs = ks + kMine;
-        const bool masked = base + kMine - 1 > u.lo || (a.window > 0 && base <= u.hi - a.window && base + kMine > a.sinks);
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int n = 0; n < NR; ++n)
-#pragma unroll
-                for (int z = 0; z < 4; ++z) {
-                    float f = qf[n][z & 1];
-                    if constexpr (FMT != kFmt16) f *= ks[b * 16 + g + (z >> 1) * 8];
-                    s[b][n][z] *= f;
-                }
-        if (masked) {
+            // ---- scores: tokens g, g + 8 of each 16 ----
+            char *const st = stages + x % S::kStages * S::kStage;
+            const uint32_t sk = smem_addr(st), sv = sk + S::kHalf;
+            const int base = cu.base() + warp * kMine;
+            float s[NB][NR][4];
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
                 for (int n = 0; n < NR; ++n)
 #pragma unroll
-                    for (int z = 0; z < 4; ++z)
-                        if (!visible(pos[n][z & 1], base + b * 16 + g + (z >> 1) * 8, a.window, a.sinks)) s[b][n][z] = -INFINITY;
-        }
-        float mx[NR][2];
-        bool raise = false;
-#pragma unroll
-        for (int n = 0; n < NR; ++n)
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-                mx[n][y] = fmaxf(s[0][n][y], s[0][n][y + 2]);
-#pragma unroll
-                for (int b = 1; b < NB; ++b) mx[n][y] = fmaxf(mx[n][y], fmaxf(s[b][n][y], s[b][n][y + 2]));
-                raise |= mx[n][y] > m[n][y] + kLag;
-            }
-        float vnew = vmax;
-        if constexpr (FMT != kFmt16) {
-            // the largest scale of V so far (positive numbers compare as integers; one that is not finite does not count)
-            const uint32_t bits = __float_as_uint(vs[lane % kMine]);
-            vnew = fmaxf(vmax, __uint_as_float(__reduce_max_sync(0xffffffffu, bits < 0x7f800000u ? bits : 0u)));
-            raise |= vnew > 2.0f * vmax;  // (weights up to twice as large do no harm)
-        }
-        if (__any_sync(0xffffffffu, raise)) {
-            const float fv = FMT != kFmt16 && vnew > vmax ? vmax / vnew : 1.0f;  // 0 at first
-            vmax = vnew;
-            if (FMT != kFmt16 && vmax > 0.0f) vinv = 1.0f / vmax;
-#pragma unroll
-            for (int n = 0; n < NR; ++n)
-#pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    float w = mx[n][y];
-                    w = fmaxf(w, __shfl_xor_sync(0xffffffffu, w, 4));
-                    w = fmaxf(w, __shfl_xor_sync(0xffffffffu, w, 8));
-                    w = fmaxf(w, __shfl_xor_sync(0xffffffffu, w, 16));
-                    const float mn = fmaxf(m[n][y], w), f = mn == -INFINITY ? 1.0f : exp2_fast(m[n][y] - mn);
-                    m[n][y] = mn;
-                    less[n][y] = mn == -INFINITY ? 0.0f : mn;
-                    l[n][y] *= f;
-#pragma unroll
-                    for (int k = 0; k < KS; ++k) {
-                        o[k][n][y] *= f * fv;
-                        o[k][n][y + 2] *= f * fv;
-                    }
-                }
-        }
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int n = 0; n < NR; ++n)
-#pragma unroll
-                for (int z = 0; z < 4; ++z) {
-                    const float p = exp2_fast(s[b][n][z] - less[n][z & 1]);
-                    l[n][z & 1] += p;
-                    if constexpr (FMT != kFmt16) {
-                        // (a scale that is not finite stays away from a weight that the mask takes)
-                        const float w = p * (vinv * vs[b * 16 + g + (z >> 1) * 8]);
-                        s[b][n][z] = masked && s[b][n][z] == -INFINITY ? 0.0f : w;
-                    } else {
-                        s[b][n][z] = p;
-                    }
-                }
-
-        // ---- weighted sum ----
-        bool slow = false;
-        if constexpr (FMT == kFmt16) {
-            if (masked) {  // V that is not finite: as above
-                bool z = false;
-                for (int k = lane; k < kMine * S::kChunks; k += 32) {
-                    const uint4 w = lds16(sv + k * 16);
-                    z |= not_finite<BF16>(w.x) || not_finite<BF16>(w.y) || not_finite<BF16>(w.z) || not_finite<BF16>(w.w);
-                }
-                slow = __any_sync(0xffffffffu, z);
-            }
-        }
-        if (!slow) {
+                    for (int z = 0; z < 4; ++z) s[b][n][z] = 0.0f;
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
-                // the weights turned, from a lane's token to a lane's row
-                uint32_t p[NR][2];
-#pragma unroll
-                for (int n = 0; n < NR; ++n)
-#pragma unroll
-                    for (int y = 0; y < 2; ++y)
-                        asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(p[n][y]) : "r"(pack16<MB>(s[b][n][2 * y], s[b][n][2 * y + 1])));
-                const int mi = lane / 8;
                 if constexpr (FMT == kFmt16) {
 #pragma unroll
                     for (int k = 0; k < KS; ++k) {
                         uint32_t w[4];
-                        const int row = b * 16 + (mi >> 1) * 8 + lane % 8;
-                        ldsm4t(w, sv + row * S::kRow + swizzle<DP, FMT, true>(row, k * 2 + (mi & 1)) * 16);
+                        const int row = b * 16 + lane % 16;
+                        ldsm4(w, sk + row * S::kRow + swizzle<DP, FMT, false>(row, k * 2 + lane / 16) * 16);
 #pragma unroll
-                        for (int n = 0; n < NR; ++n) mma<MB>(o[k][n], w, p[n][0], p[n][1]);
+                        for (int n = 0; n < NR; ++n) mma<MB>(s[b][n], w, q[k][n][0], q[k][n][1]);
                     }
                 } else {
-                    // pairs of neighbouring elements move as one: rows g of the product are the even ones of 16, rows
-                    // g + 8 the odd ones
 #pragma unroll
-                    for (int k = 0; k < KS; k += 2) {
-                        uint32_t w[4];
-                        const int row = b * 16 + (mi & 1) * 8 + lane % 8;
-                        ldsm4t(w, sv + row * S::kRow + swizzle<DP, FMT, true>(row, k + (mi >> 1)) * 16);
+                    for (int hf = 0; hf < DP / 64; ++hf) {
+                        const int row = b * 16 + g;
+                        const uint4 w = lds16(sk + row * S::kRow + swizzle<DP, FMT, false>(row, hf * 4 + i4) * 16);
+                        const uint4 v = lds16(sk + (row + 8) * S::kRow + swizzle<DP, FMT, false>(row + 8, hf * 4 + i4) * 16);
+                        const uint32_t ww[4] = {w.x, w.y, w.z, w.w}, vv[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            if (FMT == kFmtE4M3 && masked) {  // codes of NaN stay away from weights that the mask takes
-                                w[2 * e] = without_nan(w[2 * e]);
-                                w[2 * e + 1] = without_nan(w[2 * e + 1]);
-                            }
+                        for (int k = 0; k < 4; ++k) {
                             uint32_t f[4];
-                            to_half<FMT, true>(w[2 * e], f[0], f[1]);
-                            to_half<FMT, true>(w[2 * e + 1], f[2], f[3]);
+                            to_half<FMT, false>(ww[k], f[0], f[2]);
+                            to_half<FMT, false>(vv[k], f[1], f[3]);
 #pragma unroll
-                            for (int n = 0; n < NR; ++n) mma<MB>(o[k + e][n], f, p[n][0], p[n][1]);
+                            for (int n = 0; n < NR; ++n) mma<MB>(s[b][n], f, q[hf * 4 + k][n][0], q[hf * 4 + k][n][1]);
                         }
                     }
                 }
             }
-        } else if constexpr (FMT == kFmt16) {
-            for (int t = 0; t < kMine; ++t) {
-                const int src = (t & 7) * 4 + i4;
+            // ---- softmax ----
+            const float *const ks = scales + x % S::kStages * 2 * kMine, *const vs = ks + kMine;
+            const bool masked = base + kMine - 1 > u.lo || (a.window > 0 && base <= u.hi - a.window && base + kMine > a.sinks);
 #pragma unroll
-                for (int n = 0; n < NR; ++n) {
-                    float w[2];
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int n = 0; n < NR; ++n)
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) {
+                        float f = qf[n][z & 1];
+                        if constexpr (FMT != kFmt16) f *= ks[b * 16 + g + (z >> 1) * 8];
+                        s[b][n][z] *= f;
+                    }
+            if (masked) {
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int n = 0; n < NR; ++n)
+#pragma unroll
+                        for (int z = 0; z < 4; ++z)
+                            if (!visible(pos[n][z & 1], base + b * 16 + g + (z >> 1) * 8, a.window, a.sinks)) s[b][n][z] = -INFINITY;
+            }
+            float mx[NR][2];
+            bool raise = false;
+#pragma unroll
+            for (int n = 0; n < NR; ++n)
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    mx[n][y] = fmaxf(s[0][n][y], s[0][n][y + 2]);
+#pragma unroll
+                    for (int b = 1; b < NB; ++b) mx[n][y] = fmaxf(mx[n][y], fmaxf(s[b][n][y], s[b][n][y + 2]));
+                    raise |= mx[n][y] > m[n][y] + kLag;
+                }
+            float vnew = vmax;
+            if constexpr (FMT != kFmt16) {
+                // the largest scale of V so far (positive numbers compare as integers; one that is not finite does not count)
+                const uint32_t bits = __float_as_uint(vs[lane % kMine]);
+                vnew = fmaxf(vmax, __uint_as_float(__reduce_max_sync(0xffffffffu, bits < 0x7f800000u ? bits : 0u)));
+                raise |= vnew > 2.0f * vmax;  // (weights up to twice as large do no harm)
+            }
+            if (__any_sync(0xffffffffu, raise)) {
+                const float fv = FMT != kFmt16 && vnew > vmax ? vmax / vnew : 1.0f;  // 0 at first
+                vmax = vnew;
+                if (FMT != kFmt16 && vmax > 0.0f) vinv = 1.0f / vmax;
+#pragma unroll
+                for (int n = 0; n < NR; ++n)
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
-                        const float e0 = __shfl_sync(0xffffffffu, s[0][n][y], src), e1 = __shfl_sync(0xffffffffu, s[0][n][y + 2], src);
-                        w[y] = unpack16<BF16>(pack16<BF16>(t & 8 ? e1 : e0, 0.0f)).x;
-                    }
-                    const bool v0 = visible(pos[n][0], base + t, a.window, a.sinks), v1 = visible(pos[n][1], base + t, a.window, a.sinks);
+                        float w = mx[n][y];
+                        w = fmaxf(w, __shfl_xor_sync(0xffffffffu, w, 4));
+                        w = fmaxf(w, __shfl_xor_sync(0xffffffffu, w, 8));
+                        w = fmaxf(w, __shfl_xor_sync(0xffffffffu, w, 16));
+                        const float mn = fmaxf(m[n][y], w), f = mn == -INFINITY ? 1.0f : exp2_fast(m[n][y] - mn);
+                        m[n][y] = mn;
+                        less[n][y] = mn == -INFINITY ? 0.0f : mn;
+                        l[n][y] *= f;
 #pragma unroll
-                    for (int k = 0; k < KS; ++k)
-#pragma unroll
-                        for (int y = 0; y < 2; ++y) {
-                            const float v = unpack16<BF16>(*reinterpret_cast<const uint16_t *>(
-                                st + S::kHalf + t * S::kRow + swizzle<DP, FMT, true>(t, k * 2 + y) * 16 + g * 2)).x;
-                            if (v0) o[k][n][2 * y] += w[0] * v;
-                            if (v1) o[k][n][2 * y + 1] += w[1] * v;
+                        for (int k = 0; k < KS; ++k) {
+                            o[k][n][y] *= f * fv;
+                            o[k][n][y + 2] *= f * fv;
                         }
+                    }
+            }
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int n = 0; n < NR; ++n)
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) {
+                        const float p = exp2_fast(s[b][n][z] - less[n][z & 1]);
+                        l[n][z & 1] += p;
+                        if constexpr (FMT != kFmt16) {
+                            // (a scale that is not finite stays away from a weight that the mask takes)
+                            const float w = p * (vinv * vs[b * 16 + g + (z >> 1) * 8]);
+                            s[b][n][z] = masked && s[b][n][z] == -INFINITY ? 0.0f : w;
+                        } else {
+                            s[b][n][z] = p;
+                        }
+                    }
+
+            // ---- weighted sum ----
+            bool slow = false;
+            if constexpr (FMT == kFmt16) {
+                // an infinity or a NaN in V that some row may not see: 0 times it is not 0, so such a tile is
+                // summed without the tensor cores, skipping what a row does not see
+                if (masked) {
+                    bool z = false;
+                    for (int k = lane; k < kMine * S::kChunks; k += 32) {
+                        const uint4 w = lds16(sv + k * 16);
+                        z |= not_finite<BF16>(w.x) || not_finite<BF16>(w.y) || not_finite<BF16>(w.z) || not_finite<BF16>(w.w);
+                    }
+                    slow = __any_sync(0xffffffffu, z);
                 }
             }
-        }
-        __syncwarp();
+            if (!slow) {
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    // the weights turned, from a lane's token to a lane's row
+                    uint32_t p[NR][2];
+#pragma unroll
+                    for (int n = 0; n < NR; ++n)
+#pragma unroll
+                        for (int y = 0; y < 2; ++y)
+                            asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(p[n][y]) : "r"(pack16<MB>(s[b][n][2 * y], s[b][n][2 * y + 1])));
+                    const int mi = lane / 8;
+                    if constexpr (FMT == kFmt16) {
+#pragma unroll
+                        for (int k = 0; k < KS; ++k) {
+                            uint32_t w[4];
+                            const int row = b * 16 + (mi >> 1) * 8 + lane % 8;
+                            ldsm4t(w, sv + row * S::kRow + swizzle<DP, FMT, true>(row, k * 2 + (mi & 1)) * 16);
+#pragma unroll
+                            for (int n = 0; n < NR; ++n) mma<MB>(o[k][n], w, p[n][0], p[n][1]);
+                        }
+                    } else {
+                        // pairs of neighbouring elements move as one: rows g of the product are the even ones of 16, rows
+                        // g + 8 the odd ones
+#pragma unroll
+                        for (int k = 0; k < KS; k += 2) {
+                            uint32_t w[4];
+                            const int row = b * 16 + (mi & 1) * 8 + lane % 8;
+                            ldsm4t(w, sv + row * S::kRow + swizzle<DP, FMT, true>(row, k + (mi >> 1)) * 16);
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                if (FMT == kFmtE4M3 && masked) {  // codes of NaN stay away from weights that the mask takes
+                                    w[2 * e] = without_nan(w[2 * e]);
+                                    w[2 * e + 1] = without_nan(w[2 * e + 1]);
+                                }
+                                uint32_t f[4];
+                                to_half<FMT, true>(w[2 * e], f[0], f[1]);
+                                to_half<FMT, true>(w[2 * e + 1], f[2], f[3]);
+#pragma unroll
+                                for (int n = 0; n < NR; ++n) mma<MB>(o[k + e][n], f, p[n][0], p[n][1]);
+                            }
+                        }
+                    }
+                }
+            } else if constexpr (FMT == kFmt16) {
+                for (int t = 0; t < kMine; ++t) {
+                    const int src = (t & 7) * 4 + i4;
+#pragma unroll
+                    for (int n = 0; n < NR; ++n) {
+                        float w[2];
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            const float e0 = __shfl_sync(0xffffffffu, s[0][n][y], src), e1 = __shfl_sync(0xffffffffu, s[0][n][y + 2], src);
+                            w[y] = unpack16<BF16>(pack16<BF16>(t & 8 ? e1 : e0, 0.0f)).x;
+                        }
+                        const bool v0 = visible(pos[n][0], base + t, a.window, a.sinks), v1 = visible(pos[n][1], base + t, a.window, a.sinks);
+#pragma unroll
+                        for (int k = 0; k < KS; ++k)
+#pragma unroll
+                            for (int y = 0; y < 2; ++y) {
+                                const float v = unpack16<BF16>(*reinterpret_cast<const uint16_t *>(
+                                    st + S::kHalf + t * S::kRow + swizzle<DP, FMT, true>(t, k * 2 + y) * 16 + g * 2)).x;
+                                if (v0) o[k][n][2 * y] += w[0] * v;
+                                if (v1) o[k][n][2 * y + 1] += w[1] * v;
+                            }
+                    }
+                }
+            }
+            __syncwarp();
         }
 
         // ---- the unit ends here, for this CTA: the warps' sums to their stages just used, [row][element] ----
