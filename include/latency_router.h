@@ -482,8 +482,11 @@ LR_API int lr_cache_read(lr_cache *c, const lr_cache_batch *b, int32_t T, int32_
  * the first `sinks` of the sequence (j < sinks).  For each query head,
  *   out = sum_j softmax_j(scale * q . k_j) v_j   and   lse = ln sum_j exp(scale * q . k_j)
  * over the visible j; a row that sees nothing (a negative position) gives 0 and -inf.  Products of
- * 16-bit numbers are summed in fp32; the softmax weights are rounded to the cache's dtype for the
- * second product (e4m3 and int8 codes are exact in it, the scales are applied in fp32).
+ * 16-bit numbers are summed in fp32; the softmax weights are rounded to 16 bits for the second
+ * product, to the cache's dtype or, over 8-bit codes, to fp16 (the codes are exact in either; their
+ * scales are applied in fp32).  Codes of e4m3's NaN, which lr_cache_write never stores, have no defined value.
+ * The same call gives the same bits: parts of a row that several CTAs sum are joined in a fixed order.
+ * Two calls on one cache share its workspace: order them (one stream, or events).
  * q, out: element d of (row, head) at row * token_stride + head * head_stride + d, aligned as for
  * lr_cache_write.  lse_out: [T][num_q_heads] fp32 or NULL.  scale: finite, > 0.  window in
  * [0, 2^30] (0: no window), sinks in [0, 2^30].  Rows of no sequence are not written.

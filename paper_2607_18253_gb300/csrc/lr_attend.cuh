@@ -239,48 +239,22 @@ __device__ __forceinline__ bool visible(int pos, int j, int window, int sinks) {
     return j <= pos && (window == 0 || j > pos - window || j < sinks);
 }
 
-// Two 8-bit codes to two 16-bit numbers, exactly.  e4m3: sign, four exponent and three mantissa bits
-// moved to their places, then a product with the power of two between the biases (subnormal codes
-// become subnormal 16-bit numbers first, which the product turns right as well).
-// int8 to bf16: 128 + the low seven bits, less 128 or, for a negative code, 256.  To fp16: 1024 +
-// (code + 128), less 1152.
-// `t` holds the codes in the high bytes of its halves.
-template <bool BF16>
-__device__ __forceinline__ uint32_t from_e4m3(uint32_t t) {
-    if constexpr (BF16) {
-        const uint32_t r = (t & 0x80008000u) | ((t >> 4) & 0x07f007f0u);
-        const uint32_t k = 0x7b807b80u;  // 2^120
-        uint32_t d;
-        asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(r), "r"(k));
-        return d;
-    } else {
-        const uint32_t r = (t & 0x80008000u) | ((t >> 1) & 0x3f803f80u);
-        const uint32_t k = 0x5c005c00u;  // 2^8
-        uint32_t d;
-        asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(r), "r"(k));
-        return d;
-    }
-}
-// `t` holds the codes in the low bytes of its halves.
-template <bool BF16>
-__device__ __forceinline__ uint32_t from_int8(uint32_t t) {
+// Bytes i and j of w, 8-bit codes, as two bf16 numbers (i in the low half), exactly.  e4m3: sign, four exponent
+// and three mantissa bits moved to their places, then a product with 2^120, the power of two between the
+// biases (subnormal codes are subnormal bf16 numbers first, which the product turns right as well).
+// int8: 128 + the low seven bits, less 128 or, for a negative code, 256.
+template <int FMT>
+__device__ __forceinline__ uint32_t to_bf16(uint32_t w, int i, int j) {
     uint32_t d;
-    if constexpr (BF16) {
-        const uint32_t x = (t & 0x007f007fu) | 0x43004300u, y = (t & 0x00800080u) | 0x43004300u;
-        asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(x), "r"(y));
+    if constexpr (FMT == kFmtE4M3) {
+        const uint32_t t = __byte_perm(w, 0, 0x0404u | i << 4 | j << 12);
+        asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"((t & 0x80008000u) | ((t >> 4) & 0x07f007f0u)), "r"(0x7b807b80u));
     } else {
-        const uint32_t x = ((t & 0x00ff00ffu) ^ 0x00800080u) | 0x64006400u;
-        asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(x), "r"(0x64806480u));
+        const uint32_t t = __byte_perm(w, 0, 0x4040u | i | j << 8);
+        asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"((t & 0x007f007fu) | 0x43004300u), "r"((t & 0x00800080u) | 0x43004300u));
     }
     return d;
 }
-// Bytes i and j of w as two 16-bit numbers (i in the low half).
-template <bool BF16, int FMT>
-__device__ __forceinline__ uint32_t from_codes(uint32_t w, int i, int j) {
-    if constexpr (FMT == kFmtE4M3) return from_e4m3<BF16>(__byte_perm(w, 0, 0x0404u | i << 4 | j << 12));
-    else return from_int8<BF16>(__byte_perm(w, 0, 0x4040u | i | j << 8));
-}
-
 // Four 8-bit codes to fp16 numbers, exactly, as two pairs: codes (0, 1) and (2, 3), or with SPLIT (0, 2) and
 // (1, 3).  e4m3 by the conversion instruction.  int8: 1024 + (code + 128), less 1152.
 template <int FMT, bool SPLIT>

@@ -826,8 +826,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
 #pragma unroll
                             for (int z = 0; z < 4; ++z) {
                                 if constexpr (BF16) {
-                                    v[2 * z] = from_codes<true, FMT>(w[k][z], 0, 1);
-                                    v[2 * z + 1] = from_codes<true, FMT>(w[k][z], 2, 3);
+                                    v[2 * z] = to_bf16<FMT>(w[k][z], 0, 1);
+                                    v[2 * z + 1] = to_bf16<FMT>(w[k][z], 2, 3);
                                 } else {
                                     if (FMT == kFmtE4M3 && y) w[k][z] = without_nan(w[k][z]);  // (a hidden weight's zero times it is not zero)
                                     to_half<FMT, false>(w[k][z], v[2 * z], v[2 * z + 1]);

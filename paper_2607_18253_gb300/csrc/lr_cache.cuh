@@ -66,8 +66,8 @@ struct RwLaunch {
     int64_t in_t, in_h;  // bytes
     char *k_out, *v_out;
 };
-cudaError_t launch_cache_write(const RwLaunch &a, bool bf16, int fmt, int sms, cudaStream_t st);
-cudaError_t launch_cache_read(const RwLaunch &a, bool bf16, int fmt, bool f32, int sms, cudaStream_t st);
+cudaError_t launch_cache_write(const RwLaunch &a, bool bf16, int fmt, cudaStream_t st);
+cudaError_t launch_cache_read(const RwLaunch &a, bool bf16, int fmt, bool f32, cudaStream_t st);
 
 // Partial results of the attention kernels: a unit (sequence, KV head, tile of rows) whose cached
 // tokens are split over several CTAs is joined by the last of them to finish.  A CTA works

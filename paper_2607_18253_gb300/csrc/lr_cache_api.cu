@@ -67,7 +67,7 @@ bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0;
 bool good_stride(int64_t s, int size) { return s >= 0 && s < (1ll << 56) && s * size % 16 == 0; }
 
 // The checks that the calls share; 0 if the batch may be launched.
-const char *bad_batch(const lr_cache *c, const lr_cache_batch *b, int32_t T) {
+const char *bad_batch(const lr_cache_batch *b, int32_t T) {
     if (!b) return "null batch";
     if (T < 0) return "T < 0";
     if (b->num_seqs < 0) return "num_seqs < 0";
@@ -163,7 +163,7 @@ int lr_cache_write(lr_cache *c, const lr_cache_batch *b, int32_t T, const void *
                    int64_t head_stride, void *stream) {
     if (!c) return LR_EINVAL;
     c->err.clear();
-    if (const char *m = bad_batch(c, b, T)) return fail(c, LR_EINVAL, m);
+    if (const char *m = bad_batch(b, T)) return fail(c, LR_EINVAL, m);
     if (b->num_seqs > c->cfg.max_seqs) return fail(c, LR_ECAPACITY, "num_seqs exceeds max_seqs");
     if (T == 0 || b->num_seqs == 0) return LR_OK;
     if (!k || !v || !aligned16(k) || !aligned16(v)) return fail(c, LR_EINVAL, "k and v must be 16-byte aligned");
@@ -177,14 +177,14 @@ int lr_cache_write(lr_cache *c, const lr_cache_batch *b, int32_t T, const void *
     a.v_in = static_cast<const char *>(v);
     a.in_t = token_stride * 2;
     a.in_h = head_stride * 2;
-    cudaError_t e = lr::launch_cache_write(a, c->bf16, c->cfg.format, c->sms, (cudaStream_t)stream);
+    cudaError_t e = lr::launch_cache_write(a, c->bf16, c->cfg.format, (cudaStream_t)stream);
     return e == cudaSuccess ? LR_OK : cuda_fail(c, e, "cache write launch");
 }
 
 int lr_cache_read(lr_cache *c, const lr_cache_batch *b, int32_t T, int32_t out_dtype, void *k_out, void *v_out, void *stream) {
     if (!c) return LR_EINVAL;
     c->err.clear();
-    if (const char *m = bad_batch(c, b, T)) return fail(c, LR_EINVAL, m);
+    if (const char *m = bad_batch(b, T)) return fail(c, LR_EINVAL, m);
     if (b->num_seqs > c->cfg.max_seqs) return fail(c, LR_ECAPACITY, "num_seqs exceeds max_seqs");
     if (out_dtype != c->cfg.dtype && out_dtype != LR_FP32) return fail(c, LR_EINVAL, "out_dtype must be the cache's dtype or LR_FP32");
     if (T == 0 || b->num_seqs == 0) return LR_OK;
@@ -195,7 +195,7 @@ int lr_cache_read(lr_cache *c, const lr_cache_batch *b, int32_t T, int32_t out_d
     a.b = batch_dev(b, T);
     a.k_out = static_cast<char *>(k_out);
     a.v_out = static_cast<char *>(v_out);
-    cudaError_t e = lr::launch_cache_read(a, c->bf16, c->cfg.format, out_dtype == LR_FP32, c->sms, (cudaStream_t)stream);
+    cudaError_t e = lr::launch_cache_read(a, c->bf16, c->cfg.format, out_dtype == LR_FP32, (cudaStream_t)stream);
     return e == cudaSuccess ? LR_OK : cuda_fail(c, e, "cache read launch");
 }
 
@@ -204,7 +204,7 @@ int lr_cache_attend(lr_cache *c, const lr_cache_batch *b, int32_t T, const void 
                     int64_t out_head_stride, float *lse_out, void *stream) {
     if (!c) return LR_EINVAL;
     c->err.clear();
-    if (const char *m = bad_batch(c, b, T)) return fail(c, LR_EINVAL, m);
+    if (const char *m = bad_batch(b, T)) return fail(c, LR_EINVAL, m);
     if (b->num_seqs > c->cfg.max_seqs) return fail(c, LR_ECAPACITY, "num_seqs exceeds max_seqs");
     if (!(std::isfinite(scale) && scale > 0.0f)) return fail(c, LR_EINVAL, "scale must be finite and positive");
     if (window < 0 || window > lr::kMaxTokens || sinks < 0 || sinks > lr::kMaxTokens)

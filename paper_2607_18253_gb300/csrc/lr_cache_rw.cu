@@ -293,7 +293,7 @@ int grid_of(const RwLaunch &a, int items) {
 
 }  // namespace
 
-cudaError_t launch_cache_write(const RwLaunch &a, bool bf16, int fmt, int, cudaStream_t st) {
+cudaError_t launch_cache_write(const RwLaunch &a, bool bf16, int fmt, cudaStream_t st) {
     auto go = [&](void (*k)(const RwLaunch)) { return launch_chained(k, grid_of(a, fmt == kFmt16 ? kStoreItems<kFmt16> : kStoreItems<kFmtInt8>), kThreads, 0, st, a); };
     switch (fmt) {
         case kFmtE4M3: return go(bf16 ? k_cache_write<true, kFmtE4M3> : k_cache_write<false, kFmtE4M3>);
@@ -302,7 +302,7 @@ cudaError_t launch_cache_write(const RwLaunch &a, bool bf16, int fmt, int, cudaS
     }
 }
 
-cudaError_t launch_cache_read(const RwLaunch &a, bool bf16, int fmt, bool f32, int, cudaStream_t st) {
+cudaError_t launch_cache_read(const RwLaunch &a, bool bf16, int fmt, bool f32, cudaStream_t st) {
     auto go = [&](void (*k)(const RwLaunch)) { return launch_chained(k, grid_of(a, kLoadItems), kThreads, 0, st, a); };
     switch (fmt) {
         case kFmtE4M3:

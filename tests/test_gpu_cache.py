@@ -293,6 +293,24 @@ def test_tokens_split_over_the_gpu(fmt, seqs):
     assert torch.equal(a, b) and torch.equal(la, lb)  # joined in one order
 
 
+@pytest.mark.parametrize("fmt", ["16", "int8"])
+def test_more_sequences_than_threads(fmt):
+    # 1,500 sequences, some without new tokens, one chunk among them: every round of the walks over a batch
+    seqs = [(1 if i % 7 else 0, 1 + i % 90) for i in range(1499)]
+    seqs.insert(700, (70, 200))
+    c = Case(seqs, H=1, G=2, D=64, fmt=fmt, seed=27)
+    c.check()
+    x = torch.randn((c.T, 1, 64), device="cuda").to(torch.bfloat16)
+    c.cache.write(x, x, c.batch)
+    k, v = c.cache.read(c.batch, c.T)
+    assert c.cache.status() == R().LR_OK and torch.equal(k, v)
+    want = x
+    if fmt != "16":
+        codes, sc = quantised(x.float(), fmt)
+        want = (codes.float() * sc[..., None]).to(torch.bfloat16)
+    assert torch.equal(k, want)
+
+
 def test_strided_queries_and_outputs():
     c = Case(SEQS["mixed"], H=2, G=4, D=64, seed=18)
     T = c.T
