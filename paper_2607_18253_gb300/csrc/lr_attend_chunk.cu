@@ -466,6 +466,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
                 const int base = (tile < ns ? tile : tile + skip) * kTok;
                 const int slot = x & 3;
                 const bool masked = base + kTok - 1 > lo || (a.window > 0 && base <= hi - a.window && base + kTok > a.sinks);
+                [[maybe_unused]] bool wipe = false, gone = false, clear = false;
                 if constexpr (FMT == kFmt16) {
                     // (hidden from a row of either half: they share V)
                     if (base + kTok - 1 > ulo || (a.window > 0 && base <= uhi - a.window && base + kTok > a.sinks)) {
@@ -473,26 +474,32 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
                         bool bad = false;
                         const char *const p = v_row<BF16>(a, u, base + (tid & 127));
                         for (int d = 0; p && d < c.D; d += 8) bad |= lost_in<BF16>(__ldg(reinterpret_cast<const uint4 *>(p + d * 2)));
-                        const bool gone = LOAD == kTma && !p;  // no token of the unit: whatever was copied, or nothing
+                        gone = LOAD == kTma && !p;  // no token of the unit: whatever was copied, or nothing
                         int *const found = s_lost + half * 2 + (n_scan & 1);
                         if (bad) *found = x;
                         bar_arrive_warp(scanned + 8 * half);
                         ok = bar_wait(scanned + 8 * half, n_scan & 1, dead);
+                        if (!ok) break;
                         ++n_scan;
                         lost |= *reinterpret_cast<volatile int *>(found) == x;
-                        if (__any_sync(0xffffffffu, bad || gone)) {
-                            const uint32_t v = 2 * x + 1;
-                            ok = ok && bar_wait(kv_full + 8 * (v % kStages), v / kStages & 1, dead);
-                            if (ok && (bad || gone)) clear_row<BF16, DP>(smem_addr(tiles + v % kStages * S::kTile), tid & 127, gone);
-                            shared_to_async();
-                            __syncwarp();
-                        }
-                        if (!ok) break;
+                        wipe = bad || gone;
+                        clear = __any_sync(0xffffffffu, wipe);
                     }
                 }
-                // (the scores first: a half that skips units may be ahead of the scales' barrier by a phase)
+                // (the scores before the scales and before V: a half that skips units may be ahead of those barriers by
+                // phases, which their parity does not tell apart; this tile's scores mean that K has landed, and all before it)
                 ok = bar_wait(s_full + 8 * half, n_s & 1, dead) && (FMT == kFmt16 || bar_wait(sc_full + 8 * slot, x >> 2 & 1, dead));
                 if (!ok) break;
+                if constexpr (FMT == kFmt16) {
+                    if (clear) {
+                        const uint32_t v = 2 * x + 1;
+                        ok = bar_wait(kv_full + 8 * (v % kStages), v / kStages & 1, dead);
+                        if (!ok) break;
+                        if (wipe) clear_row<BF16, DP>(smem_addr(tiles + v % kStages * S::kTile), tid & 127, gone);
+                        shared_to_async();
+                        __syncwarp();
+                    }
+                }
                 ++n_s;
                 const float *const ks = scales + slot * 2 * kTok, *const vs = ks + kTok;
                 after_sync();

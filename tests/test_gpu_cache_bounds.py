@@ -1,0 +1,53 @@
+"""Attention over the paged cache at the edges of its range, with the bound of test_gpu_cache.py and no slack in it.
+
+The terms of that bound that do not shrink with the values, derived for each product:
+  16-bit caches   weights are rounded to the cache's type: fp16 ones below its normal range are off by 2^-25 each,
+                  n 2^-25 V in all (n tokens, V = max |v|); an fp16 output is off by 2^-25 more
+  8-bit caches    the weights' products are fp16 ones (single tokens, and chunks of an fp16 cache) or bf16 ones; what
+                  an fp16 weight multiplies is at most V, or 2^-15 where V is below it (codes of up to 448 times
+                  2^-24, the smallest power of two of fp16); such a product's own rounding is 2^-25 at most, once,
+                  since the weights' sum is one
+"""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import test_gpu_cache as base  # noqa: E402
+from test_gpu_cache import C, DT, R, _built  # noqa: E402,F401
+
+pytestmark = pytest.mark.gpu
+
+
+class Case(base.Case):
+    def reference(self, scale=None, window=0, sinks=0):
+        out, lse, tol, ltol = super().reference(scale, window, sinks)
+        t0 = 0
+        for s, (ql, kv) in enumerate(self.seqs):
+            rows = slice(t0, t0 + ql)
+            t0 += ql
+            if kv == 0 or ql == 0:
+                continue
+            for h in range(self.H):
+                top = float(torch.nan_to_num(self.values("v", s, h, kv), 0.0, 0.0, 0.0).abs().max())
+                slack = (kv + 1) * 2.0 ** -25 * (top + 1.0) if self.dt == "fp16" else 0.0
+                mine = 0.0
+                if self.fmt != "16":
+                    mine = kv * 2.0 ** -25 * max(top, 2.0 ** -15) + (2.0 ** -24 if self.dt == "fp16" else 0.0)
+                elif self.dt == "fp16":
+                    mine = kv * 2.0 ** -25 * top + 2.0 ** -25
+                tol[rows, h * self.G:(h + 1) * self.G] += mine - slack
+        return out, lse, tol.clamp_(min=1e-30), ltol
+
+
+@pytest.mark.parametrize("D,b", [(128, 16), (64, 32), (128, 5)])
+@pytest.mark.parametrize("seqs,window,sinks", [([(1500, 1500), (2000, 2000)], 0, 0), ([(1000, 6000), (1048, 9000)], 1024, 4),
+                                               ([(333, 333), (1111, 1111), (801, 2001)], 0, 0)])
+def test_chunks_of_several_sequences(D, b, seqs, window, sinks):
+    # CTAs that go from many tiles of a unit of at most 128 rows to a wider unit whose first tile has places of no token
+    c = Case(seqs, H=8, G=4, D=D, b=b, seed=31, garbage=math.nan)
+    a, la = c.check(window=window, sinks=sinks)
+    for _ in range(3):
+        x, lx = c.check(window=window, sinks=sinks)
+        assert torch.equal(a, x) and torch.equal(la, lx)
