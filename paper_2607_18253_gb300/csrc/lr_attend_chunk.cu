@@ -253,6 +253,45 @@ __device__ __noinline__ void add_lost(const AttendLaunch &a, const Unit &u, int 
     }
 }
 
+// V's scales over 8-bit codes in fp16: code * (2^e * rest) with 1 <= |rest| < 2.  The power of two goes to the codes as
+// they are converted (a power of two times a code is a number of fp16, or below 2^-14 off by 2^-25 at most), the
+// rest to the weights, which so are as far from the ends of fp16's range as those of a 16-bit cache, however large or
+// small V is.  e stays in [-24, 5], where the codes' products are finite; what a scale has beyond is in the
+// rest: weights of up to 2^4 stay numbers with scales of up to 2^16.
+constexpr int kLeast = -24, kMost = 5;
+__device__ __forceinline__ int power(float scale) { return min(max((int)(__float_as_uint(scale) >> 23 & 0xff) - 127, kLeast), kMost); }
+__device__ __forceinline__ float rest_of(float scale) { return scale * __uint_as_float((uint32_t)(127 - power(scale)) << 23); }
+// 2^e as fp16's bits; of e4m3 2^8 as much, for the codes that to_half_times makes.
+template <int FMT>
+__device__ __forceinline__ uint32_t power_of(float scale) {
+    return __half_as_ushort(__float2half_rn(__uint_as_float((uint32_t)(127 + power(scale) + (FMT == kFmtE4M3 ? 8 : 0)) << 23)));
+}
+template <int FMT>
+__device__ __forceinline__ uint32_t half_times(uint32_t two) {
+    uint32_t r = 0;
+    if constexpr (FMT == kFmtInt8) asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(two), "r"(0xe480e480u));  // -1152 * 2^e
+    return r;
+}
+// Four codes (0, 1), (2, 3) times 2^e, `two`.  int8: (1024 + (code + 128)) * 2^e - 1152 * 2^e in one rounding.  e4m3:
+// the code's bits moved to fp16's places are 2^-8 times its value (and its NaN a number, which hidden weights need).
+template <int FMT>
+__device__ __forceinline__ void to_half_times(uint32_t w, uint32_t two, uint32_t shift, uint32_t &a, uint32_t &b) {
+    if constexpr (FMT == kFmtE4M3) {
+        a = __byte_perm(w, 0, 0x1404);
+        b = __byte_perm(w, 0, 0x3424);
+        a = (a & 0x80008000u) | ((a >> 1) & 0x3f803f80u);
+        b = (b & 0x80008000u) | ((b >> 1) & 0x3f803f80u);
+        asm("mul.rn.f16x2 %0, %0, %1;" : "+r"(a) : "r"(two));
+        asm("mul.rn.f16x2 %0, %0, %1;" : "+r"(b) : "r"(two));
+    } else {
+        w ^= 0x80808080u;
+        a = __byte_perm(w, 0x64646464u, 0x4140);
+        b = __byte_perm(w, 0x64646464u, 0x4342);
+        asm("fma.rn.f16x2 %0, %0, %1, %2;" : "+r"(a) : "r"(two), "r"(shift));
+        asm("fma.rn.f16x2 %0, %0, %1, %2;" : "+r"(b) : "r"(two), "r"(shift));
+    }
+}
+
 struct ChunkLaunch {
     AttendLaunch a;
     CacheMaps m;
@@ -303,7 +342,7 @@ __device__ __noinline__ bool sees_lost(const AttendLaunch &a, const Unit &u, int
 // Joins the parts of 32 rows of a unit, in the order of the CTAs: a lane first a row's maximum and sum, then four
 // elements each of 16 rows at a time (of 2 x 8 with 64 elements), their loads in flight together.
 template <bool BF16, int DP>
-__device__ __noinline__ void join_rows(const AttendLaunch &a, const Unit &u, int c0, int parts, int slot0, int row0, float lift) {
+__device__ __noinline__ void join_rows(const AttendLaunch &a, const Unit &u, int c0, int parts, int slot0, int row0) {
     constexpr int kLanes = DP / 4, kTwo = 32 / kLanes, kStep = 16;
     const CacheDev &c = a.c;
     const int lane = threadIdx.x % 32, sub = lane / kLanes, e = lane % kLanes * 4;
@@ -343,7 +382,7 @@ __device__ __noinline__ void join_rows(const AttendLaunch &a, const Unit &u, int
             const int r = r0 + z * kTwo + sub;
             const float l = __shfl_sync(0xffffffffu, ll, r - row0);
             const int gr = u.qt * 256 + r, t = quot(gr, c.div_g), hd = u.h * c.G + gr - t * c.G;
-            const float iv = l == 0.0f ? 0.0f : 1.0f / (l * lift);
+            const float iv = l == 0.0f ? 0.0f : 1.0f / l;
             if (r < u.rows && e < c.D)
                 *reinterpret_cast<uint2 *>(a.out + (int64_t)(u.q0 + t) * a.o_t + (int64_t)hd * a.o_h + e * 2) =
                     make_uint2(pack16<BF16>(acc[z].x * iv, acc[z].y * iv), pack16<BF16>(acc[z].z * iv, acc[z].w * iv));
@@ -362,9 +401,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
     constexpr int kKvArrive = LOAD == kTma ? 1 : 4;  // arrivals that hand over a tile: one a warp
     constexpr int kStages = S::kStages;
     constexpr float kLag = BF16 || FMT == kFmt16 ? 8.0f : 4.0f;
-    // fp16 weights that carry 8-bit scales: lifted from fp16's subnormal numbers (scales are at most
-    // 65504/127 = 516 and weights 2^kLag = 16, so 4 times them stays below 65504)
-    constexpr float kLift = FMT != kFmt16 && !BF16 ? 4.0f : 1.0f;
+    constexpr bool kSplit = FMT != kFmt16 && !BF16;  // V's scales are split (below)
     // (no static shared memory, so that the tiles start where the swizzle's 1,024-byte pattern does)
     extern __shared__ __align__(1024) char smem[];
     char *const tiles = smem + S::kQ;
@@ -618,7 +655,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
             const int64_t slot = job.slot;
             char *const po = a.out + (int64_t)(u.q0 + t) * a.o_t + (int64_t)hd * a.o_h;
             float *const pw = a.part_o + (slot * 256 + r) * 128;
-            const float inv = l == 0.0f ? 0.0f : 1.0f / (l * kLift);
+            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
             bool gone = false;
 #pragma unroll 1
             for (int k = 0; k < DP; k += 32) {  // (short code: it is fetched anew for each unit)
@@ -675,7 +712,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
                 before = __shfl_sync(0xffffffffu, before, 0);
                 if (before == (uint32_t)(c1 - c0)) {
                     __threadfence();
-                    join_rows<BF16, DP>(a, u, c0, c1 - c0 + 1, job.slot0, warp * 32, kLift);
+                    join_rows<BF16, DP>(a, u, c0, c1 - c0 + 1, job.slot0, warp * 32);
                 }
             }
             bar_arrive_warp(job_free + 8 * (frag % kJobs));
@@ -736,13 +773,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
         const int ch = i % CH, r0 = i / CH;
         const bool in = ch * (FMT == kFmt16 ? 8 : 16) < c.D;
         auto put = [&](int x, const Found &f) {
-            places[(x & 1) * kTok + i] = f.off;
+            if constexpr (kSplit) places[(x & 1) * kTok + i] = (int64_t)((uint64_t)power_of<FMT>(f.vs) << 48 | ((uint64_t)f.off << 16 >> 16));
+            else places[(x & 1) * kTok + i] = f.off;
             int flags = __any_sync(0xffffffffu, f.bad) ? 1 : 0;
             if constexpr (FMT != kFmt16) {
                 // scales that are not finite are kept from rows that do not see them: 2 and 4 say that there are such
                 const bool kb = !(fabsf(f.ks) < INFINITY), vb = !(fabsf(f.vs) < INFINITY);
                 scales[(x & 3) * 2 * kTok + i] = kb ? 1.0f : f.ks;
-                scales[(x & 3) * 2 * kTok + kTok + i] = vb ? 0.0f : f.vs * kLift;
+                scales[(x & 3) * 2 * kTok + kTok + i] = vb ? 0.0f : kSplit ? rest_of(f.vs) : f.vs;
                 const unsigned kw = __ballot_sync(0xffffffffu, kb);
                 flags |= (kw ? 2 : 0) | (__any_sync(0xffffffffu, vb) ? 4 : 0);
                 if (lane == 0) s_kbad[(x & 3) * 4 + warp - 12] = kw;
@@ -766,7 +804,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
         auto request = [&](bool any) {
             const uint32_t it = ahead / kIts, k = ahead % kIts;
             if (any) {
-                const int64_t off = places[(it >> 1 & 1) * kTok + r0 + k * kStep];
+                int64_t off = places[(it >> 1 & 1) * kTok + r0 + k * kStep];
+                if constexpr (kSplit) off = (int64_t)((uint64_t)off << 16) >> 16;
                 const bool have = in && off >= 0;
                 copy16(smem_addr(raw + (ahead % S::kSlots * 128 + i) * 16), (it & 1 ? c.v : c.k) + (have ? off + ch * 16 : 0), have);
             }
@@ -830,15 +869,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
                         for (int k = 0; k < 4; ++k) {
                             const int r = r0 + (k0 + k) * kStep;
                             uint32_t v[8];
+                            if constexpr (BF16) {
 #pragma unroll
-                            for (int z = 0; z < 4; ++z) {
-                                if constexpr (BF16) {
+                                for (int z = 0; z < 4; ++z) {
                                     v[2 * z] = to_bf16<FMT>(w[k][z], 0, 1);
                                     v[2 * z + 1] = to_bf16<FMT>(w[k][z], 2, 3);
-                                } else {
-                                    if (FMT == kFmtE4M3 && y) w[k][z] = without_nan(w[k][z]);  // (a hidden weight's zero times it is not zero)
-                                    to_half<FMT, false>(w[k][z], v[2 * z], v[2 * z + 1]);
                                 }
+                            } else if (y) {
+                                const uint32_t two = __byte_perm(reinterpret_cast<const uint32_t *>(places + (x & 1) * kTok + r)[1], 0, 0x3232);
+                                const uint32_t shift = half_times<FMT>(two);
+#pragma unroll
+                                for (int z = 0; z < 4; ++z) to_half_times<FMT>(w[k][z], two, shift, v[2 * z], v[2 * z + 1]);
+                            } else {
+#pragma unroll
+                                for (int z = 0; z < 4; ++z) to_half<FMT, false>(w[k][z], v[2 * z], v[2 * z + 1]);
                             }
                             asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to + swizzled<DP>(r, 2 * ch)), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
                             asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to + swizzled<DP>(r, 2 * ch + 1)), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");

@@ -51,3 +51,38 @@ def test_chunks_of_several_sequences(D, b, seqs, window, sinks):
     for _ in range(3):
         x, lx = c.check(window=window, sinks=sinks)
         assert torch.equal(a, x) and torch.equal(la, lx)
+
+
+STEPS = [(1, 3000), (2, 777), (1, 100)]   # at most 8 rows a sequence: the kernel of single tokens
+CHUNKS = [(90, 2500), (300, 700)]         # more: the kernel of chunks
+
+
+@pytest.mark.parametrize("seqs", [STEPS, CHUNKS], ids=["steps", "chunks"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("fmt", ["16", "e4m3", "int8"])
+@pytest.mark.parametrize("size", [1e-4, 1e-3, 1e-2, 30.0])
+def test_values_of_any_size(seqs, dtype, fmt, size):
+    c = Case(seqs, D=64, dtype=dtype, fmt=fmt, seed=32)
+    if fmt == "16":
+        c.v.mul_(size)
+    else:
+        c.v_scale.mul_(size)
+    c.check()
+
+
+@pytest.mark.parametrize("seqs", [STEPS, CHUNKS], ids=["steps", "chunks"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("scale", [2000.0, 20000.0])
+def test_large_scales_of_small_codes(seqs, dtype, fmt, scale):
+    # a caller's cache: code * scale is a number of either type, whatever the scale alone
+    c = Case(seqs, D=64, dtype=dtype, fmt=fmt, seed=35)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(36)
+    codes = torch.randint(-2, 3, c.v.shape, device="cuda", generator=g)
+    if fmt == "e4m3":
+        c.v.view(torch.int8).copy_((codes.float() * 0.75).to(torch.float8_e4m3fn).view(torch.int8))
+    else:
+        c.v.copy_(codes.to(torch.int8))
+    c.v_scale.fill_(scale)
+    c.check()
