@@ -150,7 +150,8 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
     // 8-bit codes are multiplied in fp16, which holds them exactly and converts them in the fewest
     // instructions.  The queries come to fp16 as they are, or from bf16 divided by a power of two
     // a row that brings the largest to [1, 2): what fp16 then rounds is below 2^-24 of it.  The weights
-    // carry V's scales divided by the largest so far.
+    // carry V's scales, and are divided by a power of two a row that brings the largest such product of the tokens
+    // that the row sees to [1, 16]: a large scale where the weight is small, or hidden, leaves the others what they are.
     constexpr bool MB = FMT == kFmt16 ? BF16 : false;  // type of the products
     // The maximum that the weights refer to is left behind until a score exceeds it by this (log2): any
     // reference gives the same quotient, and a tile that raises none needs no exchange between lanes.
@@ -256,7 +257,8 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
 
     // a lane's columns are the rows n * 8 + 2 * i4, + 1 of the unit
     uint32_t q[KS][NR][2];
-    float o[KS][NR][4], m[NR][2], l[NR][2], qf[NR][2], less[NR][2], vmax = 0.0f, vinv = 0.0f;  // less: m, 0 where it is -inf
+    float o[KS][NR][4], m[NR][2], l[NR][2], qf[NR][2], less[NR][2];  // less: m, 0 where it is -inf
+    [[maybe_unused]] float down[NR][2];  // 8 bits: the power of two that the row's weights are multiplied by
     int pos[NR][2];
     for (int x = 0;;) {
         const Unit &u = cu.u;
@@ -313,9 +315,9 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
                     m[n][y] = -INFINITY;
                     less[n][y] = 0.0f;
                     l[n][y] = 0.0f;
+                    down[n][y] = 1.0f;
                 }
             }
-            vmax = vinv = 0.0f;
             bad = false;
         }
         for (; cu.j < cu.end; ++x, ++cu.j) {
@@ -407,17 +409,13 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
                     for (int b = 1; b < NB; ++b) mx[n][y] = fmaxf(mx[n][y], fmaxf(s[b][n][y], s[b][n][y + 2]));
                     raise |= mx[n][y] > m[n][y] + kLag;
                 }
-            float vnew = vmax;
+            const bool raised = __any_sync(0xffffffffu, raise);
+            [[maybe_unused]] float fo[NR][2];
             if constexpr (FMT != kFmt16) {
-                // the largest scale of V so far (positive numbers compare as integers; one that is not finite does not count)
-                const uint32_t bits = __float_as_uint(vs[lane % kMine]);
-                vnew = fmaxf(vmax, __uint_as_float(__reduce_max_sync(0xffffffffu, bits < 0x7f800000u ? bits : 0u)));
-                raise |= vnew > 2.0f * vmax;  // (weights up to twice as large do no harm)
+#pragma unroll
+                for (int n = 0; n < NR; ++n) fo[n][0] = fo[n][1] = 1.0f;
             }
-            if (__any_sync(0xffffffffu, raise)) {
-                const float fv = FMT != kFmt16 && vnew > vmax ? vmax / vnew : 1.0f;  // 0 at first
-                vmax = vnew;
-                if (FMT != kFmt16 && vmax > 0.0f) vinv = 1.0f / vmax;
+            if (raised) {
 #pragma unroll
                 for (int n = 0; n < NR; ++n)
 #pragma unroll
@@ -430,12 +428,21 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
                         m[n][y] = mn;
                         less[n][y] = mn == -INFINITY ? 0.0f : mn;
                         l[n][y] *= f;
+                        if constexpr (FMT == kFmt16) {
 #pragma unroll
-                        for (int k = 0; k < KS; ++k) {
-                            o[k][n][y] *= f * fv;
-                            o[k][n][y + 2] *= f * fv;
+                            for (int k = 0; k < KS; ++k) {
+                                o[k][n][y] *= f;
+                                o[k][n][y + 2] *= f;
+                            }
+                        } else {
+                            fo[n][y] = f;
                         }
                     }
+            }
+            [[maybe_unused]] float wx[NR][2];
+            if constexpr (FMT != kFmt16) {
+#pragma unroll
+                for (int n = 0; n < NR; ++n) wx[n][0] = wx[n][1] = 0.0f;
             }
 #pragma unroll
             for (int b = 0; b < NB; ++b)
@@ -447,12 +454,48 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
                         l[n][z & 1] += p;
                         if constexpr (FMT != kFmt16) {
                             // (a scale that is not finite stays away from a weight that the mask takes)
-                            const float w = p * (vinv * vs[b * 16 + g + (z >> 1) * 8]);
+                            const float w = p * vs[b * 16 + g + (z >> 1) * 8];
                             s[b][n][z] = masked && s[b][n][z] == -INFINITY ? 0.0f : w;
+                            wx[n][z & 1] = fmaxf(wx[n][z & 1], fabsf(s[b][n][z]));
                         } else {
                             s[b][n][z] = p;
                         }
                     }
+            if constexpr (FMT != kFmt16) {
+                bool grow = raised;
+#pragma unroll
+                for (int n = 0; n < NR; ++n)
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) grow |= wx[n][y] * down[n][y] > 16.0f;
+                if (__any_sync(0xffffffffu, grow)) {
+                    constexpr uint32_t kOne = 127u << 23, kFar = 120u << 23;
+#pragma unroll
+                    for (int n = 0; n < NR; ++n)
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            float w = wx[n][y];
+                            w = fmaxf(w, __shfl_xor_sync(0xffffffffu, w, 4));
+                            w = fmaxf(w, __shfl_xor_sync(0xffffffffu, w, 8));
+                            w = fmaxf(w, __shfl_xor_sync(0xffffffffu, w, 16));
+                            // the largest product so far against the maximum as it is now, and its power of two
+                            const float was = fo[n][y] * __uint_as_float(2 * kOne - __float_as_uint(down[n][y]));
+                            const uint32_t e = __float_as_uint(fmaxf(was, w)) & 0x7f800000u;
+                            down[n][y] = __uint_as_float(2 * kOne - min(max(e, kOne - kFar), kOne + kFar));
+                            const float f = was * down[n][y];  // at most 2: no part of it overflows
+#pragma unroll
+                            for (int k = 0; k < KS; ++k) {
+                                o[k][n][y] *= f;
+                                o[k][n][y + 2] *= f;
+                            }
+                        }
+                }
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int n = 0; n < NR; ++n)
+#pragma unroll
+                        for (int z = 0; z < 4; ++z) s[b][n][z] *= down[n][z & 1];
+            }
 
             // ---- weighted sum ----
             bool slow = false;
@@ -552,7 +595,7 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
                 const int r = n * 8 + 2 * i4 + y;
                 if (r >= u.rows) continue;
                 if (g == 0) s_ml[warp * kRows + r] = make_float2(m[n][y], w);
-                const float f = FMT == kFmt16 ? 1.0f : vmax;
+                const float f = FMT == kFmt16 ? 1.0f : __uint_as_float((254u << 23) - __float_as_uint(down[n][y]));
 #pragma unroll
                 for (int k = 0; k < KS; ++k) {
                     if constexpr (FMT == kFmt16) {

@@ -73,6 +73,22 @@ def test_values_of_any_size(seqs, dtype, fmt, size):
 @pytest.mark.parametrize("seqs", [STEPS, CHUNKS], ids=["steps", "chunks"])
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 @pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_values_of_mixed_sizes_and_signs(seqs, dtype, fmt):
+    # a factor of 1e4 between tokens, and scales that a caller has made negative
+    c = Case(seqs, D=64, dtype=dtype, fmt=fmt, seed=33)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(34)
+    c.v_scale.mul_(10.0 ** (4.0 * torch.rand(c.v_scale.shape, device="cuda", generator=g) - 3.0))
+    c.check()
+    c.v_scale.mul_(torch.where(torch.rand(c.v_scale.shape, device="cuda", generator=g) < 0.5, -1.0, 1.0))
+    c.check()
+    c.v_scale.copy_(-c.v_scale.abs())
+    c.check()
+
+
+@pytest.mark.parametrize("seqs", [STEPS, CHUNKS], ids=["steps", "chunks"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
 @pytest.mark.parametrize("scale", [2000.0, 20000.0])
 def test_large_scales_of_small_codes(seqs, dtype, fmt, scale):
     # a caller's cache: code * scale is a number of either type, whatever the scale alone
@@ -86,3 +102,34 @@ def test_large_scales_of_small_codes(seqs, dtype, fmt, scale):
         c.v.copy_(codes.to(torch.int8))
     c.v_scale.fill_(scale)
     c.check()
+
+
+@pytest.mark.parametrize("dtype,times", [("bf16", 1e7), ("fp16", 1e4)])
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("ql,G", [(4, 2), (3, 5), (40, 4), (200, 2)])
+def test_a_large_value_reaches_only_the_rows_that_see_it(dtype, times, fmt, ql, G):
+    c = Case([(ql, 300)], H=2, G=G, D=64, dtype=dtype, fmt=fmt, seed=37)
+    ref, _, tol, _ = c.reference()
+    where = 300 - ql // 2
+    c.v_scale[c.table[0, where // c.b].long(), where % c.b] *= times
+    out = c.cache.attend(c.q, c.batch)[0].double()
+    assert c.cache.status() == R().LR_OK
+    hidden = ql - (300 - where)  # rows before it
+    assert bool(((out - ref).abs() <= tol)[:hidden].all())
+    assert bool(((out - ref).abs() > tol)[hidden:].any())
+
+
+@pytest.mark.parametrize("dtype,times", [("bf16", 1e7), ("fp16", 1e4)])
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_a_large_value_of_no_weight(dtype, times, fmt):
+    # single tokens: fp16 weights are taken against the largest product of weight and scale, not the largest scale
+    c = Case([(1, 300), (2, 80)], H=2, G=2, D=64, dtype=dtype, fmt=fmt, seed=38)
+    c.q.abs_()
+    blk, off = c.table[0, 5].long(), 7
+    c.k.view(torch.int8)[blk, off] = torch.full((2, 64), -8.0).to(torch.float8_e4m3fn).view(torch.int8).cuda() if fmt == "e4m3" else -8
+    c.k_scale[blk, off] = 10.0  # a score of about -80 * 1.2 * 64 / 8: its weight is nothing
+    ref, _, tol, _ = c.reference()
+    c.v_scale[blk, off] *= times
+    out = c.cache.attend(c.q, c.batch)[0].double()
+    assert c.cache.status() == R().LR_OK
+    assert bool(((out - ref).abs() <= tol).all())
