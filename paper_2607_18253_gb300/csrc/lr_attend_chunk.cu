@@ -301,7 +301,7 @@ struct ChunkLaunch {
 
 // Scores that a row does not see to -inf (at most `last`, and above `low` or below `sink` it does), in tensor
 // memory and out of the way of the loop, which nearly every tile goes through without; kbad: a bit for each
-// token whose K has a scale that is not finite, to NaN.
+// token whose block is out of range or whose K has a scale that is not finite, to NaN where a row sees it.
 __device__ __noinline__ void mask_scores(uint32_t ts, int last, int low, int sink, const uint32_t *kbad) {
     auto below = [](int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; };
 #pragma unroll 1
@@ -411,11 +411,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
     uint64_t *const bars = reinterpret_cast<uint64_t *>(places + 2 * kTok);
     long long *const scratch = reinterpret_cast<long long *>(bars + S::kBars);
     Job *const jobs = reinterpret_cast<Job *>(scratch + kThreads / 32 + 2);
-    int *const s_bad = reinterpret_cast<int *>(jobs + kJobs);  // [4] 1: a block of the tile is out of range
+    int *const s_bad = reinterpret_cast<int *>(jobs + kJobs);  // [4] of a tile, 1: s_kbad names tokens, 2: a scale of V is not finite
     int *const s_lost = s_bad + 4;                             // [half][2] the last scan that found V not finite
     int &s_dead = s_bad[8];
     uint32_t &s_tmem = *reinterpret_cast<uint32_t *>(s_bad + 9);
-    uint32_t *const s_kbad = reinterpret_cast<uint32_t *>(s_bad + 10);  // [4][4] a bit a token: K's scale is not finite
+    uint32_t *const s_kbad = reinterpret_cast<uint32_t *>(s_bad + 10);  // [4][4] a bit a token: its scores are NaN
     const uint32_t b0 = smem_addr(bars);
     const uint32_t q_full = b0, q_free = b0 + 8, kv_full = b0 + 16, kv_free = kv_full + 8 * kStages, s_full = kv_free + 8 * kStages,
                    p_half = s_full + 16, p_full = p_half + 16, o_full = p_full + 16, o_free = o_full + 16, sc_full = o_free + 16,
@@ -541,9 +541,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
                 const float *const ks = scales + slot * 2 * kTok, *const vs = ks + kTok;
                 after_sync();
                 const int flags = *const_cast<volatile int *>(s_bad + slot);
-                if (masked || (flags & 2))
+                if (masked || (flags & 1))
                     mask_scores(ts, pos - base, a.window > 0 ? pos - a.window - base : -1, a.sinks - base,
-                                flags & 2 ? s_kbad + slot * 4 : nullptr);
+                                flags & 1 ? s_kbad + slot * 4 : nullptr);
                 // 32 scores from tensor memory as they enter the softmax: times the scales of K
                 auto enter = [&](float *s, int k0) {
                     if constexpr (FMT != kFmt16) {
@@ -639,8 +639,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
                 enter(sb, 32);
                 weigh(sb, 32);
                 tm_store_wait();
-                if (flags & 1) l2.x = __uint_as_float(0x7fffffffu);
-                if (FMT != kFmt16 && (flags & 4)) lost = true;
+                if (FMT != kFmt16 && (flags & 2)) lost = true;
                 before_sync();
                 bar_arrive_warp(p_full + 8 * half);
             }
@@ -775,16 +774,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
         auto put = [&](int x, const Found &f) {
             if constexpr (kSplit) places[(x & 1) * kTok + i] = (int64_t)((uint64_t)power_of<FMT>(f.vs) << 48 | ((uint64_t)f.off << 16 >> 16));
             else places[(x & 1) * kTok + i] = f.off;
-            int flags = __any_sync(0xffffffffu, f.bad) ? 1 : 0;
+            // blocks out of range and scales that are not finite are kept from rows that do not see them
+            bool kb = f.bad;
+            int flags = 0;
             if constexpr (FMT != kFmt16) {
-                // scales that are not finite are kept from rows that do not see them: 2 and 4 say that there are such
-                const bool kb = !(fabsf(f.ks) < INFINITY), vb = !(fabsf(f.vs) < INFINITY);
+                kb |= !(fabsf(f.ks) < INFINITY);
+                const bool vb = !(fabsf(f.vs) < INFINITY);
                 scales[(x & 3) * 2 * kTok + i] = kb ? 1.0f : f.ks;
                 scales[(x & 3) * 2 * kTok + kTok + i] = vb ? 0.0f : kSplit ? rest_of(f.vs) : f.vs;
-                const unsigned kw = __ballot_sync(0xffffffffu, kb);
-                flags |= (kw ? 2 : 0) | (__any_sync(0xffffffffu, vb) ? 4 : 0);
-                if (lane == 0) s_kbad[(x & 3) * 4 + warp - 12] = kw;
+                flags |= __any_sync(0xffffffffu, vb) ? 2 : 0;
             }
+            const unsigned kw = __ballot_sync(0xffffffffu, kb);
+            flags |= kw ? 1 : 0;
+            if (lane == 0) s_kbad[(x & 3) * 4 + warp - 12] = kw;
             if (lane == 0 && flags) atomicOr(s_bad + (x & 3), flags);
         };
         // stage of the next item, free to be written
@@ -930,9 +932,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
                     cu.next(a, sh);
                     blk = look(place, bad);
                 }
-                if (!is_v && lane == 0) {
-                    s_bad[x & 3] = any != 0;
-                    bar_arrive(sc_full + 8 * (x & 3));
+                if (!is_v) {
+                    if (any && lane < 4) {  // a bit a box to a bit a token
+                        uint32_t tokens = 0;
+#pragma unroll 1
+                        for (int k = 0; k < 32; ++k) tokens |= (any >> (lane * 32 + k) / box & 1) << k;
+                        s_kbad[(x & 3) * 4 + lane] = tokens;
+                    }
+                    if (lane == 0) s_bad[x & 3] = any != 0;
+                    bar_arrive_warp(sc_full + 8 * (x & 3));
                 }
                 const uint32_t st = item % kStages, round = item / kStages;
                 item += 2;

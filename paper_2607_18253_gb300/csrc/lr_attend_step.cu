@@ -143,6 +143,12 @@ __device__ __noinline__ void join_parts(const AttendLaunch &a, int c0, int parts
     }
 }
 
+// Whether token t of a unit has a block out of range.
+__device__ __forceinline__ bool no_block(const AttendLaunch &a, const Unit &u, int t) {
+    int place;
+    return t <= u.hi && block_of(a.c, a.b, u.s, t, place) < 0;
+}
+
 template <bool BF16, int FMT, int DP, int NR>
 __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_step(const __grid_constant__ AttendLaunch a) {
     using S = Solo<DP, FMT, NR>;
@@ -157,7 +163,7 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
     // reference gives the same quotient, and a tile that raises none needs no exchange between lanes.
     constexpr float kLag = MB ? 8.0f : 4.0f;
     extern __shared__ __align__(128) char smem[];
-    __shared__ int s_last, s_bad;  // (s_bad: 1 + the last tile of the unit in which a block was out of range)
+    __shared__ int s_last;
     __shared__ long long s_scratch[kThreads / 32 + 2];
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, g = lane / 4, i4 = lane % 4;
     char *const stages = smem + warp * S::kWarp;
@@ -166,7 +172,6 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
     const CacheDev &c = a.c;
 
     chain_wait();
-    if (tid == 0) s_bad = 0;
     Cursor<kRows, S::kTile, kStepWeight> cu, lk;
     Share sh;
     if (!take_share<kRows, S::kTile, kStepWeight, kThreads, 1>(a, cu, sh, s_scratch)) {
@@ -192,8 +197,7 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
         const bool any = t <= lk.u.hi && (a.window == 0 || last > lk.u.lo - a.window || t < a.sinks);
         if (lane < kMine && any && i < a.b.max_blocks) blk = __ldg(a.b.table + (int64_t)lk.u.s * a.b.table_stride + i);
     };
-    unsigned bad_tiles = 0;  // a bit for each tile on its way that has a block out of range
-    bool bad = false;
+    [[maybe_unused]] unsigned bad_tiles = 0;  // 16 bits: a bit for each tile on its way that has a block out of range
     auto issue = [&](int tile) {
         char *const st = stages + tile % S::kStages * S::kStage;
         constexpr int kStep = 32 / S::kChunks;
@@ -203,7 +207,7 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
         const bool there = mine && (uint32_t)myblk < (uint32_t)c.nb;
         const unsigned have = __ballot_sync(0xffffffffu, there);  // a bit a token
         if (__any_sync(0xffffffffu, mine && !there)) {
-            bad_tiles |= 1u << (tile & 31);
+            if constexpr (FMT == kFmt16) bad_tiles |= 1u << (tile & 31);
             report(c.status, kEInval);
         }
         if (even) {
@@ -237,7 +241,7 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
             if (lane < kMine) {
                 const int64_t so = there ? (int64_t)myblk * c.ssb + (place + (even ? lane & 15 : 0)) * c.sst + lk.u.h * c.ssh : 0;
                 float *const to = scales + tile % S::kStages * 2 * kMine + lane;
-                copy4(smem_addr(to), c.ks + so, there);
+                copy4(smem_addr(to), there || !mine ? c.ks + so : c.nan, mine);  // (NaN where the block is out of range)
                 copy4(smem_addr(to + kMine), c.vs + so, there);
             }
         }
@@ -318,7 +322,6 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
                     down[n][y] = 1.0f;
                 }
             }
-            bad = false;
         }
         for (; cu.j < cu.end; ++x, ++cu.j) {
             // the copies of the tile ahead, then the places of the one after it (their latency is the tile's work)
@@ -333,13 +336,19 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
             copy_commit();
             copy_wait<S::kStages - 1>();
             __syncwarp();
-            bad |= bad_tiles >> (x & 31) & 1;
-            bad_tiles &= ~(1u << (x & 31));
 
             // ---- scores: tokens g, g + 8 of each 16 ----
             char *const st = stages + x % S::kStages * S::kStage;
             const uint32_t sk = smem_addr(st), sv = sk + S::kHalf;
             const int base = cu.base() + warp * kMine;
+            if constexpr (FMT == kFmt16) {
+                if (bad_tiles >> (x & 31) & 1) {  // K of a token whose block is out of range: NaN, as are its scores where a row sees them
+                    bad_tiles &= ~(1u << (x & 31));
+                    if (lane < kMine && no_block(a, u, base + lane))
+                        *reinterpret_cast<uint16_t *>(st + lane * S::kRow + swizzle<DP, FMT, false>(lane, 0) * 16) = 0x7fff;
+                    __syncwarp();
+                }
+            }
             float s[NB][NR][4];
 #pragma unroll
             for (int b = 0; b < NB; ++b)
@@ -606,11 +615,9 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
                     }
                 }
             }
-        if (__any_sync(0xffffffffu, bad) && lane == 0) s_bad = x;
         __syncthreads();
         constexpr int kLanes = DP / 4;  // four elements a thread
         const int d = tid % kLanes * 4;
-        const bool lost = s_bad == x;
         int64_t slot = 0;
         if (!whole) slot = slot_of(sh, blockIdx.x, cu.at);
         for (int r = tid / kLanes; r < u.rows; r += kThreads / kLanes) {
@@ -621,7 +628,6 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
 #pragma unroll
             for (int w = 0; w < 4; ++w)
                 add_part(s_ml[w * kRows + r], *reinterpret_cast<const float4 *>(smem + w * S::kWarp + used + (r * DP + d) * 4), mm, ll, acc);
-            if (lost) ll = __uint_as_float(0x7fffffffu);
             if (whole) {
                 write_row<BF16>(a, r, d, u.q0, u.h, mm, ll, acc);
             } else {

@@ -39,6 +39,7 @@ struct CacheDev {
     int32_t nb, b;          // blocks, tokens a block
     FastDiv div_b, div_g;
     int32_t *status;
+    const float *nan;  // one
 };
 
 struct BatchDev {

@@ -143,7 +143,9 @@ int lr_cache_create(const lr_cache_config *cfg, lr_cache **out) {
     d.div_g = lr::fast_div(d.G);
     if (cfg->format == LR_CACHE_16BIT) lr::encode_maps(d, c->bf16, c->maps);
     e = cudaMalloc(&d.status, 16);
-    if (e == cudaSuccess) e = cudaMemset(d.status, 0, 16);
+    const uint32_t words[4] = {0, 0x7fffffffu, 0, 0};  // the status word, a NaN
+    if (e == cudaSuccess) e = cudaMemcpy(d.status, words, sizeof(words), cudaMemcpyHostToDevice);
+    d.nan = reinterpret_cast<const float *>(d.status + 1);
     if (e == cudaSuccess) e = alloc_parts(c->step, lr::attend_step_ctas(c->sms), lr::kStepRows, lr::attend_step_ctas(c->sms));
     if (e == cudaSuccess) e = alloc_parts(c->chunk, c->sms, lr::kChunkRows, 8 * (size_t)c->sms);
     if (e != cudaSuccess) return bail(LR_ENOMEM, cudaGetErrorString(e));

@@ -133,3 +133,24 @@ def test_a_large_value_of_no_weight(dtype, times, fmt):
     out = c.cache.attend(c.q, c.batch)[0].double()
     assert c.cache.status() == R().LR_OK
     assert bool(((out - ref).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("fmt", ["16", "e4m3", "int8"])
+@pytest.mark.parametrize("D,b", [(64, 16), (128, 5), (64, 1), (64, 64)])
+@pytest.mark.parametrize("ql,kv,G,window,sinks,place", [(90, 300, 4, 0, 0, 295), (200, 300, 2, 0, 0, 150), (200, 300, 2, 40, 3, 130),
+                                                        (150, 400, 4, 40, 3, 1), (4, 290, 2, 0, 0, 289), (8, 261, 2, 0, 0, 258),
+                                                        (8, 261, 1, 5, 2, 250), (1, 300, 4, 0, 0, 70)])
+def test_a_block_out_of_range_reaches_only_the_rows_that_read_it(fmt, D, b, ql, kv, G, window, sinks, place):
+    c = Case([(ql, kv), (2, 50)], H=2, G=G, D=D, b=b, fmt=fmt, seed=39)
+    ref, rl, tol, ltol = c.reference(window=window, sinks=sinks)
+    c.table[0, place // b] = c.nb
+    out, lse = c.cache.attend(c.q, c.batch, window=window, sinks=sinks, lse=True)
+    at = torch.arange(kv - ql, kv, device="cuda")[:, None]
+    j = torch.arange(place // b * b, min(kv, place // b * b + b), device="cuda")[None]
+    see = j <= at
+    if window:
+        see &= (j > at - window) | (j < sinks)
+    reads = torch.cat([see.any(1), torch.zeros(2, dtype=torch.bool, device="cuda")])
+    assert c.cache.status() == (R().LR_EINVAL if reads.any() else R().LR_OK)
+    assert torch.isnan(out[reads]).all() and torch.isnan(lse[reads]).all()
+    assert bool(((out.double() - ref).abs() <= tol)[~reads].all()) and bool(((lse.double() - rl).abs() <= ltol)[~reads].all())
