@@ -463,8 +463,9 @@ LR_API int lr_cache_destroy(lr_cache *c);
  * k, v: element d of (row, head) at row * token_stride + head * head_stride + d (elements; both
  * strides multiples of 16 bytes, base 16-byte aligned; the same strides for k and v).
  * Device errors: a token without a place in the cache (a sequence with more new tokens than
- * kv_len, a position past max_blocks, a block outside [0, num_blocks), a q_start out of order) is not
- * stored and records LR_EINVAL. */
+ * kv_len, a position past max_blocks, a block outside [0, num_blocks), one that several sequences
+ * claim) is not stored and records LR_EINVAL.  A q_start out of order records it too; in batches of more than 1,024
+ * sequences a token that several claim may be stored for one of them. */
 LR_API int lr_cache_write(lr_cache *c, const lr_cache_batch *b, int32_t T, const void *k, const void *v,
                           int64_t token_stride, int64_t head_stride, void *cuda_stream);
 
@@ -495,7 +496,8 @@ LR_API int lr_cache_read(lr_cache *c, const lr_cache_batch *b, int32_t T, int32_
  * [0, 2^30] (0: no window), sinks in [0, 2^30].  Rows of no sequence are not written.
  * Device errors, each LR_EINVAL: a sequence whose q_start, number of new tokens (over max_q) or
  * kv_len (over max_blocks * block_size) is out of range is left out, its rows not written;
- * a block outside [0, num_blocks) makes the rows that would read it NaN.
+ * a block outside [0, num_blocks) makes the rows that would read it NaN.  Rows that several sequences
+ * claim, by a q_start out of order (which is recorded), have no defined values.
  * What a row may not see does not reach it, whatever it holds. */
 LR_API int lr_cache_attend(lr_cache *c, const lr_cache_batch *b, int32_t T, const void *q, int64_t q_token_stride,
                            int64_t q_head_stride, float scale, int32_t window, int32_t sinks, void *out,

@@ -43,20 +43,39 @@ __device__ __forceinline__ Place find_place(const CacheDev &c, const BatchDev &b
 // them are found by all threads together, a sequence each: one round of loads for 256 sequences, where a
 // search takes one a halving (64 tokens of 64 sequences stored and read back: 8.6 us, searched for
 // 9.5).  More than kScan sequences are searched for.
+// Where q_start is out of order several sequences may claim a token, which then has no place: the scan finds
+// that out, and each token counts its claims.  (A search does not: its token goes to one of them; the launch's CTAs look
+// through the order together.)
 constexpr int kScan = 1024;
+__device__ __noinline__ int2 only_claim(const BatchDev &b, int t) {
+    int2 e = make_int2(-1, 0);
+    for (int s = 0; s < b.n; ++s) {
+        const int end = __ldg(b.q_start + s + 1);
+        if (__ldg(b.q_start + s) > t || t >= end) continue;
+        if (e.x >= 0) return make_int2(-2, 0);
+        e = make_int2(s, end);
+    }
+    return e;
+}
 __device__ __forceinline__ void find_places(Place *sp, int2 *seq, const CacheDev &c, const BatchDev &b, int t0, int t1) {
     const int mine = t0 + (int)threadIdx.x;
     if (mine < t1) seq[threadIdx.x] = make_int2(-1, 0);
+    bool disorder = false;
     __syncthreads();
     if (b.n <= kScan) {
         for (int s = threadIdx.x; s < b.n; s += kThreads) {
             const int begin = __ldg(b.q_start + s), end = __ldg(b.q_start + s + 1);
-            if (begin > end) report(c.status, kEInval);  // out of order
+            if (begin > end) {
+                report(c.status, kEInval);
+                disorder = true;
+            }
             for (int t = max(begin, t0); t < min(end, t1); ++t) seq[t - t0] = make_int2(s, end);
         }
-    } else if (mine < t1) {
+    } else {
+        for (int64_t s = (int64_t)blockIdx.x * kThreads + threadIdx.x; s < b.n; s += (int64_t)gridDim.x * kThreads)
+            if (__ldg(b.q_start + s) > __ldg(b.q_start + s + 1)) report(c.status, kEInval);
         // the last sequence that begins at or before the token
-        int lo = 0, hi = b.n;
+        int lo = 0, hi = mine < t1 ? b.n : 0;
         while (lo < hi) {
             const int mid = (lo + hi) >> 1;
             if (__ldg(b.q_start + mid) <= mine) lo = mid + 1;
@@ -68,10 +87,10 @@ __device__ __forceinline__ void find_places(Place *sp, int2 *seq, const CacheDev
             else if (lo < b.n) report(c.status, kEInval);
         }
     }
-    __syncthreads();
+    disorder = __syncthreads_or(disorder);
     if (mine < t1) {
-        const int2 e = seq[threadIdx.x];
-        Place p{-2, 0};
+        const int2 e = disorder ? only_claim(b, mine) : seq[threadIdx.x];
+        Place p{e.x == -1 ? -2 : -1, 0};
         if (e.x >= 0) p = find_place(c, b, e.x, e.y, mine);
         if (p.off == -1) report(c.status, kEInval);
         sp[threadIdx.x] = p;

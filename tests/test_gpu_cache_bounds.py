@@ -154,3 +154,35 @@ def test_a_block_out_of_range_reaches_only_the_rows_that_read_it(fmt, D, b, ql, 
     assert c.cache.status() == (R().LR_EINVAL if reads.any() else R().LR_OK)
     assert torch.isnan(out[reads]).all() and torch.isnan(lse[reads]).all()
     assert bool(((out.double() - ref).abs() <= tol)[~reads].all()) and bool(((lse.double() - rl).abs() <= ltol)[~reads].all())
+
+
+@pytest.mark.parametrize("many", [0, 1500])
+@pytest.mark.parametrize("fmt", ["16", "int8"])
+def test_a_token_that_two_sequences_claim_has_no_place(fmt, many):
+    # q_start 0, 5, 3, 8: the first sequence has tokens 0-4, the third 3-7, the second none
+    c = Case([(5, 20), (0, 9), (5, 30)] + [(0, 1)] * many, H=2, G=1, D=32, b=8, fmt=fmt, seed=40)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    batch = C().CacheBatch(torch.tensor([0, 5, 3, 8] + [8] * many, **i32), c.kv_len, c.table, 8)
+    before = [t.clone() for t in (c.k, c.v)]
+    x = torch.randn((8, 2, 32), device="cuda").to(torch.bfloat16)
+    c.cache.write(x, x, batch)
+    assert c.cache.status() == R().LR_EINVAL
+    k, v = c.cache.read(batch, 8)
+    assert c.cache.status() == R().LR_EINVAL
+    place = {t: (0, 15 + t) for t in range(5)}           # token: (sequence, position)
+    place.update({t: (2, 25 + t - 3) for t in range(5, 8)})
+    for got, now, was in ((k, c.k, before[0]), (v, c.v, before[1])):
+        changed = (now != was).any(-1).any(-1)
+        if not many:  # (in larger batches one of the two may have them)
+            assert torch.isnan(got[3:5]).all()
+            mine = torch.zeros_like(changed)
+            for t in (0, 1, 2, 5, 6, 7):
+                s, p = place[t]
+                mine[c.table[s, p // 8].long(), p % 8] = True
+            assert not changed[~mine].any()
+        want = x
+        if fmt != "16":
+            codes, sc = base.quantised(x.float(), fmt)
+            want = (codes.float() * sc[..., None]).to(torch.bfloat16)
+        for t in (0, 1, 2, 5, 6, 7):
+            assert torch.equal(got[t], want[t])
