@@ -149,6 +149,9 @@ int lr_cache_create(const lr_cache_config *cfg, lr_cache **out) {
     if (e == cudaSuccess) e = alloc_parts(c->step, lr::attend_step_ctas(c->sms), lr::kStepRows, lr::attend_step_ctas(c->sms));
     if (e == cudaSuccess) e = alloc_parts(c->chunk, c->sms, lr::kChunkRows, 8 * (size_t)c->sms);
     if (e != cudaSuccess) return bail(LR_ENOMEM, cudaGetErrorString(e));
+    // (what was set above, on the default stream, has to be there for streams that do not wait for it)
+    e = cudaDeviceSynchronize();
+    if (e != cudaSuccess) return bail(LR_ECUDA, cudaGetErrorString(e));
     *out = c;
     return LR_OK;
 }
