@@ -269,7 +269,8 @@ int lr_cache_status(lr_cache *c, void *stream) {
     if (e == cudaSuccess) e = cudaStreamSynchronize(st);
     if (e == cudaSuccess) e = cudaMemsetAsync(c->dev.status, 0, sizeof(int32_t), st);
     if (e == cudaSuccess) e = cudaStreamSynchronize(st);
-    if (e == cudaSuccess && h == LR_ECUDA) {  // a kernel gave up: its counts of finished parts start again
+    // a kernel may have given up, whatever error came first: its counts of finished parts start again
+    if (e == cudaSuccess && h != LR_OK) {
         e = cudaMemsetAsync(c->chunk.done, 0, 8 * (size_t)c->sms * sizeof(uint32_t), st);
         if (e == cudaSuccess) e = cudaStreamSynchronize(st);
     }

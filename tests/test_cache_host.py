@@ -107,3 +107,18 @@ def attend(lib, h):
 def test_a_new_handle_is_ready_on_every_stream(lib, cache):
     # counts and status word are set by work of the default stream, which streams that do not block on it would not wait for
     assert lib.fake_pending() == 0
+
+
+@pytest.mark.parametrize("earlier", [0, 1])
+def test_counts_start_again_after_a_launch_that_gave_up(lib, cache, earlier):
+    # the word keeps the first error, an earlier LR_EINVAL too
+    from paper_2607_18253_gb300 import router as R
+    if earlier:
+        lib.fake_chunk(R.LR_EINVAL, 0)
+        attend(lib, cache)
+    lib.fake_chunk(0, 1)
+    attend(lib, cache)
+    assert lib.fake_count() == 1
+    assert lib.lr_cache_status(cache, None) == (R.LR_EINVAL if earlier else R.LR_ECUDA)
+    assert lib.fake_count() == 0
+    assert lib.lr_cache_status(cache, None) == R.LR_OK
