@@ -69,7 +69,7 @@ struct Shape {
     static constexpr int kBytes = kQ + kStages * kTile + kRaw;
     static constexpr int kBars = 2 + 2 * kStages + 10 + 4 + 1 + 2 * kJobs + 2;
     static constexpr int kScales = FMT == kFmt16 ? 0 : 4 * 2 * kTok * 4;
-    static constexpr int kSmem = kBytes + kScales + 2 * kTok * 8 + kBars * 8 + (kThreads / 32 + 2) * 8 + 26 * 4 + kJobs * sizeof(Job);
+    static constexpr int kSmem = kBytes + kScales + 2 * kTok * 8 + kBars * 8 + (kThreads / 32 + 2) * 8 + 29 * 4 + kJobs * sizeof(Job);
     static_assert(kSmem <= 227 * 1024, "shared memory");
 };
 
@@ -416,6 +416,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
     int &s_dead = s_bad[8];
     uint32_t &s_tmem = *reinterpret_cast<uint32_t *>(s_bad + 9);
     uint32_t *const s_kbad = reinterpret_cast<uint32_t *>(s_bad + 10);  // [4][4] a bit a token: its scores are NaN
+    uint32_t *const s_sent = s_kbad + 16;  // tiles of K and of V, and units of Q, that the copy engine was asked for
     const uint32_t b0 = smem_addr(bars);
     const uint32_t q_full = b0, q_free = b0 + 8, kv_full = b0 + 16, kv_free = kv_full + 8 * kStages, s_full = kv_free + 8 * kStages,
                    p_half = s_full + 16, p_full = p_half + 16, o_full = p_full + 16, o_free = o_full + 16, sc_full = o_free + 16,
@@ -456,6 +457,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         shared_to_async();
         s_dead = 0;
+        s_sent[0] = s_sent[1] = s_sent[2] = 0;
     }
     if (warp == 8) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&s_tmem)) : "memory");
@@ -908,7 +910,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
             const int box = in.m.box;
             const bool is_v = warp == 10;
             const CUtensorMap *const map = is_v ? &in.m.v : &in.m.k;
-            uint32_t item = is_v;
+            uint32_t item = is_v, sent = 0;
             bool ok = true;
             auto look = [&](int &place, bool &bad) {
                 const int t = cu.base() + lane * box;
@@ -946,6 +948,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
                 item += 2;
                 if (round > 0) ok = ok && bar_wait(kv_free + 8 * st, (round - 1) & 1, dead);
                 if (!ok) continue;
+                ++sent;
                 const uint32_t bar = kv_full + 8 * st, to = smem_addr(tiles + st * S::kTile) + lane * box * 128;
                 if (lane == 0)
                     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(boxes * box * 2 * DP) : "memory");
@@ -959,6 +962,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
                             : "memory");
                 }
             }
+            if (lane == 0) s_sent[is_v] = sent;
         } else if (warp >= S::kQueryWarp && warp < S::kQueryWarp + S::kQueryWarps) {
             // ================= queries to shared memory =================
             constexpr int QC = DP / 8, QS = S::kQueryWarps * 32 / QC;
@@ -992,6 +996,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
                     if (lane == 0) {
                         const int halves = u.rows > 128 ? 2 : 1;
                         if (i == 0) {
+                            s_sent[2] = frag + 1;
                             asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(q_full), "r"(halves * S::kTile) : "memory");
                             for (int k = 0; k < halves; ++k)
                                 for (int p = 0; p < DP / 64; ++p)
@@ -1103,15 +1108,29 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
                 }
                 if (last) break;
             }
-            if (!ok) {  // what was issued ends before its memory is given back
-                if (one) commit(ended);
-                for (uint32_t i = 0; i < kSpin && !bar_test(ended, 0); ++i) {
-                }
-            }
         }
         __syncwarp();
     }
     __syncthreads();
+    if (*dead && warp == 8) {
+        // the launch gave up: products and copies that were asked for end before their memory is given back (each wait
+        // has a limit; a tile of K or V that another has followed in its stage is not waited for)
+        auto over = [&](uint32_t bar, uint32_t parity) {
+            for (uint32_t i = 0; i < kSpin / 64 && !bar_test(bar, parity); ++i) {
+            }
+        };
+        if (elect()) commit(ended);  // (the thread that issued the products)
+        __syncwarp();
+        over(ended, 0);
+        const uint32_t nk = s_sent[0], nv = s_sent[1];  // items 2 * (nk - 1) and 2 * nv - 1 are the last
+        for (uint32_t st = 0; st < kStages; ++st) {
+            uint32_t last = ~0u;
+            for (uint32_t it = st; it < 2 * max(nk, nv); it += kStages)
+                if (it / 2 < (it & 1 ? nv : nk)) last = it;
+            if (last != ~0u) over(kv_full + 8 * st, last / kStages & 1);
+        }
+        if (s_sent[2]) over(q_full, (s_sent[2] - 1) & 1);
+    }
     if (warp == 8) {
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tm));
         if (lane == 0 && *dead) report(c.status, kECuda);
