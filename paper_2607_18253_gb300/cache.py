@@ -19,6 +19,11 @@ LR_CACHE_16BIT, LR_CACHE_E4M3, LR_CACHE_INT8 = 0, 1, 2
 _DTYPES = {torch.bfloat16: LR_BF16, torch.float16: LR_FP16, torch.float32: LR_FP32}
 
 
+def _i32(x) -> int:
+    """x, or the nearest 32-bit number, which the library refuses: ctypes alone takes it modulo 2^32."""
+    return x if -0x80000000 <= x <= 0x7FFFFFFF else -0x80000000 if x < 0 else 0x7FFFFFFF
+
+
 class CacheBatch:
     """One token batch (lr_cache_batch): sequence s brings its last q_start[s+1] - q_start[s] of kv_len[s] tokens.
 
@@ -32,7 +37,7 @@ class CacheBatch:
         if not block_table.is_cuda or block_table.dtype != torch.int32:
             raise TypeError("block_table must be an int32 CUDA tensor")
         self._keep = (q_start, kv_len, block_table)
-        self._c = _CacheBatch(n, int(max_q), _dev(q_start, torch.int32, "q_start", n + 1),
+        self._c = _CacheBatch(n, _i32(int(max_q)), _dev(q_start, torch.int32, "q_start", n + 1),
                               _dev(kv_len, torch.int32, "kv_len", n), block_table.data_ptr(),
                               max(int(block_table.stride(0)), int(block_table.shape[1])) if n <= 1 else int(block_table.stride(0)),
                               int(block_table.shape[1]))
@@ -87,7 +92,7 @@ class PagedCache:
         st = [0 if n == 1 else s for n, s in zip((nb, bs, H), k.stride())]
         ss = list(k_scale.stride()) if fmt else [0, 0, 0]
         self.num_q_heads, self.num_kv_heads, self.head_dim, self.dtype = int(num_q_heads), int(H), int(D), dtype
-        cfg = _CacheConfig(self.num_q_heads, H, D, _DTYPES[dtype], fmt, bs, nb, int(max_seqs), k.data_ptr(), v.data_ptr(),
+        cfg = _CacheConfig(_i32(int(num_q_heads)), H, D, _DTYPES[dtype], fmt, bs, nb, _i32(int(max_seqs)), k.data_ptr(), v.data_ptr(),
                            k_scale.data_ptr() if fmt else None, v_scale.data_ptr() if fmt else None, *st, *ss)
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self._scale = 1.0 / math.sqrt(self.head_dim)
@@ -160,7 +165,7 @@ class PagedCache:
             lse = None if lse is False else lse
             lp = _dev(lse, torch.float32, "lse_out", T * Hq)
         rc = self._lib.lr_cache_attend(self._h, batch._ref, T, q.data_ptr(), qt, qh, self._scale if scale is None else scale,
-                                       window, sinks, out.data_ptr(), ot, oh, lp, _stream(stream))
+                                       _i32(window), _i32(sinks), out.data_ptr(), ot, oh, lp, _stream(stream))
         if rc:
             self._check(rc, "lr_cache_attend")
         return out, lse

@@ -186,3 +186,21 @@ def test_a_token_that_two_sequences_claim_has_no_place(fmt, many):
             want = (codes.float() * sc[..., None]).to(torch.bfloat16)
         for t in (0, 1, 2, 5, 6, 7):
             assert torch.equal(got[t], want[t])
+
+
+def test_numbers_beyond_32_bits_are_refused():
+    # not taken modulo 2^32, where they could be others' valid ones
+    c = Case([(2, 30), (1, 20)], H=2, G=4, D=64, seed=41)
+    far = 1 << 32
+    for kw in (dict(window=far), dict(window=far + 5), dict(window=-far + 5), dict(window=3, sinks=far + 1)):
+        with pytest.raises(R().LRError) as e:
+            c.cache.attend(c.q, c.batch, **kw)
+        assert e.value.code == R().LR_EINVAL
+    for max_q in (far + 2, -far + 2):
+        with pytest.raises(R().LRError) as e:
+            c.cache.attend(c.q, C().CacheBatch(c.q_start, c.kv_len, c.table, max_q))
+        assert e.value.code == R().LR_EINVAL
+    for kw in (dict(num_q_heads=far + 8), dict(max_seqs=far + 1)):
+        with pytest.raises(R().LRError) as e:
+            C().PagedCache(**{**dict(k=c.k, v=c.v, num_q_heads=8), **kw})
+        assert e.value.code == R().LR_EINVAL
