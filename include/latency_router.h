@@ -488,7 +488,7 @@ LR_API int lr_cache_read(lr_cache *c, const lr_cache_batch *b, int32_t T, int32_
  * the weights before they are rounded: to fp16, but to bf16 in sequences of many rows of a bf16 cache.  (In
  * those of an fp16 cache a power of two of V's scale goes to the codes, which at values below 2^-14 are then
  * off by 2^-25 at most.)  A cache that lr_cache_write has not filled may have scales of either sign, V's of
- * an fp16 cache up to 2^16.  Codes of e4m3's NaN, which lr_cache_write never stores, have no defined value.
+ * an fp16 cache up to 2^15.  Codes of e4m3's NaN, which lr_cache_write never stores, have no defined value.
  * The same call gives the same bits: parts of a row that several CTAs sum are joined in a fixed order.
  * Two calls on one cache share its workspace: order them (one stream, or events).
  * q, out: element d of (row, head) at row * token_stride + head * head_stride + d, aligned as for

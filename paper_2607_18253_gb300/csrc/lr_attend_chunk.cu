@@ -254,14 +254,15 @@ __device__ __noinline__ void add_lost(const AttendLaunch &a, const Unit &u, int 
 }
 
 // V's scales over 8-bit codes in fp16: code * (2^e * rest) with 1 <= |rest| < 2.  The power of two goes to the codes as
-// they are converted (a power of two times a code is a number of fp16, or below 2^-14 off by 2^-25 at most), the
-// rest to the weights, which so are as far from the ends of fp16's range as those of a 16-bit cache, however large or
-// small V is.  e stays in [-24, 5], where the codes' products are finite; what a scale has beyond is in the
-// rest: weights of up to 2^4 stay numbers with scales of up to 2^16.
+// they are converted, the rest to the weights, which so are as far from the ends of fp16's range as those of a 16-bit
+// cache, however large or small V is.  The codes get 2^(e + 1), and the sums are halved: a product below 2^-14 that fp16 rounds
+// by up to 2^-25 is off by half that times the rest, less than 2^-25 of V.  e + 1 stays in [-24, 5], where the
+// products are finite; what a scale has beyond is in the rest: weights of up to 2^4 stay numbers with
+// scales of up to 2^15.
 constexpr int kLeast = -24, kMost = 5;
-__device__ __forceinline__ int power(float scale) { return min(max((int)(__float_as_uint(scale) >> 23 & 0xff) - 127, kLeast), kMost); }
-__device__ __forceinline__ float rest_of(float scale) { return scale * __uint_as_float((uint32_t)(127 - power(scale)) << 23); }
-// 2^e as fp16's bits; of e4m3 2^8 as much, for the codes that to_half_times makes.
+__device__ __forceinline__ int power(float scale) { return min(max((int)(__float_as_uint(scale) >> 23 & 0xff) - 126, kLeast), kMost); }
+__device__ __forceinline__ float rest_of(float scale) { return scale * __uint_as_float((uint32_t)(128 - power(scale)) << 23); }
+// The codes' power of two as fp16's bits; of e4m3 2^8 as much, for the codes that to_half_times makes.
 template <int FMT>
 __device__ __forceinline__ uint32_t power_of(float scale) {
     return __half_as_ushort(__float2half_rn(__uint_as_float((uint32_t)(127 + power(scale) + (FMT == kFmtE4M3 ? 8 : 0)) << 23)));
@@ -269,10 +270,10 @@ __device__ __forceinline__ uint32_t power_of(float scale) {
 template <int FMT>
 __device__ __forceinline__ uint32_t half_times(uint32_t two) {
     uint32_t r = 0;
-    if constexpr (FMT == kFmtInt8) asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(two), "r"(0xe480e480u));  // -1152 * 2^e
+    if constexpr (FMT == kFmtInt8) asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(two), "r"(0xe480e480u));  // -1152 times it
     return r;
 }
-// Four codes (0, 1), (2, 3) times 2^e, `two`.  int8: (1024 + (code + 128)) * 2^e - 1152 * 2^e in one rounding.  e4m3:
+// Four codes (0, 1), (2, 3) times `two`.  int8: (1024 + (code + 128)) * two - 1152 * two in one rounding.  e4m3:
 // the code's bits moved to fp16's places are 2^-8 times its value (and its NaN a number, which hidden weights need).
 template <int FMT>
 __device__ __forceinline__ void to_half_times(uint32_t w, uint32_t two, uint32_t shift, uint32_t &a, uint32_t &b) {
@@ -656,7 +657,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
             const int64_t slot = job.slot;
             char *const po = a.out + (int64_t)(u.q0 + t) * a.o_t + (int64_t)hd * a.o_h;
             float *const pw = a.part_o + (slot * 256 + r) * 128;
-            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+            constexpr float kHalf = kSplit ? 0.5f : 1.0f;  // (V's codes were taken twice)
+            const float inv = l == 0.0f ? 0.0f : kHalf / l;
             bool gone = false;
 #pragma unroll 1
             for (int k = 0; k < DP; k += 32) {  // (short code: it is fetched anew for each unit)
@@ -689,7 +691,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
                                            pack16<BF16>(o[z + 4] * inv, o[z + 5] * inv), pack16<BF16>(o[z + 6] * inv, o[z + 7] * inv));
                 } else if (real) {
 #pragma unroll
-                    for (int z = 0; z < 32; z += 4) *reinterpret_cast<float4 *>(pw + k + z) = make_float4(o[z], o[z + 1], o[z + 2], o[z + 3]);
+                    for (int z = 0; z < 32; z += 4) *reinterpret_cast<float4 *>(pw + k + z) = make_float4(o[z] * kHalf, o[z + 1] * kHalf, o[z + 2] * kHalf, o[z + 3] * kHalf);
                 }
             }
             __syncwarp();

@@ -204,3 +204,12 @@ def test_numbers_beyond_32_bits_are_refused():
         with pytest.raises(R().LRError) as e:
             C().PagedCache(**{**dict(k=c.k, v=c.v, num_q_heads=8), **kw})
         assert e.value.code == R().LR_EINVAL
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("size", [1e-5, 1e-4, 3e-4, 1e-3, 1e-2])
+def test_rows_that_see_one_small_value(fmt, size):
+    # a window of one token: the output is its V, and nothing averages what the product rounds
+    c = Case([(300, 300), (200, 900)], H=2, G=2, D=64, dtype="fp16", fmt=fmt, seed=42)
+    c.v_scale.mul_(size)
+    c.check(window=1)
