@@ -452,7 +452,10 @@ typedef struct {
 typedef struct lr_cache lr_cache;  /* opaque, owned by the library */
 
 /* Create a cache handle on the current CUDA device over the caller's memory (nothing of it is read
- * or written here) and allocate the workspace the calls need.  *out is set on LR_OK. */
+ * or written here) and allocate the workspace the calls need: parts of rows that several SMs sum, 50 MB
+ * with 152 SMs, whatever the sizes.  A program of many layers may keep them in one cache, a range of blocks a layer, and
+ * give each layer's calls a block table of its own: one handle then serves all.  Synchronizes the device.
+ * *out is set on LR_OK. */
 LR_API int lr_cache_create(const lr_cache_config *cfg, lr_cache **out);
 
 /* Free everything lr_cache_create allocated.  Synchronizes the device first.  NULL is a no-op. */
@@ -484,10 +487,12 @@ LR_API int lr_cache_read(lr_cache *c, const lr_cache_batch *b, int32_t T, int32_
  *   out = sum_j softmax_j(scale * q . k_j) v_j   and   lse = ln sum_j exp(scale * q . k_j)
  * over the visible j; a row that sees nothing (a negative position) gives 0 and -inf.  Products of
  * 16-bit numbers are summed in fp32; the softmax weights are rounded to 16 bits for the second
- * product.  8-bit codes are exact in either 16-bit type; K's scales are applied to the scores in fp32, V's to
- * the weights before they are rounded: to fp16, but to bf16 in sequences of many rows of a bf16 cache.  (In
- * those of an fp16 cache a power of two of V's scale goes to the codes, which at values below 2^-14 are then
- * off by 2^-25 at most.)  A cache that lr_cache_write has not filled may have scales of either sign, V's of
+ * product, over 16-bit caches to the cache's type.  8-bit codes are exact in either 16-bit type; K's scales are
+ * applied to the scores in fp32, V's to the weights before they are rounded: in sequences of few rows (new tokens
+ * times query heads a KV head: up to 8, or 16 where the batch has no more) to fp16, in others to the cache's dtype.
+ * In the former, bf16 queries are multiplied in fp16, divided by a power of two a row: elements below 2^-14 of the
+ * row's largest are off by 2^-25 of it at most.  In the latter, values of V below 2^-14 in an fp16 cache are off by 2^-25
+ * at most.  A cache that lr_cache_write has not filled may have scales of either sign, V's of
  * an fp16 cache up to 2^15.  Codes of e4m3's NaN, which lr_cache_write never stores, have no defined value.
  * The same call gives the same bits: parts of a row that several CTAs sum are joined in a fixed order.
  * Two calls on one cache share its workspace: order them (one stream, or events).

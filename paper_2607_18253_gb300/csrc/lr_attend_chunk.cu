@@ -18,10 +18,11 @@
 // What it takes: a half's chain -- scores, softmax, weights, products -- has to fit while the other half's products
 // run, so what is off that chain is kept out of it and out of the loop's code, which 16 warps of six kinds
 // share an instruction cache for: hidden scores are set apart (mask_scores: 1,554 -> 1,402 us for 4,096 tokens over
-// 32,768), the walk is another warp's (Job), and a warp waits for a barrier with all its lanes
+// 32,768, one state repeated as in the next figure), the walk is another warp's (Job), and a warp waits for a barrier with all its lanes
 // (a single lane's wait took some 250 cycles even where the phase was over: 2,262 -> 1,596 us).
-// Measured (32 query heads on 8 KV heads of 128): 4,096 tokens at the end of 32,768, 16 bits: 1,363 us, 1,510
-// TFLOP/s, 78% of the library's largest product; a half's chain is ~2,700 cycles a tile against 2,048 of products.
+// Measured (32 query heads on 8 KV heads of 128): 4,096 tokens at the end of 32,768, 16 bits: 1,477 us with inputs in
+// turn, 1,396 TFLOP/s, 72% of the library's largest product (on one state again and again 1,353: the card's power differs);
+// a half's chain is ~2,700 cycles a tile against 2,048 of products.
 #include "lr_attend.cuh"
 
 namespace lr {

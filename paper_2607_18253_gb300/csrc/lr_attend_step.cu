@@ -16,8 +16,10 @@
 //     a 16-row operand, in instructions and registers, and more warps fit an SM;
 //   - the maximum that the weights refer to lags behind the true one, so most tiles exchange nothing between lanes.
 // Measured (32 query heads on 8 KV heads of 128, blocks of 16): a 16-bit cache 5.9 TB/s (63 sequences of
-// 512 to 6,001 tokens, 98 us) and 4.7 (one of 200,001, 86 us); e4m3 4.6 (64 of 128 to 8,192, 56 us), bound
-// by instructions: an 8-bit token is as many as a 16-bit one, and its conversion.
+// 512 to 6,001 tokens, 96 us) and 4.8 (one of 200,001, 86 us: at the first rate its bytes are 69, the rest
+// is the start and the join of 76 parts); e4m3 4.6 (64 of 128 to 8,192, 56 us), where a token is as many
+// instructions as in 16 bits, and its conversion, for half the bytes: nothing is full (47% of issue slots, 56% of
+// DRAM), the latency of a tile's steps at 12 warps an SM shows.
 #include "lr_attend.cuh"
 
 namespace lr {
