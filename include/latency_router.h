@@ -489,7 +489,7 @@ LR_API int lr_cache_read(lr_cache *c, const lr_cache_batch *b, int32_t T, int32_
  * 16-bit numbers are summed in fp32; the softmax weights are rounded to 16 bits for the second
  * product, over 16-bit caches to the cache's type.  8-bit codes are exact in either 16-bit type; K's scales are
  * applied to the scores in fp32, V's to the weights before they are rounded: in sequences of few rows (new tokens
- * times query heads a KV head: up to 8, or 16 where the batch has no more) to fp16, in others to the cache's dtype.
+ * times query heads a KV head: up to 8 or 16, by the batch) to fp16, in others to the cache's dtype.
  * In the former, bf16 queries are multiplied in fp16, divided by a power of two a row: elements below 2^-14 of the
  * row's largest are off by 2^-25 of it at most.  In the latter, values of V below 2^-14 in an fp16 cache are off by 2^-25
  * at most.  A cache that lr_cache_write has not filled may have scales of either sign, V's of
