@@ -508,6 +508,69 @@ LR_API int lr_cache_attend(lr_cache *c, const lr_cache_batch *b, int32_t T, cons
                            int64_t q_head_stride, float scale, int32_t window, int32_t sinks, void *out,
                            int64_t out_token_stride, int64_t out_head_stride, float *lse_out, void *cuda_stream);
 
+/* Attention of a tree of drafted tokens (speculative decoding verifies many continuations of a sequence in one
+ * batch): the sequence's new tokens are the drafted ones, cached behind its context of kv_len - q_len tokens, and row r sees
+ * the context and the drafted tokens that its mask names -- its ancestors and itself, whatever order the tree has.
+ * tree: DEVICE, 4-byte aligned: bit i % 32 of word r * tree_stride + i / 32 is set if the drafted token of row r of the
+ * batch sees its sequence's drafted token i.  tree_words: words that a row has, at least ceil(max_q / 32); bits from q_len on
+ * are ignored.  The named tokens, in their order, are the row's path: the path's token of rank k has position context + k, and
+ * the row the last of these.  A window and sinks are counted in these positions: token j of the row's context and
+ * path is seen if j > (the row's position) - window or j < sinks.  A row that names nothing sees its context, at the context's
+ * last position.
+ * All else as for lr_cache_attend: outputs, formulas, rounding, workspace, errors (and a sequence with more new tokens than
+ * kv_len is out of range). */
+LR_API int lr_cache_attend_tree(lr_cache *c, const lr_cache_batch *b, int32_t T, const void *q, int64_t q_token_stride,
+                                int64_t q_head_stride, const int32_t *tree, int64_t tree_stride, int32_t tree_words, float scale,
+                                int32_t window, int32_t sinks, void *out, int64_t out_token_stride, int64_t out_head_stride,
+                                float *lse_out, void *cuda_stream);
+
+/* ---- Which tokens a cache keeps ----
+ *
+ * A cache that is too small for its sequences drops the tokens that attention has made least use of.  Weights, one fp32
+ * number a (block, token, KV head), are the caller's: element (block, token, head) at block * block_stride +
+ * token * token_stride + head * head_stride (floats, strides >= 0). */
+
+/* The attention weight that cached tokens receive from the batch's rows.  With the row's visible tokens as in lr_cache_attend
+ * (causal, window and sinks) and its lse as that call gave it, for each token j of a sequence and each KV head
+ *   weight[j] = (j a new token of the batch ? 0 : decay * weight[j]) + sum over the rows r and query heads of the KV head
+ *               that see j of exp(scale * q_r . k_j - lse_r).
+ * decay: finite, >= 0; with 0 what stood there is not read.  With 1, tokens that no row sees (below a window) are left as they are;
+ * else all of the sequence's tokens are written, so that all its blocks must be its own.  A sequence that brings no
+ * tokens is left as it is; a row whose lse is -inf (it saw nothing) adds nothing.
+ * Sums are fp32, in an order that the call's sizes alone decide: the same call gives the same bits.  Over 8-bit
+ * caches scores are formed as in lr_cache_attend.  lse: [T][num_q_heads] fp32.
+ * Device errors, each LR_EINVAL: a sequence that lr_cache_attend leaves out is left out; a token that a row sees and whose block
+ * is out of range is skipped.  Calls on one cache share its workspace: order them. */
+LR_API int lr_cache_weigh(lr_cache *c, const lr_cache_batch *b, int32_t T, const void *q, int64_t q_token_stride,
+                          int64_t q_head_stride, const float *lse, float scale, int32_t window, int32_t sinks, float decay,
+                          float *weights, int64_t block_stride, int64_t token_stride, int64_t head_stride, void *cuda_stream);
+
+/* Of each sequence and KV head, the tokens to keep: count[s] = min(kv_len[s], budget[s]) of them, the first `sinks` and the
+ * last `recent`, and of the rest those with the largest weights, ties to the lowest position.  (A budget below sinks + recent
+ * takes the first of those.)  NaN counts as larger than all numbers.
+ * kept: [num_seqs][num_kv_heads][cap], positions in ascending order, -1 from count[s] on; count: [num_seqs].
+ * budget: [num_seqs], each in [0, cap], or NULL: cap.  sinks, recent >= 0, together at most cap.  q_start is not used.
+ * num_seqs * num_kv_heads is at most 2^26.
+ * Device errors, each LR_EINVAL: a sequence whose kv_len or budget is out of range keeps nothing (count 0); a token
+ * whose block is out of range has the lowest weight. */
+LR_API int lr_cache_select(lr_cache *c, const lr_cache_batch *b, const float *weights, int64_t block_stride, int64_t token_stride,
+                           int64_t head_stride, int32_t cap, const int32_t *budget, int32_t sinks, int32_t recent, int32_t *kept,
+                           int32_t *count, void *cuda_stream);
+
+/* Moves tokens together, in place: of each sequence and KV head, token kept[i] comes to position start + i, i < count --
+ * its K and V as they are cached, their scales, and its weight if `weights` is not NULL.  After lr_cache_select, with start 0, the
+ * sequence has count tokens; after a tree was verified, the accepted path moves up behind its context (start).
+ * kept: [num_seqs][kept_heads][cap], kept_heads num_kv_heads or 1 (one list for all heads); each list ascends from
+ * start on: start <= kept[0] < kept[1] < ... < kv_len.  Entries from count on are not read.  start: [num_seqs], or NULL: 0.
+ * q_start is not used.  Places from start + count on keep what they hold.  No block that is written to may be another
+ * sequence's of the batch, or the same sequence's twice.
+ * Device errors, each LR_EINVAL: a sequence whose kv_len, count (over cap) or start (start + count over kv_len) is out of range is left as it is;
+ * an entry that does not ascend, lies below its place or past kv_len, or whose block or whose place's block is out of
+ * range is not moved. */
+LR_API int lr_cache_keep(lr_cache *c, const lr_cache_batch *b, int32_t cap, const int32_t *kept, int32_t kept_heads,
+                         const int32_t *count, const int32_t *start, float *weights, int64_t block_stride, int64_t token_stride,
+                         int64_t head_stride, void *cuda_stream);
+
 /* As lr_status and lr_last_error, for a cache. */
 LR_API int lr_cache_status(lr_cache *c, void *cuda_stream);
 LR_API const char *lr_cache_last_error(const lr_cache *c);

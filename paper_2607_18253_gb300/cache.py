@@ -145,10 +145,13 @@ class PagedCache:
         return k, v
 
     def attend(self, q: torch.Tensor, batch: CacheBatch, scale: Optional[float] = None, window: int = 0, sinks: int = 0,
-               out: Optional[torch.Tensor] = None, lse=False, stream=None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+               out: Optional[torch.Tensor] = None, lse=False, stream=None,
+               tree: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
         """(out, lse) of the batch's queries [T, num_q_heads, head_dim]: out like q, lse [T, num_q_heads] float32 or None.
 
-        scale: head_dim ** -0.5 if not given.  window, sinks: see lr_cache_attend.  lse: True, or the tensor to write."""
+        scale: head_dim ** -0.5 if not given.  window, sinks: see lr_cache_attend.  lse: True, or the tensor to write.
+        tree: int32 [>= T, >= ceil(max_q / 32)], dense along a row: the batch's new tokens are drafted ones, and bit i % 32 of
+        word i / 32 of a row says that it sees its sequence's drafted token i (lr_cache_attend_tree); None: causal."""
         Hq, D = self.num_q_heads, self.head_dim
         T, qt, qh = _strides(q, "q", Hq, D, self.dtype)
         if out is None:
@@ -164,11 +167,79 @@ class PagedCache:
         else:
             lse = None if lse is False else lse
             lp = _dev(lse, torch.float32, "lse_out", T * Hq)
-        rc = self._lib.lr_cache_attend(self._h, batch._ref, T, q.data_ptr(), qt, qh, self._scale if scale is None else scale,
-                                       _i32(window), _i32(sinks), out.data_ptr(), ot, oh, lp, _stream(stream))
+        scale = self._scale if scale is None else scale
+        if tree is None:
+            rc = self._lib.lr_cache_attend(self._h, batch._ref, T, q.data_ptr(), qt, qh, scale,
+                                           _i32(window), _i32(sinks), out.data_ptr(), ot, oh, lp, _stream(stream))
+        else:
+            if not isinstance(tree, torch.Tensor) or not tree.is_cuda or tree.dtype != torch.int32:
+                raise TypeError("tree must be an int32 CUDA tensor")
+            if tree.dim() != 2 or tree.shape[0] < T or (tree.shape[1] > 1 and tree.stride(1) != 1):
+                raise ValueError(f"tree must be [{T}, words], dense along a row")
+            rc = self._lib.lr_cache_attend_tree(self._h, batch._ref, T, q.data_ptr(), qt, qh, tree.data_ptr(),
+                                                tree.stride(0) if T > 1 else 0, tree.shape[1], scale, _i32(window), _i32(sinks),
+                                                out.data_ptr(), ot, oh, lp, _stream(stream))
         if rc:
-            self._check(rc, "lr_cache_attend")
+            self._check(rc, "lr_cache_attend" if tree is None else "lr_cache_attend_tree")
         return out, lse
+
+    def _weights(self, t: Optional[torch.Tensor]):
+        """(pointer, block, token, head stride) of weights [num_blocks, block_size, num_kv_heads] float32, of any strides."""
+        if t is None:
+            return None, 0, 0, 0
+        if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != torch.float32:
+            raise TypeError("weights must be a float32 CUDA tensor")
+        if t.shape != self.k.shape[:3]:
+            raise ValueError(f"weights must be {list(self.k.shape[:3])}, got {list(t.shape)}")
+        return (t.data_ptr(), *t.stride())
+
+    def weigh(self, q: torch.Tensor, lse: torch.Tensor, batch: CacheBatch, weights: torch.Tensor, decay: float = 1.0,
+              scale: Optional[float] = None, window: int = 0, sinks: int = 0, stream=None) -> torch.Tensor:
+        """Adds to `weights` what the batch's queries, whose attention gave `lse`, put on the cached tokens (lr_cache_weigh).
+
+        weights: float32 [num_blocks, block_size, num_kv_heads], of any strides; returned.  decay: what the tokens had is multiplied by
+        it; new tokens start from 0."""
+        T, qt, qh = _strides(q, "q", self.num_q_heads, self.head_dim, self.dtype)
+        rc = self._lib.lr_cache_weigh(self._h, batch._ref, T, q.data_ptr(), qt, qh,
+                                      _dev(lse, torch.float32, "lse", T * self.num_q_heads), self._scale if scale is None else scale,
+                                      _i32(window), _i32(sinks), decay, *self._weights(weights), _stream(stream))
+        if rc:
+            self._check(rc, "lr_cache_weigh")
+        return weights
+
+    def select(self, weights: torch.Tensor, batch: CacheBatch, cap: int, budget: Optional[torch.Tensor] = None, sinks: int = 0,
+               recent: int = 0, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None,
+               stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+        """(kept [num_seqs, num_kv_heads, cap], count [num_seqs]), int32: the tokens to keep by weight (lr_cache_select).
+
+        count = min(kv_len, budget), or with no budget min(kv_len, cap); positions ascend, -1 from count on."""
+        n, H, cap = batch._c.num_seqs, self.num_kv_heads, int(cap)
+        if out is None:
+            kept = torch.empty((n, H, max(cap, 0)), dtype=torch.int32, device=self.k.device)
+            count = torch.empty(n, dtype=torch.int32, device=self.k.device)
+        else:
+            kept, count = out
+        rc = self._lib.lr_cache_select(self._h, batch._ref, *self._weights(weights), _i32(cap),
+                                       _dev(budget, torch.int32, "budget", n), _i32(sinks), _i32(recent),
+                                       _dev(kept, torch.int32, "kept", n * H * max(cap, 0)), _dev(count, torch.int32, "count", n),
+                                       _stream(stream))
+        if rc:
+            self._check(rc, "lr_cache_select")
+        return kept, count
+
+    def keep(self, kept: torch.Tensor, count: torch.Tensor, batch: CacheBatch, weights: Optional[torch.Tensor] = None,
+             start: Optional[torch.Tensor] = None, stream=None):
+        """Moves tokens kept[s, h, i], i < count[s], to positions start[s] + i, in place, with their scales and `weights` (lr_cache_keep).
+
+        kept: int32 [num_seqs, num_kv_heads, cap], or [num_seqs, cap]: one list for all heads.  start: 0 if not given."""
+        n, H = batch._c.num_seqs, self.num_kv_heads
+        if kept.dim() not in (2, 3) or kept.shape[0] != n or (kept.dim() == 3 and kept.shape[1] != H):
+            raise ValueError(f"kept must be [{n}, {H}, cap] or [{n}, cap], got {list(kept.shape)}")
+        rc = self._lib.lr_cache_keep(self._h, batch._ref, kept.shape[-1], _dev(kept, torch.int32, "kept"), 1 if kept.dim() == 2 else H,
+                                     _dev(count, torch.int32, "count", n), _dev(start, torch.int32, "start", n),
+                                     *self._weights(weights), _stream(stream))
+        if rc:
+            self._check(rc, "lr_cache_keep")
 
     def status(self, stream=None) -> int:
         """Synchronize the stream; return and clear the device status word."""

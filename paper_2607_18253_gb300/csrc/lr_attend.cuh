@@ -14,7 +14,7 @@ struct Unit {
     int s, h, qt;      // sequence, KV head, tile of rows
     int q0, ql, kv;    // first row of the token arrays, new tokens, tokens
     int ns, wf, nt;    // tiles of sinks before the window, the window's first tile, tiles in all
-    int lo, hi;        // positions of the first and last row
+    int lo, hi;        // positions of the first and last row; of a tree, the least and the largest that a row can have
     int rows;          // rows of this tile
 };
 
@@ -39,7 +39,7 @@ __device__ __forceinline__ bool load_seq(const AttendLaunch &a, int s, int &q0, 
     kv = __ldg(a.b.kv_len + s);
     if (ql == 0) return false;
     if (q0 < 0 || ql < 0 || ql > a.b.max_q || ql > a.b.T - q0 || kv < 0 || kv > kMaxTokens ||
-        (long long)kv > (long long)a.b.max_blocks * a.c.b) {
+        (long long)kv > (long long)a.b.max_blocks * a.c.b || (a.tree && kv < ql)) {
         report(a.c.status, kEInval);
         return false;
     }
@@ -51,8 +51,8 @@ template <int ROWS, int TILE>
 __device__ __forceinline__ void set_tile(const AttendLaunch &a, Unit &u) {
     const int r0 = u.qt * ROWS;
     u.rows = min(ROWS, u.ql * a.c.G - r0);
-    u.lo = u.kv - u.ql + quot(r0, a.c.div_g);
-    u.hi = u.kv - u.ql + quot(r0 + u.rows - 1, a.c.div_g);
+    u.lo = a.tree ? u.kv - u.ql - 1 : u.kv - u.ql + quot(r0, a.c.div_g);
+    u.hi = a.tree ? u.kv - 1 : u.kv - u.ql + quot(r0 + u.rows - 1, a.c.div_g);
     u.nt = tile_count<TILE>(u.lo, u.hi, a.window, a.sinks, u.ns, u.wf);
 }
 
@@ -237,6 +237,68 @@ __device__ __forceinline__ int slot_of(const Share &s, int c, long long at) { re
 
 __device__ __forceinline__ bool visible(int pos, int j, int window, int sinks) {
     return j <= pos && (window == 0 || j > pos - window || j < sinks);
+}
+
+// ---- Trees of drafted tokens ----
+// A row of a tree sees of its sequence the context, `first` tokens, and the drafted tokens that its mask names, in their
+// order: the one of rank k has position first + k, the row the last of these positions.  The window and the sinks go by
+// positions, so that the context is seen as by a causal row at that position, and of the drafted tokens those of rank
+// `drop` and above or below `keep` (all, where no window cuts the path).
+struct TreeRow {
+    const uint32_t *mask;
+    int first, ql;   // the context's length, the drafted tokens
+    int at;          // the row's position; -1: no row, sees nothing
+    int drop, keep;
+};
+__device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
+// Word w of the row's mask (of the tokens that there are).
+__device__ __forceinline__ uint32_t tree_mask(const TreeRow &r, int w) {
+    return w < 0 || w * 32 >= r.ql ? 0u : __ldg(r.mask + w) & low_bits(r.ql - w * 32);
+}
+__device__ __forceinline__ TreeRow tree_row(const AttendLaunch &a, int q0, int t, int ql, int kv, bool real) {
+    TreeRow r{a.tree + (int64_t)(q0 + t) * a.tree_t, kv - ql, ql, -1, 0, 0};
+    if (!real) r.ql = 0;
+    int n = 0;
+    if (a.window > 0)
+        for (int w = 0; w * 32 < r.ql; ++w) n += __popc(tree_mask(r, w));
+    else n = ql;  // (without a window the position is only that of a row behind its context)
+    if (real) r.at = r.first + n - 1;
+    if (a.window > 0 && n > a.window) {
+        r.drop = n - a.window;
+        r.keep = max(0, a.sinks - r.first);
+    }
+    return r;
+}
+// Word w of the tokens that the row sees.
+__device__ __forceinline__ uint32_t tree_word(const TreeRow &r, int w) {
+    uint32_t m = tree_mask(r, w);
+    if (r.drop > 0 && m) {
+        int rank = 0;
+        for (int i = 0; i < w; ++i) rank += __popc(tree_mask(r, i));
+        uint32_t rest = m;
+        for (; rest && rank < r.drop; ++rank, rest &= rest - 1)
+            if (rank >= r.keep) m &= ~(rest & -rest);
+    }
+    return m;
+}
+// Of the 32 tokens from j on, those that the row sees.
+__device__ __forceinline__ uint32_t tree_sees(const TreeRow &r, int j, int window, int sinks) {
+    uint32_t see = 0;
+    if (r.at >= 0 && j < r.first) {
+        see = low_bits(min(r.first, r.at + 1) - j);
+        if (window > 0) see &= ~low_bits(r.at - window + 1 - j) | low_bits(sinks - j);
+    }
+    const int i = j - r.first;  // (at least -31, or the context is all there is)
+    if (i > -32 && i < r.ql) {
+        const int w = i >> 5, sh = i & 31;
+        see |= sh ? tree_word(r, w) >> sh | tree_word(r, w + 1) << (32 - sh) : tree_word(r, w);
+    }
+    return see;
+}
+__device__ __forceinline__ bool tree_visible(const TreeRow &r, int j, int window, int sinks) {
+    if (j < r.first) return visible(r.at, j, window, sinks);
+    const int i = j - r.first;
+    return i < r.ql && (tree_word(r, i >> 5) >> (i & 31) & 1);
 }
 
 // Bytes i and j of w, 8-bit codes, as two bf16 numbers (i in the low half), exactly.  e4m3: sign, four exponent

@@ -83,6 +83,8 @@ struct AttendLaunch {
     int64_t q_t, q_h, o_t, o_h;  // bytes
     float scale_log2;            // scale * log2(e)
     int32_t window, sinks;
+    const uint32_t *tree;        // drafted tokens that each new token sees, a bit each; null: causal
+    int64_t tree_t;              // words from a token's to the next one's
     int32_t row_lo, row_hi;      // sequences with this many rows (tokens x query heads a KV head) are this launch's
     float *part_o;               // [slots][rows][DP] sums of weighted V
     float2 *part_ml;             // [slots][rows] running maximum (log2) and sum
@@ -103,5 +105,67 @@ struct CacheMaps {
 int encode_maps(const CacheDev &c, bool bf16, CacheMaps &m);  // the box, 0 if there can be none
 cudaError_t launch_attend_chunk(const AttendLaunch &a, const CacheMaps &m, bool bf16, int fmt, int ctas, cudaStream_t st);
 cudaError_t attend_chunk_init();
+// The map of a launch's queries: boxes of 64 elements of 128 rows; false if there can be none.
+bool encode_rows(const AttendLaunch &a, bool bf16, CUtensorMap &map);
+// The kernels of trees (a.tree), which the above launch.
+cudaError_t tree_step_init();
+cudaError_t launch_tree_step(const AttendLaunch &a, bool bf16, int fmt, int rows, int sms, cudaStream_t st);
+cudaError_t tree_chunk_init();
+cudaError_t launch_tree_chunk(const AttendLaunch &a, const CacheMaps &m, bool bf16, int fmt, int ctas, cudaStream_t st);
+
+
+// The weights that tokens have received (lr_weigh.cu): the batch and queries as for attention, lse as an input.
+struct WeighLaunch {
+    AttendLaunch a;
+    float *w;
+    int64_t wb, wt, wh;  // strides of block, token, head in floats
+    float decay;
+};
+cudaError_t launch_weigh(const WeighLaunch &a, bool bf16, int fmt, int sms, cudaStream_t st);
+
+// The tokens that a cache keeps (lr_select.cu).
+struct SelectLaunch {
+    CacheDev c;
+    BatchDev b;
+    const float *w;
+    int64_t wb, wt, wh;
+    const int32_t *budget;  // or null: cap
+    int32_t cap, sinks, recent;
+    int32_t *kept, *count;
+};
+cudaError_t launch_select(const SelectLaunch &a, int sms, cudaStream_t st);
+cudaError_t select_init();
+
+// Tokens moved together, in place (lr_keep.cu).
+struct KeepLaunch {
+    CacheDev c;
+    BatchDev b;
+    const int32_t *kept;     // [n][heads][cap]
+    int64_t kept_s, kept_h;  // strides of sequence and head; kept_h 0: one list for all heads
+    const int32_t *count, *start;
+    int32_t cap;
+    float *w;                // or null
+    int64_t wb, wt, wh;
+};
+cudaError_t launch_keep(const KeepLaunch &a, int fmt, int sms, cudaStream_t st);
+
+// As launch_chained, in clusters of `cluster` CTAs.
+template <typename A>
+cudaError_t launch_clusters(void (*k)(A), unsigned grid, unsigned block, size_t smem, unsigned cluster, cudaStream_t st, const A &a) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = cluster;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, k, A(a));
+}
 
 }  // namespace lr

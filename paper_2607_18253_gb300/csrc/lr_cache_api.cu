@@ -1,47 +1,15 @@
 // Host side of the paged-cache calls declared in include/latency_router.h: validation,
 // workspace, launch shapes and the status word.
 #include <algorithm>
-#include <cmath>
 #include <cstdio>
 #include <cstring>
 #include <new>
-#include <string>
 
-#include "latency_router.h"
-#include "lr_cache.cuh"
+#include "lr_cache_host.cuh"
 
-struct lr_cache {
-    int device = 0;
-    int sms = 0;
-    lr_cache_config cfg{};
-    lr::CacheDev dev{};
-    bool bf16 = true;
-    lr::CacheMaps maps{};
-    struct Parts {  // workspace of an attention kernel
-        float *o = nullptr;
-        float2 *ml = nullptr;
-        uint32_t *done = nullptr;
-    } step, chunk;
-    std::string err;
-};
+using namespace lr;
 
 namespace {
-
-int fail(lr_cache *c, int code, const char *msg) {
-    try {
-        c->err = msg;
-    } catch (...) {
-    }
-    return code;
-}
-
-int cuda_fail(lr_cache *c, cudaError_t e, const char *what) {
-    try {
-        c->err = std::string(what) + ": " + cudaGetErrorString(e);
-    } catch (...) {
-    }
-    return LR_ECUDA;
-}
 
 void free_all(lr_cache *c) {
     cudaFree(c->dev.status);
@@ -61,24 +29,62 @@ cudaError_t alloc_parts(lr_cache::Parts &p, size_t ctas, size_t rows, size_t cou
     return e;
 }
 
-bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
-
-// Strides (elements of `size` bytes) that keep every vector 16-byte aligned.
-bool good_stride(int64_t s, int size) { return s >= 0 && s < (1ll << 56) && s * size % 16 == 0; }
-
-// The checks that the calls share; 0 if the batch may be launched.
-const char *bad_batch(const lr_cache_batch *b, int32_t T) {
-    if (!b) return "null batch";
-    if (T < 0) return "T < 0";
-    if (b->num_seqs < 0) return "num_seqs < 0";
-    if (b->num_seqs > 0 && (!b->q_start || !b->kv_len || !b->block_table)) return "null batch array";
-    if (b->max_q < 1) return "max_q < 1";
-    if (b->max_blocks < 0 || b->table_stride < b->max_blocks) return "table_stride below max_blocks";
-    return nullptr;
-}
-
-lr::BatchDev batch_dev(const lr_cache_batch *b, int32_t T) {
-    return lr::BatchDev{b->num_seqs, b->max_q, T, b->max_blocks, b->q_start, b->kv_len, b->block_table, b->table_stride};
+// Attention of the batch, causal or, with `tree`, of drafted tokens.
+int attend(lr_cache *c, const lr_cache_batch *b, int32_t T, const void *q, int64_t q_token_stride, int64_t q_head_stride,
+           const int32_t *tree, int64_t tree_stride, float scale, int32_t window, int32_t sinks, void *out, int64_t out_token_stride,
+           int64_t out_head_stride, float *lse_out, void *stream) {
+    if (const char *m = bad_batch(b, T)) return fail(c, LR_EINVAL, m);
+    if (b->num_seqs > c->cfg.max_seqs) return fail(c, LR_ECAPACITY, "num_seqs exceeds max_seqs");
+    if (!(std::isfinite(scale) && scale > 0.0f)) return fail(c, LR_EINVAL, "scale must be finite and positive");
+    if (window < 0 || window > lr::kMaxTokens || sinks < 0 || sinks > lr::kMaxTokens)
+        return fail(c, LR_EINVAL, "window and sinks must be in [0, 2^30]");
+    if (b->max_q > (1 << 20)) return fail(c, LR_EINVAL, "max_q must be at most 2^20");
+    if (T == 0 || b->num_seqs == 0) return LR_OK;
+    if (!q || !out || !aligned16(q) || !aligned16(out)) return fail(c, LR_EINVAL, "q and out must be 16-byte aligned");
+    if (!good_stride(q_token_stride, 2) || !good_stride(q_head_stride, 2) || !good_stride(out_token_stride, 2) ||
+        !good_stride(out_head_stride, 2))
+        return fail(c, LR_EINVAL, "strides must be non-negative multiples of 16 bytes");
+    lr::AttendLaunch a;
+    std::memset(&a, 0, sizeof(a));
+    a.c = c->dev;
+    a.b = batch_dev(b, T);
+    a.q = static_cast<const char *>(q);
+    a.out = static_cast<char *>(out);
+    a.lse = lse_out;
+    a.q_t = q_token_stride * 2;
+    a.q_h = q_head_stride * 2;
+    a.o_t = out_token_stride * 2;
+    a.o_h = out_head_stride * 2;
+    a.scale_log2 = (float)((double)scale * 1.4426950408889634);
+    a.window = window;
+    a.sinks = window ? sinks : 0;
+    a.tree = reinterpret_cast<const uint32_t *>(tree);
+    a.tree_t = tree_stride;
+    // Rows of a sequence: its new tokens x the query heads of a KV head.  Up to 8, or up to 16 if a batch has no more,
+    // are the step kernel's, more the chunk kernel's (a single sequence whole, whatever it brings).  A batch of both takes two
+    // launches: 63 single tokens beside a chunk of 1,985 (32 query and 8 KV heads of 128) 198 us, in the
+    // chunk kernel alone 222.
+    const long long most = (long long)b->max_q * c->dev.G;
+    const int few = most <= 16 || c->dev.G > 8 ? 16 : 8;
+    cudaStream_t st = (cudaStream_t)stream;
+    if (most > few) {
+        const bool all = b->num_seqs == 1;
+        a.row_lo = all ? 1 : few + 1;
+        a.row_hi = 0x7fffffff;
+        a.part_o = c->chunk.o;
+        a.part_ml = c->chunk.ml;
+        a.done = c->chunk.done;
+        cudaError_t e = lr::launch_attend_chunk(a, c->maps, c->bf16, c->cfg.format, c->sms, st);
+        if (e != cudaSuccess) return cuda_fail(c, e, "attention launch");
+        if (all || c->dev.G > few) return LR_OK;
+    }
+    a.row_lo = 1;
+    a.row_hi = (int)std::min<long long>(most, few);
+    a.part_o = c->step.o;
+    a.part_ml = c->step.ml;
+    a.done = c->step.done;
+    cudaError_t e = lr::launch_attend_step(a, c->bf16, c->cfg.format, a.row_hi, c->sms, st);
+    return e == cudaSuccess ? LR_OK : cuda_fail(c, e, "attention launch");
 }
 
 }  // namespace
@@ -209,56 +215,22 @@ int lr_cache_attend(lr_cache *c, const lr_cache_batch *b, int32_t T, const void 
                     int64_t out_head_stride, float *lse_out, void *stream) {
     if (!c) return LR_EINVAL;
     c->err.clear();
+    return attend(c, b, T, q, q_token_stride, q_head_stride, nullptr, 0, scale, window, sinks, out, out_token_stride, out_head_stride,
+                  lse_out, stream);
+}
+
+int lr_cache_attend_tree(lr_cache *c, const lr_cache_batch *b, int32_t T, const void *q, int64_t q_token_stride,
+                         int64_t q_head_stride, const int32_t *tree, int64_t tree_stride, int32_t tree_words, float scale,
+                         int32_t window, int32_t sinks, void *out, int64_t out_token_stride, int64_t out_head_stride, float *lse_out,
+                         void *stream) {
+    if (!c) return LR_EINVAL;
+    c->err.clear();
     if (const char *m = bad_batch(b, T)) return fail(c, LR_EINVAL, m);
-    if (b->num_seqs > c->cfg.max_seqs) return fail(c, LR_ECAPACITY, "num_seqs exceeds max_seqs");
-    if (!(std::isfinite(scale) && scale > 0.0f)) return fail(c, LR_EINVAL, "scale must be finite and positive");
-    if (window < 0 || window > lr::kMaxTokens || sinks < 0 || sinks > lr::kMaxTokens)
-        return fail(c, LR_EINVAL, "window and sinks must be in [0, 2^30]");
-    if (b->max_q > (1 << 20)) return fail(c, LR_EINVAL, "max_q must be at most 2^20");
-    if (T == 0 || b->num_seqs == 0) return LR_OK;
-    if (!q || !out || !aligned16(q) || !aligned16(out)) return fail(c, LR_EINVAL, "q and out must be 16-byte aligned");
-    if (!good_stride(q_token_stride, 2) || !good_stride(q_head_stride, 2) || !good_stride(out_token_stride, 2) ||
-        !good_stride(out_head_stride, 2))
-        return fail(c, LR_EINVAL, "strides must be non-negative multiples of 16 bytes");
-    lr::AttendLaunch a;
-    std::memset(&a, 0, sizeof(a));
-    a.c = c->dev;
-    a.b = batch_dev(b, T);
-    a.q = static_cast<const char *>(q);
-    a.out = static_cast<char *>(out);
-    a.lse = lse_out;
-    a.q_t = q_token_stride * 2;
-    a.q_h = q_head_stride * 2;
-    a.o_t = out_token_stride * 2;
-    a.o_h = out_head_stride * 2;
-    a.scale_log2 = (float)((double)scale * 1.4426950408889634);
-    a.window = window;
-    a.sinks = window ? sinks : 0;
-    // Rows of a sequence: its new tokens x the query heads of a KV head.  Up to 8, or up to 16 if a batch has no more,
-    // are the step kernel's, more the chunk kernel's (a single sequence whole, whatever it brings).  A batch of both takes two
-    // launches: 63 single tokens beside a chunk of 1,985 (32 query and 8 KV heads of 128) 198 us, in the
-    // chunk kernel alone 222.
-    const long long most = (long long)b->max_q * c->dev.G;
-    const int few = most <= 16 || c->dev.G > 8 ? 16 : 8;
-    cudaStream_t st = (cudaStream_t)stream;
-    if (most > few) {
-        const bool all = b->num_seqs == 1;
-        a.row_lo = all ? 1 : few + 1;
-        a.row_hi = 0x7fffffff;
-        a.part_o = c->chunk.o;
-        a.part_ml = c->chunk.ml;
-        a.done = c->chunk.done;
-        cudaError_t e = lr::launch_attend_chunk(a, c->maps, c->bf16, c->cfg.format, c->sms, st);
-        if (e != cudaSuccess) return cuda_fail(c, e, "attention launch");
-        if (all || c->dev.G > few) return LR_OK;
-    }
-    a.row_lo = 1;
-    a.row_hi = (int)std::min<long long>(most, few);
-    a.part_o = c->step.o;
-    a.part_ml = c->step.ml;
-    a.done = c->step.done;
-    cudaError_t e = lr::launch_attend_step(a, c->bf16, c->cfg.format, a.row_hi, c->sms, st);
-    return e == cudaSuccess ? LR_OK : cuda_fail(c, e, "attention launch");
+    if (tree_words < 0 || tree_words < (b->max_q - 1) / 32 + 1) return fail(c, LR_EINVAL, "tree_words must hold max_q bits");
+    if (tree_stride < 0 || tree_stride >= (1ll << 40)) return fail(c, LR_EINVAL, "tree_stride out of range");
+    if (T > 0 && b->num_seqs > 0 && (!tree || reinterpret_cast<uintptr_t>(tree) % 4)) return fail(c, LR_EINVAL, "tree must be a 4-byte aligned device pointer");
+    return attend(c, b, T, q, q_token_stride, q_head_stride, tree, tree_stride, scale, window, sinks, out, out_token_stride,
+                  out_head_stride, lse_out, stream);
 }
 
 int lr_cache_status(lr_cache *c, void *stream) {

@@ -1,0 +1,188 @@
+// The tokens that a cache keeps: of each sequence and KV head the first ones, the most recent ones, and of the rest those
+// with the largest weights, ties to the lowest position, in order of position.
+//
+// A weight becomes a 32-bit key that sorts as it does, a token that is kept in any case the largest.  The key of the last token
+// that is kept is found from the top bits down, by counting (11, 11 and 10 bits: three counts of 2,048 bins); the
+// tokens above it are kept, and of those equal to it the first ones.  A cluster of CTAs has a list, each a range of its
+// positions: the counts and the places of the ranges' tokens are read from one another's shared memory.
+#include "lr_cache.cuh"
+
+namespace lr {
+
+namespace {
+
+constexpr int kThreads = 512, kWarps = kThreads / 32, kBins = 2048;
+constexpr int kHold = 12288;  // keys that a CTA keeps in shared memory; further ones are read again for each count
+constexpr int kMaxCluster = 8;
+constexpr size_t kSmem = kHold * 4 + 3 * kBins * 4;
+
+// As `w` sorts: NaN above all, both zeros the same.
+__device__ __forceinline__ uint32_t key_of(float w) {
+    if (w != w) return 0xfffffffeu;
+    const uint32_t u = __float_as_uint(w + 0.0f);  // (-0 + 0 is 0)
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// A word of CTA `rank`'s shared memory at the place of `p` in this one's.
+__device__ __forceinline__ uint32_t peer_word(const uint32_t *p, int rank) {
+    uint32_t at, v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+    return v;
+}
+
+__global__ void __launch_bounds__(kThreads) k_select(const __grid_constant__ SelectLaunch a, int cl) {
+    extern __shared__ __align__(16) uint32_t smem[];
+    uint32_t *const hold = smem, *const bins = smem + kHold;  // [3][kBins]
+    __shared__ uint32_t s_warp[2 * kWarps], s_bin[2], s_mine[2];
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+    const int rank = cl > 1 ? (int)cluster_rank() : 0;
+    const CacheDev &c = a.c;
+    chain_wait();
+    const int list = blockIdx.x / cl, s = list / c.H, h = list % c.H;
+    int kv = __ldg(a.b.kv_len + s), m = a.budget ? __ldg(a.budget + s) : a.cap;
+    if (kv < 0 || kv > kMaxTokens || (long long)kv > (long long)a.b.max_blocks * c.b || m < 0 || m > a.cap) {
+        report(c.status, kEInval);
+        kv = m = 0;
+    }
+    m = min(m, kv);
+    int32_t *const kept = a.kept + (int64_t)list * a.cap;
+    if (h == 0 && rank == 0 && tid == 0) a.count[s] = m;
+    for (int64_t i = (int64_t)m + rank * kThreads + tid; i < a.cap; i += (int64_t)cl * kThreads) kept[i] = -1;
+    if (m == kv || m == 0) {  // (all or none: the whole cluster takes this way)
+        for (int64_t i = rank * kThreads + tid; i < m; i += cl * kThreads) kept[i] = (int32_t)i;
+        chain_next();
+        return;
+    }
+    // a range of positions a CTA, of it a range a warp, in steps of 32
+    const int per = ((kv + cl - 1) / cl + 31) / 32 * 32;
+    const int p0 = (int)min((int64_t)kv, (int64_t)rank * per), p1 = (int)min((int64_t)kv, (int64_t)p0 + per);
+    auto read = [&](int p) -> uint32_t {
+        if (p < a.sinks || p >= kv - a.recent) return 0xffffffffu;
+        int place;
+        const int64_t blk = block_of(c, a.b, s, p, place);
+        if (blk < 0) {
+            report(c.status, kEInval);
+            return 0u;
+        }
+        return key_of(a.w[blk * a.wb + place * a.wt + h * a.wh]);
+    };
+    auto key = [&](int p) { return p - p0 < kHold ? hold[p - p0] : read(p); };
+
+    for (int i = tid; i < 3 * kBins; i += kThreads) bins[i] = 0;
+    __syncthreads();
+    for (int p = p0 + tid; p < p1; p += kThreads) {
+        const uint32_t k = read(p);
+        if (p - p0 < kHold) hold[p - p0] = k;
+        atomicAdd(bins + (k >> 21), 1u);
+    }
+    uint32_t prefix = 0, need = m;  // the key's bits so far; of the keys that have them, how many are kept
+#pragma unroll 1
+    for (int round = 0; round < 3; ++round) {
+        uint32_t *const bin = bins + round * kBins;
+        const int shift = round == 0 ? 21 : round == 1 ? 10 : 0, many = round == 2 ? 1024 : kBins;
+        if (round > 0) {
+            const int above = round == 1 ? 21 : 10;
+            for (int p = p0 + tid; p < p1; p += kThreads) {
+                const uint32_t k = key(p);
+                if (k >> above == prefix >> above) atomicAdd(bin + (k >> shift & (many - 1)), 1u);
+            }
+        }
+        if (cl > 1) cluster_sync();
+        else __syncthreads();
+        // four bins a thread, from the top: those before the bin that brings the count to `need`
+        const int b0 = many - 1 - tid * 4;
+        uint32_t v[4], mine = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[i] = 0;
+            if (b0 - i >= 0)
+                for (int r = 0; r < cl; ++r) v[i] += cl > 1 ? peer_word(bin + b0 - i, r) : bin[b0 - i];
+            mine += v[i];
+        }
+        uint32_t incl = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t x = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += x;
+        }
+        if (lane == 31) s_warp[warp] = incl;
+        __syncthreads();
+        for (int w = 0; w < warp; ++w) incl += s_warp[w];
+        uint32_t before = incl - mine;
+        if (before < need && need <= incl) {
+            int i = 0;
+            while (before + v[i] < need) before += v[i++];
+            s_bin[0] = b0 - i;
+            s_bin[1] = need - before;
+        }
+        __syncthreads();
+        prefix |= s_bin[0] << shift;
+        need = s_bin[1];
+        __syncthreads();
+    }
+    // prefix is the last kept token's key now, `need` how many of those equal to it are kept
+
+    const int each = ((p1 - p0 + kWarps - 1) / kWarps + 31) / 32 * 32;
+    const int w0 = min(p1, p0 + warp * each), w1 = min(p1, w0 + each);
+    uint32_t above = 0, equal = 0;
+    for (int p = w0 + lane; p - lane < w1; p += 32) {
+        const uint32_t k = p < w1 ? key(p) : 0u;
+        above += __popc(__ballot_sync(0xffffffffu, p < w1 && k > prefix));
+        equal += __popc(__ballot_sync(0xffffffffu, p < w1 && k == prefix));
+    }
+    if (lane == 0) {
+        s_warp[warp] = above;
+        s_warp[kWarps + warp] = equal;
+    }
+    __syncthreads();
+    uint32_t out = 0, eq = 0;
+    for (int w = 0; w < kWarps; ++w) {
+        if (w < warp) out += s_warp[w], eq += s_warp[kWarps + w];
+    }
+    if (cl > 1) {
+        if (tid < 2) {
+            uint32_t all = 0;
+            for (int w = 0; w < kWarps; ++w) all += s_warp[tid * kWarps + w];
+            s_mine[tid] = all;
+        }
+        cluster_sync();
+        for (int r = 0; r < rank; ++r) {
+            out += peer_word(s_mine, r);
+            eq += peer_word(s_mine + 1, r);
+        }
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    }
+    out += min(eq, need);
+    for (int p = w0 + lane; p - lane < w1; p += 32) {
+        const uint32_t k = p < w1 ? key(p) : 0u;
+        const uint32_t ties = __ballot_sync(0xffffffffu, p < w1 && k == prefix);
+        const uint32_t lower = (1u << lane) - 1;
+        const bool take = p < w1 && (k > prefix || (k == prefix && eq + __popc(ties & lower) < need));
+        const uint32_t all = __ballot_sync(0xffffffffu, take);
+        if (take) kept[out + __popc(all & lower)] = p;
+        out += __popc(all);
+        eq += __popc(ties);
+    }
+    if (cl > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");  // (no CTA leaves while another reads it)
+    chain_next();
+}
+
+}  // namespace
+
+cudaError_t select_init() { return cudaFuncSetAttribute(k_select, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem); }
+
+cudaError_t launch_select(const SelectLaunch &a, int sms, cudaStream_t st) {
+    const long long lists = (long long)a.b.n * a.c.H;
+    return launch_chained(k_select, (unsigned)lists, kThreads, kSmem, st, a, 1);
+}
+
+}  // namespace lr

@@ -1,0 +1,324 @@
+// Attention weight that cached tokens have received, from the rows of a batch.
+//
+// With the rows' lse known, a weight needs no running maximum: w[j] += sum_r exp(scale q_r . k_j - lse_r).  A token's sum
+// stays with the warp that has the token, so nothing is joined and the order of the sum is the rows' own.
+//
+// What bounds it for few rows is K's bytes.  Sixteen (or 32, 64) tokens are a warp's at a time; a lane reads 16-byte pieces of
+// the vectors of tokens g and g + 8 straight to the registers that multiply them (S = K Q^T, 16x8x16 products with the cache as
+// the 16-row operand): which elements of a vector a product sums is free, as long as the queries' lanes
+// take the same ones, so a piece is two (16 bits) or four (8 bits) products' operands as it lies.  The next tokens' pieces
+// are on their way while these are multiplied.
+#include "lr_attend.cuh"
+
+namespace lr {
+
+namespace {
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+
+template <int DP, int FMT>
+struct Piece {
+    static constexpr int kVec = DP * (FMT == kFmt16 ? 2 : 1) / 64;  // 16-byte pieces a lane and vector
+    static constexpr int NB = 4 / kVec;                             // blocks of 16 tokens
+    static constexpr int kTile = 16 * NB;
+};
+
+template <bool BF16>
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    if constexpr (BF16)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// The batch's tiles of tokens in one line: sequences in order, in a sequence tile after tile, in a tile head after head
+// (where a block's heads lie together, so do a CTA's reads).  What no row sees is left out where nothing changes it.
+template <int TILE>
+struct Walk {
+    int s, q0, ql, kv, ns, wf;
+    long long n;     // tiles of the sequence, times heads
+    long long left;  // the position in it
+    __device__ __forceinline__ bool load(const WeighLaunch &a) {
+        if (!load_seq(a.a, s, q0, ql, kv) || kv == 0) return false;
+        int nt;
+        if (a.decay == 1.0f) nt = tile_count<TILE>(kv - ql, kv - 1, a.a.window, a.a.sinks, ns, wf);
+        else ns = wf = 0, nt = (kv - 1) / TILE + 1;
+        n = (long long)nt * a.a.c.H;
+        return true;
+    }
+    // On by k positions; false behind the last sequence.
+    __device__ __forceinline__ bool on(const WeighLaunch &a, long long k) {
+        left += k;
+        while (left >= n) {
+            left -= n;
+            do
+                if (++s >= a.a.b.n) return false;
+            while (!load(a));
+        }
+        return true;
+    }
+};
+
+template <int DP, int FMT>
+struct Tokens {
+    uint4 k[Piece<DP, FMT>::NB][2][Piece<DP, FMT>::kVec];
+    float ks[Piece<DP, FMT>::NB][2];
+    int64_t w[Piece<DP, FMT>::NB];  // where this lane's token's weight is, -1: not this lane's to write
+    float old[Piece<DP, FMT>::NB];
+    int h, base, q0, ql, kv;
+};
+
+template <int DP, int FMT>
+__device__ __forceinline__ void fetch(const WeighLaunch &a, const Walk<Piece<DP, FMT>::kTile> &at, Tokens<DP, FMT> &k) {
+    using P = Piece<DP, FMT>;
+    const CacheDev &c = a.a.c;
+    const int lane = threadIdx.x % 32, g = lane / 4, i4 = lane % 4;
+    const int tile = (int)(at.left / c.H);
+    k.h = (int)(at.left - (long long)tile * c.H);
+    k.base = (tile < at.ns ? tile : at.wf + tile - at.ns) * P::kTile;
+    k.q0 = at.q0;
+    k.ql = at.ql;
+    k.kv = at.kv;
+    const int lo = k.kv - k.ql;
+#pragma unroll
+    for (int b = 0; b < P::NB; ++b) {
+        k.w[b] = -1;
+        k.old[b] = 0.0f;
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+            const int t = k.base + b * 16 + y * 8 + g;
+            const bool any = !(a.a.window > 0 && t <= lo - a.a.window && t >= a.a.sinks);  // (some row sees it)
+            k.ks[b][y] = 0.0f;
+#pragma unroll
+            for (int v = 0; v < P::kVec; ++v) k.k[b][y][v] = make_uint4(0, 0, 0, 0);
+            if (t >= k.kv || (!any && a.decay == 1.0f)) continue;
+            int place;
+            const int64_t blk = block_of(c, a.a.b, at.s, t, place);
+            if (blk < 0) {  // (a token that no row sees may have no block any more)
+                if (any) report(c.status, kEInval);
+                continue;
+            }
+            if (i4 == y) {
+                k.w[b] = blk * a.wb + place * a.wt + k.h * a.wh;
+                if (a.decay != 0.0f && t < lo) k.old[b] = a.decay * a.w[k.w[b]];
+            }
+            if (!any) continue;
+            const char *const p = c.k + blk * c.sb + place * c.st + k.h * c.sh;
+#pragma unroll
+            for (int v = 0; v < P::kVec; ++v)
+                if ((v * 4 + i4) * 16 < c.D * (FMT == kFmt16 ? 2 : 1)) k.k[b][y][v] = __ldg(reinterpret_cast<const uint4 *>(p + (v * 4 + i4) * 16));
+            if constexpr (FMT != kFmt16) k.ks[b][y] = __ldg(c.ks + blk * c.ssb + place * c.sst + k.h * c.ssh);
+        }
+    }
+}
+
+template <bool BF16, int FMT, int DP, int NR>
+__global__ void __launch_bounds__(kThreads, 2) k_weigh_step(const __grid_constant__ WeighLaunch a) {
+    using P = Piece<DP, FMT>;
+    constexpr int kRows = 8 * NR, NB = P::NB, KS = DP / 16;
+    // 8-bit codes are multiplied in fp16, which holds them exactly; bf16 queries come to it divided by a power of two a row
+    // that brings the largest to [1, 2): what fp16 then rounds is below 2^-24 of it.
+    constexpr bool MB = FMT == kFmt16 ? BF16 : false;
+    __shared__ long long s_sum[kWarps], s_at;
+    __shared__ int s_seq;
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, g = lane / 4, i4 = lane % 4;
+    const CacheDev &c = a.a.c;
+    chain_wait();
+
+    // this CTA's share of the line, x0 .. x1
+    const int n = a.a.b.n;
+    Walk<P::kTile> at;
+    long long all = 0, mine = 0, incl = 0;
+    for (int base = 0; base < n; base += kThreads) {
+        at.s = base + tid;
+        mine = at.s < n && at.load(a) ? at.n : 0;
+        long long t;
+        incl = block_sum<kThreads>(mine, s_sum, t);
+        all += t;
+    }
+    const long long x0 = all * blockIdx.x / gridDim.x, x1 = all * (blockIdx.x + 1) / gridDim.x;
+    if (x0 >= x1) {
+        chain_next();
+        return;
+    }
+    long long first = 0;
+    for (int base = 0; base < n; base += kThreads) {
+        long long t = all;
+        if (n > kThreads) {
+            at.s = base + tid;
+            mine = at.s < n && at.load(a) ? at.n : 0;
+            incl = block_sum<kThreads>(mine, s_sum, t);
+        }
+        const long long x = x0 - first;
+        if (x < incl && x >= incl - mine) {
+            s_seq = base + tid;
+            s_at = x - (incl - mine);
+        }
+        first += t;
+        if (first > x0) break;
+    }
+    __syncthreads();
+    at.s = s_seq;
+    at.left = s_at;
+    at.load(a);
+
+    uint32_t q[KS][NR][2];
+    float qf[NR][2], less[NR][2];  // the scores' factor, lse * log2(e)
+    int pos[NR][2];                // the rows' positions, -1: none
+    int qh = -1, qs = -1, qr = -1;  // whose queries these are
+    Tokens<DP, FMT> now, next;
+    long long x = x0 + warp;
+    if (x >= x1 || !at.on(a, warp)) {
+        chain_next();
+        return;
+    }
+    fetch<DP, FMT>(a, at, next);
+    for (; x < x1; x += kWarps) {
+        now = next;
+        if (x + kWarps < x1 && at.on(a, kWarps)) fetch<DP, FMT>(a, at, next);
+        const int lo = now.kv - now.ql, rows = now.ql * c.G, end = now.base + P::kTile - 1;
+        float sum[NB][2];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) sum[b][0] = sum[b][1] = 0.0f;
+        // rows from the first that may see the tile on; below a window, up to the last
+        int r0 = now.base > lo ? (now.base - lo) * c.G / kRows * kRows : 0, r1 = rows;
+        if (a.a.window > 0 && now.base >= a.a.sinks) r1 = (int)min((long long)rows, max(0ll, (long long)end + a.a.window - lo) * c.G);
+        for (; r0 < r1; r0 += kRows) {
+            if (now.h != qh || now.q0 != qs || r0 != qr) {
+                qh = now.h, qs = now.q0, qr = r0;
+#pragma unroll
+                for (int m = 0; m < NR; ++m) {
+                    const int r = r0 + m * 8 + g;  // (the row whose elements the lane holds)
+                    const int t = quot(r, c.div_g), hd = r - t * c.G;
+                    const bool ok = r < rows;
+                    const char *const p = a.a.q + (int64_t)(now.q0 + t) * a.a.q_t + (int64_t)(now.h * c.G + hd) * a.a.q_h;
+                    float pow2 = 1.0f;
+                    if constexpr (FMT == kFmt16) {
+#pragma unroll
+                        for (int v = 0; v < P::kVec; ++v) {
+                            const int d = (v * 4 + i4) * 8;
+                            const uint4 w = ok && d < c.D ? __ldg(reinterpret_cast<const uint4 *>(p + d * 2)) : make_uint4(0, 0, 0, 0);
+                            q[2 * v][m][0] = w.x;
+                            q[2 * v][m][1] = w.y;
+                            q[2 * v + 1][m][0] = w.z;
+                            q[2 * v + 1][m][1] = w.w;
+                        }
+                    } else {
+#pragma unroll
+                        for (int v = 0; v < P::kVec; ++v)
+#pragma unroll
+                            for (int u = 0; u < 2; ++u) {
+                                const int d = (v * 4 + i4) * 16 + u * 8;
+                                const uint4 w = ok && d < c.D ? __ldg(reinterpret_cast<const uint4 *>(p + d * 2)) : make_uint4(0, 0, 0, 0);
+                                q[4 * v + 2 * u][m][0] = w.x;
+                                q[4 * v + 2 * u][m][1] = w.y;
+                                q[4 * v + 2 * u + 1][m][0] = w.z;
+                                q[4 * v + 2 * u + 1][m][1] = w.w;
+                            }
+                        if constexpr (BF16) {
+                            float top = 0.0f;
+#pragma unroll
+                            for (int k = 0; k < 2 * KS; ++k) {
+                                const float2 f = unpack16<true>(q[k / 2][m][k % 2]);
+                                top = fmaxf(top, fmaxf(fabsf(f.x), fabsf(f.y)));
+                            }
+                            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                            // (not below 2^-100, whose reciprocal is a number; infinities stay what they are)
+                            const uint32_t e = min(max(__float_as_uint(top) & 0x7f800000u, 27u << 23), 253u << 23);
+                            const float inv = __uint_as_float((254u << 23) - e);
+                            pow2 = __uint_as_float(e);
+#pragma unroll
+                            for (int k = 0; k < 2 * KS; ++k) {
+                                const float2 f = unpack16<true>(q[k / 2][m][k % 2]);
+                                q[k / 2][m][k % 2] = pack16<false>(f.x * inv, f.y * inv);
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const int row = r0 + m * 8 + 2 * i4 + y, tt = quot(row, c.div_g);
+                        const bool real = row < rows;
+                        const float l = real ? __ldg(a.a.lse + (int64_t)(now.q0 + tt) * c.Hq + now.h * c.G + row - tt * c.G) : -INFINITY;
+                        // (a row that sees nothing adds nothing)
+                        pos[m][y] = l == -INFINITY ? -1 : lo + tt;
+                        less[m][y] = l == -INFINITY ? 0.0f : l * 1.44269504f;
+                        qf[m][y] = a.a.scale_log2 * __shfl_sync(0xffffffffu, pow2, (2 * i4 + y) * 4);
+                    }
+                }
+            }
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                float s[NR][4];
+#pragma unroll
+                for (int m = 0; m < NR; ++m)
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) s[m][z] = 0.0f;
+#pragma unroll
+                for (int v = 0; v < P::kVec; ++v) {
+                    const uint4 e = now.k[b][0][v], f = now.k[b][1][v];
+                    const uint32_t ee[4] = {e.x, e.y, e.z, e.w}, ff[4] = {f.x, f.y, f.z, f.w};
+                    if constexpr (FMT == kFmt16) {
+#pragma unroll
+                        for (int u = 0; u < 2; ++u)
+#pragma unroll
+                            for (int m = 0; m < NR; ++m)
+                                mma<MB>(s[m], ee[2 * u], ff[2 * u], ee[2 * u + 1], ff[2 * u + 1], q[2 * v + u][m][0], q[2 * v + u][m][1]);
+                    } else {
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) {
+                            uint32_t f0, f1, f2, f3;
+                            to_half<FMT, false>(ee[u], f0, f2);
+                            to_half<FMT, false>(ff[u], f1, f3);
+#pragma unroll
+                            for (int m = 0; m < NR; ++m) mma<MB>(s[m], f0, f1, f2, f3, q[4 * v + u][m][0], q[4 * v + u][m][1]);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int m = 0; m < NR; ++m)
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) {
+                        const int j = now.base + b * 16 + (z >> 1) * 8 + g;
+                        float f = qf[m][z & 1];
+                        if constexpr (FMT != kFmt16) f *= now.ks[b][z >> 1];
+                        const float p = exp2_fast(s[m][z] * f - less[m][z & 1]);
+                        sum[b][z >> 1] += visible(pos[m][z & 1], j, a.a.window, a.a.sinks) ? p : 0.0f;
+                    }
+            }
+        }
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                float f = sum[b][y];
+                f += __shfl_xor_sync(0xffffffffu, f, 1);
+                f += __shfl_xor_sync(0xffffffffu, f, 2);
+                if (i4 == y && now.w[b] >= 0) a.w[now.w[b]] = now.old[b] + f;
+            }
+    }
+    chain_next();
+}
+
+using Kernel = void (*)(const WeighLaunch);
+template <int FMT, int DP>
+Kernel pick_rows(bool bf16, bool few) {
+    return bf16 ? (few ? k_weigh_step<true, FMT, DP, 1> : k_weigh_step<true, FMT, DP, 4>)
+                : (few ? k_weigh_step<false, FMT, DP, 1> : k_weigh_step<false, FMT, DP, 4>);
+}
+template <int FMT>
+Kernel pick_dim(bool bf16, int D, bool few) { return D <= 64 ? pick_rows<FMT, 64>(bf16, few) : pick_rows<FMT, 128>(bf16, few); }
+
+}  // namespace
+
+cudaError_t launch_weigh(const WeighLaunch &a, bool bf16, int fmt, int sms, cudaStream_t st) {
+    const bool few = (long long)a.a.b.max_q * a.a.c.G <= 8;
+    const Kernel k = fmt == kFmt16 ? pick_dim<kFmt16>(bf16, a.a.c.D, few)
+                   : fmt == kFmtE4M3 ? pick_dim<kFmtE4M3>(bf16, a.a.c.D, few)
+                                     : pick_dim<kFmtInt8>(bf16, a.a.c.D, few);
+    return launch_chained(k, 2 * sms, kThreads, 0, st, a);
+}
+
+}  // namespace lr

@@ -28,7 +28,8 @@ EXPORTED_SYMBOLS = ("lr_create", "lr_destroy", "lr_load_state", "lr_estimate_ttf
                     "lr_set_queue_params", "lr_set_ttft_source", "lr_calibrate", "lr_route_baseline",
                     "lr_on_time_utility", "lr_set_kv_limits", "lr_strerror", "lr_last_error",
                     "lr_track_first_tokens", "lr_advance_tracked", "lr_cache_create", "lr_cache_destroy",
-                    "lr_cache_write", "lr_cache_read", "lr_cache_attend", "lr_cache_status", "lr_cache_last_error")
+                    "lr_cache_write", "lr_cache_read", "lr_cache_attend", "lr_cache_attend_tree", "lr_cache_weigh",
+                    "lr_cache_select", "lr_cache_keep", "lr_cache_status", "lr_cache_last_error")
 
 _P = ctypes.c_void_p
 _I32 = ctypes.c_int32
@@ -98,6 +99,14 @@ def load_library(path: str = LIB_PATH):
     lib.lr_cache_read.argtypes = [_P, ctypes.POINTER(_CacheBatch), _I32, _I32, _P, _P, _P]
     lib.lr_cache_attend.argtypes = [_P, ctypes.POINTER(_CacheBatch), _I32, _P, ctypes.c_int64, ctypes.c_int64,
                                     ctypes.c_float, _I32, _I32, _P, ctypes.c_int64, ctypes.c_int64, _P, _P]
+    lib.lr_cache_attend_tree.argtypes = [_P, ctypes.POINTER(_CacheBatch), _I32, _P, ctypes.c_int64, ctypes.c_int64, _P,
+                                         ctypes.c_int64, _I32, ctypes.c_float, _I32, _I32, _P, ctypes.c_int64, ctypes.c_int64,
+                                         _P, _P]
+    weights = [_P, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64]
+    lib.lr_cache_weigh.argtypes = [_P, ctypes.POINTER(_CacheBatch), _I32, _P, ctypes.c_int64, ctypes.c_int64, _P, ctypes.c_float,
+                                   _I32, _I32, ctypes.c_float, *weights, _P]
+    lib.lr_cache_select.argtypes = [_P, ctypes.POINTER(_CacheBatch), *weights, _I32, _P, _I32, _I32, _P, _P, _P]
+    lib.lr_cache_keep.argtypes = [_P, ctypes.POINTER(_CacheBatch), _I32, _P, _I32, _P, _P, *weights, _P]
     lib.lr_cache_status.argtypes = [_P, _P]
     lib.lr_cache_last_error.argtypes = [_P]
     lib.lr_cache_last_error.restype = ctypes.c_char_p
@@ -111,7 +120,7 @@ def load_library(path: str = LIB_PATH):
                  "lr_set_queue_params", "lr_set_ttft_source", "lr_calibrate", "lr_route_baseline",
                  "lr_on_time_utility", "lr_set_kv_limits", "lr_advance_tracked", "lr_track_first_tokens",
                  "lr_cache_create", "lr_cache_destroy", "lr_cache_write", "lr_cache_read", "lr_cache_attend",
-                 "lr_cache_status"):
+                 "lr_cache_attend_tree", "lr_cache_weigh", "lr_cache_select", "lr_cache_keep", "lr_cache_status"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
