@@ -132,6 +132,7 @@ struct SelectLaunch {
     const int32_t *budget;  // or null: cap
     int32_t cap, sinks, recent;
     int32_t *kept, *count;
+    int32_t cluster, hold;  // (set by the launch) CTAs a list, keys that a CTA holds
 };
 cudaError_t launch_select(const SelectLaunch &a, int sms, cudaStream_t st);
 cudaError_t select_init();
@@ -146,12 +147,13 @@ struct KeepLaunch {
     int32_t cap;
     float *w;                // or null
     int64_t wb, wt, wh;
+    int32_t vector, pieces, cluster;  // (set by the launch) bytes of a vector, parts that it is moved in, CTAs a list of such parts
 };
 cudaError_t launch_keep(const KeepLaunch &a, int fmt, int sms, cudaStream_t st);
 
 // As launch_chained, in clusters of `cluster` CTAs.
 template <typename A>
-cudaError_t launch_clusters(void (*k)(A), unsigned grid, unsigned block, size_t smem, unsigned cluster, cudaStream_t st, const A &a) {
+cudaError_t launch_clusters(void (*k)(const A), unsigned grid, unsigned block, size_t smem, unsigned cluster, cudaStream_t st, const A &a) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = block;

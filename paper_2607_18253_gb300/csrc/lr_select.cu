@@ -5,6 +5,8 @@
 // that is kept is found from the top bits down, by counting (11, 11 and 10 bits: three counts of 2,048 bins); the
 // tokens above it are kept, and of those equal to it the first ones.  A cluster of CTAs has a list, each a range of its
 // positions: the counts and the places of the ranges' tokens are read from one another's shared memory.
+#include <algorithm>
+
 #include "lr_cache.cuh"
 
 namespace lr {
@@ -12,9 +14,12 @@ namespace lr {
 namespace {
 
 constexpr int kThreads = 512, kWarps = kThreads / 32, kBins = 2048;
-constexpr int kHold = 12288;  // keys that a CTA keeps in shared memory; further ones are read again for each count
-constexpr int kMaxCluster = 8;
-constexpr size_t kSmem = kHold * 4 + 3 * kBins * 4;
+// Keys that a CTA holds in shared memory; further ones are read again for each count.  Of CTAs that are no more than the SMs a
+// CTA takes what there is, else what leaves room for three.
+constexpr int kHold = 12288, kHoldAlone = 49152;
+constexpr int kMaxCluster = 8, kLeast = 2048;  // (positions a CTA, at least, or a list is not divided)
+constexpr int kAhead = 8;                      // weights that a thread reads together
+constexpr size_t smem_of(int hold) { return (size_t)hold * 4 + 3 * kBins * 4; }
 
 // As `w` sorts: NaN above all, both zeros the same.
 __device__ __forceinline__ uint32_t key_of(float w) {
@@ -31,18 +36,23 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-// A word of CTA `rank`'s shared memory at the place of `p` in this one's.
-__device__ __forceinline__ uint32_t peer_word(const uint32_t *p, int rank) {
-    uint32_t at, v;
+// The place in CTA `rank`'s shared memory that `p` has in this one's.
+__device__ __forceinline__ uint32_t peer(const uint32_t *p, int rank) {
+    uint32_t at;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+    return at;
+}
+__device__ __forceinline__ uint32_t peer_word(uint32_t at) {
+    uint32_t v;
     asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
     return v;
 }
 
-__global__ void __launch_bounds__(kThreads) k_select(const __grid_constant__ SelectLaunch a, int cl) {
+__global__ void __launch_bounds__(kThreads) k_select(const __grid_constant__ SelectLaunch a) {
     extern __shared__ __align__(16) uint32_t smem[];
-    uint32_t *const hold = smem, *const bins = smem + kHold;  // [3][kBins]
+    uint32_t *const bins = smem, *const hold = smem + 3 * kBins;  // [3][kBins], keys
     __shared__ uint32_t s_warp[2 * kWarps], s_bin[2], s_mine[2];
+    const int cl = a.cluster;
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     const int rank = cl > 1 ? (int)cluster_rank() : 0;
     const CacheDev &c = a.c;
@@ -75,14 +85,23 @@ __global__ void __launch_bounds__(kThreads) k_select(const __grid_constant__ Sel
         }
         return key_of(a.w[blk * a.wb + place * a.wt + h * a.wh]);
     };
-    auto key = [&](int p) { return p - p0 < kHold ? hold[p - p0] : read(p); };
+    const int held = a.hold;
+    auto key = [&](int p) { return p - p0 < held ? hold[p - p0] : read(p); };
 
     for (int i = tid; i < 3 * kBins; i += kThreads) bins[i] = 0;
-    __syncthreads();
-    for (int p = p0 + tid; p < p1; p += kThreads) {
-        const uint32_t k = read(p);
-        if (p - p0 < kHold) hold[p - p0] = k;
-        atomicAdd(bins + (k >> 21), 1u);
+    if (cl > 1) cluster_sync();
+    else __syncthreads();
+    for (int p = p0 + tid; p < p1; p += kThreads * kAhead) {
+        uint32_t k[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) k[i] = p + i * kThreads < p1 ? read(p + i * kThreads) : 0u;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int at = p + i * kThreads;
+            if (at >= p1) break;
+            if (at - p0 < held) hold[at - p0] = k[i];
+            atomicAdd(bins + (k[i] >> 21), 1u);
+        }
     }
     uint32_t prefix = 0, need = m;  // the key's bits so far; of the keys that have them, how many are kept
 #pragma unroll 1
@@ -96,18 +115,25 @@ __global__ void __launch_bounds__(kThreads) k_select(const __grid_constant__ Sel
                 if (k >> above == prefix >> above) atomicAdd(bin + (k >> shift & (many - 1)), 1u);
             }
         }
+        // the cluster's counts come together in its first CTA
+        if (rank > 0) {
+            __syncthreads();
+            for (int i = tid; i < many; i += kThreads)
+                if (bin[i]) asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], %1;" ::"r"(peer(bin + i, 0)), "r"(bin[i]) : "memory");
+        }
         if (cl > 1) cluster_sync();
         else __syncthreads();
         // four bins a thread, from the top: those before the bin that brings the count to `need`
         const int b0 = many - 1 - tid * 4;
-        uint32_t v[4], mine = 0;
+        uint32_t v[4] = {0, 0, 0, 0};
+        if (b0 >= 0) {
+            if (cl > 1)
+                asm volatile("ld.shared::cluster.v4.u32 {%3,%2,%1,%0}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(peer(bin + b0 - 3, 0)) : "memory");
+            else
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[i] = 0;
-            if (b0 - i >= 0)
-                for (int r = 0; r < cl; ++r) v[i] += cl > 1 ? peer_word(bin + b0 - i, r) : bin[b0 - i];
-            mine += v[i];
+                for (int i = 0; i < 4; ++i) v[i] = bin[b0 - i];
         }
+        const uint32_t mine = v[0] + v[1] + v[2] + v[3];
         uint32_t incl = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -155,9 +181,11 @@ __global__ void __launch_bounds__(kThreads) k_select(const __grid_constant__ Sel
             s_mine[tid] = all;
         }
         cluster_sync();
-        for (int r = 0; r < rank; ++r) {
-            out += peer_word(s_mine, r);
-            eq += peer_word(s_mine + 1, r);
+#pragma unroll
+        for (int r = 0; r < kMaxCluster; ++r) {
+            if (r >= rank) break;
+            out += peer_word(peer(s_mine, r));
+            eq += peer_word(peer(s_mine + 1, r));
         }
         asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     }
@@ -178,11 +206,18 @@ __global__ void __launch_bounds__(kThreads) k_select(const __grid_constant__ Sel
 
 }  // namespace
 
-cudaError_t select_init() { return cudaFuncSetAttribute(k_select, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem); }
+cudaError_t select_init() {
+    return cudaFuncSetAttribute(k_select, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_of(kHoldAlone));
+}
 
 cudaError_t launch_select(const SelectLaunch &a, int sms, cudaStream_t st) {
-    const long long lists = (long long)a.b.n * a.c.H;
-    return launch_chained(k_select, (unsigned)lists, kThreads, kSmem, st, a, 1);
+    const long long lists = (long long)a.b.n * a.c.H, longest = std::min((long long)a.b.max_blocks * a.c.b, (long long)kMaxTokens);
+    SelectLaunch l = a;
+    l.cluster = 1;
+    while (l.cluster < kMaxCluster && 2 * lists * l.cluster <= 3 * sms && longest >= 2ll * kLeast * l.cluster) l.cluster *= 2;
+    const long long each = longest / l.cluster + 64;
+    l.hold = (int)std::min(each, (long long)(lists * l.cluster <= sms ? kHoldAlone : kHold));
+    return launch_clusters(k_select, (unsigned)(lists * l.cluster), kThreads, smem_of(l.hold), (unsigned)l.cluster, st, l);
 }
 
 }  // namespace lr

@@ -6,21 +6,22 @@
 // What bounds it for few rows is K's bytes.  Sixteen (or 32, 64) tokens are a warp's at a time; a lane reads 16-byte pieces of
 // the vectors of tokens g and g + 8 straight to the registers that multiply them (S = K Q^T, 16x8x16 products with the cache as
 // the 16-row operand): which elements of a vector a product sums is free, as long as the queries' lanes
-// take the same ones, so a piece is two (16 bits) or four (8 bits) products' operands as it lies.  The next tokens' pieces
-// are on their way while these are multiplied.
+// take the same ones, so a piece is two (16 bits) or four (8 bits) products' operands as it lies.  The next tokens'
+// blocks are looked up while these are multiplied; their reads are other warps' to hide.
 #include "lr_attend.cuh"
 
 namespace lr {
 
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kThreads = 128, kWarps = kThreads / 32;
 
-template <int DP, int FMT>
+template <int DP, int FMT, int NR>
 struct Piece {
     static constexpr int kVec = DP * (FMT == kFmt16 ? 2 : 1) / 64;  // 16-byte pieces a lane and vector
     static constexpr int NB = 4 / kVec;                             // blocks of 16 tokens
     static constexpr int kTile = 16 * NB;
+    static constexpr int kCtas = NR == 1 ? 5 : 4;                   // of an SM
 };
 
 template <bool BF16>
@@ -37,86 +38,34 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
 // (where a block's heads lie together, so do a CTA's reads).  What no row sees is left out where nothing changes it.
 template <int TILE>
 struct Walk {
-    int s, q0, ql, kv, ns, wf;
-    long long n;     // tiles of the sequence, times heads
-    long long left;  // the position in it
+    int s, q0, ql, kv;
+    int ns, wf, nt;  // tiles of sinks before the window, the window's first tile, tiles in all
+    int tile, h;
     __device__ __forceinline__ bool load(const WeighLaunch &a) {
         if (!load_seq(a.a, s, q0, ql, kv) || kv == 0) return false;
-        int nt;
         if (a.decay == 1.0f) nt = tile_count<TILE>(kv - ql, kv - 1, a.a.window, a.a.sinks, ns, wf);
         else ns = wf = 0, nt = (kv - 1) / TILE + 1;
-        n = (long long)nt * a.a.c.H;
         return true;
     }
-    // On by k positions; false behind the last sequence.
-    __device__ __forceinline__ bool on(const WeighLaunch &a, long long k) {
-        left += k;
-        while (left >= n) {
-            left -= n;
+    // On by so many tiles and heads (fewer than there are); false behind the last sequence.
+    __device__ __forceinline__ bool on(const WeighLaunch &a, int tiles, int heads) {
+        tile += tiles;
+        h += heads;
+        if (h >= a.a.c.H) h -= a.a.c.H, ++tile;
+        while (tile >= nt) {
+            tile -= nt;
             do
                 if (++s >= a.a.b.n) return false;
             while (!load(a));
         }
         return true;
     }
+    __device__ __forceinline__ int base() const { return (tile < ns ? tile : wf + tile - ns) * TILE; }
 };
-
-template <int DP, int FMT>
-struct Tokens {
-    uint4 k[Piece<DP, FMT>::NB][2][Piece<DP, FMT>::kVec];
-    float ks[Piece<DP, FMT>::NB][2];
-    int64_t w[Piece<DP, FMT>::NB];  // where this lane's token's weight is, -1: not this lane's to write
-    float old[Piece<DP, FMT>::NB];
-    int h, base, q0, ql, kv;
-};
-
-template <int DP, int FMT>
-__device__ __forceinline__ void fetch(const WeighLaunch &a, const Walk<Piece<DP, FMT>::kTile> &at, Tokens<DP, FMT> &k) {
-    using P = Piece<DP, FMT>;
-    const CacheDev &c = a.a.c;
-    const int lane = threadIdx.x % 32, g = lane / 4, i4 = lane % 4;
-    const int tile = (int)(at.left / c.H);
-    k.h = (int)(at.left - (long long)tile * c.H);
-    k.base = (tile < at.ns ? tile : at.wf + tile - at.ns) * P::kTile;
-    k.q0 = at.q0;
-    k.ql = at.ql;
-    k.kv = at.kv;
-    const int lo = k.kv - k.ql;
-#pragma unroll
-    for (int b = 0; b < P::NB; ++b) {
-        k.w[b] = -1;
-        k.old[b] = 0.0f;
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-            const int t = k.base + b * 16 + y * 8 + g;
-            const bool any = !(a.a.window > 0 && t <= lo - a.a.window && t >= a.a.sinks);  // (some row sees it)
-            k.ks[b][y] = 0.0f;
-#pragma unroll
-            for (int v = 0; v < P::kVec; ++v) k.k[b][y][v] = make_uint4(0, 0, 0, 0);
-            if (t >= k.kv || (!any && a.decay == 1.0f)) continue;
-            int place;
-            const int64_t blk = block_of(c, a.a.b, at.s, t, place);
-            if (blk < 0) {  // (a token that no row sees may have no block any more)
-                if (any) report(c.status, kEInval);
-                continue;
-            }
-            if (i4 == y) {
-                k.w[b] = blk * a.wb + place * a.wt + k.h * a.wh;
-                if (a.decay != 0.0f && t < lo) k.old[b] = a.decay * a.w[k.w[b]];
-            }
-            if (!any) continue;
-            const char *const p = c.k + blk * c.sb + place * c.st + k.h * c.sh;
-#pragma unroll
-            for (int v = 0; v < P::kVec; ++v)
-                if ((v * 4 + i4) * 16 < c.D * (FMT == kFmt16 ? 2 : 1)) k.k[b][y][v] = __ldg(reinterpret_cast<const uint4 *>(p + (v * 4 + i4) * 16));
-            if constexpr (FMT != kFmt16) k.ks[b][y] = __ldg(c.ks + blk * c.ssb + place * c.sst + k.h * c.ssh);
-        }
-    }
-}
 
 template <bool BF16, int FMT, int DP, int NR>
-__global__ void __launch_bounds__(kThreads, 2) k_weigh_step(const __grid_constant__ WeighLaunch a) {
-    using P = Piece<DP, FMT>;
+__global__ void __launch_bounds__(kThreads, Piece<DP, FMT, NR>::kCtas) k_weigh_step(const __grid_constant__ WeighLaunch a) {
+    using P = Piece<DP, FMT, NR>;
     constexpr int kRows = 8 * NR, NB = P::NB, KS = DP / 16;
     // 8-bit codes are multiplied in fp16, which holds them exactly; bf16 queries come to it divided by a power of two a row
     // that brings the largest to [1, 2): what fp16 then rounds is below 2^-24 of it.
@@ -130,10 +79,13 @@ __global__ void __launch_bounds__(kThreads, 2) k_weigh_step(const __grid_constan
     // this CTA's share of the line, x0 .. x1
     const int n = a.a.b.n;
     Walk<P::kTile> at;
+    auto tiles_of = [&](int s) -> long long {
+        at.s = s;
+        return s < n && at.load(a) ? (long long)at.nt * c.H : 0;
+    };
     long long all = 0, mine = 0, incl = 0;
     for (int base = 0; base < n; base += kThreads) {
-        at.s = base + tid;
-        mine = at.s < n && at.load(a) ? at.n : 0;
+        mine = tiles_of(base + tid);
         long long t;
         incl = block_sum<kThreads>(mine, s_sum, t);
         all += t;
@@ -147,8 +99,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_weigh_step(const __grid_constan
     for (int base = 0; base < n; base += kThreads) {
         long long t = all;
         if (n > kThreads) {
-            at.s = base + tid;
-            mine = at.s < n && at.load(a) ? at.n : 0;
+            mine = tiles_of(base + tid);
             incl = block_sum<kThreads>(mine, s_sum, t);
         }
         const long long x = x0 - first;
@@ -161,39 +112,78 @@ __global__ void __launch_bounds__(kThreads, 2) k_weigh_step(const __grid_constan
     }
     __syncthreads();
     at.s = s_seq;
-    at.left = s_at;
     at.load(a);
+    at.tile = (int)(s_at / c.H);
+    at.h = (int)(s_at - (long long)at.tile * c.H);
+    const int on_t = kWarps / c.H, on_h = kWarps % c.H;
+    if (x0 + warp >= x1 || !at.on(a, warp / c.H, warp % c.H)) {
+        chain_next();
+        return;
+    }
 
+    // the blocks of a lane's tokens (g and g + 8 of each 16), as the table has them: looked up a tile ahead
+    int blk[NB][2];
+    auto look = [&]() {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                const int t = at.base() + b * 16 + y * 8 + g, i = quot(t, c.div_b);
+                blk[b][y] = t < at.kv && i < a.a.b.max_blocks ? __ldg(a.a.b.table + (int64_t)at.s * a.a.b.table_stride + i) : -1;
+            }
+    };
+    look();
     uint32_t q[KS][NR][2];
     float qf[NR][2], less[NR][2];  // the scores' factor, lse * log2(e)
     int pos[NR][2];                // the rows' positions, -1: none
     int qh = -1, qs = -1, qr = -1;  // whose queries these are
-    Tokens<DP, FMT> now, next;
-    long long x = x0 + warp;
-    if (x >= x1 || !at.on(a, warp)) {
-        chain_next();
-        return;
-    }
-    fetch<DP, FMT>(a, at, next);
-    for (; x < x1; x += kWarps) {
-        now = next;
-        if (x + kWarps < x1 && at.on(a, kWarps)) fetch<DP, FMT>(a, at, next);
-        const int lo = now.kv - now.ql, rows = now.ql * c.G, end = now.base + P::kTile - 1;
-        float sum[NB][2];
+    long long left = (x1 - x0 - warp + kWarps - 1) / kWarps;
+    while (left-- > 0) {
+        const int q0 = at.q0, ql = at.ql, kv = at.kv, h = at.h, tile0 = at.base();
+        const int lo = kv - ql, rows = ql * c.G, end = tile0 + P::kTile - 1;
+        uint4 k[NB][2][P::kVec];
+        [[maybe_unused]] float ks[NB][2];
+        int64_t to[NB];  // where this lane's token's weight is, -1: not this lane's to write
+        float old[NB], sum[NB][2];
 #pragma unroll
-        for (int b = 0; b < NB; ++b) sum[b][0] = sum[b][1] = 0.0f;
+        for (int b = 0; b < NB; ++b) {
+            to[b] = -1;
+            old[b] = sum[b][0] = sum[b][1] = 0.0f;
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                const int t = tile0 + b * 16 + y * 8 + g, place = t - quot(t, c.div_b) * c.b;
+                const bool any = !(a.a.window > 0 && t <= lo - a.a.window && t >= a.a.sinks);  // (some row sees it)
+                bool ok = t < kv && (any || a.decay != 1.0f);
+                if (ok && (uint32_t)blk[b][y] >= (uint32_t)c.nb) {  // (a token that no row sees may have no block any more)
+                    if (any) report(c.status, kEInval);
+                    ok = false;
+                }
+                const char *const p = c.k + (int64_t)blk[b][y] * c.sb + place * c.st + h * c.sh;
+#pragma unroll
+                for (int v = 0; v < P::kVec; ++v) {
+                    const int e = (v * 4 + i4) * 16;
+                    k[b][y][v] = ok && any && e < c.D * (FMT == kFmt16 ? 2 : 1) ? __ldg(reinterpret_cast<const uint4 *>(p + e)) : make_uint4(0, 0, 0, 0);
+                }
+                if constexpr (FMT != kFmt16) ks[b][y] = ok && any ? __ldg(c.ks + (int64_t)blk[b][y] * c.ssb + place * c.sst + h * c.ssh) : 0.0f;
+                if (ok && i4 == y) {
+                    to[b] = (int64_t)blk[b][y] * a.wb + place * a.wt + h * a.wh;
+                    if (a.decay != 0.0f && t < lo) old[b] = a.decay * a.w[to[b]];
+                }
+            }
+        }
+        if (left > 0 && at.on(a, on_t, on_h)) look();
         // rows from the first that may see the tile on; below a window, up to the last
-        int r0 = now.base > lo ? (now.base - lo) * c.G / kRows * kRows : 0, r1 = rows;
-        if (a.a.window > 0 && now.base >= a.a.sinks) r1 = (int)min((long long)rows, max(0ll, (long long)end + a.a.window - lo) * c.G);
+        int r0 = tile0 > lo ? (tile0 - lo) * c.G / kRows * kRows : 0, r1 = rows;
+        if (a.a.window > 0 && tile0 >= a.a.sinks) r1 = (int)min((long long)rows, max(0ll, (long long)end + a.a.window - lo) * c.G);
         for (; r0 < r1; r0 += kRows) {
-            if (now.h != qh || now.q0 != qs || r0 != qr) {
-                qh = now.h, qs = now.q0, qr = r0;
+            if (h != qh || q0 != qs || r0 != qr) {
+                qh = h, qs = q0, qr = r0;
 #pragma unroll
                 for (int m = 0; m < NR; ++m) {
                     const int r = r0 + m * 8 + g;  // (the row whose elements the lane holds)
                     const int t = quot(r, c.div_g), hd = r - t * c.G;
                     const bool ok = r < rows;
-                    const char *const p = a.a.q + (int64_t)(now.q0 + t) * a.a.q_t + (int64_t)(now.h * c.G + hd) * a.a.q_h;
+                    const char *const p = a.a.q + (int64_t)(q0 + t) * a.a.q_t + (int64_t)(h * c.G + hd) * a.a.q_h;
                     float pow2 = 1.0f;
                     if constexpr (FMT == kFmt16) {
 #pragma unroll
@@ -241,7 +231,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_weigh_step(const __grid_constan
                     for (int y = 0; y < 2; ++y) {
                         const int row = r0 + m * 8 + 2 * i4 + y, tt = quot(row, c.div_g);
                         const bool real = row < rows;
-                        const float l = real ? __ldg(a.a.lse + (int64_t)(now.q0 + tt) * c.Hq + now.h * c.G + row - tt * c.G) : -INFINITY;
+                        const float l = real ? __ldg(a.a.lse + (int64_t)(q0 + tt) * c.Hq + h * c.G + row - tt * c.G) : -INFINITY;
                         // (a row that sees nothing adds nothing)
                         pos[m][y] = l == -INFINITY ? -1 : lo + tt;
                         less[m][y] = l == -INFINITY ? 0.0f : l * 1.44269504f;
@@ -258,7 +248,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_weigh_step(const __grid_constan
                     for (int z = 0; z < 4; ++z) s[m][z] = 0.0f;
 #pragma unroll
                 for (int v = 0; v < P::kVec; ++v) {
-                    const uint4 e = now.k[b][0][v], f = now.k[b][1][v];
+                    const uint4 e = k[b][0][v], f = k[b][1][v];
                     const uint32_t ee[4] = {e.x, e.y, e.z, e.w}, ff[4] = {f.x, f.y, f.z, f.w};
                     if constexpr (FMT == kFmt16) {
 #pragma unroll
@@ -281,9 +271,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_weigh_step(const __grid_constan
                 for (int m = 0; m < NR; ++m)
 #pragma unroll
                     for (int z = 0; z < 4; ++z) {
-                        const int j = now.base + b * 16 + (z >> 1) * 8 + g;
+                        const int j = tile0 + b * 16 + (z >> 1) * 8 + g;
                         float f = qf[m][z & 1];
-                        if constexpr (FMT != kFmt16) f *= now.ks[b][z >> 1];
+                        if constexpr (FMT != kFmt16) f *= ks[b][z >> 1];
                         const float p = exp2_fast(s[m][z] * f - less[m][z & 1]);
                         sum[b][z >> 1] += visible(pos[m][z & 1], j, a.a.window, a.a.sinks) ? p : 0.0f;
                     }
@@ -296,7 +286,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_weigh_step(const __grid_constan
                 float f = sum[b][y];
                 f += __shfl_xor_sync(0xffffffffu, f, 1);
                 f += __shfl_xor_sync(0xffffffffu, f, 2);
-                if (i4 == y && now.w[b] >= 0) a.w[now.w[b]] = now.old[b] + f;
+                if (i4 == y && to[b] >= 0) a.w[to[b]] = old[b] + f;
             }
     }
     chain_next();
@@ -305,8 +295,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_weigh_step(const __grid_constan
 using Kernel = void (*)(const WeighLaunch);
 template <int FMT, int DP>
 Kernel pick_rows(bool bf16, bool few) {
-    return bf16 ? (few ? k_weigh_step<true, FMT, DP, 1> : k_weigh_step<true, FMT, DP, 4>)
-                : (few ? k_weigh_step<false, FMT, DP, 1> : k_weigh_step<false, FMT, DP, 4>);
+    return bf16 ? (few ? k_weigh_step<true, FMT, DP, 1> : k_weigh_step<true, FMT, DP, 2>)
+                : (few ? k_weigh_step<false, FMT, DP, 1> : k_weigh_step<false, FMT, DP, 2>);
 }
 template <int FMT>
 Kernel pick_dim(bool bf16, int D, bool few) { return D <= 64 ? pick_rows<FMT, 64>(bf16, few) : pick_rows<FMT, 128>(bf16, few); }
@@ -318,7 +308,7 @@ cudaError_t launch_weigh(const WeighLaunch &a, bool bf16, int fmt, int sms, cuda
     const Kernel k = fmt == kFmt16 ? pick_dim<kFmt16>(bf16, a.a.c.D, few)
                    : fmt == kFmtE4M3 ? pick_dim<kFmtE4M3>(bf16, a.a.c.D, few)
                                      : pick_dim<kFmtInt8>(bf16, a.a.c.D, few);
-    return launch_chained(k, 2 * sms, kThreads, 0, st, a);
+    return launch_chained(k, (few ? 5 : 4) * sms, kThreads, 0, st, a);
 }
 
 }  // namespace lr
