@@ -51,7 +51,7 @@ int encode_maps(const CacheDev &c, bool bf16, CacheMaps &m) {
 
 bool encode_rows(const AttendLaunch &a, bool bf16, CUtensorMap &map) {
     const CacheDev &c = a.c;
-    if (c.G > 128 || 128 % c.G != 0) return false;
+    if (c.G > 128) return false;
     const cuuint64_t dims[3] = {(cuuint64_t)c.D, (cuuint64_t)c.Hq, (cuuint64_t)a.b.T};
     const cuuint64_t strides[2] = {(cuuint64_t)(c.Hq > 1 ? a.q_h : 256), (cuuint64_t)(a.b.T > 1 ? a.q_t : 256)};
     const cuuint32_t box[3] = {64, (cuuint32_t)c.G, (cuuint32_t)(128 / c.G)};
@@ -61,6 +61,7 @@ bool encode_rows(const AttendLaunch &a, bool bf16, CUtensorMap &map) {
 cudaError_t attend_chunk_init() {
     cudaError_t e = chunk_init<false>();
     if (e == cudaSuccess) e = tree_chunk_init();
+    if (e == cudaSuccess) e = weigh_init();
     if (e == cudaSuccess) e = select_init();  // (those of the other calls with much shared memory beside it)
     return e;
 }

@@ -26,17 +26,16 @@
 #pragma once
 
 #include "lr_attend.cuh"
+#include "lr_tensor.cuh"
 
 namespace lr {
 
 namespace {
 
-constexpr int kTok = 128;     // tokens of a tile
 constexpr int kWeight = 4;    // tiles that a unit's beginning and end take the time of
 constexpr int kThreads = 512;
 // registers a thread of the softmax warps and of the others: together the 512 x 128 of the launch
 constexpr int kSoftRegs = 192, kOtherRegs = 64;
-constexpr uint32_t kSpin = 1u << 28;  // polls before a wait gives up
 
 // How K and V reach shared memory.
 enum : int {
@@ -75,139 +74,6 @@ struct Shape {
     static constexpr int kSmem = kBytes + kScales + 2 * kTok * 8 + kBars * 8 + (kThreads / 32 + 2) * 8 + 29 * 4 + kJobs * sizeof(Job);
     static_assert(kSmem <= 227 * 1024, "shared memory");
 };
-
-// ---- barriers in shared memory ----
-__device__ __forceinline__ void bar_init(uint32_t bar, int count) {
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void bar_arrive(uint32_t bar) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-// One arrival for the warp, after all its lanes have come.
-__device__ __forceinline__ void bar_arrive_warp(uint32_t bar) {
-    __syncwarp();
-    if ((threadIdx.x & 31) == 0) bar_arrive(bar);
-}
-__device__ __forceinline__ bool bar_test(uint32_t bar, uint32_t parity) {
-    uint32_t done;
-    asm volatile("{\n .reg .pred P;\n mbarrier.test_wait.parity.shared::cta.b64 P, [%1], %2;\n selp.u32 %0, 1, 0, P;\n}"
-                 : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-    return done;
-}
-// Waits until the phase of the given parity is over; false if it gives up, or another thread has.  All lanes
-// of a warp come together and go on together (`distant`: the wait is long, its tests sleep between).
-template <bool DISTANT = false>
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *dead) {
-    for (uint32_t i = 1; i < kSpin; ++i) {
-        uint32_t done;
-        asm volatile(
-            "{\n .reg .pred P;\n mbarrier.try_wait.parity.shared::cta.b64 P, [%1], %2;\n selp.u32 %0, 1, 0, P;\n}"
-            : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-        if (__all_sync(0xffffffffu, done)) return true;
-        if (DISTANT) __nanosleep(200);
-        if (i % 1024 == 0 && __any_sync(0xffffffffu, *dead)) return false;
-    }
-    *dead = 1;
-    return false;
-}
-__device__ __forceinline__ bool elect() {
-    uint32_t r;
-    asm volatile("{\n .reg .pred P;\n elect.sync _|P, 0xffffffff;\n selp.u32 %0, 1, 0, P;\n}" : "=r"(r));
-    return r;
-}
-
-// ---- tensor cores ----
-__device__ __forceinline__ void after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
-// Operand descriptor of a 128-byte-swizzled tile: 8-row groups 1,024 bytes apart; `lead`, the distance of
-// 64-element panels, matters where the rows are the summed dimension (V).
-__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t lead) {
-    return (uint64_t)(addr >> 4 & 0x3fff) | (uint64_t)(lead >> 4 & 0x3fff) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
-}
-// fp32 sums of 16-bit products, 128 rows, N columns; `along_n`: B's elements are contiguous along N.
-template <bool BF16, int N, bool ALONG_N>
-constexpr uint32_t shape_of() {
-    return 1u << 4 | (BF16 ? 1u : 0u) << 7 | (BF16 ? 1u : 0u) << 10 | (ALONG_N ? 1u : 0u) << 16 | (N / 8u) << 17 | 8u << 24;
-}
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t shape, bool add) {
-    asm volatile(
-        "{\n .reg .pred P;\n setp.ne.b32 P, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, P;\n}" ::"r"(d), "l"(a),
-        "l"(b), "r"(shape), "r"((uint32_t)add)
-        : "memory");
-}
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t shape, bool add) {
-    asm volatile(
-        "{\n .reg .pred P;\n setp.ne.b32 P, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, P;\n}" ::"r"(d), "r"(a),
-        "l"(b), "r"(shape), "r"((uint32_t)add)
-        : "memory");
-}
-// 32 columns of the warp's 32 lanes of tensor memory, a lane a thread.
-__device__ __forceinline__ void tm_load(float *r, uint32_t addr) {
-    uint32_t *u = reinterpret_cast<uint32_t *>(r);
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,"
-        "%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-        : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]), "=r"(u[9]),
-          "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15]), "=r"(u[16]), "=r"(u[17]), "=r"(u[18]),
-          "=r"(u[19]), "=r"(u[20]), "=r"(u[21]), "=r"(u[22]), "=r"(u[23]), "=r"(u[24]), "=r"(u[25]), "=r"(u[26]), "=r"(u[27]),
-          "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
-        : "r"(addr));
-}
-// (the registers pass through, so that nothing reads them earlier)
-__device__ __forceinline__ void tm_load_wait(float *r) {
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-    uint32_t *u = reinterpret_cast<uint32_t *>(r);
-    asm volatile(""
-                 : "+r"(u[0]), "+r"(u[1]), "+r"(u[2]), "+r"(u[3]), "+r"(u[4]), "+r"(u[5]), "+r"(u[6]), "+r"(u[7]), "+r"(u[8]), "+r"(u[9]),
-                   "+r"(u[10]), "+r"(u[11]), "+r"(u[12]), "+r"(u[13]), "+r"(u[14]), "+r"(u[15]));
-    asm volatile(""
-                 : "+r"(u[16]), "+r"(u[17]), "+r"(u[18]), "+r"(u[19]), "+r"(u[20]), "+r"(u[21]), "+r"(u[22]), "+r"(u[23]), "+r"(u[24]),
-                   "+r"(u[25]), "+r"(u[26]), "+r"(u[27]), "+r"(u[28]), "+r"(u[29]), "+r"(u[30]), "+r"(u[31]));
-}
-// 16 columns, a lane a thread.
-__device__ __forceinline__ void tm_store(uint32_t addr, const uint32_t *u) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::"r"(u[0]), "r"(u[1]),
-        "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]), "r"(u[10]), "r"(u[11]), "r"(u[12]),
-        "r"(u[13]), "r"(u[14]), "r"(u[15]), "r"(addr)
-        : "memory");
-}
-__device__ __forceinline__ void tm_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-
-// Two fp32 operations an instruction.
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-    float2 d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;"
-        : "=l"(reinterpret_cast<unsigned long long &>(d))
-        : "l"(reinterpret_cast<unsigned long long &>(a)), "l"(reinterpret_cast<unsigned long long &>(b)),
-          "l"(reinterpret_cast<unsigned long long &>(c)));
-    return d;
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-    float2 d;
-    asm("add.rn.f32x2 %0, %1, %2;"
-        : "=l"(reinterpret_cast<unsigned long long &>(d))
-        : "l"(reinterpret_cast<unsigned long long &>(a)), "l"(reinterpret_cast<unsigned long long &>(b)));
-    return d;
-}
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-    float2 d;
-    asm("mul.rn.f32x2 %0, %1, %2;"
-        : "=l"(reinterpret_cast<unsigned long long &>(d))
-        : "l"(reinterpret_cast<unsigned long long &>(a)), "l"(reinterpret_cast<unsigned long long &>(b)));
-    return d;
-}
-
-__device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
-__device__ __forceinline__ void shared_to_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-
-template <int DP>
-__device__ __forceinline__ uint32_t swizzled(int row, int chunk) {  // byte offset of a 16-byte chunk in a tile
-    return (chunk >> 3) * (kTok * 128) + row * 128 + ((chunk ^ row) & 7) * 16;
-}
 
 // Tokens that a row does not see have weight zero, but zero times an infinity or a NaN in V is not
 // zero.  In a tile that is hidden from some of its rows, such elements of V are therefore set to zero in
@@ -1213,7 +1079,7 @@ cudaError_t launch_chunk(const AttendLaunch &a, const CacheMaps &m, bool bf16, i
     ChunkLaunch l;
     l.a = a;
     l.m = m;
-    l.q_map = encode_rows(a, bf16, l.q);
+    l.q_map = 128 % a.c.G == 0 && encode_rows(a, bf16, l.q);
     return launch_chained(p.k, ctas, kThreads, p.smem, st, l);
 }
 

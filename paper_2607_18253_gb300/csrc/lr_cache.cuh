@@ -105,7 +105,7 @@ struct CacheMaps {
 int encode_maps(const CacheDev &c, bool bf16, CacheMaps &m);  // the box, 0 if there can be none
 cudaError_t launch_attend_chunk(const AttendLaunch &a, const CacheMaps &m, bool bf16, int fmt, int ctas, cudaStream_t st);
 cudaError_t attend_chunk_init();
-// The map of a launch's queries: boxes of 64 elements of 128 rows; false if there can be none.
+// The map of a launch's queries: boxes of 64 elements of as many tokens' rows of a KV head as 128 holds; false if there can be none.
 bool encode_rows(const AttendLaunch &a, bool bf16, CUtensorMap &map);
 // The kernels of trees (a.tree), which the above launch.
 cudaError_t tree_step_init();
@@ -122,6 +122,10 @@ struct WeighLaunch {
     float decay;
 };
 cudaError_t launch_weigh(const WeighLaunch &a, bool bf16, int fmt, int sms, cudaStream_t st);
+// (its kernels: of sequences of `rows` rows at most, 8 or 16; of others, one CTA an SM, whose parts of 256 tokens are joined)
+cudaError_t launch_weigh_step(const WeighLaunch &a, bool bf16, int fmt, int rows, int sms, cudaStream_t st);
+cudaError_t launch_weigh_chunk(const WeighLaunch &a, bool bf16, int fmt, int sms, cudaStream_t st);
+cudaError_t weigh_init();
 
 // The tokens that a cache keeps (lr_select.cu).
 struct SelectLaunch {

@@ -13,7 +13,7 @@ namespace {
 
 void free_all(lr_cache *c) {
     cudaFree(c->dev.status);
-    for (lr_cache::Parts *p : {&c->step, &c->chunk}) {
+    for (lr_cache::Parts *p : {&c->step, &c->chunk, &c->weigh}) {
         cudaFree(p->o);
         cudaFree(p->ml);
         cudaFree(p->done);
@@ -154,6 +154,7 @@ int lr_cache_create(const lr_cache_config *cfg, lr_cache **out) {
     d.nan = reinterpret_cast<const float *>(d.status + 1);
     if (e == cudaSuccess) e = alloc_parts(c->step, lr::attend_step_ctas(c->sms), lr::kStepRows, lr::attend_step_ctas(c->sms));
     if (e == cudaSuccess) e = alloc_parts(c->chunk, c->sms, lr::kChunkRows, 8 * (size_t)c->sms);
+    if (e == cudaSuccess) e = alloc_parts(c->weigh, c->sms, 2, 8 * (size_t)c->sms);  // (parts of 256 sums)
     if (e != cudaSuccess) return bail(LR_ENOMEM, cudaGetErrorString(e));
     // (what was set above, on the default stream, has to be there for streams that do not wait for it)
     e = cudaDeviceSynchronize();
@@ -244,6 +245,7 @@ int lr_cache_status(lr_cache *c, void *stream) {
     // a kernel may have given up, whatever error came first: its counts of finished parts start again
     if (e == cudaSuccess && h != LR_OK) {
         e = cudaMemsetAsync(c->chunk.done, 0, 8 * (size_t)c->sms * sizeof(uint32_t), st);
+        if (e == cudaSuccess) e = cudaMemsetAsync(c->weigh.done, 0, 8 * (size_t)c->sms * sizeof(uint32_t), st);
         if (e == cudaSuccess) e = cudaStreamSynchronize(st);
     }
     if (e != cudaSuccess) return cuda_fail(c, e, "status");

@@ -18,7 +18,7 @@ struct lr_cache {
         float *o = nullptr;
         float2 *ml = nullptr;
         uint32_t *done = nullptr;
-    } step, chunk;
+    } step, chunk, weigh;
     std::string err;
 };
 

@@ -55,8 +55,8 @@ int lr_cache_weigh(lr_cache *c, const lr_cache_batch *b, int32_t T, const void *
     a.scale_log2 = (float)((double)scale * 1.4426950408889634);
     a.window = window;
     a.sinks = window ? sinks : 0;
-    a.row_lo = 1;
-    a.row_hi = 0x7fffffff;
+    a.part_o = c->weigh.o;
+    a.done = c->weigh.done;
     l.w = weights;
     l.wb = block_stride;
     l.wt = token_stride;

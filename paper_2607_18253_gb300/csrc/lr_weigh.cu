@@ -8,6 +8,8 @@
 // the 16-row operand): which elements of a vector a product sums is free, as long as the queries' lanes
 // take the same ones, so a piece is two (16 bits) or four (8 bits) products' operands as it lies.  The next tokens'
 // blocks are looked up while these are multiplied; their reads are other warps' to hide.
+#include <algorithm>
+
 #include "lr_attend.cuh"
 
 namespace lr {
@@ -303,12 +305,30 @@ Kernel pick_dim(bool bf16, int D, bool few) { return D <= 64 ? pick_rows<FMT, 64
 
 }  // namespace
 
-cudaError_t launch_weigh(const WeighLaunch &a, bool bf16, int fmt, int sms, cudaStream_t st) {
-    const bool few = (long long)a.a.b.max_q * a.a.c.G <= 8;
+cudaError_t launch_weigh_step(const WeighLaunch &a, bool bf16, int fmt, int rows, int sms, cudaStream_t st) {
+    const bool few = rows <= 8;
     const Kernel k = fmt == kFmt16 ? pick_dim<kFmt16>(bf16, a.a.c.D, few)
                    : fmt == kFmtE4M3 ? pick_dim<kFmtE4M3>(bf16, a.a.c.D, few)
                                      : pick_dim<kFmtInt8>(bf16, a.a.c.D, few);
     return launch_chained(k, (few ? 5 : 4) * sms, kThreads, 0, st, a);
+}
+
+// Sequences of up to 8 rows (new tokens x query heads of a KV head), or up to 16 if a batch has no more, are the step
+// kernel's, others the chunk kernel's; a single sequence takes one launch.
+cudaError_t launch_weigh(const WeighLaunch &a, bool bf16, int fmt, int sms, cudaStream_t st) {
+    const long long most = (long long)a.a.b.max_q * a.a.c.G;
+    const int few = most <= 16 || a.a.c.G > 8 ? 16 : 8;
+    WeighLaunch l = a;
+    if (most > few) {
+        const bool all = a.a.b.n == 1;
+        l.a.row_lo = all ? 1 : few + 1;
+        l.a.row_hi = 0x7fffffff;
+        const cudaError_t e = launch_weigh_chunk(l, bf16, fmt, sms, st);
+        if (e != cudaSuccess || all || a.a.c.G > few) return e;
+    }
+    l.a.row_lo = 1;
+    l.a.row_hi = (int)std::min<long long>(most, few);
+    return launch_weigh_step(l, bf16, fmt, l.a.row_hi, sms, st);
 }
 
 }  // namespace lr
