@@ -120,11 +120,12 @@ struct WeighLaunch {
     float *w;
     int64_t wb, wt, wh;  // strides of block, token, head in floats
     float decay;
+    float lse_log2, lse_log2_rest;  // scale_log2 / scale: with the rounding of scale_log2 in it, so that it cancels where a score is near its lse
 };
-cudaError_t launch_weigh(const WeighLaunch &a, bool bf16, int fmt, int sms, cudaStream_t st);
+cudaError_t launch_weigh(const WeighLaunch &a, const CacheMaps &m, bool bf16, int fmt, int sms, cudaStream_t st);
 // (its kernels: of sequences of `rows` rows at most, 8 or 16; of others, one CTA an SM, whose parts of 256 tokens are joined)
 cudaError_t launch_weigh_step(const WeighLaunch &a, bool bf16, int fmt, int rows, int sms, cudaStream_t st);
-cudaError_t launch_weigh_chunk(const WeighLaunch &a, bool bf16, int fmt, int sms, cudaStream_t st);
+cudaError_t launch_weigh_chunk(const WeighLaunch &a, const CacheMaps &m, bool bf16, int fmt, int sms, cudaStream_t st);
 cudaError_t weigh_init();
 
 // The tokens that a cache keeps (lr_select.cu).

@@ -62,7 +62,10 @@ int lr_cache_weigh(lr_cache *c, const lr_cache_batch *b, int32_t T, const void *
     l.wt = token_stride;
     l.wh = head_stride;
     l.decay = decay;
-    cudaError_t e = launch_weigh(l, c->bf16, c->cfg.format, c->sms, (cudaStream_t)stream);
+    const double ratio = (double)a.scale_log2 / (double)scale;
+    l.lse_log2 = (float)ratio;
+    l.lse_log2_rest = (float)(ratio - (double)l.lse_log2);
+    cudaError_t e = launch_weigh(l, c->maps, c->bf16, c->cfg.format, c->sms, (cudaStream_t)stream);
     return e == cudaSuccess ? LR_OK : cuda_fail(c, e, "weigh launch");
 }
 

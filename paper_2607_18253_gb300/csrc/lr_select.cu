@@ -214,7 +214,9 @@ cudaError_t launch_select(const SelectLaunch &a, int sms, cudaStream_t st) {
     const long long lists = (long long)a.b.n * a.c.H, longest = std::min((long long)a.b.max_blocks * a.c.b, (long long)kMaxTokens);
     SelectLaunch l = a;
     l.cluster = 1;
-    while (l.cluster < kMaxCluster && 2 * lists * l.cluster <= 3 * sms && longest >= 2ll * kLeast * l.cluster) l.cluster *= 2;
+    // as many CTAs a list as hold its keys, and more of them for few lists
+    while (l.cluster < kMaxCluster && (longest > (long long)kHold * l.cluster || (2 * lists * l.cluster <= 3 * sms && longest >= 2ll * kLeast * l.cluster)))
+        l.cluster *= 2;
     const long long each = longest / l.cluster + 64;
     l.hold = (int)std::min(each, (long long)(lists * l.cluster <= sms ? kHoldAlone : kHold));
     return launch_clusters(k_select, (unsigned)(lists * l.cluster), kThreads, smem_of(l.hold), (unsigned)l.cluster, st, l);

@@ -23,7 +23,7 @@ struct Piece {
     static constexpr int kVec = DP * (FMT == kFmt16 ? 2 : 1) / 64;  // 16-byte pieces a lane and vector
     static constexpr int NB = 4 / kVec;                             // blocks of 16 tokens
     static constexpr int kTile = 16 * NB;
-    static constexpr int kCtas = NR == 1 ? 5 : 4;                   // of an SM
+    static constexpr int kCtas = NR == 1 && FMT == kFmt16 ? 5 : 4;                   // of an SM
 };
 
 template <bool BF16>
@@ -36,8 +36,10 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// The batch's tiles of tokens in one line: sequences in order, in a sequence tile after tile, in a tile head after head
-// (where a block's heads lie together, so do a CTA's reads).  What no row sees is left out where nothing changes it.
+__device__ __forceinline__ float lse_log2(const WeighLaunch &a, float l) { return fmaf(l, a.lse_log2, l * a.lse_log2_rest); }
+
+// The batch's tiles of tokens in one line: sequences in order, in a sequence head after head, so that a warp keeps its queries
+// from tile to tile.  What no row sees is left out where nothing changes it.
 template <int TILE>
 struct Walk {
     int s, q0, ql, kv;
@@ -49,13 +51,13 @@ struct Walk {
         else ns = wf = 0, nt = (kv - 1) / TILE + 1;
         return true;
     }
-    // On by so many tiles and heads (fewer than there are); false behind the last sequence.
-    __device__ __forceinline__ bool on(const WeighLaunch &a, int tiles, int heads) {
+    // On by so many tiles; false behind the last sequence.
+    __device__ __forceinline__ bool on(const WeighLaunch &a, int tiles) {
         tile += tiles;
-        h += heads;
-        if (h >= a.a.c.H) h -= a.a.c.H, ++tile;
         while (tile >= nt) {
             tile -= nt;
+            if (++h < a.a.c.H) continue;
+            h = 0;
             do
                 if (++s >= a.a.b.n) return false;
             while (!load(a));
@@ -115,10 +117,9 @@ __global__ void __launch_bounds__(kThreads, Piece<DP, FMT, NR>::kCtas) k_weigh_s
     __syncthreads();
     at.s = s_seq;
     at.load(a);
-    at.tile = (int)(s_at / c.H);
-    at.h = (int)(s_at - (long long)at.tile * c.H);
-    const int on_t = kWarps / c.H, on_h = kWarps % c.H;
-    if (x0 + warp >= x1 || !at.on(a, warp / c.H, warp % c.H)) {
+    at.h = (int)(s_at / at.nt);
+    at.tile = (int)(s_at - (long long)at.h * at.nt);
+    if (x0 + warp >= x1 || !at.on(a, warp)) {
         chain_next();
         return;
     }
@@ -173,7 +174,7 @@ __global__ void __launch_bounds__(kThreads, Piece<DP, FMT, NR>::kCtas) k_weigh_s
                 }
             }
         }
-        if (left > 0 && at.on(a, on_t, on_h)) look();
+        if (left > 0 && at.on(a, kWarps)) look();
         // rows from the first that may see the tile on; below a window, up to the last
         int r0 = tile0 > lo ? (tile0 - lo) * c.G / kRows * kRows : 0, r1 = rows;
         if (a.a.window > 0 && tile0 >= a.a.sinks) r1 = (int)min((long long)rows, max(0ll, (long long)end + a.a.window - lo) * c.G);
@@ -236,7 +237,7 @@ __global__ void __launch_bounds__(kThreads, Piece<DP, FMT, NR>::kCtas) k_weigh_s
                         const float l = real ? __ldg(a.a.lse + (int64_t)(q0 + tt) * c.Hq + h * c.G + row - tt * c.G) : -INFINITY;
                         // (a row that sees nothing adds nothing)
                         pos[m][y] = l == -INFINITY ? -1 : lo + tt;
-                        less[m][y] = l == -INFINITY ? 0.0f : l * 1.44269504f;
+                        less[m][y] = l == -INFINITY ? 0.0f : lse_log2(a, l);
                         qf[m][y] = a.a.scale_log2 * __shfl_sync(0xffffffffu, pow2, (2 * i4 + y) * 4);
                     }
                 }
@@ -310,12 +311,12 @@ cudaError_t launch_weigh_step(const WeighLaunch &a, bool bf16, int fmt, int rows
     const Kernel k = fmt == kFmt16 ? pick_dim<kFmt16>(bf16, a.a.c.D, few)
                    : fmt == kFmtE4M3 ? pick_dim<kFmtE4M3>(bf16, a.a.c.D, few)
                                      : pick_dim<kFmtInt8>(bf16, a.a.c.D, few);
-    return launch_chained(k, (few ? 5 : 4) * sms, kThreads, 0, st, a);
+    return launch_chained(k, (few && fmt == kFmt16 ? 5 : 4) * sms, kThreads, 0, st, a);
 }
 
 // Sequences of up to 8 rows (new tokens x query heads of a KV head), or up to 16 if a batch has no more, are the step
 // kernel's, others the chunk kernel's; a single sequence takes one launch.
-cudaError_t launch_weigh(const WeighLaunch &a, bool bf16, int fmt, int sms, cudaStream_t st) {
+cudaError_t launch_weigh(const WeighLaunch &a, const CacheMaps &m, bool bf16, int fmt, int sms, cudaStream_t st) {
     const long long most = (long long)a.a.b.max_q * a.a.c.G;
     const int few = most <= 16 || a.a.c.G > 8 ? 16 : 8;
     WeighLaunch l = a;
@@ -323,7 +324,7 @@ cudaError_t launch_weigh(const WeighLaunch &a, bool bf16, int fmt, int sms, cuda
         const bool all = a.a.b.n == 1;
         l.a.row_lo = all ? 1 : few + 1;
         l.a.row_hi = 0x7fffffff;
-        const cudaError_t e = launch_weigh_chunk(l, bf16, fmt, sms, st);
+        const cudaError_t e = launch_weigh_chunk(l, m, bf16, fmt, sms, st);
         if (e != cudaSuccess || all || a.a.c.G > few) return e;
     }
     l.a.row_lo = 1;

@@ -21,9 +21,14 @@ constexpr int kThreads = 512, kUnit = 2 * kTok, kRowTile = 128;
 // of 128 stay zero, and their lse makes nothing of them).
 struct ChunkLaunch {
     WeighLaunch w;
+    CacheMaps m;
     CUtensorMap q;
     int32_t q_map, rt;
 };
+
+// How K reaches shared memory: a 16-bit cache's by the copy engine, or where blocks are odd 16 bytes a thread; 8-bit codes by
+// threads, converted on the way.
+enum : int { kTma = 0, kGather = 1, kConvert = 2 };
 constexpr int kWeight = 2;  // tiles that a unit's beginning and end take the time of
 constexpr int kLeast = 3;   // of a CTA's share
 
@@ -31,9 +36,10 @@ template <int DP>
 struct Shape {
     static constexpr int kPanel = kTok * 128, kTile = kTok * DP * 2;
     static constexpr int kKeys = DP == 128 ? 3 : 6, kRows = DP == 128 ? 3 : 4;  // stages of K and Q
-    static constexpr int kBars = 2 * kKeys + 2 * kRows + 8 + 1;
+    static constexpr int kLess = 8;  // tiles of lse: they are held until the exponentials are taken, Q only for the products
+    static constexpr int kBars = 2 * kKeys + 2 * kRows + 2 * kLess + 8 + 1;
     static constexpr int kTiles = (kKeys + kRows) * kTile;
-    static constexpr int kSmem = kTiles + kKeys * kTok * 12 + kRows * kRowTile * 4 + 2 * kTok * 8 + kBars * 8 + (kThreads / 32 + 2) * 8 + kRows * 4 + 16;
+    static constexpr int kSmem = kTiles + kKeys * kTok * 12 + kLess * kRowTile * 4 + 2 * kTok * 8 + kBars * 8 + (kThreads / 32 + 2) * 8 + kLess * 4 + 16;
     static_assert(kSmem <= 227 * 1024, "shared memory");
 };
 
@@ -165,24 +171,25 @@ __device__ __forceinline__ bool take_line(const WeighLaunch &a, Line &l, Share &
     return l.j < l.end;  // (a share may end in a unit's weight)
 }
 
-template <bool BF16, int FMT, int DP>
+template <bool BF16, int FMT, int DP, int LOAD>
 __global__ void __launch_bounds__(kThreads, 1) k_weigh_chunk(const __grid_constant__ ChunkLaunch in) {
     const WeighLaunch &a = in.w;
     using S = Shape<DP>;
     extern __shared__ __align__(1024) char smem[];
     char *const keys = smem, *const rows = smem + S::kKeys * S::kTile;
     float *const s_less = reinterpret_cast<float *>(smem + S::kTiles);  // [stage][row] -lse * log2(e); -inf: adds nothing
-    float *const s_scale = s_less + S::kRows * kRowTile;                // [stage][token] the scores' factor
+    float *const s_scale = s_less + S::kLess * kRowTile;                // [stage][token] the scores' factor
     int64_t *const s_to = reinterpret_cast<int64_t *>(s_scale + S::kKeys * kTok);  // [stage][token] where its weight is, -1: no place
     int64_t *const s_from = s_to + S::kKeys * kTok;                                // [2][token] where its K is
     uint64_t *const bars = reinterpret_cast<uint64_t *>(s_from + 2 * kTok);
     long long *const scratch = reinterpret_cast<long long *>(bars + S::kBars);
     int *const s_odd = reinterpret_cast<int *>(scratch + kThreads / 32 + 2);  // [stage] a row whose lse is -inf
-    int &s_dead = s_odd[S::kRows];
-    uint32_t &s_tmem = *reinterpret_cast<uint32_t *>(s_odd + S::kRows + 1);
-    uint32_t &s_sent = *reinterpret_cast<uint32_t *>(s_odd + S::kRows + 2);  // tiles of Q that the copy engine was asked for
+    int &s_dead = s_odd[S::kLess];
+    uint32_t &s_tmem = *reinterpret_cast<uint32_t *>(s_odd + S::kLess + 1);
+    uint32_t &s_sent = *reinterpret_cast<uint32_t *>(s_odd + S::kLess + 2);  // tiles of Q, and of K, that the copy engine was asked for
+    uint32_t &s_sent_k = *reinterpret_cast<uint32_t *>(s_odd + S::kLess + 3);
     const uint32_t k_full = smem_addr(bars), k_free = k_full + 8 * S::kKeys, q_full = k_free + 8 * S::kKeys, q_free = q_full + 8 * S::kRows,
-                   s_full = q_free + 8 * S::kRows, s_free = s_full + 32, ended = s_free + 32;  // scores: [half][buffer]
+                   l_full = q_free + 8 * S::kRows, l_free = l_full + 8 * S::kLess, s_full = l_free + 8 * S::kLess, s_free = s_full + 32, ended = s_free + 32;  // scores: [half][buffer]
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     const CacheDev &c = a.a.c;
 
@@ -196,12 +203,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_weigh_chunk(const __grid_consta
     }
     if (tid == 0) {
         for (int i = 0; i < S::kKeys; ++i) {
-            bar_init(k_full + 8 * i, 4);
+            bar_init(k_full + 8 * i, LOAD == kTma ? 5 : 4);
             bar_init(k_free + 8 * i, 5);
         }
         for (int i = 0; i < S::kRows; ++i) {
             bar_init(q_full + 8 * i, 1);
-            bar_init(q_free + 8 * i, 9);
+            bar_init(q_free + 8 * i, 1);
+        }
+        for (int i = 0; i < S::kLess; ++i) {
+            bar_init(l_full + 8 * i, 1);
+            bar_init(l_free + 8 * i, 8);
         }
         for (int i = 0; i < 4; ++i) {
             bar_init(s_full + 8 * i, 1);
@@ -211,7 +222,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_weigh_chunk(const __grid_consta
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         shared_to_async();
         s_dead = 0;
-        s_sent = 0;
+        s_sent = s_sent_k = 0;
     }
     for (int i = tid; i < S::kRows * (kRowTile - in.rt) * DP / 8; i += kThreads) {  // rows of Q's stages that no tile fills
         const int r = i / (DP / 8) % (kRowTile - in.rt) + in.rt, st = i / (DP / 8) / (kRowTile - in.rt);
@@ -257,9 +268,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_weigh_chunk(const __grid_consta
             float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
             const float2 f2 = make_float2(f, f);
             for (int j = l.j; j < l.end; ++j, ++qi) {
-                const uint32_t st = qi % S::kRows;
-                if (on) ok = bar_wait(s_full + 16 * half + 8 * (n_s & 1), n_s >> 1 & 1, dead);
-                ok = ok && bar_wait(q_full + 8 * st, qi / S::kRows & 1, dead);
+                const uint32_t st = qi % S::kLess;
+                ok = bar_wait(l_full + 8 * st, qi / S::kLess & 1, dead);
+                if (on) ok = ok && bar_wait(s_full + 16 * half + 8 * (n_s & 1), n_s >> 1 & 1, dead);
                 if (!ok) break;
                 if (on) {
                     after_sync();
@@ -316,7 +327,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_weigh_chunk(const __grid_consta
                     }
                     ++n_s;
                 }
-                bar_arrive_warp(q_free + 8 * st);
+                bar_arrive_warp(l_free + 8 * st);
             }
             if (!ok) break;
             // ---- the unit ends here, for this CTA ----
@@ -449,7 +460,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_weigh_chunk(const __grid_consta
             if (more) then = look(g);
             const uint32_t st = key % S::kKeys, round = key / S::kKeys;
             if (round > 0) {
-                if constexpr (FMT == kFmt16) {
+                if constexpr (LOAD == kGather) {
                     // a warp that has to wait hands over what it has copied first
                     if (!__all_sync(0xffffffffu, bar_test(k_free + 8 * st, (round - 1) & 1))) drain();
                 }
@@ -459,7 +470,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_weigh_chunk(const __grid_consta
             s_scale[st * kTok + i] = now.scale;
             const uint32_t into = smem_addr(keys + st * S::kTile);
             if (!ok) {
-            } else if constexpr (FMT == kFmt16) {
+            } else if constexpr (LOAD == kTma) {
+                bar_arrive_warp(k_full + 8 * st);  // (the vectors are another warp's)
+            } else if constexpr (LOAD == kGather) {
 #pragma unroll
                 for (int k = 0; k < kIts; ++k) {
                     const int64_t from = s_from[(key & 1) * kTok + r0 + k * kStep];
@@ -496,14 +509,53 @@ __global__ void __launch_bounds__(kThreads, 1) k_weigh_chunk(const __grid_consta
                 bar_arrive_warp(k_full + 8 * st);
             }
             // the next tile's places, for all the warps
-            s_from[(key + 1 & 1) * kTok + i] = then.from;
-            named_sync(1, 128);
+            if constexpr (LOAD != kTma) {
+                s_from[(key + 1 & 1) * kTok + i] = then.from;
+                named_sync(1, 128);
+            }
             if constexpr (FMT != kFmt16) {
                 if (more) fetch(key + 1);
             }
             now = then;
         }
         drain();
+    } else if (LOAD == kTma && warp == 9) {
+        // ================= K by the copy engine: lane i is box i of the tile =================
+        const int box = in.m.box;
+        int g = 0;
+        auto look = [&](int &place) {
+            const int p = l.base() + g * kTok + lane * box;
+            // (what no row sees is not looked up: its block may be gone)
+            if (lane * box >= kTok || p >= l.kv || (a.a.window > 0 && p + box - 1 <= l.lo - a.a.window && p >= a.a.sinks)) return -1;
+            return (int)block_of(c, a.a.b, l.s, p, place);
+        };
+        int place = 0, blk = look(place);
+        for (bool more = true; more; ++key) {  // (l and g stand at the tile, then at the next)
+            const int h = l.h, now = blk, at = place;
+            if (++g == l.halves()) {
+                g = 0;
+                more = !l.last;
+                if (more) l.next(a, sh);
+            }
+            if (more) blk = look(place);
+            const uint32_t st = key % S::kKeys, round = key / S::kKeys, boxes = __popc(__ballot_sync(0xffffffffu, now >= 0));
+            if (round > 0) ok = bar_wait(k_free + 8 * st, (round - 1) & 1, dead);
+            if (!ok) break;
+            const uint32_t bar = k_full + 8 * st, into = smem_addr(keys + st * S::kTile) + lane * box * 128;
+            if (lane == 0) {
+                s_sent_k = key + 1;
+                asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(boxes * box * 2 * DP) : "memory");
+            }
+            __syncwarp();
+            if (now >= 0) {
+#pragma unroll
+                for (int p = 0; p < DP / 64; ++p)
+                    asm volatile(
+                        "cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(
+                            into + p * S::kPanel), "l"(&in.m.k), "r"(bar), "r"(p * 64), "r"(at), "r"(h), "r"(now)
+                        : "memory");
+            }
+        }
     } else if (warp == 11) {
         // ================= queries and their lse to shared memory =================
         // lse of a tile, four rows a lane; asked for a tile ahead
@@ -525,19 +577,22 @@ __global__ void __launch_bounds__(kThreads, 1) k_weigh_chunk(const __grid_consta
                 j = l.j;
             }
             if (more) lse_of(j, then);
-            const uint32_t st = qi % S::kRows, round = qi / S::kRows;
-            if (round > 0) ok = bar_wait(q_free + 8 * st, (round - 1) & 1, dead);
+            const uint32_t st = qi % S::kRows, round = qi / S::kRows, ls = qi % S::kLess;
+            if (qi >= S::kLess) ok = bar_wait(l_free + 8 * ls, (qi / S::kLess - 1) & 1, dead);
             if (!ok) break;
             bool odd = false;
             float less[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 odd |= now[k] == -INFINITY;  // (a row that saw nothing adds nothing)
-                less[k] = now[k] == -INFINITY ? -INFINITY : now[k] * -1.44269504f;
+                less[k] = now[k] == -INFINITY ? -INFINITY : -fmaf(now[k], a.lse_log2, now[k] * a.lse_log2_rest);
             }
-            *reinterpret_cast<float4 *>(s_less + st * kRowTile + lane * 4) = make_float4(less[0], less[1], less[2], less[3]);
+            *reinterpret_cast<float4 *>(s_less + ls * kRowTile + lane * 4) = make_float4(less[0], less[1], less[2], less[3]);
             odd = __any_sync(0xffffffffu, odd);
-            if (lane == 0) s_odd[st] = odd;
+            if (lane == 0) s_odd[ls] = odd;
+            bar_arrive_warp(l_full + 8 * ls);
+            if (round > 0) ok = bar_wait(q_free + 8 * st, (round - 1) & 1, dead);
+            if (!ok) break;
             const uint32_t into = smem_addr(rows + st * S::kTile);
             if (in.q_map) {
                 __syncwarp();
@@ -582,6 +637,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_weigh_chunk(const __grid_consta
             over(ended, 0);
             const uint32_t sent = s_sent;
             for (uint32_t i = sent > S::kRows ? sent - S::kRows : 0; i < sent; ++i) over(q_full + 8 * (i % S::kRows), i / S::kRows & 1);
+            const uint32_t sent_k = s_sent_k;
+            for (uint32_t i = sent_k > S::kKeys ? sent_k - S::kKeys : 0; i < sent_k; ++i) over(k_full + 8 * (i % S::kKeys), i / S::kKeys & 1);
         }
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tm));
         if (lane == 0 && *dead) report(c.status, kECuda);
@@ -594,32 +651,36 @@ struct Pick {
     Kernel k;
     int smem;
 };
-template <int FMT>
-Pick pick_fmt(bool bf16, int D) {
-    if (D <= 64) return {bf16 ? k_weigh_chunk<true, FMT, 64> : k_weigh_chunk<false, FMT, 64>, Shape<64>::kSmem};
-    return {bf16 ? k_weigh_chunk<true, FMT, 128> : k_weigh_chunk<false, FMT, 128>, Shape<128>::kSmem};
+template <int FMT, int LOAD>
+Pick pick_load(bool bf16, int D) {
+    if (D <= 64) return {bf16 ? k_weigh_chunk<true, FMT, 64, LOAD> : k_weigh_chunk<false, FMT, 64, LOAD>, Shape<64>::kSmem};
+    return {bf16 ? k_weigh_chunk<true, FMT, 128, LOAD> : k_weigh_chunk<false, FMT, 128, LOAD>, Shape<128>::kSmem};
 }
-Pick pick(bool bf16, int fmt, int D) {
-    return fmt == kFmt16 ? pick_fmt<kFmt16>(bf16, D) : fmt == kFmtE4M3 ? pick_fmt<kFmtE4M3>(bf16, D) : pick_fmt<kFmtInt8>(bf16, D);
+Pick pick(bool bf16, int fmt, int D, bool tma) {
+    return fmt == kFmtE4M3 ? pick_load<kFmtE4M3, kConvert>(bf16, D)
+         : fmt == kFmtInt8 ? pick_load<kFmtInt8, kConvert>(bf16, D)
+         : tma             ? pick_load<kFmt16, kTma>(bf16, D)
+                           : pick_load<kFmt16, kGather>(bf16, D);
 }
 
 }  // namespace
 
 cudaError_t weigh_init() {
     for (int bf16 = 0; bf16 < 2; ++bf16)
-        for (int fmt = 0; fmt < 3; ++fmt)
+        for (int load = 0; load < 4; ++load)
             for (int D = 64; D <= 128; D += 64) {
-                const Pick p = pick(bf16, fmt, D);
+                const Pick p = pick(bf16, load == 3 ? (int)kFmt16 : load, D, load == 3);
                 const cudaError_t e = cudaFuncSetAttribute(p.k, cudaFuncAttributeMaxDynamicSharedMemorySize, p.smem);
                 if (e != cudaSuccess) return e;
             }
     return cudaSuccess;
 }
 
-cudaError_t launch_weigh_chunk(const WeighLaunch &a, bool bf16, int fmt, int sms, cudaStream_t st) {
-    const Pick p = pick(bf16, fmt, a.a.c.D);
+cudaError_t launch_weigh_chunk(const WeighLaunch &a, const CacheMaps &m, bool bf16, int fmt, int sms, cudaStream_t st) {
+    const Pick p = pick(bf16, fmt, a.a.c.D, m.box > 0);
     ChunkLaunch l;
     l.w = a;
+    l.m = m;
     l.rt = a.a.c.G <= kRowTile ? kRowTile / a.a.c.G * a.a.c.G : kRowTile;
     l.q_map = encode_rows(a.a, bf16, l.q);
     return launch_chained(p.k, sms, kThreads, p.smem, st, l);

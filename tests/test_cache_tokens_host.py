@@ -12,7 +12,7 @@ from test_cache_host import LAUNCHES, RUNTIME
 MORE = r"""
 namespace lr {
 static int launched;
-cudaError_t launch_weigh(const WeighLaunch &, bool, int, int, cudaStream_t) { ++launched; return cudaSuccess; }
+cudaError_t launch_weigh(const WeighLaunch &, const CacheMaps &, bool, int, int, cudaStream_t) { ++launched; return cudaSuccess; }
 cudaError_t launch_select(const SelectLaunch &, int, cudaStream_t) { ++launched; return cudaSuccess; }
 cudaError_t launch_keep(const KeepLaunch &, int, int, cudaStream_t) { ++launched; return cudaSuccess; }
 }
