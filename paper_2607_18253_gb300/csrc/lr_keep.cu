@@ -6,8 +6,9 @@
 // vectors.  A list, or each such part of it where lists are few, is moved by a cluster of CTAs that read a batch, meet,
 // and write it, with no other wait.
 //
-// What bounds it is the bytes moved, and for short lists the chain list -> block table -> vectors.  The chain is
-// taken a batch ahead, by a thread a token, and left in shared memory; of all threads a batch is two times kItems accesses of 16 bytes.
+// What bounds it is the bytes moved, and for short lists the chain list -> block table -> vectors.  Of a long list the chain
+// is taken for 512 tokens at once and left in shared memory, with their scales and weights; the vectors then
+// follow batch after batch, the next one's read before the last one's is written.
 #include <algorithm>
 
 #include "lr_cache.cuh"
@@ -16,14 +17,13 @@ namespace lr {
 
 namespace {
 
-constexpr int kThreads = 256, kItems = 4, kMaxCluster = 8;
+constexpr int kThreads = 256, kItems = 2, kMaxCluster = 8;
+constexpr int kAhead = 2, kRun = kThreads * kAhead;  // tokens of a CTA that are looked up together
 
-// LANES lanes a piece of a vector, 16 bytes a lane; BOTH: K and V by the same CTA.
 template <int LANES, bool BOTH>
-__global__ void __launch_bounds__(kThreads, 5) k_keep(const __grid_constant__ KeepLaunch a) {
-    constexpr int kLanes = LANES * (BOTH ? 2 : 1), kBatch = kThreads * kItems / kLanes;
-    static_assert(kBatch <= kThreads, "a thread a token");
-    __shared__ int4 s_move[2][kBatch];  // block and place of a token, and of where it goes; -1: not moved
+__global__ void __launch_bounds__(kThreads, 4) k_keep(const __grid_constant__ KeepLaunch a) {
+    constexpr int kLanes = LANES * (BOTH ? 2 : 1);
+    __shared__ int4 s_move[kRun];  // block and place of a token, and of where it goes; -1: not moved
     const CacheDev &c = a.c;
     const int tid = threadIdx.x, lane = tid % LANES, cl = a.cluster;
     int x = blockIdx.x / cl;
@@ -45,64 +45,110 @@ __global__ void __launch_bounds__(kThreads, 5) k_keep(const __grid_constant__ Ke
     }
     const int32_t *const kept = a.kept + s * a.kept_s + h * a.kept_h;
     char *const data = (is_v ? c.v : c.k) + h * c.sh + byte;
-    // A thread's token of the batch that begins at i0: block and place of its source and of its place, the first -1 if it is not moved.
-    auto look = [&](int i0) {
-        int4 m = make_int4(-1, 0, 0, 0);
-        const int i = i0 + rank * batch + tid;
-        if (i < count) {
-            const int src = __ldg(kept + i), dst = start + i, prev = i > 0 ? __ldg(kept + i - 1) : -1;
-            const bool good = src >= dst && src < kv && prev < src;
-            if (good && src != dst) {
-                m.x = (int)block_of(c, a.b, s, src, m.y);
-                m.z = (int)block_of(c, a.b, s, dst, m.w);
-                if (m.z < 0) m.x = -1;
-            }
-            if (!good || (src != dst && m.x < 0)) report(c.status, kEInval);
-        }
-        return m;
-    };
-    // scales and weight of a token, which its thread moves with the first piece
+    // scales and weights move with the first piece
     const bool k_too = (BOTH || !(x & 1)) && piece == 0, v_too = (BOTH || (x & 1)) && piece == 0;
     auto scale_at = [&](int blk, int place) { return (int64_t)blk * c.ssb + place * c.sst + h * c.ssh; };
     auto weight_at = [&](int blk, int place) { return (int64_t)blk * a.wb + place * a.wt + h * a.wh; };
-    if (tid < batch) s_move[0][tid] = look(0);
-    __syncthreads();
-    int buf = 0;
-    for (int i0 = 0; i0 < count; i0 += cl * batch, buf ^= 1) {
-        uint4 v[kItems];
-        char *to[kItems];
-#pragma unroll
-        for (int u = 0; u < kItems; ++u) {
-            const int4 m = s_move[buf][u * groups + tid / kLanes];
-            to[u] = mine && m.x >= 0 ? data + m.z * c.sb + m.w * c.st : nullptr;
-            if (to[u]) v[u] = __ldcs(reinterpret_cast<const uint4 *>(data + m.x * c.sb + m.y * c.st));
-        }
-        float ks, vs, w;
-        if (tid < batch) {
-            const int4 m = s_move[buf][tid];
-            if (m.x >= 0 && c.ks && k_too) ks = c.ks[scale_at(m.x, m.y)];
-            if (m.x >= 0 && c.ks && v_too) vs = c.vs[scale_at(m.x, m.y)];
-            if (m.x >= 0 && a.w && k_too) w = a.w[weight_at(m.x, m.y)];
-        }
-        const bool more = i0 + cl * batch < count;
-        int4 next;
-        if (more && tid < batch) next = look(i0 + cl * batch);
-        // (the next batch's reads need not wait for these writes: nothing that it reads is written before)
-        if (cl > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
-        else __syncthreads();
-#pragma unroll
-        for (int u = 0; u < kItems; ++u)
-            if (to[u]) *reinterpret_cast<uint4 *>(to[u]) = v[u];
-        if (tid < batch) {
-            const int4 m = s_move[buf][tid];
-            if (m.x >= 0 && c.ks && k_too) c.ks[scale_at(m.z, m.w)] = ks;
-            if (m.x >= 0 && c.ks && v_too) c.vs[scale_at(m.z, m.w)] = vs;
-            if (m.x >= 0 && a.w && k_too) a.w[weight_at(m.z, m.w)] = w;
-        }
-        if (more) {
-            if (tid < batch) s_move[buf ^ 1][tid] = next;
+    // The cluster has read what it was to read before it writes.  (Later reads need not wait for these writes: nothing
+    // that is read later is written before.)  `seen`: of a value read; it has come when it goes into the CTA's barrier, so that the
+    // cluster's need not order memory, which would wait for the last batch's writes.
+    auto meet = [&](uint32_t seen) {
+        if (cl > 1) {
+            __syncthreads_or(seen == 0x5bd1e995u);
+            asm volatile("barrier.cluster.arrive.relaxed.aligned;\n barrier.cluster.wait.aligned;" ::: "memory");
+        } else {
             __syncthreads();
         }
+    };
+    const int run = min(kRun, threads * kAhead) / batch * batch;  // of this CTA; the cluster's CTAs take batches in turn
+    for (int64_t r0 = 0; r0 < count; r0 += (int64_t)cl * run) {
+        // the token of element e of the run
+        auto token = [&](int e) { return r0 + ((int64_t)(e / batch) * cl + rank) * batch + e % batch; };
+        int4 m[kAhead];
+        float ks[kAhead], vs[kAhead], w[kAhead];
+        int src[kAhead], prev[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int e = u * threads + tid;
+            const int64_t i = token(e);
+            src[u] = e < run && i < count ? __ldg(kept + i) : -1;
+            prev[u] = e < run && i < count && i > 0 ? __ldg(kept + i - 1) : -1;
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int e = u * threads + tid;
+            const int64_t i = token(e);
+            m[u] = make_int4(-1, 0, -1, 0);
+            if (e >= run || i >= count) continue;
+            const int dst = start + (int)i;
+            if (src[u] < dst || src[u] >= kv || prev[u] >= src[u]) {
+                report(c.status, kEInval);
+            } else if (src[u] != dst) {
+                m[u].x = (int)block_of(c, a.b, s, src[u], m[u].y);
+                m[u].z = (int)block_of(c, a.b, s, dst, m[u].w);
+                if (m[u].x < 0 || m[u].z < 0) {
+                    report(c.status, kEInval);
+                    m[u].x = -1;
+                }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (u * threads + tid < run) s_move[u * threads + tid] = m[u];
+            if (m[u].x >= 0 && c.ks && k_too) ks[u] = c.ks[scale_at(m[u].x, m[u].y)];
+            if (m[u].x >= 0 && c.ks && v_too) vs[u] = c.vs[scale_at(m[u].x, m[u].y)];
+            if (m[u].x >= 0 && a.w && k_too) w[u] = a.w[weight_at(m[u].x, m[u].y)];
+        }
+        uint32_t seen = 0;
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (m[u].x >= 0 && c.ks && k_too) seen |= __float_as_uint(ks[u]);
+            if (m[u].x >= 0 && c.ks && v_too) seen |= __float_as_uint(vs[u]);
+            if (m[u].x >= 0 && a.w && k_too) seen |= __float_as_uint(w[u]);
+        }
+        meet(seen);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (m[u].x >= 0 && c.ks && k_too) c.ks[scale_at(m[u].z, m[u].w)] = ks[u];
+            if (m[u].x >= 0 && c.ks && v_too) c.vs[scale_at(m[u].z, m[u].w)] = vs[u];
+            if (m[u].x >= 0 && a.w && k_too) a.w[weight_at(m[u].z, m[u].w)] = w[u];
+        }
+        // the cluster's batches of the run: as many for each of its CTAs, though the last may have none of their tokens
+        const int batches = (int)min((int64_t)(run / batch), (count - r0 + (int64_t)cl * batch - 1) / ((int64_t)cl * batch));
+        uint4 v[2][kItems];
+        char *to[2][kItems];
+        auto read = [&](int n, uint4 (&v)[kItems], char *(&to)[kItems]) {
+#pragma unroll
+            for (int u = 0; u < kItems; ++u) {
+                const int4 at = s_move[n * batch + u * groups + tid / kLanes];
+                to[u] = mine && at.x >= 0 ? data + at.z * c.sb + at.w * c.st : nullptr;
+                if (to[u]) v[u] = __ldcs(reinterpret_cast<const uint4 *>(data + at.x * c.sb + at.y * c.st));
+            }
+        };
+        auto write = [&](uint4 (&v)[kItems], char *(&to)[kItems]) {
+#pragma unroll
+            for (int u = 0; u < kItems; ++u)
+                if (to[u]) *reinterpret_cast<uint4 *>(to[u]) = v[u];
+        };
+        auto all = [&](uint4 (&v)[kItems], char *(&to)[kItems]) {
+            uint32_t x = 0;
+#pragma unroll
+            for (int u = 0; u < kItems; ++u)
+                if (to[u]) x |= v[u].x;
+            return x;
+        };
+        // (a batch is written after a meeting that all CTAs come to when they have read the batch behind it)
+        read(0, v[0], to[0]);
+        for (int n = 0; n < batches; n += 2) {
+            if (n + 1 < batches) read(n + 1, v[1], to[1]);
+            meet(all(v[0], to[0]));
+            write(v[0], to[0]);
+            if (n + 1 >= batches) break;
+            if (n + 2 < batches) read(n + 2, v[0], to[0]);
+            meet(all(v[1], to[1]));
+            write(v[1], to[1]);
+        }
+        if (r0 + (int64_t)cl * run < count) __syncthreads();
     }
     chain_next();
 }

@@ -2,9 +2,9 @@
 // with the largest weights, ties to the lowest position, in order of position.
 //
 // A weight becomes a 32-bit key that sorts as it does, a token that is kept in any case the largest.  The key of the last token
-// that is kept is found from the top bits down, by counting (11, 11 and 10 bits: three counts of 2,048 bins); the
-// tokens above it are kept, and of those equal to it the first ones.  A cluster of CTAs has a list, each a range of its
-// positions: the counts and the places of the ranges' tokens are read from one another's shared memory.
+// that is kept is found from the top byte down, by counting (four counts of 256 bins); the tokens above it
+// are kept, and of those equal to it the first ones.  A cluster of CTAs has a list, each a range of its positions, whose keys it
+// holds in shared memory; the counts come together in the first CTA's, and the places of the ranges' tokens are read from one another's.
 #include <algorithm>
 
 #include "lr_cache.cuh"
@@ -13,13 +13,13 @@ namespace lr {
 
 namespace {
 
-constexpr int kThreads = 512, kWarps = kThreads / 32, kBins = 2048;
-// Keys that a CTA holds in shared memory; further ones are read again for each count.  Of CTAs that are no more than the SMs a
-// CTA takes what there is, else what leaves room for three.
-constexpr int kHold = 12288, kHoldAlone = 49152;
-constexpr int kMaxCluster = 8, kLeast = 2048;  // (positions a CTA, at least, or a list is not divided)
-constexpr int kAhead = 8;                      // weights that a thread reads together
-constexpr size_t smem_of(int hold) { return (size_t)hold * 4 + 3 * kBins * 4; }
+constexpr int kMostThreads = 1024, kMostWarps = kMostThreads / 32, kBins = 256;
+// Keys that a CTA holds in shared memory; further ones are read again for each count.  CTAs that are no more than the SMs take
+// what there is, and 1,024 threads; others leave room for four, of 256 threads.
+constexpr int kHold = 10240, kHoldAlone = 49152;
+constexpr int kMaxCluster = 16, kLeast = 2048;  // (positions a CTA, at least, or a list is not divided)
+constexpr int kAhead = 16;                      // weights that a thread reads together
+constexpr size_t smem_of(int hold) { return (size_t)hold * 4 + 4 * kBins * 4; }
 
 // As `w` sorts: NaN above all, both zeros the same.
 __device__ __forceinline__ uint32_t key_of(float w) {
@@ -28,6 +28,7 @@ __device__ __forceinline__ uint32_t key_of(float w) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
+__device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
     asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
@@ -48,12 +49,12 @@ __device__ __forceinline__ uint32_t peer_word(uint32_t at) {
     return v;
 }
 
-__global__ void __launch_bounds__(kThreads) k_select(const __grid_constant__ SelectLaunch a) {
+__global__ void __launch_bounds__(kMostThreads) k_select(const __grid_constant__ SelectLaunch a) {
     extern __shared__ __align__(16) uint32_t smem[];
-    uint32_t *const bins = smem, *const hold = smem + 3 * kBins;  // [3][kBins], keys
-    __shared__ uint32_t s_warp[2 * kWarps], s_bin[2], s_mine[2];
+    uint32_t *const bins = smem, *const hold = smem + 4 * kBins;  // [4][kBins], keys
+    __shared__ uint32_t s_warp[2 * kMostWarps], s_bin[2], s_mine[2];
     const int cl = a.cluster;
-    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, threads = blockDim.x, warps = threads / 32;
     const int rank = cl > 1 ? (int)cluster_rank() : 0;
     const CacheDev &c = a.c;
     chain_wait();
@@ -66,9 +67,9 @@ __global__ void __launch_bounds__(kThreads) k_select(const __grid_constant__ Sel
     m = min(m, kv);
     int32_t *const kept = a.kept + (int64_t)list * a.cap;
     if (h == 0 && rank == 0 && tid == 0) a.count[s] = m;
-    for (int64_t i = (int64_t)m + rank * kThreads + tid; i < a.cap; i += (int64_t)cl * kThreads) kept[i] = -1;
+    for (int64_t i = (int64_t)m + rank * threads + tid; i < a.cap; i += (int64_t)cl * threads) kept[i] = -1;
     if (m == kv || m == 0) {  // (all or none: the whole cluster takes this way)
-        for (int64_t i = rank * kThreads + tid; i < m; i += cl * kThreads) kept[i] = (int32_t)i;
+        for (int64_t i = rank * threads + tid; i < m; i += cl * threads) kept[i] = (int32_t)i;
         chain_next();
         return;
     }
@@ -88,67 +89,57 @@ __global__ void __launch_bounds__(kThreads) k_select(const __grid_constant__ Sel
     const int held = a.hold;
     auto key = [&](int p) { return p - p0 < held ? hold[p - p0] : read(p); };
 
-    for (int i = tid; i < 3 * kBins; i += kThreads) bins[i] = 0;
+    for (int i = tid; i < 4 * kBins; i += threads) bins[i] = 0;
     if (cl > 1) cluster_sync();
     else __syncthreads();
-    for (int p = p0 + tid; p < p1; p += kThreads * kAhead) {
+    for (int p = p0 + tid; p < p1; p += threads * kAhead) {
         uint32_t k[kAhead];
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) k[i] = p + i * kThreads < p1 ? read(p + i * kThreads) : 0u;
+        for (int i = 0; i < kAhead; ++i) k[i] = p + i * threads < p1 ? read(p + i * threads) : 0u;
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            const int at = p + i * kThreads;
+            const int at = p + i * threads;
             if (at >= p1) break;
             if (at - p0 < held) hold[at - p0] = k[i];
-            atomicAdd(bins + (k[i] >> 21), 1u);
+            atomicAdd(bins + (k[i] >> 24), 1u);
         }
     }
     uint32_t prefix = 0, need = m;  // the key's bits so far; of the keys that have them, how many are kept
 #pragma unroll 1
-    for (int round = 0; round < 3; ++round) {
-        uint32_t *const bin = bins + round * kBins;
-        const int shift = round == 0 ? 21 : round == 1 ? 10 : 0, many = round == 2 ? 1024 : kBins;
-        if (round > 0) {
-            const int above = round == 1 ? 21 : 10;
-            for (int p = p0 + tid; p < p1; p += kThreads) {
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        uint32_t *const bin = bins + (3 - shift / 8) * kBins;
+        if (shift < 24) {
+#pragma unroll 4
+            for (int p = p0 + tid; p < p1; p += threads) {
                 const uint32_t k = key(p);
-                if (k >> above == prefix >> above) atomicAdd(bin + (k >> shift & (many - 1)), 1u);
+                if ((k ^ prefix) >> shift < 256u) atomicAdd(bin + (k >> shift & 255), 1u);
             }
         }
         // the cluster's counts come together in its first CTA
         if (rank > 0) {
             __syncthreads();
-            for (int i = tid; i < many; i += kThreads)
-                if (bin[i]) asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], %1;" ::"r"(peer(bin + i, 0)), "r"(bin[i]) : "memory");
+            if (tid < kBins && bin[tid]) asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], %1;" ::"r"(peer(bin + tid, 0)), "r"(bin[tid]) : "memory");
         }
         if (cl > 1) cluster_sync();
         else __syncthreads();
-        // four bins a thread, from the top: those before the bin that brings the count to `need`
-        const int b0 = many - 1 - tid * 4;
-        uint32_t v[4] = {0, 0, 0, 0};
-        if (b0 >= 0) {
-            if (cl > 1)
-                asm volatile("ld.shared::cluster.v4.u32 {%3,%2,%1,%0}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(peer(bin + b0 - 3, 0)) : "memory");
-            else
+        // a bin a thread, from the top: the bin that brings the count to `need`
+        if (tid < kBins) {
+            const uint32_t mine = cl > 1 ? peer_word(peer(bin + kBins - 1 - tid, 0)) : bin[kBins - 1 - tid];
+            uint32_t incl = mine;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = bin[b0 - i];
-        }
-        const uint32_t mine = v[0] + v[1] + v[2] + v[3];
-        uint32_t incl = mine;
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t x = __shfl_up_sync(0xffffffffu, incl, o);
+                if (lane >= o) incl += x;
+            }
+            if (lane == 31) s_warp[warp] = incl;
+            named_sync(1, kBins);
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const uint32_t x = __shfl_up_sync(0xffffffffu, incl, o);
-            if (lane >= o) incl += x;
-        }
-        if (lane == 31) s_warp[warp] = incl;
-        __syncthreads();
-        for (int w = 0; w < warp; ++w) incl += s_warp[w];
-        uint32_t before = incl - mine;
-        if (before < need && need <= incl) {
-            int i = 0;
-            while (before + v[i] < need) before += v[i++];
-            s_bin[0] = b0 - i;
-            s_bin[1] = need - before;
+            for (int w = 0; w < kBins / 32; ++w)
+                if (w < warp) incl += s_warp[w];
+            if (incl - mine < need && need <= incl) {
+                s_bin[0] = kBins - 1 - tid;
+                s_bin[1] = need - (incl - mine);
+            }
         }
         __syncthreads();
         prefix |= s_bin[0] << shift;
@@ -157,9 +148,10 @@ __global__ void __launch_bounds__(kThreads) k_select(const __grid_constant__ Sel
     }
     // prefix is the last kept token's key now, `need` how many of those equal to it are kept
 
-    const int each = ((p1 - p0 + kWarps - 1) / kWarps + 31) / 32 * 32;
+    const int each = ((p1 - p0 + warps - 1) / warps + 31) / 32 * 32;
     const int w0 = min(p1, p0 + warp * each), w1 = min(p1, w0 + each);
     uint32_t above = 0, equal = 0;
+#pragma unroll 4
     for (int p = w0 + lane; p - lane < w1; p += 32) {
         const uint32_t k = p < w1 ? key(p) : 0u;
         above += __popc(__ballot_sync(0xffffffffu, p < w1 && k > prefix));
@@ -167,17 +159,20 @@ __global__ void __launch_bounds__(kThreads) k_select(const __grid_constant__ Sel
     }
     if (lane == 0) {
         s_warp[warp] = above;
-        s_warp[kWarps + warp] = equal;
+        s_warp[kMostWarps + warp] = equal;
     }
     __syncthreads();
     uint32_t out = 0, eq = 0;
-    for (int w = 0; w < kWarps; ++w) {
-        if (w < warp) out += s_warp[w], eq += s_warp[kWarps + w];
+    if (lane < warp) out = s_warp[lane], eq = s_warp[kMostWarps + lane];
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) {
+        out += __shfl_xor_sync(0xffffffffu, out, o);
+        eq += __shfl_xor_sync(0xffffffffu, eq, o);
     }
     if (cl > 1) {
         if (tid < 2) {
             uint32_t all = 0;
-            for (int w = 0; w < kWarps; ++w) all += s_warp[tid * kWarps + w];
+            for (int w = 0; w < warps; ++w) all += s_warp[tid * kMostWarps + w];
             s_mine[tid] = all;
         }
         cluster_sync();
@@ -207,19 +202,22 @@ __global__ void __launch_bounds__(kThreads) k_select(const __grid_constant__ Sel
 }  // namespace
 
 cudaError_t select_init() {
-    return cudaFuncSetAttribute(k_select, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_of(kHoldAlone));
+    const cudaError_t e = cudaFuncSetAttribute(k_select, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    return e != cudaSuccess ? e : cudaFuncSetAttribute(k_select, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_of(kHoldAlone));
 }
 
 cudaError_t launch_select(const SelectLaunch &a, int sms, cudaStream_t st) {
     const long long lists = (long long)a.b.n * a.c.H, longest = std::min((long long)a.b.max_blocks * a.c.b, (long long)kMaxTokens);
     SelectLaunch l = a;
     l.cluster = 1;
-    // as many CTAs a list as hold its keys, and more of them for few lists
-    while (l.cluster < kMaxCluster && (longest > (long long)kHold * l.cluster || (2 * lists * l.cluster <= 3 * sms && longest >= 2ll * kLeast * l.cluster)))
+    // as many CTAs a list as hold its keys (eight at most), and more of them for few lists
+    while ((l.cluster < 8 && longest > (long long)kHold * l.cluster) ||
+           (l.cluster < kMaxCluster && 2 * lists * l.cluster <= sms && longest >= 2ll * kLeast * l.cluster))
         l.cluster *= 2;
+    const bool alone = lists * l.cluster <= sms;
     const long long each = longest / l.cluster + 64;
-    l.hold = (int)std::min(each, (long long)(lists * l.cluster <= sms ? kHoldAlone : kHold));
-    return launch_clusters(k_select, (unsigned)(lists * l.cluster), kThreads, smem_of(l.hold), (unsigned)l.cluster, st, l);
+    l.hold = (int)std::min(each, (long long)(alone ? kHoldAlone : kHold));
+    return launch_clusters(k_select, (unsigned)(lists * l.cluster), alone ? kMostThreads : 256, smem_of(l.hold), (unsigned)l.cluster, st, l);
 }
 
 }  // namespace lr

@@ -24,6 +24,7 @@ struct ChunkLaunch {
     CacheMaps m;
     CUtensorMap q;
     int32_t q_map, rt;
+    FastDiv div_rt;
 };
 
 // How K reaches shared memory: a 16-bit cache's by the copy engine, or where blocks are odd 16 bytes a thread; 8-bit codes by
@@ -48,7 +49,7 @@ struct Line {
     int s, q0, ql, kv, lo, rows, nq;  // sequence: first new token's position, rows of a KV head, tiles of them
     int ns, wf, nu;                   // units of sinks before the window, the window's first unit, units in all
     int h, u;                         // KV head, unit
-    int rt;                           // rows of a tile
+    FastDiv div_rt;                   // rows of a tile
     int r0, n;                        // the unit's first tile of rows, and how many
     int j, end;                       // tile of rows from r0 on; the CTA's tiles of the unit end there
     bool last;                        // its last unit
@@ -58,7 +59,7 @@ struct Line {
         if (!load_seq(a.a, s, q0, ql, kv) || kv == 0) return false;
         lo = kv - ql;
         rows = ql * a.a.c.G;
-        nq = (rows - 1) / rt + 1;
+        nq = quot(rows - 1, div_rt) + 1;
         if (a.decay == 1.0f) nu = tile_count<kUnit>(lo, kv - 1, a.a.window, a.a.sinks, ns, wf);
         else ns = wf = 0, nu = (kv - 1) / kUnit + 1;
         return true;
@@ -67,11 +68,11 @@ struct Line {
     // The unit's tiles of rows that see one of its tokens (one at least, which may see none).
     __device__ __forceinline__ void span(const WeighLaunch &a) {
         const int b = base(), G = a.a.c.G;
-        r0 = b > lo ? (int)min((long long)(nq - 1), (long long)(b - lo) * G / rt) : 0;
+        r0 = b > lo ? quot((int)min((long long)(rows - 1), (long long)(b - lo) * G), div_rt) : 0;
         int r1 = nq;
         if (a.a.window > 0 && b >= a.a.sinks) {
             const long long e = ((long long)min(b + kUnit - 1, kv - 1) + a.a.window - lo) * G;  // rows before this one
-            r1 = e <= 0 ? 0 : (int)min((long long)nq, (e + rt - 1) / rt);
+            r1 = e <= 0 ? 0 : quot((int)min((long long)rows, e) - 1, div_rt) + 1;
         }
         n = max(1, r1 - r0);
     }
@@ -195,7 +196,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_weigh_chunk(const __grid_consta
 
     chain_wait();
     Line l;
-    l.rt = in.rt;
+    l.div_rt = in.div_rt;
     Share sh;
     if (!take_line(a, l, sh, scratch)) {
         chain_next();
@@ -267,7 +268,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_weigh_chunk(const __grid_consta
             if (a.a.window > 0 && p >= a.a.sinks) end = (int)min((long long)end, max(0ll, ((long long)p + a.a.window - l.lo) * c.G));
             float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
             const float2 f2 = make_float2(f, f);
-            for (int j = l.j; j < l.end; ++j, ++qi) {
+            const int j1 = l.end, unit_r0 = l.r0, unit_rows = l.rows;
+            for (int j = l.j; j < j1; ++j, ++qi) {
                 const uint32_t st = qi % S::kLess;
                 ok = bar_wait(l_full + 8 * st, qi / S::kLess & 1, dead);
                 if (on) ok = ok && bar_wait(s_full + 16 * half + 8 * (n_s & 1), n_s >> 1 & 1, dead);
@@ -276,7 +278,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_weigh_chunk(const __grid_consta
                     after_sync();
                     const float *const less = s_less + st * kRowTile;
                     const uint32_t from = ts + (n_s & 1) * 128;
-                    const int row0 = (l.r0 + j) * in.rt, some = min(in.rt, l.rows - row0);
+                    const int row0 = (unit_r0 + j) * in.rt, some = min(in.rt, unit_rows - row0);
                     // 32 scores of the token
                     auto add = [&](const float *s, int k0) {
 #pragma unroll
@@ -364,10 +366,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_weigh_chunk(const __grid_consta
         const bool one = elect();
         uint32_t n_s[2] = {0, 0};
         for (;; l.next(a, sh)) {
-            const int halves = l.halves();
-            for (int j = l.j; j < l.end && ok; ++j, ++qi) {
+            const int halves = l.halves(), j0 = l.j, j1 = l.end, unit_r0 = l.r0, unit_rows = l.rows;
+            for (int j = j0; j < j1 && ok; ++j, ++qi) {
                 const uint32_t sq = qi % S::kRows;
-                const int many = min(kRowTile, (min(in.rt, l.rows - (l.r0 + j) * in.rt) + 15) / 16 * 16);
+                // (a full tile has all 128 columns, of which those of no row are zero)
+                const int some = unit_rows - (unit_r0 + j) * in.rt, many = some >= in.rt ? kRowTile : (some + 15) / 16 * 16;
                 const uint32_t shape = shape_of<BF16, 0, false>() | (uint32_t)(many / 8) << 17;
                 ok = bar_wait(q_full + 8 * sq, qi / S::kRows & 1, dead);
                 const uint64_t dq = operand(smem_addr(rows + sq * S::kTile), 16);
@@ -375,7 +378,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_weigh_chunk(const __grid_consta
                 for (int g = 0; g < 2; ++g) {
                     if (g >= halves || !ok) continue;
                     const uint32_t st = (key + g) % S::kKeys, buf = 16 * g + 8 * (n_s[g] & 1);
-                    if (j == l.j) ok = bar_wait(k_full + 8 * st, (key + g) / S::kKeys & 1, dead);
+                    if (j == j0) ok = bar_wait(k_full + 8 * st, (key + g) / S::kKeys & 1, dead);
                     if (ok && n_s[g] >= 2) ok = bar_wait(s_free + buf, ((n_s[g] >> 1) - 1) & 1, dead);
                     if (!ok) continue;
                     after_sync();
@@ -387,7 +390,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_weigh_chunk(const __grid_consta
                             mma_ss(tm + g * 256 + (n_s[g] & 1) * 128, dk + at, dq + at, shape, k > 0);
                         }
                         commit(s_full + buf);
-                        if (j + 1 == l.end) commit(k_free + 8 * st);
+                        if (j + 1 == j1) commit(k_free + 8 * st);
                     }
                     __syncwarp();
                     ++n_s[g];
@@ -682,6 +685,7 @@ cudaError_t launch_weigh_chunk(const WeighLaunch &a, const CacheMaps &m, bool bf
     l.w = a;
     l.m = m;
     l.rt = a.a.c.G <= kRowTile ? kRowTile / a.a.c.G * a.a.c.G : kRowTile;
+    l.div_rt = fast_div((uint32_t)l.rt);
     l.q_map = encode_rows(a.a, bf16, l.q);
     return launch_chained(p.k, sms, kThreads, p.smem, st, l);
 }
