@@ -32,10 +32,7 @@ namespace lr {
 
 namespace {
 
-constexpr int kWeight = 4;    // tiles that a unit's beginning and end take the time of
-constexpr int kThreads = 512;
-// registers a thread of the softmax warps and of the others: together the 512 x 128 of the launch
-constexpr int kSoftRegs = 192, kOtherRegs = 64;
+constexpr int kWeight = 4;  // tiles that a unit's beginning and end take the time of
 
 // How K and V reach shared memory.
 enum : int {
@@ -54,19 +51,24 @@ struct Job {
     int slot, slot0;    // where this CTA's and the first one's parts go
 };
 constexpr int kJobs = 4;
+constexpr int kTogether = 6;  // parts that are joined in one step, at most
 
-template <int DP, int FMT, int LOAD>
+template <int DP, int FMT, int LOAD, bool TREE>
 struct Shape {
     // Warps 0-7 softmax, 8 products.  By the copy engine: 9 K, 10 V, 12-15 queries; else 12-15 K and V, 10
-    // and 11 queries.
+    // and 11 queries.  (12-19 for trees over 8 bits: of few rows, conversion bounds them -- 9,000 cycles a tile of 4 warps, of which
+    // the copies' latency is none and a half the other chain --, and the softmax does with fewer registers.)
+    static constexpr int kLoaders = LOAD == kConvert && TREE ? 8 : 4, kThreads = 384 + 32 * kLoaders, kLoad = 32 * kLoaders;
+    // registers a thread of the softmax warps and of the others: together those of the launch, 512 x 128 or 640 x 96
+    static constexpr int kSoftRegs = kLoaders == 8 ? 144 : 192, kOtherRegs = 64;
     static constexpr int kQueryWarp = LOAD == kTma ? 12 : 10, kQueryWarps = LOAD == kTma ? 4 : 2;
     static constexpr int kPanel = kTok * 128;                   // 128 rows of 64 16-bit elements
     static constexpr int kTile = kTok * DP * 2;                 // a tile of K or V, or half of Q, in 16 bits
     static constexpr int kStages = FMT == kFmt16 ? 5 : 4;
     // 8-bit codes on their way: 16 bytes a loading thread and slot, as many as the room takes of the
     // 2 * DP / 16 that a tile of K and one of V make
-    static constexpr int kSlots = DP == 128 ? 14 : 8;
-    static constexpr int kRaw = FMT == kFmt16 ? 0 : kSlots * 128 * 16;
+    static constexpr int kSlots = (DP == 128 ? 14 : 8) * 4 / kLoaders;
+    static constexpr int kRaw = FMT == kFmt16 ? 0 : kSlots * kLoad * 16;
     static constexpr int kQ = 2 * kTile;
     static constexpr int kBytes = kQ + kStages * kTile + kRaw;
     static constexpr int kBars = 2 + 2 * kStages + 10 + 4 + 1 + 2 * kJobs + 2;
@@ -242,12 +244,13 @@ __device__ __noinline__ bool sees_lost(const AttendLaunch &a, const Unit &u, int
 
 // Joins the parts of 32 rows of a unit, in the order of the CTAs: a lane first a row's maximum and sum, then four
 // elements each of 16 rows at a time (of 2 x 8 with 64 elements), their loads in flight together.
-template <bool BF16, int DP>
-__device__ __noinline__ void join_rows(const AttendLaunch &a, const Unit &u, int c0, int parts, int slot0, int row0) {
+// The parts are those of CTA c0 + k * step.  LAST: to the outputs; else to the first part's own place, as a part of others.
+template <bool BF16, int DP, bool LAST>
+__device__ __noinline__ void join_rows(const AttendLaunch &a, const Unit &u, int c0, int parts, int slot0, int row0, int step) {
     constexpr int kLanes = DP / 4, kTwo = 32 / kLanes, kStep = 16;
     const CacheDev &c = a.c;
     const int lane = threadIdx.x % 32, sub = lane / kLanes, e = lane % kLanes * 4;
-    auto at = [&](int k, int r) { return (int64_t)(k == 0 ? slot0 : 2 * (c0 + k)) * 256 + r; };
+    auto at = [&](int k, int r) { return (int64_t)(k == 0 ? slot0 : 2 * (c0 + k * step)) * 256 + r; };
     const bool mine = row0 + lane < u.rows;
     float mm = -INFINITY, ll = 0.0f;
 #pragma unroll 4
@@ -284,10 +287,16 @@ __device__ __noinline__ void join_rows(const AttendLaunch &a, const Unit &u, int
             const float l = __shfl_sync(0xffffffffu, ll, r - row0);
             const int gr = u.qt * 256 + r, t = quot(gr, c.div_g), hd = u.h * c.G + gr - t * c.G;
             const float iv = l == 0.0f ? 0.0f : 1.0f / l;
-            if (r < u.rows && e < c.D)
+            if (!LAST && r < u.rows)
+                *reinterpret_cast<float4 *>(a.part_o + at(0, r) * 128 + e) = acc[z];
+            if (LAST && r < u.rows && e < c.D)
                 *reinterpret_cast<uint2 *>(a.out + (int64_t)(u.q0 + t) * a.o_t + (int64_t)hd * a.o_h + e * 2) =
                     make_uint2(pack16<BF16>(acc[z].x * iv, acc[z].y * iv), pack16<BF16>(acc[z].z * iv, acc[z].w * iv));
         }
+    }
+    if constexpr (!LAST) {
+        if (mine) a.part_ml[at(0, row0 + lane)] = make_float2(mm, ll);
+        return;
     }
     if (a.lse && mine) {
         const int gr = u.qt * 256 + row0 + lane, t = quot(gr, c.div_g), hd = u.h * c.G + gr - t * c.G;
@@ -296,10 +305,11 @@ __device__ __noinline__ void join_rows(const AttendLaunch &a, const Unit &u, int
 }
 
 template <bool BF16, int FMT, int DP, int LOAD, bool TREE>
-__global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_constant__ ChunkLaunch in) {
-    using S = Shape<DP, FMT, LOAD>;
+__global__ void __launch_bounds__(Shape<DP, FMT, LOAD, TREE>::kThreads, 1) k_attend_chunk(const __grid_constant__ ChunkLaunch in) {
+    using S = Shape<DP, FMT, LOAD, TREE>;
     const AttendLaunch &a = in.a;
-    constexpr int kKvArrive = LOAD == kTma ? 1 : 4;  // arrivals that hand over a tile: one a warp
+    constexpr int kThreads = S::kThreads, kLoad = S::kLoad;
+    constexpr int kKvArrive = LOAD == kTma ? 1 : S::kLoaders;  // arrivals that hand over a tile: one a warp
     constexpr int kStages = S::kStages;
     constexpr float kLag = BF16 || FMT == kFmt16 ? 8.0f : 4.0f;
     constexpr bool kSplit = FMT != kFmt16 && !BF16;  // V's scales are split (below)
@@ -372,7 +382,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
 
     if (warp < 8) {
         // ================= softmax: a thread a row =================
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::kSoftRegs));
         const int half = warp / 4, r = tid;  // row of the unit
         const uint32_t lanes = (uint32_t)(warp % 4) << 21;
         const uint32_t ts = tm + half * 128 + lanes, to = tm + 256 + half * 128 + lanes;
@@ -607,17 +617,31 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
                 // The warps that have the same rows of the unit, one a CTA: the last of them joins the parts, in the
                 // order of the CTAs whichever came last.
                 const int c0 = job.c0, c1 = job.c1;
-                uint32_t before = 0;
-                __threadfence();
-                __syncwarp();
-                if (lane == 0) {
-                    before = atomicAdd(a.done + c0 * 8 + warp, 1u);
-                    if (before == (uint32_t)(c1 - c0)) a.done[c0 * 8 + warp] = 0;
-                }
-                before = __shfl_sync(0xffffffffu, before, 0);
-                if (before == (uint32_t)(c1 - c0)) {
+                const int parts = c1 - c0 + 1;
+                // whether this warp is the last of `all` to come to counter n, which then starts again
+                auto last_of = [&](int n, int all) {
+                    uint32_t before = 0;
                     __threadfence();
-                    join_rows<BF16, DP>(a, u, c0, c1 - c0 + 1, job.slot0, warp * 32);
+                    __syncwarp();
+                    if (lane == 0) {
+                        before = atomicAdd(a.done + n * 8 + warp, 1u);
+                        if (before == (uint32_t)(all - 1)) a.done[n * 8 + warp] = 0;
+                    }
+                    before = __shfl_sync(0xffffffffu, before, 0);
+                    __threadfence();
+                    return before == (uint32_t)(all - 1);
+                };
+                if (TREE && parts > kTogether) {
+                    // Many parts in two steps, so that as many SMs take part as there are groups (19 parts of a context of 200,001
+                    // tokens, joined by one warp a row's 32: 75 us of 218).  Groups have counters of their own, at their first CTA.
+                    const int group = parts > 36 ? 12 : parts > 16 ? 6 : 4, g = ((int)blockIdx.x - c0) / group, first = g * group;
+                    const int n = min(group, parts - first), groups = (parts + group - 1) / group;
+                    if (last_of(g == 0 ? c0 : (int)gridDim.x + c0 + first, n)) {
+                        join_rows<BF16, DP, false>(a, u, c0 + first, n, g == 0 ? job.slot0 : 2 * (c0 + first), warp * 32, 1);
+                        if (last_of(2 * (int)gridDim.x + c0, groups)) join_rows<BF16, DP, true>(a, u, c0, groups, job.slot0, warp * 32, group);
+                    }
+                } else if (last_of(c0, parts)) {
+                    join_rows<BF16, DP, true>(a, u, c0, parts, job.slot0, warp * 32, 1);
                 }
             }
             bar_arrive_warp(job_free + 8 * (frag % kJobs));
@@ -625,7 +649,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
         }
     } else if (LOAD != kTma && warp >= 12) {
         // ================= K and V to shared memory, by threads =================
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::kOtherRegs));
         const int i = tid - 384;
         uint32_t item = 0;
         bool ok = true;
@@ -657,7 +681,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
         auto look = [&](const Cursor<256, kTok, kWeight> &p) {
             Found f{-1, 1.0f, 0.0f, false};
             const int t = p.base() + i;
-            if (t > p.u.hi || (a.window > 0 && t <= p.u.lo - a.window && t >= a.sinks)) return f;
+            if (i >= kTok || t > p.u.hi || (a.window > 0 && t <= p.u.lo - a.window && t >= a.sinks)) return f;
             int place;
             const int64_t blk = block_of(c, a.b, p.u.s, t, place);
             if (blk < 0) {
@@ -674,10 +698,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
             return f;
         };
         // the copies of tile x of K (y = 0) or V of the places in slot x & 1
-        constexpr int CH = FMT == kFmt16 ? DP / 8 : DP / 16, kStep = 128 / CH, kIts = kTok / kStep;
-        const int ch = i % CH, r0 = i / CH;
+        constexpr int CH = FMT == kFmt16 ? DP / 8 : DP / 16, kStep = kLoad / CH, kIts = kTok / kStep;
+        // (8 bits: eight neighbouring threads write two rows' 64 elements, which lie in different banks; eight pieces of one row would not)
+        constexpr bool kTwoRows = FMT != kFmt16 && CH == 8;
+        const int ch = kTwoRows ? (i & 3) | (i >> 1 & 4) : i % CH, r0 = kTwoRows ? (i >> 2 & 1) | i >> 4 << 1 : i / CH;
         const bool in = ch * (FMT == kFmt16 ? 8 : 16) < c.D;
         auto put = [&](int x, const Found &f) {
+            if (i >= kTok) return;
             if constexpr (kSplit) places[(x & 1) * kTok + i] = (int64_t)((uint64_t)power_of<FMT>(f.vs) << 48 | ((uint64_t)f.off << 16 >> 16));
             else places[(x & 1) * kTok + i] = f.off;
             // blocks out of range and scales that are not finite are kept from rows that do not see them
@@ -715,15 +742,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
                 int64_t off = places[(it >> 1 & 1) * kTok + r0 + k * kStep];
                 if constexpr (kSplit) off = (int64_t)((uint64_t)off << 16) >> 16;
                 const bool have = in && off >= 0;
-                copy16(smem_addr(raw + (ahead % S::kSlots * 128 + i) * 16), (it & 1 ? c.v : c.k) + (have ? off + ch * 16 : 0), have);
+                copy16(smem_addr(raw + (ahead % S::kSlots * kLoad + i) * 16), (it & 1 ? c.v : c.k) + (have ? off + ch * 16 : 0), have);
             }
             copy_commit();
             ++ahead;
         };
         if (i < 4) s_bad[i] = 0;
-        named_sync(1, 128);
+        named_sync(1, kLoad);
         put(0, look(cu));
-        named_sync(1, 128);
+        named_sync(1, kLoad);
         if constexpr (FMT != kFmt16) {
             static_assert(FMT == kFmt16 || S::kSlots <= 2 * kIts, "the first requests are the first tile's");
             for (int k = 0; k < S::kSlots; ++k) request(true);
@@ -757,24 +784,25 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
             }
             // the next tile's places (8-bit: before this tile's codes are taken, in whose room its own are requested)
             if (i == 0) s_bad[(x + 1) & 3] = 0;
-            named_sync(1, 128);
+            named_sync(1, kLoad);
             if (more) put(x + 1, f);
-            named_sync(1, 128);
+            named_sync(1, kLoad);
             if constexpr (FMT != kFmt16) {
                 for (int y = 0; y < 2; ++y, ++item) {
                     const uint32_t st = stage();
                     const uint32_t to = smem_addr(tiles + st * S::kTile);
-                    // four pieces at a time: read, converted and written, then their slots requested again
-                    for (int k0 = 0; k0 < kIts; k0 += 4) {
-                        uint32_t w[4][4];
-                        copy_wait<S::kSlots - 4>();
+                    // four pieces (or what there are) at a time: read, converted and written, then their slots requested again
+                    constexpr int kFour = kIts < 4 ? kIts : 4;
+                    for (int k0 = 0; k0 < kIts; k0 += kFour) {
+                        uint32_t w[kFour][4];
+                        copy_wait<S::kSlots - kFour>();
 #pragma unroll
-                        for (int k = 0; k < 4; ++k)
+                        for (int k = 0; k < kFour; ++k)
                             asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
                                          : "=r"(w[k][0]), "=r"(w[k][1]), "=r"(w[k][2]), "=r"(w[k][3])
-                                         : "r"(smem_addr(raw + ((item * kIts + k0 + k) % S::kSlots * 128 + i) * 16)) : "memory");
+                                         : "r"(smem_addr(raw + ((item * kIts + k0 + k) % S::kSlots * kLoad + i) * 16)) : "memory");
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
+                        for (int k = 0; k < kFour; ++k) {
                             const int r = r0 + (k0 + k) * kStep;
                             uint32_t v[8];
                             if constexpr (BF16) {
@@ -797,7 +825,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
                         }
                         // the copies that take these slots next are of this tile's V or of the next tile
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) request(ahead / (2 * kIts) <= (uint32_t)x + (more ? 1 : 0));
+                        for (int k = 0; k < kFour; ++k) request(ahead / (2 * kIts) <= (uint32_t)x + (more ? 1 : 0));
                     }
                     shared_to_async();
                     bar_arrive_warp(kv_full + 8 * st);
@@ -807,7 +835,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const __grid_const
         if constexpr (FMT == kFmt16) drain();
         copy_wait<0>();
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::kOtherRegs));
         if (LOAD == kTma && (warp == 9 || warp == 10)) {
             // ================= K and V to shared memory, by the copy engine =================
             // lane i: box i of the tile; warp 9 takes K, warp 10 V
@@ -1046,12 +1074,13 @@ using Kernel = void (*)(const ChunkLaunch);
 struct Pick {
     Kernel k;
     size_t smem;
+    int threads;
 };
 
 template <int FMT, int DP, int LOAD, bool TREE>
 Pick pick_type(bool bf16) {
-    using S = Shape<DP, FMT, LOAD>;
-    return {bf16 ? k_attend_chunk<true, FMT, DP, LOAD, TREE> : k_attend_chunk<false, FMT, DP, LOAD, TREE>, S::kSmem};
+    using S = Shape<DP, FMT, LOAD, TREE>;
+    return {bf16 ? k_attend_chunk<true, FMT, DP, LOAD, TREE> : k_attend_chunk<false, FMT, DP, LOAD, TREE>, S::kSmem, S::kThreads};
 }
 template <int DP, bool TREE>
 Pick pick_load(bool bf16, int fmt, bool tma) {
@@ -1080,7 +1109,7 @@ cudaError_t launch_chunk(const AttendLaunch &a, const CacheMaps &m, bool bf16, i
     l.a = a;
     l.m = m;
     l.q_map = 128 % a.c.G == 0 && encode_rows(a, bf16, l.q);
-    return launch_chained(p.k, ctas, kThreads, p.smem, st, l);
+    return launch_chained(p.k, ctas, p.threads, p.smem, st, l);
 }
 
 }  // namespace

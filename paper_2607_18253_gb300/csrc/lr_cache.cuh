@@ -88,13 +88,14 @@ struct AttendLaunch {
     int32_t row_lo, row_hi;      // sequences with this many rows (tokens x query heads a KV head) are this launch's
     float *part_o;               // [slots][rows][DP] sums of weighted V
     float2 *part_ml;             // [slots][rows] running maximum (log2) and sum
-    uint32_t *done;              // parts finished of the unit that began in a CTA ([CTAs]; chunk kernel [CTAs][8 warps]); zero
+    uint32_t *done;              // parts finished of the unit that began in a CTA ([CTAs]; chunk kernel [3][CTAs][8 warps]); zero
                                  // between calls
 };
 constexpr int kStepRows = 16;   // rows of a unit of the step kernel, at most
 cudaError_t launch_attend_step(const AttendLaunch &a, bool bf16, int fmt, int rows, int sms, cudaStream_t st);
 cudaError_t attend_step_init();
 int attend_step_ctas(int sms);  // CTAs of a launch, at most
+constexpr int kChunkCounts = 24;  // counters of finished parts a CTA
 constexpr int kChunkRows = 256;  // rows of a unit of the chunk kernel; one CTA an SM
 // Tensor maps of a 16-bit cache's K and V: boxes of 64 elements of `box` tokens, the largest number that
 // divides a block and the chunk kernel's tiles; box 0: none (blocks that are no multiple of 8 tokens).

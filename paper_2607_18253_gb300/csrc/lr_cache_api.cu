@@ -153,7 +153,7 @@ int lr_cache_create(const lr_cache_config *cfg, lr_cache **out) {
     if (e == cudaSuccess) e = cudaMemcpy(d.status, words, sizeof(words), cudaMemcpyHostToDevice);
     d.nan = reinterpret_cast<const float *>(d.status + 1);
     if (e == cudaSuccess) e = alloc_parts(c->step, lr::attend_step_ctas(c->sms), lr::kStepRows, lr::attend_step_ctas(c->sms));
-    if (e == cudaSuccess) e = alloc_parts(c->chunk, c->sms, lr::kChunkRows, 8 * (size_t)c->sms);
+    if (e == cudaSuccess) e = alloc_parts(c->chunk, c->sms, lr::kChunkRows, lr::kChunkCounts * (size_t)c->sms);
     if (e == cudaSuccess) e = alloc_parts(c->weigh, c->sms, 2, 8 * (size_t)c->sms);  // (parts of 256 sums)
     if (e != cudaSuccess) return bail(LR_ENOMEM, cudaGetErrorString(e));
     // (what was set above, on the default stream, has to be there for streams that do not wait for it)
@@ -244,7 +244,7 @@ int lr_cache_status(lr_cache *c, void *stream) {
     if (e == cudaSuccess) e = cudaStreamSynchronize(st);
     // a kernel may have given up, whatever error came first: its counts of finished parts start again
     if (e == cudaSuccess && h != LR_OK) {
-        e = cudaMemsetAsync(c->chunk.done, 0, 8 * (size_t)c->sms * sizeof(uint32_t), st);
+        e = cudaMemsetAsync(c->chunk.done, 0, lr::kChunkCounts * (size_t)c->sms * sizeof(uint32_t), st);
         if (e == cudaSuccess) e = cudaMemsetAsync(c->weigh.done, 0, 8 * (size_t)c->sms * sizeof(uint32_t), st);
         if (e == cudaSuccess) e = cudaStreamSynchronize(st);
     }
