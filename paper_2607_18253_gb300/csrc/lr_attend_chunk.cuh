@@ -262,10 +262,12 @@ __device__ __noinline__ void join_rows(const AttendLaunch &a, const Unit &u, int
         ll = 0.0f;
         for (int k = 0; k < parts; ++k) {
             float4 w[kStep / kTwo];
+            const float4 *const from = reinterpret_cast<const float4 *>(a.part_o + at(k, r0 + sub) * 128 + e);
 #pragma unroll
-            for (int z = 0; z < kStep / kTwo; ++z) {
-                const int r = r0 + z * kTwo + sub;
-                w[z] = r < u.rows ? __ldcg(reinterpret_cast<const float4 *>(a.part_o + at(k, r) * 128 + e)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            for (int z = 0; z < kStep / kTwo; ++z) {  // (asked for together, whether they count or not)
+                w[z] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (r0 + z * kTwo + sub < u.rows)
+                    asm volatile("ld.global.cg.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(w[z].x), "=f"(w[z].y), "=f"(w[z].z), "=f"(w[z].w) : "l"(from + z * kTwo * 32));
             }
             const float2 ml = mine ? __ldcg(a.part_ml + at(k, row0 + lane)) : make_float2(-INFINITY, 0.0f);
             const float f = ml.x == -INFINITY ? 0.0f : exp2_fast(ml.x - mm);  // (one that saw nothing: no part of it)
@@ -273,12 +275,11 @@ __device__ __noinline__ void join_rows(const AttendLaunch &a, const Unit &u, int
 #pragma unroll
             for (int z = 0; z < kStep / kTwo; ++z) {
                 const float g = __shfl_sync(0xffffffffu, f, r0 - row0 + z * kTwo + sub);
-                if (g != 0.0f) {
-                    acc[z].x += w[z].x * g;
-                    acc[z].y += w[z].y * g;
-                    acc[z].z += w[z].z * g;
-                    acc[z].w += w[z].w * g;
-                }
+                const bool on = g != 0.0f;
+                acc[z].x += on ? w[z].x * g : 0.0f;
+                acc[z].y += on ? w[z].y * g : 0.0f;
+                acc[z].z += on ? w[z].z * g : 0.0f;
+                acc[z].w += on ? w[z].w * g : 0.0f;
             }
         }
 #pragma unroll
