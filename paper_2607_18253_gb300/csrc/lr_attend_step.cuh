@@ -95,7 +95,7 @@ __device__ __forceinline__ void add_part(float2 ml, const float4 &w, float mm, f
     acc.w += w.w * f;
 }
 
-// Elements d .. d + 3 of a finished row of a unit whose only tile of rows it is.
+// Elements d .. d + 3 of a finished row of a sequence and KV head.
 template <bool BF16>
 __device__ __forceinline__ void write_row(const AttendLaunch &a, int r, int d, int q0, int h, float mm, float ll, float4 w) {
     const CacheDev &c = a.c;
@@ -111,7 +111,7 @@ __device__ __forceinline__ void write_row(const AttendLaunch &a, int r, int d, i
 // parts' maxima and sums, then four elements each of 16 parts at a time (of 2 x 16 with 64 elements).  The
 // first part is in slot0, the others each the first of their CTAs.  (Not inlined: its registers are not the loop's.)
 template <bool BF16, int DP>
-__device__ __noinline__ void join_parts(const AttendLaunch &a, int c0, int parts, int slot0, int rows, int q0, int h) {
+__device__ __noinline__ void join_parts(const AttendLaunch &a, int c0, int parts, int slot0, int rows, int row0, int q0, int h) {
     constexpr int kLanes = DP / 4, kTwo = 32 / kLanes;
     const int lane = threadIdx.x % 32, part0 = lane / kLanes, e = lane % kLanes * 4;
     for (int r = threadIdx.x / 32; r < rows; r += kThreads / 32) {
@@ -143,7 +143,7 @@ __device__ __noinline__ void join_parts(const AttendLaunch &a, int c0, int parts
             acc.z += __shfl_xor_sync(0xffffffffu, acc.z, 16);
             acc.w += __shfl_xor_sync(0xffffffffu, acc.w, 16);
         }
-        if (part0 == 0) write_row<BF16>(a, r, e, q0, h, mm, ll, acc);
+        if (part0 == 0) write_row<BF16>(a, row0 + r, e, q0, h, mm, ll, acc);
     }
 }
 
@@ -268,7 +268,7 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
     float o[KS][NR][4], m[NR][2], l[NR][2], qf[NR][2], less[NR][2];  // less: m, 0 where it is -inf
     [[maybe_unused]] float down[NR][2];  // 8 bits: the power of two that the row's weights are multiplied by
     int pos[NR][2];
-    [[maybe_unused]] uint32_t drafted[NR][2];  // of a tree: the drafted tokens that the row sees (at most 16 rows are at most 16 tokens)
+    [[maybe_unused]] uint32_t drafted[NR][2];  // of a tree: the drafted tokens that the row sees (at most 32 rows are at most 32 tokens)
     auto sees = [&](int n, int y, int j, const Unit &u) {
         if constexpr (TREE) {
             const int i = j - (u.kv - u.ql);
@@ -279,11 +279,12 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
     for (int x = 0;;) {
         const Unit &u = cu.u;
         const bool whole = cu.whole(), last_unit = cu.last;
+        const int row0 = TREE ? u.qt * kRows : 0;  // (causal units are a sequence's only tile of rows)
         {  // its queries, straight to the registers that multiply them
 #pragma unroll
             for (int n = 0; n < NR; ++n) {
                 const int r = n * 8 + g;  // (the row whose elements the lane holds)
-                const int t = quot(r, c.div_g), hd = r - t * c.G;
+                const int t = quot(row0 + r, c.div_g), hd = row0 + r - t * c.G;
                 const bool ok = r < u.rows;
                 const char *const p = a.q + (int64_t)(u.q0 + t) * a.q_t + (int64_t)(u.h * c.G + hd) * a.q_h;
 #pragma unroll
@@ -327,7 +328,7 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
                 for (int y = 0; y < 2; ++y) {
                     const int row = n * 8 + 2 * i4 + y;
                     if constexpr (TREE) {
-                        const TreeRow tr = tree_row(a, u.q0, quot(row, c.div_g), u.ql, u.kv, row < u.rows);
+                        const TreeRow tr = tree_row(a, u.q0, quot(row0 + row, c.div_g), u.ql, u.kv, row < u.rows);
                         pos[n][y] = tr.at;
                         drafted[n][y] = tree_word(tr, 0);
                     } else {
@@ -647,7 +648,7 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
             for (int w = 0; w < 4; ++w)
                 add_part(s_ml[w * kRows + r], *reinterpret_cast<const float4 *>(smem + w * S::kWarp + used + (r * DP + d) * 4), mm, ll, acc);
             if (whole) {
-                write_row<BF16>(a, r, d, u.q0, u.h, mm, ll, acc);
+                write_row<BF16>(a, row0 + r, d, u.q0, u.h, mm, ll, acc);
             } else {
                 if (d == 0) a.part_ml[slot * kStepRows + r] = make_float2(mm, ll);
                 *reinterpret_cast<float4 *>(a.part_o + (slot * kStepRows + r) * 128 + d) = acc;
@@ -665,7 +666,7 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
             __syncthreads();
             if (s_last) {
                 __threadfence();
-                join_parts<BF16, DP>(a, c0, c1 - c0 + 1, slot_of(sh, c0, cu.at), u.rows, u.q0, u.h);
+                join_parts<BF16, DP>(a, c0, c1 - c0 + 1, slot_of(sh, c0, cu.at), u.rows, row0, u.q0, u.h);
             }
         }
         __syncthreads();  // the stages are free again
