@@ -95,6 +95,7 @@ class PagedCache:
         cfg = _CacheConfig(_i32(int(num_q_heads)), H, D, _DTYPES[dtype], fmt, bs, nb, _i32(int(max_seqs)), k.data_ptr(), v.data_ptr(),
                            k_scale.data_ptr() if fmt else None, v_scale.data_ptr() if fmt else None, *st, *ss)
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self._places = torch.Size((nb, bs, H))
         self._scale = 1.0 / math.sqrt(self.head_dim)
         torch.cuda.init()
         h = _P()
@@ -187,11 +188,12 @@ class PagedCache:
         """(pointer, block, token, head stride) of weights [num_blocks, block_size, num_kv_heads] float32, of any strides."""
         if t is None:
             return None, 0, 0, 0
-        if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != torch.float32:
+        if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype is not torch.float32:
             raise TypeError("weights must be a float32 CUDA tensor")
-        if t.shape != self.k.shape[:3]:
-            raise ValueError(f"weights must be {list(self.k.shape[:3])}, got {list(t.shape)}")
-        return (t.data_ptr(), *t.stride())
+        if t.shape != self._places:
+            raise ValueError(f"weights must be {list(self._places)}, got {list(t.shape)}")
+        sb, st, sh = t.stride()
+        return t.data_ptr(), sb, st, sh
 
     def weigh(self, q: torch.Tensor, lse: torch.Tensor, batch: CacheBatch, weights: torch.Tensor, decay: float = 1.0,
               scale: Optional[float] = None, window: int = 0, sinks: int = 0, stream=None) -> torch.Tensor:
@@ -217,12 +219,13 @@ class PagedCache:
         if out is None:
             kept = torch.empty((n, H, max(cap, 0)), dtype=torch.int32, device=self.k.device)
             count = torch.empty(n, dtype=torch.int32, device=self.k.device)
+            kp, cp = kept.data_ptr(), count.data_ptr()
         else:
             kept, count = out
-        rc = self._lib.lr_cache_select(self._h, batch._ref, *self._weights(weights), _i32(cap),
-                                       _dev(budget, torch.int32, "budget", n), _i32(sinks), _i32(recent),
-                                       _dev(kept, torch.int32, "kept", n * H * max(cap, 0)), _dev(count, torch.int32, "count", n),
-                                       _stream(stream))
+            kp, cp = _dev(kept, torch.int32, "kept", n * H * max(cap, 0)), _dev(count, torch.int32, "count", n)
+        wp, wb, wt, wh = self._weights(weights)
+        rc = self._lib.lr_cache_select(self._h, batch._ref, wp, wb, wt, wh, _i32(cap), _dev(budget, torch.int32, "budget", n),
+                                       _i32(sinks), _i32(recent), kp, cp, _stream(stream))
         if rc:
             self._check(rc, "lr_cache_select")
         return kept, count
@@ -233,11 +236,14 @@ class PagedCache:
 
         kept: int32 [num_seqs, num_kv_heads, cap], or [num_seqs, cap]: one list for all heads.  start: 0 if not given."""
         n, H = batch._c.num_seqs, self.num_kv_heads
-        if kept.dim() not in (2, 3) or kept.shape[0] != n or (kept.dim() == 3 and kept.shape[1] != H):
-            raise ValueError(f"kept must be [{n}, {H}, cap] or [{n}, cap], got {list(kept.shape)}")
-        rc = self._lib.lr_cache_keep(self._h, batch._ref, kept.shape[-1], _dev(kept, torch.int32, "kept"), 1 if kept.dim() == 2 else H,
+        shape = kept.shape
+        heads = H if len(shape) == 3 else 1
+        if len(shape) not in (2, 3) or shape[0] != n or (len(shape) == 3 and shape[1] != H):
+            raise ValueError(f"kept must be [{n}, {H}, cap] or [{n}, cap], got {list(shape)}")
+        wp, wb, wt, wh = self._weights(weights)
+        rc = self._lib.lr_cache_keep(self._h, batch._ref, shape[-1], _dev(kept, torch.int32, "kept"), heads,
                                      _dev(count, torch.int32, "count", n), _dev(start, torch.int32, "start", n),
-                                     *self._weights(weights), _stream(stream))
+                                     wp, wb, wt, wh, _stream(stream))
         if rc:
             self._check(rc, "lr_cache_keep")
 

@@ -255,19 +255,26 @@ __device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 
 __device__ __forceinline__ uint32_t tree_mask(const TreeRow &r, int w) {
     return w < 0 || w * 32 >= r.ql ? 0u : __ldg(r.mask + w) & low_bits(r.ql - w * 32);
 }
-__device__ __forceinline__ TreeRow tree_row(const AttendLaunch &a, int q0, int t, int ql, int kv, bool real) {
-    TreeRow r{a.tree + (int64_t)(q0 + t) * a.tree_t, kv - ql, ql, -1, 0, 0};
-    if (!real) r.ql = 0;
-    int n = 0;
-    if (a.window > 0)
-        for (int w = 0; w * 32 < r.ql; ++w) n += __popc(tree_mask(r, w));
-    else n = ql;  // (without a window the position is only that of a row behind its context)
-    if (real) r.at = r.first + n - 1;
+// The row of token t, whose position is known.
+__device__ __forceinline__ TreeRow tree_row_at(const AttendLaunch &a, int q0, int t, int ql, int kv, int at) {
+    TreeRow r{a.tree + (int64_t)(q0 + t) * a.tree_t, kv - ql, at < 0 ? 0 : ql, at, 0, 0};
+    const int n = at - r.first + 1;
     if (a.window > 0 && n > a.window) {
         r.drop = n - a.window;
         r.keep = max(0, a.sinks - r.first);
     }
     return r;
+}
+__device__ __forceinline__ TreeRow tree_row(const AttendLaunch &a, int q0, int t, int ql, int kv, bool real) {
+    TreeRow r{a.tree + (int64_t)(q0 + t) * a.tree_t, kv - ql, ql, -1, 0, 0};
+    int n = 0;
+    if (a.window > 0) {
+#pragma unroll 4
+        for (int w = 0; w * 32 < ql; ++w) n += real ? __popc(tree_mask(r, w)) : 0;
+    } else {
+        n = ql;  // (without a window the position is only that of a row behind its context)
+    }
+    return tree_row_at(a, q0, t, ql, kv, real ? r.first + n - 1 : -1);
 }
 // Word w of the tokens that the row sees.
 __device__ __forceinline__ uint32_t tree_word(const TreeRow &r, int w) {

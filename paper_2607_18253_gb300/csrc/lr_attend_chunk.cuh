@@ -203,9 +203,9 @@ __device__ __noinline__ void mask_scores(uint32_t ts, int last, int low, int sin
     tm_store_wait();
 }
 // The same for the rows of a tree, whose context and drafted tokens are hidden by different rules.
-__device__ __noinline__ void mask_tree(uint32_t ts, const AttendLaunch &a, int q0, int t, int ql, int kv, bool real, int base,
+__device__ __noinline__ void mask_tree(uint32_t ts, const AttendLaunch &a, int q0, int t, int ql, int kv, int at, int base,
                                        const uint32_t *kbad) {
-    const TreeRow row = tree_row(a, q0, t, ql, kv, real);
+    const TreeRow row = tree_row_at(a, q0, t, ql, kv, at);
 #pragma unroll 1
     for (int k0 = 0; k0 < kTok; k0 += 32) {
         const uint32_t see = tree_sees(row, base + k0, a.window, a.sinks), nan = kbad ? kbad[k0 / 32] : 0u;
@@ -405,7 +405,7 @@ __global__ void __launch_bounds__(Shape<DP, FMT, LOAD, TREE>::kThreads, 1) k_att
             }
             const int gr = u.qt * 256 + r, t = quot(gr, c.div_g);
             const bool real = r < u.rows;
-            [[maybe_unused]] const int pos = real ? u.kv - u.ql + t : -1;
+            const int pos = TREE ? tree_row(a, u.q0, t, u.ql, u.kv, real).at : real ? u.kv - u.ql + t : -1;
             // positions of the half's first and last row
             const int f0 = u.qt * 256 + half * 128, f1 = u.qt * 256 + min(u.rows, half * 128 + 128) - 1;
             const int lo = TREE ? u.lo : u.kv - u.ql + quot(f0, c.div_g), hi = TREE ? u.hi : u.kv - u.ql + quot(f1, c.div_g);
@@ -456,7 +456,7 @@ __global__ void __launch_bounds__(Shape<DP, FMT, LOAD, TREE>::kThreads, 1) k_att
                 after_sync();
                 const int flags = *const_cast<volatile int *>(s_bad + slot);
                 if (TREE && (masked || (flags & 1)))
-                    mask_tree(ts, a, u.q0, t, u.ql, u.kv, real, base, flags & 1 ? s_kbad + slot * 4 : nullptr);
+                    mask_tree(ts, a, u.q0, t, u.ql, u.kv, pos, base, flags & 1 ? s_kbad + slot * 4 : nullptr);
                 else if (masked || (flags & 1))
                     mask_scores(ts, pos - base, a.window > 0 ? pos - a.window - base : -1, a.sinks - base,
                                 flags & 1 ? s_kbad + slot * 4 : nullptr);

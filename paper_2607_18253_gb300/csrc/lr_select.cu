@@ -1,8 +1,7 @@
 // The tokens that a cache keeps: of each sequence and KV head the first ones, the most recent ones, and of the rest those
 // with the largest weights, ties to the lowest position, in order of position.
 //
-// A weight becomes a 32-bit key that sorts as it does, a token that is kept in any case the largest.  The key of the last token
-// that is kept is found from the top byte down, by counting (four counts of 256 bins); the tokens above it
+// A weight becomes a 32-bit key that sorts as it does.  The key of the last token that is chosen is found from the top byte down, by counting (four counts of 256 bins); the tokens above it
 // are kept, and of those equal to it the first ones.  A cluster of CTAs has a list, each a range of its positions, whose keys it
 // holds in shared memory; the counts come together in the first CTA's, and the places of the ranges' tokens are read from one another's.
 #include <algorithm>
@@ -13,12 +12,12 @@ namespace lr {
 
 namespace {
 
-constexpr int kMostThreads = 1024, kMostWarps = kMostThreads / 32, kBins = 256;
-// Keys that a CTA holds in shared memory; further ones are read again for each count.  CTAs that are no more than the SMs take
-// what there is, and 1,024 threads; others leave room for four, of 256 threads.
-constexpr int kHold = 10240, kHoldAlone = 49152;
+constexpr int kBins = 256;
+// Keys that a CTA holds in shared memory; further ones are read again for each count.  CTAs that are no more than the SMs have
+// 1,024 threads and take what room there is, others have 512 and leave room for three.
+constexpr int kHold = 17408, kHoldAlone = 49152;
 constexpr int kMaxCluster = 16, kLeast = 2048;  // (positions a CTA, at least, or a list is not divided)
-constexpr int kAhead = 16;                      // weights that a thread reads together
+constexpr int kAhead = 8;                       // weights that a thread reads together
 constexpr size_t smem_of(int hold) { return (size_t)hold * 4 + 4 * kBins * 4; }
 
 // As `w` sorts: NaN above all, both zeros the same.
@@ -49,12 +48,13 @@ __device__ __forceinline__ uint32_t peer_word(uint32_t at) {
     return v;
 }
 
-__global__ void __launch_bounds__(kMostThreads) k_select(const __grid_constant__ SelectLaunch a) {
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS == 512 ? 3 : 1) k_select(const __grid_constant__ SelectLaunch a) {
+    constexpr int kWarps = THREADS / 32;
     extern __shared__ __align__(16) uint32_t smem[];
     uint32_t *const bins = smem, *const hold = smem + 4 * kBins;  // [4][kBins], keys
-    __shared__ uint32_t s_warp[2 * kMostWarps], s_bin[2], s_mine[2];
-    const int cl = a.cluster;
-    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, threads = blockDim.x, warps = threads / 32;
+    __shared__ uint32_t s_warp[2 * kWarps], s_bin[2], s_mine[2];
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, cl = a.cluster;
     const int rank = cl > 1 ? (int)cluster_rank() : 0;
     const CacheDev &c = a.c;
     chain_wait();
@@ -67,53 +67,73 @@ __global__ void __launch_bounds__(kMostThreads) k_select(const __grid_constant__
     m = min(m, kv);
     int32_t *const kept = a.kept + (int64_t)list * a.cap;
     if (h == 0 && rank == 0 && tid == 0) a.count[s] = m;
-    for (int64_t i = (int64_t)m + rank * threads + tid; i < a.cap; i += (int64_t)cl * threads) kept[i] = -1;
-    if (m == kv || m == 0) {  // (all or none: the whole cluster takes this way)
-        for (int64_t i = rank * threads + tid; i < m; i += cl * threads) kept[i] = (int32_t)i;
+    // The first tokens, and the last ones: kept in any case.  Between them are the tokens that are chosen from, `need` of them.
+    const int head = min(a.sinks, kv), tail = min(a.recent, kv - head), from = head, to = kv - tail;
+    uint32_t need = max(0, m - head - tail);
+    const int at_tail = head + (int)need;  // where the last ones go (a budget below what is kept in any case takes the first of it)
+    for (int64_t i = rank * THREADS + tid; i < a.cap; i += cl * THREADS)
+        if (i >= m) kept[i] = -1;
+        else if (i < head) kept[i] = (int32_t)i;
+        else if (i >= at_tail) kept[i] = to + (int32_t)i - at_tail;
+    const int all = to - from;
+    if (need == 0 || need == (uint32_t)all) {  // (the whole cluster takes this way)
+        if (need)
+            for (int i = rank * THREADS + tid; i < all; i += cl * THREADS) kept[head + i] = from + i;
         chain_next();
         return;
     }
     // a range of positions a CTA, of it a range a warp, in steps of 32
-    const int per = ((kv + cl - 1) / cl + 31) / 32 * 32;
-    const int p0 = (int)min((int64_t)kv, (int64_t)rank * per), p1 = (int)min((int64_t)kv, (int64_t)p0 + per);
+    const int per = ((all + cl - 1) / cl + 31) / 32 * 32;
+    const int p0 = (int)min((int64_t)to, from + (int64_t)rank * per), p1 = (int)min((int64_t)to, (int64_t)p0 + per);
+    const int mid = min(p1, p0 + a.hold);  // (the keys from here on are not held)
+    const int32_t *const table = a.b.table + (int64_t)s * a.b.table_stride;
+    const float *const weights = a.w + h * a.wh;
     auto read = [&](int p) -> uint32_t {
-        if (p < a.sinks || p >= kv - a.recent) return 0xffffffffu;
-        int place;
-        const int64_t blk = block_of(c, a.b, s, p, place);
-        if (blk < 0) {
+        const int i = quot(p, c.div_b);
+        const int blk = i < a.b.max_blocks ? __ldg(table + i) : -1;
+        if ((uint32_t)blk >= (uint32_t)c.nb) {
             report(c.status, kEInval);
             return 0u;
         }
-        return key_of(a.w[blk * a.wb + place * a.wt + h * a.wh]);
+        return key_of(weights[blk * a.wb + (p - i * c.b) * a.wt]);
     };
-    const int held = a.hold;
-    auto key = [&](int p) { return p - p0 < held ? hold[p - p0] : read(p); };
 
-    for (int i = tid; i < 4 * kBins; i += threads) bins[i] = 0;
+    for (int i = tid; i < 4 * kBins; i += THREADS) bins[i] = 0;
     if (cl > 1) cluster_sync();
     else __syncthreads();
-    for (int p = p0 + tid; p < p1; p += threads * kAhead) {
+    for (int p = p0 + tid; p < p1; p += THREADS * kAhead) {
         uint32_t k[kAhead];
+        if (p + (kAhead - 1) * THREADS < p1) {
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) k[i] = p + i * threads < p1 ? read(p + i * threads) : 0u;
+            for (int i = 0; i < kAhead; ++i) k[i] = read(p + i * THREADS);
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const int at = p + i * threads;
-            if (at >= p1) break;
-            if (at - p0 < held) hold[at - p0] = k[i];
-            atomicAdd(bins + (k[i] >> 24), 1u);
+            for (int i = 0; i < kAhead; ++i) {
+                if (p + i * THREADS < mid) hold[p + i * THREADS - p0] = k[i];
+                atomicAdd(bins + (k[i] >> 24), 1u);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) k[i] = p + i * THREADS < p1 ? read(p + i * THREADS) : 0u;
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                if (p + i * THREADS >= p1) break;
+                if (p + i * THREADS < mid) hold[p + i * THREADS - p0] = k[i];
+                atomicAdd(bins + (k[i] >> 24), 1u);
+            }
         }
     }
-    uint32_t prefix = 0, need = m;  // the key's bits so far; of the keys that have them, how many are kept
+    uint32_t prefix = 0;  // the key's bits so far; of the keys that have them, `need` are kept
 #pragma unroll 1
     for (int shift = 24; shift >= 0; shift -= 8) {
         uint32_t *const bin = bins + (3 - shift / 8) * kBins;
         if (shift < 24) {
-#pragma unroll 4
-            for (int p = p0 + tid; p < p1; p += threads) {
-                const uint32_t k = key(p);
+            auto count = [&](uint32_t k) {
                 if ((k ^ prefix) >> shift < 256u) atomicAdd(bin + (k >> shift & 255), 1u);
-            }
+            };
+            const int held = mid - p0;
+#pragma unroll 4
+            for (int i = tid; i < held; i += THREADS) count(hold[i]);
+            for (int p = mid + tid; p < p1; p += THREADS) count(read(p));
         }
         // the cluster's counts come together in its first CTA
         if (rank > 0) {
@@ -148,10 +168,11 @@ __global__ void __launch_bounds__(kMostThreads) k_select(const __grid_constant__
     }
     // prefix is the last kept token's key now, `need` how many of those equal to it are kept
 
-    const int each = ((p1 - p0 + warps - 1) / warps + 31) / 32 * 32;
+    const int each = ((p1 - p0 + kWarps - 1) / kWarps + 31) / 32 * 32;
     const int w0 = min(p1, p0 + warp * each), w1 = min(p1, w0 + each);
     uint32_t above = 0, equal = 0;
-#pragma unroll 4
+    auto key = [&](int p) { return p < mid ? hold[p - p0] : read(p); };
+#pragma unroll 2
     for (int p = w0 + lane; p - lane < w1; p += 32) {
         const uint32_t k = p < w1 ? key(p) : 0u;
         above += __popc(__ballot_sync(0xffffffffu, p < w1 && k > prefix));
@@ -159,11 +180,11 @@ __global__ void __launch_bounds__(kMostThreads) k_select(const __grid_constant__
     }
     if (lane == 0) {
         s_warp[warp] = above;
-        s_warp[kMostWarps + warp] = equal;
+        s_warp[kWarps + warp] = equal;
     }
     __syncthreads();
     uint32_t out = 0, eq = 0;
-    if (lane < warp) out = s_warp[lane], eq = s_warp[kMostWarps + lane];
+    if (lane < warp) out = s_warp[lane], eq = s_warp[kWarps + lane];
 #pragma unroll
     for (int o = 16; o >= 1; o >>= 1) {
         out += __shfl_xor_sync(0xffffffffu, out, o);
@@ -171,14 +192,12 @@ __global__ void __launch_bounds__(kMostThreads) k_select(const __grid_constant__
     }
     if (cl > 1) {
         if (tid < 2) {
-            uint32_t all = 0;
-            for (int w = 0; w < warps; ++w) all += s_warp[tid * kMostWarps + w];
-            s_mine[tid] = all;
+            uint32_t sum = 0;
+            for (int w = 0; w < kWarps; ++w) sum += s_warp[tid * kWarps + w];
+            s_mine[tid] = sum;
         }
         cluster_sync();
-#pragma unroll
-        for (int r = 0; r < kMaxCluster; ++r) {
-            if (r >= rank) break;
+        for (int r = 0; r < rank; ++r) {
             out += peer_word(peer(s_mine, r));
             eq += peer_word(peer(s_mine + 1, r));
         }
@@ -190,9 +209,9 @@ __global__ void __launch_bounds__(kMostThreads) k_select(const __grid_constant__
         const uint32_t ties = __ballot_sync(0xffffffffu, p < w1 && k == prefix);
         const uint32_t lower = (1u << lane) - 1;
         const bool take = p < w1 && (k > prefix || (k == prefix && eq + __popc(ties & lower) < need));
-        const uint32_t all = __ballot_sync(0xffffffffu, take);
-        if (take) kept[out + __popc(all & lower)] = p;
-        out += __popc(all);
+        const uint32_t mask = __ballot_sync(0xffffffffu, take);
+        if (take) kept[head + out + __popc(mask & lower)] = p;
+        out += __popc(mask);
         eq += __popc(ties);
     }
     if (cl > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");  // (no CTA leaves while another reads it)
@@ -202,22 +221,23 @@ __global__ void __launch_bounds__(kMostThreads) k_select(const __grid_constant__
 }  // namespace
 
 cudaError_t select_init() {
-    const cudaError_t e = cudaFuncSetAttribute(k_select, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    return e != cudaSuccess ? e : cudaFuncSetAttribute(k_select, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_of(kHoldAlone));
+    cudaError_t e = cudaFuncSetAttribute(k_select<1024>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_select<512>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_select<1024>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_of(kHoldAlone));
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_select<512>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_of(kHold));
+    return e;
 }
 
 cudaError_t launch_select(const SelectLaunch &a, int sms, cudaStream_t st) {
     const long long lists = (long long)a.b.n * a.c.H, longest = std::min((long long)a.b.max_blocks * a.c.b, (long long)kMaxTokens);
     SelectLaunch l = a;
     l.cluster = 1;
-    // as many CTAs a list as hold its keys (eight at most), and more of them for few lists
-    while ((l.cluster < 8 && longest > (long long)kHold * l.cluster) ||
-           (l.cluster < kMaxCluster && 2 * lists * l.cluster <= sms && longest >= 2ll * kLeast * l.cluster))
+    // as many CTAs a list as hold its keys, and more of them for few lists
+    while (l.cluster < kMaxCluster && (longest > (long long)kHold * l.cluster || (2 * lists * l.cluster <= sms && longest >= 2ll * kLeast * l.cluster)))
         l.cluster *= 2;
     const bool alone = lists * l.cluster <= sms;
-    const long long each = longest / l.cluster + 64;
-    l.hold = (int)std::min(each, (long long)(alone ? kHoldAlone : kHold));
-    return launch_clusters(k_select, (unsigned)(lists * l.cluster), alone ? kMostThreads : 256, smem_of(l.hold), (unsigned)l.cluster, st, l);
+    l.hold = (int)std::min(longest / l.cluster + 64, (long long)(alone ? kHoldAlone : kHold));
+    return launch_clusters(alone ? k_select<1024> : k_select<512>, (unsigned)(lists * l.cluster), alone ? 1024 : 512, smem_of(l.hold), (unsigned)l.cluster, st, l);
 }
 
 }  // namespace lr

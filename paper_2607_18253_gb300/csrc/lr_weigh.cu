@@ -67,7 +67,7 @@ struct Walk {
     __device__ __forceinline__ int base() const { return (tile < ns ? tile : wf + tile - ns) * TILE; }
 };
 
-template <bool BF16, int FMT, int DP, int NR>
+template <bool BF16, int FMT, int DP, int NR, bool EVEN>
 __global__ void __launch_bounds__(kThreads, Piece<DP, FMT, NR>::kCtas) k_weigh_step(const __grid_constant__ WeighLaunch a) {
     using P = Piece<DP, FMT, NR>;
     constexpr int kRows = 8 * NR, NB = P::NB, KS = DP / 16;
@@ -124,14 +124,16 @@ __global__ void __launch_bounds__(kThreads, Piece<DP, FMT, NR>::kCtas) k_weigh_s
         return;
     }
 
-    // the blocks of a lane's tokens (g and g + 8 of each 16), as the table has them: looked up a tile ahead
-    int blk[NB][2];
+    // The blocks of a lane's tokens (g and g + 8 of each 16), as the table has them: looked up a tile ahead.  Where blocks are
+    // multiples of 16 tokens, the 16 share one, and their addresses follow from the first's.
+    constexpr int kLooks = EVEN ? 1 : 2;
+    int blk[NB][kLooks];
     auto look = [&]() {
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int y = 0; y < 2; ++y) {
-                const int t = at.base() + b * 16 + y * 8 + g, i = quot(t, c.div_b);
+            for (int y = 0; y < kLooks; ++y) {
+                const int t = at.base() + b * 16 + (EVEN ? 0 : y * 8 + g), i = quot(t, c.div_b);
                 blk[b][y] = t < at.kv && i < a.a.b.max_blocks ? __ldg(a.a.b.table + (int64_t)at.s * a.a.b.table_stride + i) : -1;
             }
     };
@@ -148,28 +150,34 @@ __global__ void __launch_bounds__(kThreads, Piece<DP, FMT, NR>::kCtas) k_weigh_s
         [[maybe_unused]] float ks[NB][2];
         int64_t to[NB];  // where this lane's token's weight is, -1: not this lane's to write
         float old[NB], sum[NB][2];
+        // (no window hides a token of the tile, and it has no end: nearly always)
+        const bool full = end < kv && !(a.a.window > 0 && tile0 <= lo - a.a.window && end >= a.a.sinks);
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
             to[b] = -1;
             old[b] = sum[b][0] = sum[b][1] = 0.0f;
+            [[maybe_unused]] const int t16 = tile0 + b * 16, place16 = EVEN ? t16 - quot(t16, c.div_b) * c.b + g : 0;
+            [[maybe_unused]] const char *const p16 = EVEN ? c.k + (int64_t)blk[b][0] * c.sb + place16 * c.st + h * c.sh + i4 * 16 : nullptr;
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-                const int t = tile0 + b * 16 + y * 8 + g, place = t - quot(t, c.div_b) * c.b;
-                const bool any = !(a.a.window > 0 && t <= lo - a.a.window && t >= a.a.sinks);  // (some row sees it)
-                bool ok = t < kv && (any || a.decay != 1.0f);
-                if (ok && (uint32_t)blk[b][y] >= (uint32_t)c.nb) {  // (a token that no row sees may have no block any more)
+                const int t = tile0 + b * 16 + y * 8 + g, bk = blk[b][EVEN ? 0 : y];
+                const int place = EVEN ? place16 + y * 8 : t - quot(t, c.div_b) * c.b;
+                const bool any = full || !(a.a.window > 0 && t <= lo - a.a.window && t >= a.a.sinks);  // (some row sees it)
+                bool ok = full || (t < kv && (any || a.decay != 1.0f));
+                if (ok && (uint32_t)bk >= (uint32_t)c.nb) {  // (a token that no row sees may have no block any more)
                     if (any) report(c.status, kEInval);
                     ok = false;
                 }
-                const char *const p = c.k + (int64_t)blk[b][y] * c.sb + place * c.st + h * c.sh;
+                const char *const p = EVEN ? p16 + y * 8 * c.st : c.k + (int64_t)bk * c.sb + place * c.st + h * c.sh + i4 * 16;
 #pragma unroll
                 for (int v = 0; v < P::kVec; ++v) {
                     const int e = (v * 4 + i4) * 16;
-                    k[b][y][v] = ok && any && e < c.D * (FMT == kFmt16 ? 2 : 1) ? __ldg(reinterpret_cast<const uint4 *>(p + e)) : make_uint4(0, 0, 0, 0);
+                    k[b][y][v] = make_uint4(0, 0, 0, 0);
+                    if (ok && any && e < c.D * (FMT == kFmt16 ? 2 : 1)) k[b][y][v] = __ldg(reinterpret_cast<const uint4 *>(p + v * 64));
                 }
-                if constexpr (FMT != kFmt16) ks[b][y] = ok && any ? __ldg(c.ks + (int64_t)blk[b][y] * c.ssb + place * c.sst + h * c.ssh) : 0.0f;
+                if constexpr (FMT != kFmt16) ks[b][y] = ok && any ? __ldg(c.ks + (int64_t)bk * c.ssb + place * c.sst + h * c.ssh) : 0.0f;
                 if (ok && i4 == y) {
-                    to[b] = (int64_t)blk[b][y] * a.wb + place * a.wt + h * a.wh;
+                    to[b] = (int64_t)bk * a.wb + place * a.wt + h * a.wh;
                     if (a.decay != 0.0f && t < lo) old[b] = a.decay * a.w[to[b]];
                 }
             }
@@ -270,16 +278,26 @@ __global__ void __launch_bounds__(kThreads, Piece<DP, FMT, NR>::kCtas) k_weigh_s
                         }
                     }
                 }
+                const bool masked = !full || end > lo || (a.a.window > 0 && tile0 <= kv - 1 - a.a.window && end >= a.a.sinks);
 #pragma unroll
                 for (int m = 0; m < NR; ++m)
 #pragma unroll
                     for (int z = 0; z < 4; ++z) {
-                        const int j = tile0 + b * 16 + (z >> 1) * 8 + g;
                         float f = qf[m][z & 1];
                         if constexpr (FMT != kFmt16) f *= ks[b][z >> 1];
-                        const float p = exp2_fast(s[m][z] * f - less[m][z & 1]);
-                        sum[b][z >> 1] += visible(pos[m][z & 1], j, a.a.window, a.a.sinks) ? p : 0.0f;
+                        s[m][z] = exp2_fast(s[m][z] * f - less[m][z & 1]);
                     }
+                if (masked) {
+#pragma unroll
+                    for (int m = 0; m < NR; ++m)
+#pragma unroll
+                        for (int z = 0; z < 4; ++z)
+                            if (!visible(pos[m][z & 1], tile0 + b * 16 + (z >> 1) * 8 + g, a.a.window, a.a.sinks)) s[m][z] = 0.0f;
+                }
+#pragma unroll
+                for (int m = 0; m < NR; ++m)
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) sum[b][z >> 1] += pos[m][z & 1] >= 0 ? s[m][z] : 0.0f;
             }
         }
 #pragma unroll
@@ -296,21 +314,24 @@ __global__ void __launch_bounds__(kThreads, Piece<DP, FMT, NR>::kCtas) k_weigh_s
 }
 
 using Kernel = void (*)(const WeighLaunch);
-template <int FMT, int DP>
-Kernel pick_rows(bool bf16, bool few) {
-    return bf16 ? (few ? k_weigh_step<true, FMT, DP, 1> : k_weigh_step<true, FMT, DP, 2>)
-                : (few ? k_weigh_step<false, FMT, DP, 1> : k_weigh_step<false, FMT, DP, 2>);
+template <int FMT, int DP, int NR>
+Kernel pick_even(bool bf16, bool even) {
+    return even ? (bf16 ? k_weigh_step<true, FMT, DP, NR, true> : k_weigh_step<false, FMT, DP, NR, true>)
+                : (bf16 ? k_weigh_step<true, FMT, DP, NR, false> : k_weigh_step<false, FMT, DP, NR, false>);
 }
 template <int FMT>
-Kernel pick_dim(bool bf16, int D, bool few) { return D <= 64 ? pick_rows<FMT, 64>(bf16, few) : pick_rows<FMT, 128>(bf16, few); }
+Kernel pick_dim(bool bf16, int D, bool few, bool even) {
+    return D <= 64 ? (few ? pick_even<FMT, 64, 1>(bf16, even) : pick_even<FMT, 64, 2>(bf16, even))
+                   : (few ? pick_even<FMT, 128, 1>(bf16, even) : pick_even<FMT, 128, 2>(bf16, even));
+}
 
 }  // namespace
 
 cudaError_t launch_weigh_step(const WeighLaunch &a, bool bf16, int fmt, int rows, int sms, cudaStream_t st) {
-    const bool few = rows <= 8;
-    const Kernel k = fmt == kFmt16 ? pick_dim<kFmt16>(bf16, a.a.c.D, few)
-                   : fmt == kFmtE4M3 ? pick_dim<kFmtE4M3>(bf16, a.a.c.D, few)
-                                     : pick_dim<kFmtInt8>(bf16, a.a.c.D, few);
+    const bool few = rows <= 8, even = a.a.c.b % 16 == 0;
+    const Kernel k = fmt == kFmt16 ? pick_dim<kFmt16>(bf16, a.a.c.D, few, even)
+                   : fmt == kFmtE4M3 ? pick_dim<kFmtE4M3>(bf16, a.a.c.D, few, even)
+                                     : pick_dim<kFmtInt8>(bf16, a.a.c.D, few, even);
     return launch_chained(k, (few && fmt == kFmt16 ? 5 : 4) * sms, kThreads, 0, st, a);
 }
 
