@@ -128,7 +128,10 @@ __device__ __noinline__ void join_parts(const AttendLaunch &a, int c0, int parts
 #pragma unroll
             for (int z = 0; z < 16; ++z) {
                 const int k = k0 + z * kTwo + part0;
-                w[z] = k < parts ? __ldcg(reinterpret_cast<const float4 *>(a.part_o + at(k) * 128 + e)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                w[z] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (k < parts)  // (asked for together, whether they count or not)
+                    asm volatile("ld.global.cg.v4.f32 {%0,%1,%2,%3}, [%4];"
+                                 : "=f"(w[z].x), "=f"(w[z].y), "=f"(w[z].z), "=f"(w[z].w) : "l"(a.part_o + at(k) * 128 + e));
             }
 #pragma unroll
             for (int z = 0; z < 16; ++z) {
@@ -176,9 +179,12 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
     const CacheDev &c = a.c;
 
     chain_wait();
+    // tiles of a CTA's share: of a small tree's, whose units have many parts to join, two (8 tokens of 32 query heads over 1,339, 16
+    // bits: 27.5 us with one, 21 with two, 24 with four)
+    constexpr int kLeast = TREE && FMT == kFmt16 ? 2 : 1;
     Cursor<kRows, S::kTile, kStepWeight> cu, lk;
     Share sh;
-    if (!take_share<kRows, S::kTile, kStepWeight, kThreads, 1>(a, cu, sh, s_scratch)) {
+    if (!take_share<kRows, S::kTile, kStepWeight, kThreads, kLeast>(a, cu, sh, s_scratch)) {
         chain_next();
         return;
     }
