@@ -62,7 +62,8 @@ cudaError_t attend_chunk_init() {
     cudaError_t e = chunk_init<false>();
     if (e == cudaSuccess) e = tree_chunk_init();
     if (e == cudaSuccess) e = weigh_init();
-    if (e == cudaSuccess) e = select_init();  // (those of the other calls with much shared memory beside it)
+    if (e == cudaSuccess) e = select_init();
+    if (e == cudaSuccess) e = keep_init();
     return e;
 }
 

@@ -156,6 +156,7 @@ struct KeepLaunch {
     int64_t wb, wt, wh;
     int32_t vector, pieces, cluster;  // (set by the launch) bytes of a vector, parts that it is moved in, CTAs a list of such parts
 };
+cudaError_t keep_init();
 cudaError_t launch_keep(const KeepLaunch &a, int fmt, int sms, cudaStream_t st);
 
 // As launch_chained, in clusters of `cluster` CTAs.

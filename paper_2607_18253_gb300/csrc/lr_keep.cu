@@ -17,7 +17,7 @@ namespace lr {
 
 namespace {
 
-constexpr int kThreads = 256, kItems = 2, kMaxCluster = 8;
+constexpr int kThreads = 256, kItems = 2, kMaxCluster = 16;
 constexpr int kAhead = 2, kRun = kThreads * kAhead;  // tokens of a CTA that are looked up together
 
 template <int LANES, bool BOTH>
@@ -155,15 +155,22 @@ __global__ void __launch_bounds__(kThreads, 4) k_keep(const __grid_constant__ Ke
 
 }  // namespace
 
+cudaError_t keep_init() {
+    cudaError_t e = cudaSuccess;
+    for (void (*const k)(const KeepLaunch) : {k_keep<4, false>, k_keep<8, false>, k_keep<16, false>})
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(k, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    return e;
+}
+
 // Lists that fill the GPU take K and V together, a CTA each; fewer are divided into K and V, clusters, and pieces of vectors (64
 // bytes at least) while a list is more than a batch.
 cudaError_t launch_keep(const KeepLaunch &a, int fmt, int sms, cudaStream_t st) {
     KeepLaunch l = a;
     l.vector = a.c.D * (fmt == kFmt16 ? 2 : 1);
     if (fmt == kFmt16) l.c.ks = l.c.vs = nullptr;
-    const long long lists = (long long)a.b.n * a.c.H, room = 2ll * sms;
+    const long long lists = (long long)a.b.n * a.c.H, room = 4ll * sms;
     int lanes = l.vector <= 64 ? 4 : l.vector <= 128 ? 8 : 16;
-    const bool both = lists * 2 > room || (long long)a.cap * 2 * lanes <= kThreads;
+    const bool both = lists * 4 > room || (long long)a.cap * 2 * lanes <= kThreads;
     const int kl = lanes * (both ? 2 : 1);
     // (a short list is one or two batches of a smaller CTA: 2,048 lists of up to 16 tokens in 256 threads 14.4 us)
     const int threads = (int)std::min<long long>(kThreads, std::max<long long>(32, ((long long)a.cap * kl / 4 + 31) / 32 * 32));

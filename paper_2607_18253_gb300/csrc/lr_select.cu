@@ -14,8 +14,8 @@ namespace {
 
 constexpr int kBins = 256;
 // Keys that a CTA holds in shared memory; further ones are read again for each count.  CTAs that are no more than the SMs have
-// 1,024 threads and take what room there is, others have 512 and leave room for three.
-constexpr int kHold = 17408, kHoldAlone = 49152;
+// 1,024 threads and take what room there is, others have 512 and leave room for four.
+constexpr int kHold = 8704, kHoldAlone = 49152;
 constexpr int kMaxCluster = 16, kLeast = 2048;  // (positions a CTA, at least, or a list is not divided)
 constexpr int kAhead = 8;                       // weights that a thread reads together
 constexpr size_t smem_of(int hold) { return (size_t)hold * 4 + 4 * kBins * 4; }
@@ -49,7 +49,7 @@ __device__ __forceinline__ uint32_t peer_word(uint32_t at) {
 }
 
 template <int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS == 512 ? 3 : 1) k_select(const __grid_constant__ SelectLaunch a) {
+__global__ void __launch_bounds__(THREADS, THREADS == 512 ? 4 : 1) k_select(const __grid_constant__ SelectLaunch a) {
     constexpr int kWarps = THREADS / 32;
     extern __shared__ __align__(16) uint32_t smem[];
     uint32_t *const bins = smem, *const hold = smem + 4 * kBins;  // [4][kBins], keys

@@ -98,6 +98,12 @@ struct Line {
     __device__ __forceinline__ void next(const WeighLaunch &a, const Share &sh) {  // (not the last)
         j = 0;
         at += n + kWeight;
+        if (a.a.window == 0 && u + 1 < nu && (u + 1) * kUnit <= lo) {  // (nearly always: another unit that all rows see)
+            ++u;
+            end = (int)min((long long)n, sh.x1 - at - kWeight);
+            last = at + n + 2 * kWeight >= sh.x1;
+            return;
+        }
         if (++u == nu) {
             u = 0;
             if (++h == a.a.c.H) {
