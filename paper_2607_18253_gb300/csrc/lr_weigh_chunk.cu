@@ -285,7 +285,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_weigh_chunk(const __grid_consta
                     const float *const less = s_less + st * kRowTile;
                     const uint32_t from = ts + (n_s & 1) * 128;
                     const int row0 = (unit_r0 + j) * in.rt, some = min(in.rt, unit_rows - row0);
-                    // 32 scores of the token
+                    // 32 scores of the token; a tile's are summed by themselves first (16,384 rows one after the other are off by 2e-6)
+                    float2 part[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
                     auto add = [&](const float *s, int k0) {
 #pragma unroll
                         for (int k = 0; k < 32; k += 4) {
@@ -296,8 +297,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_weigh_chunk(const __grid_consta
                             x.y = exp2_fast(x.y);
                             y.x = exp2_fast(y.x);
                             y.y = exp2_fast(y.y);
-                            sum[0] = add2(sum[0], x);
-                            sum[1] = add2(sum[1], y);
+                            part[0] = add2(part[0], x);
+                            part[1] = add2(part[1], y);
                         }
                     };
                     float x[32], y[32];
@@ -327,12 +328,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_weigh_chunk(const __grid_consta
 #pragma unroll
                             for (int k = 0; k < 32; ++k) {
                                 const float g = less[k0 + k], e = exp2_fast(x[k] * f + g);
-                                sum[k & 1].x += r + k >= first && r + k < end && g != -INFINITY ? e : 0.0f;
+                                part[k & 1].x += r + k >= first && r + k < end && g != -INFINITY ? e : 0.0f;
                             }
                         }
                         before_sync();
                         bar_arrive_warp(s_free + 16 * half + 8 * (n_s & 1));
                     }
+                    sum[0] = add2(sum[0], part[0]);
+                    sum[1] = add2(sum[1], part[1]);
                     ++n_s;
                 }
                 bar_arrive_warp(l_free + 8 * st);

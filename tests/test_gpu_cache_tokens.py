@@ -168,6 +168,16 @@ def test_hidden_tokens_do_not_reach_a_row(fmt, value):
         c.check()
 
 
+@pytest.mark.parametrize("fmt", ["16", "e4m3"])
+@pytest.mark.parametrize("seqs", [[(40, 60001)], [(9, 20000), (1, 3), (33, 9000)], [(8, 30000)], [(100, 40000), (70, 40000)]])
+def test_trees_split_over_the_gpu(fmt, seqs):
+    # few and many parts of a unit, joined at once or by groups: the same bits every time
+    c = Tree(seqs, H=1, G=4, fmt=fmt, seed=73)
+    a, la = c.check()
+    b, lb = c.check()
+    assert torch.equal(a, b) and torch.equal(la, lb)
+
+
 def test_tree_rows_and_strides():
     # more words than needed, rows of a wider tensor, rows of no sequence, one mask for all rows
     c = Tree(TREES["wide"], words=9, seed=49, pad=7)
@@ -294,6 +304,18 @@ def test_weigh_is_the_same_every_time(fmt, seqs):
 def test_weigh_many_rows_of_one_head():
     check_weights(base.Case([(1500, 1700)], H=1, G=8, seed=55))
     check_weights(base.Case([(700, 700), (900, 5000)], H=1, G=1, D=80, fmt="e4m3", dtype="fp16", seed=56), 0.0)
+
+
+@pytest.mark.parametrize("fmt", ["16", "int8"])
+def test_more_sequences_than_threads(fmt):
+    # every round of the walks over a batch, in either kernel, and of the lists
+    seqs = [(1 if i % 7 else 0, 1 + i % 90) for i in range(1299)]
+    seqs.insert(900, (70, 200))
+    c = base.Case(seqs, H=1, G=2, D=64, fmt=fmt, seed=74)
+    w = check_weights(c, 0.5)
+    kept, count = choose(c, w, 40, sinks=1, recent=7)
+    check_keep(c, kept, count, w=w)
+    Tree([(1 + i % 3, 5 + i % 60) for i in range(1200)] + [(50, 90)], H=1, G=2, D=64, fmt=fmt, seed=75).check()
 
 
 def test_weigh_sharp_rows_and_scale():
@@ -611,6 +633,44 @@ def test_a_tree_is_verified_and_its_path_kept():
     want = torch.stack([out[int(c.q_start[s]) + int(c.paths[s].sum(1).argmax())] for s in range(3)])
     # two roundings of the output and two of the weights, of values whose weighted magnitudes are at most max |v|
     assert bool(((got.double() - want).abs() <= 4.1 * base.U["bf16"] * float(c.v.abs().max())).all())
+
+
+def test_calls_on_two_streams():
+    # each with a cache of its own, at the same time: lists that clusters move, joined parts
+    cases = [Tree([(40, 30000), (3, 700)], H=2, G=4, fmt=fmt, seed=76) for fmt in ("16", "e4m3")]
+    streams = [torch.cuda.Stream() for _ in cases]
+    plan = [lists(c, 30000, share=0.4, seed=3) for c in cases]
+    want, got = [], []
+    for c, (kept, count) in zip(cases, plan):
+        state = [t.clone() for t in (c.k, c.v)]
+        w = weights_of(c)
+        out, lse = c.cache.attend(c.q, c.batch, lse=True, tree=c.tree)
+        c.cache.weigh(c.q, lse, c.batch, w)
+        c.cache.keep(kept, count, c.batch, weights=w)
+        want.append([out, lse, w, c.k.clone(), c.v.clone()])
+        c.k.copy_(state[0])
+        c.v.copy_(state[1])
+        if c.k_scale is not None:
+            want[-1] += [c.k_scale.clone()]
+    scales = [None if c.k_scale is None else base.Case([(40, 30000), (3, 700)], H=2, G=4, fmt=c.fmt, seed=76) for c in cases]
+    for c, fresh in zip(cases, scales):
+        if fresh is not None:
+            c.k_scale.copy_(fresh.k_scale)
+            c.v_scale.copy_(fresh.v_scale)
+    torch.cuda.synchronize()
+    for c, st, (kept, count) in zip(cases, streams, plan):
+        with torch.cuda.stream(st):
+            w = weights_of(c)
+            out, lse = c.cache.attend(c.q, c.batch, lse=True, tree=c.tree)
+            c.cache.weigh(c.q, lse, c.batch, w)
+            c.cache.keep(kept, count, c.batch, weights=w, stream=st)
+            got.append([out, lse, w, c.k, c.v] + ([c.k_scale] if c.k_scale is not None else []))
+    torch.cuda.synchronize()
+    for c, x, y in zip(cases, want, got):
+        assert c.cache.status() == R().LR_OK
+        for t, u in zip(x, y):
+            raw = {1: torch.int8, 2: torch.int16, 4: torch.int32}[t.element_size()]
+            assert torch.equal(t.view(raw), u.view(raw))
 
 
 def test_calls_are_captured_and_replayed():
