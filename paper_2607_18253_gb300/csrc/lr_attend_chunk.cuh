@@ -1,6 +1,7 @@
-// Attention of many rows over a paged KV cache: chunks of new tokens.
+// Attention of many rows over a paged KV cache: chunks of new tokens, and trees of drafted tokens (TREE: a row's mask instead of the
+// causal rule, which only the tiles that the drafted tokens or the window's edge lie in are looked at for).
 //
-// The same one-pass softmax as the step kernel (lr_attend_step.cu), bound by its two matrix
+// The same one-pass softmax as the step kernel (lr_attend_step.cuh), bound by its two matrix
 // products instead of the cache's bytes: 4 D operations a (row, token) pair.  A CTA takes 256 rows
 // (tokens x query heads of a KV head) against tiles of 128 cached tokens on the tensor cores of sm_103a (tcgen05):
 //   S = Q K^T    both operands in shared memory, 128 x 128 fp32 in tensor memory, one for each half of the rows

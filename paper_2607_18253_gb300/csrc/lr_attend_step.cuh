@@ -1,4 +1,5 @@
-// Attention of few rows over a paged KV cache: the single tokens of many sequences.
+// Attention of few rows over a paged KV cache: the single tokens of many sequences, and small trees of drafted tokens (TREE: a
+// row's mask instead of the causal rule; up to 32 rows a sequence in tiles of 16).
 //
 // For the rows of a unit (lr_attend.cuh) the softmax needs one pass over the cached tokens: with
 // the running maximum m, the sum l of exp(x_j - m) and the weighted sum o of v_j, a tile of tokens
