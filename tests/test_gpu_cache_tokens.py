@@ -466,6 +466,11 @@ def test_select_of_long_lists():
     choose(c, w, 20000, sinks=4, recent=1024)
     choose(c, torch.floor(w * 8), 130000)
     choose(c, torch.full_like(w, 1.0), 33333, recent=1)
+    # a CTA an SM, sixteen a list
+    c = base.Case([(1, 900001)], H=1, G=1, D=16, b=128, seed=77)
+    w = torch.rand(c.k.shape[:3], device="cuda")
+    choose(c, w, 300000, sinks=1)
+    check_keep(c, *lists(c, 300000, share=0.3), w=w)
 
 
 def moved(c, kept, count, start, w):
