@@ -1,5 +1,5 @@
 // Attention of few rows over a paged KV cache: the single tokens of many sequences, and small trees of drafted tokens (TREE: a
-// row's mask instead of the causal rule; up to 32 rows a sequence in tiles of 16).
+// row's mask instead of the causal rule; up to 128 rows a sequence in tiles of 16).
 //
 // For the rows of a unit (lr_attend.cuh) the softmax needs one pass over the cached tokens: with
 // the running maximum m, the sum l of exp(x_j - m) and the weighted sum o of v_j, a tile of tokens
@@ -275,7 +275,7 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
     float o[KS][NR][4], m[NR][2], l[NR][2], qf[NR][2], less[NR][2];  // less: m, 0 where it is -inf
     [[maybe_unused]] float down[NR][2];  // 8 bits: the power of two that the row's weights are multiplied by
     int pos[NR][2];
-    [[maybe_unused]] uint32_t drafted[NR][2];  // of a tree: the drafted tokens that the row sees (at most 32 rows are at most 32 tokens)
+    [[maybe_unused]] uint32_t drafted[NR][2];  // of a tree: the drafted tokens that the row sees (of at most 32)
     auto sees = [&](int n, int y, int j, const Unit &u) {
         if constexpr (TREE) {
             const int i = j - (u.kv - u.ql);

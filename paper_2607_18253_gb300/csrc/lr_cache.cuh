@@ -92,7 +92,8 @@ struct AttendLaunch {
                                  // between calls
 };
 constexpr int kStepRows = 16;   // rows of a unit of the step kernel, at most
-constexpr int kTreeRows = 32;   // rows of a tree that are the step kernel's, in tiles of 16: at most 32 tokens, a word of their masks
+constexpr int kTreeRows = 128;  // rows of a tree that are the step kernel's, in tiles of 16, at most; of 32 tokens, a word of their masks
+constexpr int kTreeLittle = 400000;  // tokens x KV heads x tiles of 16 rows that are little
 cudaError_t launch_attend_step(const AttendLaunch &a, bool bf16, int fmt, int rows, int sms, cudaStream_t st);
 cudaError_t attend_step_init();
 int attend_step_ctas(int sms);  // CTAs of a launch, at most

@@ -65,13 +65,14 @@ int attend(lr_cache *c, const lr_cache_batch *b, int32_t T, const void *q, int64
     // launches: 63 single tokens beside a chunk of 1,985 (32 query and 8 KV heads of 128) 198 us, in the
     // chunk kernel alone 222.
     const long long most = (long long)b->max_q * c->dev.G;
-    // Of trees up to 32, in two tiles of 16 that each read the cache, where the chunk kernel would convert 8 bits (32 rows
-    // a sequence, 64 sequences of 4,000 tokens: 286 us, there 374; 16 rows: 155 and 368), or where there is little to read (32 rows over
-    // 20,000 tokens: 54 us, there 73; 8 sequences of 4,000 are even); else up to 16 (64 sequences of 4,000: 201 us, there 222).  A batch with
-    // a larger tree is the chunk kernel's whole (64 trees of 16 to 64 rows over 8 bits: 206 us, divided 254).
-    const long long tokens = (long long)b->num_seqs * c->dev.H * std::min<long long>((long long)b->max_blocks * c->dev.b, kMaxTokens);
-    const bool two = tree && (c->cfg.format != LR_CACHE_16BIT || tokens <= 200000);
-    const int few = two ? kTreeRows : tree || most <= 16 || c->dev.G > 8 ? 16 : 8;
+    // Of trees up to 16 (64 sequences of 4,000 tokens, 16 bits: 201 us, there 222), up to 32 where the chunk kernel would convert 8 bits (32
+    // rows, 64 sequences of 4,000 tokens: 286 us, there 374; 16 rows: 155 and 368), and more where there is little to read but enough that a
+    // unit has many parts in the chunk kernel, in tiles of 16 that each read the cache (96 rows over 8,000 tokens, 2 KV heads: 34 us,
+    // there 47; 4 sequences of 64 rows and 4,000 tokens, 8 heads: 52 and 46; 16 of 500 tokens, 2 heads: 37 and 20).  A batch with a larger
+    // tree is the chunk kernel's whole (64 trees of 16 to 64 rows over 8 bits: 206 us, divided 254).
+    const long long longest = std::min<long long>((long long)b->max_blocks * c->dev.b, kMaxTokens);
+    const bool little = b->max_q <= 32 && longest > 1024 && (long long)b->num_seqs * c->dev.H * longest * ((most + 15) / 16) <= kTreeLittle;
+    const int few = !tree ? (most <= 16 || c->dev.G > 8 ? 16 : 8) : little ? kTreeRows : c->cfg.format != LR_CACHE_16BIT ? 32 : 16;
     cudaStream_t st = (cudaStream_t)stream;
     if (most > few) {
         const bool all = b->num_seqs == 1 || tree;

@@ -169,7 +169,8 @@ def test_hidden_tokens_do_not_reach_a_row(fmt, value):
 
 
 @pytest.mark.parametrize("fmt", ["16", "e4m3"])
-@pytest.mark.parametrize("seqs", [[(40, 60001)], [(9, 20000), (1, 3), (33, 9000)], [(8, 30000)], [(100, 40000), (70, 40000)]])
+@pytest.mark.parametrize("seqs", [[(40, 60001)], [(9, 20000), (1, 3), (33, 9000)], [(8, 30000)], [(100, 40000), (70, 40000)],
+                                  [(30, 12000)], [(17, 5000), (32, 3001), (1, 64)]])
 def test_trees_split_over_the_gpu(fmt, seqs):
     # few and many parts of a unit, joined at once or by groups: the same bits every time
     c = Tree(seqs, H=1, G=4, fmt=fmt, seed=73)
