@@ -13,20 +13,19 @@ namespace {
 
 void free_all(lr_cache *c) {
     cudaFree(c->dev.status);
-    for (lr_cache::Parts *p : {&c->step, &c->chunk, &c->weigh}) {
-        cudaFree(p->o);
-        cudaFree(p->ml);
-        cudaFree(p->done);
-    }
+    for (lr_cache::Parts *p : {&c->step, &c->chunk, &c->weigh}) cudaFree(p->o);
 }
 
-// Two slots of partial rows a CTA, and counters at zero.
+// Two slots of partial rows a CTA, and counters at zero: one allocation.
 cudaError_t alloc_parts(lr_cache::Parts &p, size_t ctas, size_t rows, size_t counters) {
-    cudaError_t e = cudaMalloc(&p.o, 2 * ctas * rows * 128 * sizeof(float));
-    if (e == cudaSuccess) e = cudaMalloc(&p.ml, 2 * ctas * rows * sizeof(float2));
-    if (e == cudaSuccess) e = cudaMalloc(&p.done, counters * sizeof(uint32_t));
-    if (e == cudaSuccess) e = cudaMemset(p.done, 0, counters * sizeof(uint32_t));
-    return e;
+    const size_t o = 2 * ctas * rows * 128 * sizeof(float), ml = 2 * ctas * rows * sizeof(float2), done = counters * sizeof(uint32_t);
+    void *at = nullptr;
+    cudaError_t e = cudaMalloc(&at, o + ml + done);
+    if (e != cudaSuccess) return e;
+    p.o = static_cast<float *>(at);
+    p.ml = reinterpret_cast<float2 *>(static_cast<char *>(at) + o);
+    p.done = reinterpret_cast<uint32_t *>(static_cast<char *>(at) + o + ml);
+    return cudaMemset(p.done, 0, done);
 }
 
 // Attention of the batch, causal or, with `tree`, of drafted tokens.
