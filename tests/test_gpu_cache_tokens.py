@@ -641,6 +641,17 @@ def test_a_tree_is_verified_and_its_path_kept():
     assert bool(((got.double() - want).abs() <= 4.1 * base.U["bf16"] * float(c.v.abs().max())).all())
 
 
+def test_offsets_beyond_32_bits():
+    # 4.6 GB of K and of V, the sequences' blocks anywhere in them
+    c = Tree([(8, 300), (3, 90), (40, 700)], H=8, G=2, spare=140000, seed=78)
+    assert c.k.numel() * 2 > 1 << 32 and int(c.table.max()) * c.k.stride(0) * 2 > 1 << 32
+    c.check()
+    w = check_weights(c, 0.5)
+    check_weights(Tree([(1, 300), (2, 90)], H=8, G=2, spare=140000, seed=79))
+    kept, count = choose(c, w, 128, sinks=2, recent=8)
+    check_keep(c, kept, count, w=w)
+
+
 def test_calls_on_two_streams():
     # each with a cache of its own, at the same time: lists that clusters move, joined parts
     cases = [Tree([(40, 30000), (3, 700)], H=2, G=4, fmt=fmt, seed=76) for fmt in ("16", "e4m3")]
