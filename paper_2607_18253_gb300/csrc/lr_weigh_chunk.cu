@@ -25,8 +25,9 @@ namespace {
 
 constexpr int kThreads = 512, kUnit = 2 * kTok, kRowTile = 128;
 
-// A tile of rows is as many tokens' as 128 holds, whole, so that it is one box of the tensor copy engine (`rt` rows; the others
-// of 128 stay zero, and their lse makes nothing of them).
+// A tile of rows is as many tokens' as 128 holds, whole, so that it is one box of the tensor copy engine (`rt` rows).  The other
+// columns of 128 have queries of zero and -inf for -lse, which makes nothing of them where K is finite: zero times K is zero.  Where the
+// last column's score is not, the tile takes the way that leaves out what it must.
 struct ChunkLaunch {
     WeighLaunch w;
     CacheMaps m;
@@ -310,33 +311,39 @@ __global__ void __launch_bounds__(kThreads, 1) k_weigh_chunk(const __grid_consta
                         }
                     };
                     float x[32], y[32];
-                    if (__all_sync(0xffffffffu, first <= row0 && end >= row0 + in.rt) && !s_odd[st]) {
-                        tm_load(x, from);
+                    bool all = __all_sync(0xffffffffu, first <= row0 && end >= row0 + in.rt) && !s_odd[st];
+                    if (all) {
+                        tm_load(x, from + 96);
                         tm_load_wait(x);
-                        tm_load(y, from + 32);
-                        add(x, 0);
+                        all = in.rt == kRowTile || __all_sync(0xffffffffu, x[31] * f == 0.0f);
+                    }
+                    if (all) {
+                        tm_load(y, from);
+                        add(x, 96);
                         tm_load_wait(y);
-                        tm_load(x, from + 64);
-                        add(y, 32);
+                        tm_load(x, from + 32);
+                        add(y, 0);
                         tm_load_wait(x);
-                        tm_load(y, from + 96);
-                        add(x, 64);
+                        tm_load(y, from + 64);
+                        add(x, 32);
                         tm_load_wait(y);
                         before_sync();
                         bar_arrive_warp(s_free + 16 * half + 8 * (n_s & 1));
-                        add(y, 96);
+                        add(y, 64);
                     } else {
-                        // (what a row does not see, or is no row, is left out, whatever it is)
+                        // (what a row does not see, or is no row of the tile, is left out, whatever it is; the others are summed as above)
+                        const int last = min(end, row0 + some);
 #pragma unroll 1
-                        for (int k0 = 0; k0 < some; k0 += 32) {
-                            const int r = row0 + k0;
-                            if (__all_sync(0xffffffffu, first >= r + 32 || end <= r)) continue;
+                        for (int i = 0; i < 4; ++i) {
+                            const int k0 = i == 0 ? 96 : i * 32 - 32, r = row0 + k0;
+                            if (__all_sync(0xffffffffu, first >= r + 32 || last <= r)) continue;
                             tm_load(x, from + k0);
                             tm_load_wait(x);
 #pragma unroll
                             for (int k = 0; k < 32; ++k) {
-                                const float g = less[k0 + k], e = exp2_fast(x[k] * f + g);
-                                part[k & 1].x += r + k >= first && r + k < end && g != -INFINITY ? e : 0.0f;
+                                const float g = less[k0 + k], e = exp2_fast(fmaf(x[k], f, g));
+                                float &sum_k = k & 1 ? part[k >> 1 & 1].y : part[k >> 1 & 1].x;
+                                sum_k += r + k >= first && r + k < last && g != -INFINITY ? e : 0.0f;
                             }
                         }
                         before_sync();
@@ -584,7 +591,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_weigh_chunk(const __grid_consta
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int r = lane * 4 + k, gr = row0 + r, t = quot(gr, c.div_g);
-                x[k] = r < some ? __ldg(a.a.lse + (int64_t)(l.q0 + t) * c.Hq + l.h * c.G + gr - t * c.G) : INFINITY;
+                x[k] = r < some ? __ldg(a.a.lse + (int64_t)(l.q0 + t) * c.Hq + l.h * c.G + gr - t * c.G) : 0.0f;
             }
         };
         float now[4], then[4];
@@ -605,7 +612,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_weigh_chunk(const __grid_consta
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 odd |= now[k] == -INFINITY;  // (a row that saw nothing adds nothing)
-                less[k] = now[k] == -INFINITY ? -INFINITY : -fmaf(now[k], a.lse_log2, now[k] * a.lse_log2_rest);
+                // (a column of no row: not by an infinite lse, whose two products need not have the same sign)
+                less[k] = lane * 4 + k >= some || now[k] == -INFINITY ? -INFINITY : -fmaf(now[k], a.lse_log2, now[k] * a.lse_log2_rest);
             }
             *reinterpret_cast<float4 *>(s_less + ls * kRowTile + lane * 4) = make_float4(less[0], less[1], less[2], less[3]);
             odd = __any_sync(0xffffffffu, odd);

@@ -1,0 +1,77 @@
+"""Weights of cached tokens where the kernels' tiles have columns of no row, in a comparison that a NaN fails.
+
+The reference and the bound are those of test_gpu_cache_tokens.py: |w - want| <= tol in 64 bits, and places that no call
+writes equal to the last bit (their bound is zero).
+"""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import test_gpu_cache as base  # noqa: E402
+from test_gpu_cache import R, SEQS, _built  # noqa: E402,F401
+from test_gpu_cache_tokens import expected, weights_of  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+def weighed(c, decay=1.0, window=0, sinks=0, scale=None, lse=None):
+    """The call's weights, within their bound: every one of them a number."""
+    w0 = weights_of(c)
+    if lse is None:
+        _, lse = c.cache.attend(c.q, c.batch, lse=True, window=window, sinks=sinks, scale=scale)
+    w = c.cache.weigh(c.q, lse, c.batch, w0.clone(), decay=decay, window=window, sinks=sinks, scale=scale)
+    assert c.cache.status() == R().LR_OK
+    want, tol = expected(c, lse, w0, decay, window, sinks, scale)
+    assert torch.isfinite(want).all() and torch.isfinite(tol).all()
+    inside = (w.double() - want).abs() <= tol  # (false for a NaN)
+    assert inside.all(), (int((~inside).sum()), int(torch.isnan(w).sum()))
+    return w
+
+
+# A sequence of several tiles of rows, full ones and a rest, a single token, and one whose rows are a tile and a few more (G = 3).
+CHUNKS = [(130, 420), (1, 77), (43, 43), (86, 300)]
+FORMS = [("16", "bf16", 16), ("16", "fp16", 5), ("e4m3", "bf16", 16), ("int8", "fp16", 24)]
+
+
+@pytest.mark.parametrize("G", [3, 5, 6, 7, 40])
+@pytest.mark.parametrize("D", [16, 64, 80, 96, 112, 128])
+def test_weigh_tiles_with_columns_of_no_row(G, D):
+    # G does not divide the 128 columns of a tile; scales on either side of where log2(e) times them is rounded to
+    for fmt, dtype, b in FORMS:
+        c = base.Case(CHUNKS, H=2, G=G, D=D, b=b, dtype=dtype, fmt=fmt, seed=80)
+        for scale in (None, 1.0, 0.125, 0.11, 0.1):
+            weighed(c, 0.5, scale=scale)
+        for decay, window, sinks in ((1.0, 100, 4), (0.5, 100, 4), (0.5, 33, 0), (0.0, 1 << 20, 0)):
+            weighed(c, decay, window, sinks)
+
+
+@pytest.mark.parametrize("fmt", ["16", "e4m3", "int8"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("seqs", list(SEQS))
+def test_weigh_every_weight_is_a_number(fmt, dtype, seqs):
+    for G, D, b in ((4, 128, 16), (1, 64, 1), (3, 80, 5), (8, 16, 16), (16, 96, 24), (17, 128, 64), (40, 64, 128)):
+        c = base.Case(SEQS[seqs], G=G, D=D, b=b, dtype=dtype, fmt=fmt, seed=81)
+        for decay in (1.0, 0.0, 0.9375):
+            weighed(c, decay)
+        weighed(c, 0.25, window=64, sinks=200)
+        weighed(c, 1.0, window=17, sinks=3)
+        weighed(c, 0.5, scale=0.7)
+
+
+@pytest.mark.parametrize("G,D", [(3, 64), (7, 128), (4, 128)])
+def test_weigh_infinite_keys(G, D):
+    # a token that all rows see with a score of -inf receives nothing, and the others what they do without it
+    c = base.Case([(130, 420)], H=1, G=G, D=D, seed=82)
+    c.q[..., 5] = c.q[..., 5].abs() + 0.5
+    blk, place = int(c.table[0, 2]), 7  # token 39
+    c.k[blk, place] = 0.0
+    _, lse = c.cache.attend(c.q, c.batch, lse=True)
+    w0 = weights_of(c)
+    want = c.cache.weigh(c.q, lse, c.batch, w0.clone(), decay=0.5)
+    want[blk, place] = 0.5 * w0[blk, place]
+    c.k[blk, place, :, 5] = -math.inf
+    w = c.cache.weigh(c.q, lse, c.batch, w0.clone(), decay=0.5)
+    assert c.cache.status() == R().LR_OK
+    assert torch.isfinite(want).all() and torch.equal(w, want)
