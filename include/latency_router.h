@@ -536,7 +536,7 @@ LR_API int lr_cache_attend_tree(lr_cache *c, const lr_cache_batch *b, int32_t T,
  *               that see j of exp(scale * q_r . k_j - lse_r).
  * decay: finite, >= 0; with 0 what stood there is not read.  With 1, tokens that no row sees (below a window) are left as they are;
  * else all of the sequence's tokens are written, so that all its blocks must be its own.  A sequence that brings no
- * tokens is left as it is; a row whose lse is -inf (it saw nothing) adds nothing.
+ * tokens is left as it is; a row whose lse is -inf (it saw nothing) or +inf adds nothing.
  * A token whose block several sequences of the batch share (a common prefix) has no defined weight.
  * Sums are fp32, in an order that the call's sizes alone decide: the same call gives the same bits.  Over 8-bit
  * caches scores are formed as in lr_cache_attend.  lse: [T][num_q_heads] fp32.

@@ -39,6 +39,7 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
+// (of a number: an infinity's two products need not have the same sign)
 __device__ __forceinline__ float lse_log2(const WeighLaunch &a, float l) { return fmaf(l, a.lse_log2, l * a.lse_log2_rest); }
 
 // The batch's tiles of tokens in one line: sequences in order, in a sequence head after head, so that a warp keeps its queries
@@ -246,9 +247,10 @@ __global__ void __launch_bounds__(kThreads, Piece<DP, FMT, NR>::kCtas) k_weigh_s
                         const int row = r0 + m * 8 + 2 * i4 + y, tt = quot(row, c.div_g);
                         const bool real = row < rows;
                         const float l = real ? __ldg(a.a.lse + (int64_t)(q0 + tt) * c.Hq + h * c.G + row - tt * c.G) : -INFINITY;
-                        // (a row that sees nothing adds nothing)
-                        pos[m][y] = l == -INFINITY ? -1 : lo + tt;
-                        less[m][y] = l == -INFINITY ? 0.0f : lse_log2(a, l);
+                        // (a row that saw nothing adds nothing; one with an lse of +inf neither, as exp(x - inf))
+                        const bool none = fabsf(l) == INFINITY;
+                        pos[m][y] = none ? -1 : lo + tt;
+                        less[m][y] = none ? 0.0f : lse_log2(a, l);
                         qf[m][y] = a.a.scale_log2 * __shfl_sync(0xffffffffu, pow2, (2 * i4 + y) * 4);
                     }
                 }

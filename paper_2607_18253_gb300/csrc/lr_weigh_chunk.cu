@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_weigh_chunk(const __grid_consta
     int64_t *const s_from = s_to + S::kKeys * kTok;                                // [2][token] where its K is
     uint64_t *const bars = reinterpret_cast<uint64_t *>(s_from + 2 * kTok);
     long long *const scratch = reinterpret_cast<long long *>(bars + S::kBars);
-    int *const s_odd = reinterpret_cast<int *>(scratch + kThreads / 32 + 2);  // [stage] a row whose lse is -inf
+    int *const s_odd = reinterpret_cast<int *>(scratch + kThreads / 32 + 2);  // [stage] a row whose lse is infinite
     int &s_dead = s_odd[S::kLess];
     uint32_t &s_tmem = *reinterpret_cast<uint32_t *>(s_odd + S::kLess + 1);
     uint32_t &s_sent = *reinterpret_cast<uint32_t *>(s_odd + S::kLess + 2);  // tiles of Q, and of K, that the copy engine was asked for
@@ -611,9 +611,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_weigh_chunk(const __grid_consta
             float less[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                odd |= now[k] == -INFINITY;  // (a row that saw nothing adds nothing)
-                // (a column of no row: not by an infinite lse, whose two products need not have the same sign)
-                less[k] = lane * 4 + k >= some || now[k] == -INFINITY ? -INFINITY : -fmaf(now[k], a.lse_log2, now[k] * a.lse_log2_rest);
+                // (a row that saw nothing adds nothing, and one with an lse of +inf, as exp(x - inf); neither they nor a column of no row
+                // go through the two products, which need not have the same sign)
+                const bool none = fabsf(now[k]) == INFINITY;
+                odd |= none;
+                less[k] = lane * 4 + k >= some || none ? -INFINITY : -fmaf(now[k], a.lse_log2, now[k] * a.lse_log2_rest);
             }
             *reinterpret_cast<float4 *>(s_less + ls * kRowTile + lane * 4) = make_float4(less[0], less[1], less[2], less[3]);
             odd = __any_sync(0xffffffffu, odd);

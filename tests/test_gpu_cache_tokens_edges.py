@@ -75,3 +75,23 @@ def test_weigh_infinite_keys(G, D):
     w = c.cache.weigh(c.q, lse, c.batch, w0.clone(), decay=0.5)
     assert c.cache.status() == R().LR_OK
     assert torch.isfinite(want).all() and torch.equal(w, want)
+
+
+@pytest.mark.parametrize("fmt", ["16", "e4m3"])
+@pytest.mark.parametrize("G,D", [(4, 128), (4, 64), (3, 80), (4, 112), (16, 64)])
+def test_rows_of_infinite_lse_add_nothing(fmt, G, D):
+    # exp(x - inf) is zero, whichever sign the rest of log2(e)'s rounding has; single rows, some of a tile, a tile's all
+    for seqs in ([(1, 300), (2, 90)], [(130, 420), (1, 77)]):
+        c = base.Case(seqs, G=G, D=D, fmt=fmt, seed=83)
+        _, lse = c.cache.attend(c.q, c.batch, lse=True)
+        for value in (math.inf, -math.inf):
+            l = lse.clone()
+            l[0], l[-1] = value, value
+            weighed(c, 0.5, lse=l)
+            l[::3] = value
+            weighed(c, 1.0, lse=l)
+            l[:, 1:] = value
+            weighed(c, 0.0, lse=l)
+        mixed = lse.clone()
+        mixed[::2], mixed[1::4] = math.inf, -math.inf
+        weighed(c, 0.5, lse=mixed)
