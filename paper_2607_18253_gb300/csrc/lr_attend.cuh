@@ -308,6 +308,15 @@ __device__ __forceinline__ bool tree_visible(const TreeRow &r, int j, int window
     return i < r.ql && (tree_word(r, i >> 5) >> (i & 31) & 1);
 }
 
+// Whether one of so many rows (query heads of tokens) of a tree sees token j.  What a unit of a tree reads is what a row can see
+// that names nothing, one token more under a window than where every row names itself: a block that is out of range is
+// an error only if a row is there that sees it.
+__device__ __forceinline__ bool tree_rows_see(const AttendLaunch &a, int q0, int row0, int rows, int ql, int kv, int j) {
+    for (int t = quot(row0, a.c.div_g); t <= quot(row0 + rows - 1, a.c.div_g); ++t)
+        if (tree_visible(tree_row(a, q0, t, ql, kv, true), j, a.window, a.sinks)) return true;
+    return false;
+}
+
 // Bytes i and j of w, 8-bit codes, as two bf16 numbers (i in the low half), exactly.  e4m3: sign, four exponent
 // and three mantissa bits moved to their places, then a product with 2^120, the power of two between the
 // biases (subnormal codes are subnormal bf16 numbers first, which the product turns right as well).

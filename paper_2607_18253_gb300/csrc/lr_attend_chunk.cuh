@@ -203,27 +203,40 @@ __device__ __noinline__ void mask_scores(uint32_t ts, int last, int low, int sin
     }
     tm_store_wait();
 }
-// The same for the rows of a tree, whose context and drafted tokens are hidden by different rules.
-__device__ __noinline__ void mask_tree(uint32_t ts, const AttendLaunch &a, int q0, int t, int ql, int kv, int at, int base,
+// Records a block out of range among those of sequence s's tokens j + k, k a bit of `seen` (the others have a scale that is not
+// finite).
+__device__ __noinline__ void report_blocks(const AttendLaunch &a, int s, int j, uint32_t seen) {
+    int place;
+    for (; seen; seen &= seen - 1)
+        if (block_of(a.c, a.b, s, j + __ffs(seen) - 1, place) < 0) {
+            report(a.c.status, kEInval);
+            break;
+        }
+    __syncwarp();
+}
+// The same for the rows of a tree, whose context and drafted tokens are hidden by different rules.  A block out of range is
+// recorded here, where a row sees it: what is looked up is what a row can see that names nothing.
+__device__ __noinline__ void mask_tree(uint32_t ts, const AttendLaunch &a, int s, int q0, int t, int ql, int kv, int at, int base,
                                        const uint32_t *kbad) {
     const TreeRow row = tree_row_at(a, q0, t, ql, kv, at);
 #pragma unroll 1
     for (int k0 = 0; k0 < kTok; k0 += 32) {
         const uint32_t see = tree_sees(row, base + k0, a.window, a.sinks), nan = kbad ? kbad[k0 / 32] : 0u;
         if (__all_sync(0xffffffffu, see == ~0u && nan == 0u)) continue;
-        float s[32];
-        tm_load(s, ts + k0);
-        tm_load_wait(s);
+        if (nan) report_blocks(a, s, base + k0, see & nan);
+        float x[32];
+        tm_load(x, ts + k0);
+        tm_load_wait(x);
         if (nan) {
 #pragma unroll
             for (int k = 0; k < 32; ++k)
-                if (nan >> k & 1) s[k] = __uint_as_float(0x7fffffffu);
+                if (nan >> k & 1) x[k] = __uint_as_float(0x7fffffffu);
         }
 #pragma unroll
         for (int k = 0; k < 32; ++k)
-            if (!(see >> k & 1)) s[k] = -INFINITY;
-        tm_store(ts + k0, reinterpret_cast<uint32_t *>(s));
-        tm_store(ts + k0 + 16, reinterpret_cast<uint32_t *>(s) + 16);
+            if (!(see >> k & 1)) x[k] = -INFINITY;
+        tm_store(ts + k0, reinterpret_cast<uint32_t *>(x));
+        tm_store(ts + k0 + 16, reinterpret_cast<uint32_t *>(x) + 16);
     }
     tm_store_wait();
 }
@@ -457,7 +470,7 @@ __global__ void __launch_bounds__(Shape<DP, FMT, LOAD, TREE>::kThreads, 1) k_att
                 after_sync();
                 const int flags = *const_cast<volatile int *>(s_bad + slot);
                 if (TREE && (masked || (flags & 1)))
-                    mask_tree(ts, a, u.q0, t, u.ql, u.kv, pos, base, flags & 1 ? s_kbad + slot * 4 : nullptr);
+                    mask_tree(ts, a, u.s, u.q0, t, u.ql, u.kv, pos, base, flags & 1 ? s_kbad + slot * 4 : nullptr);
                 else if (masked || (flags & 1))
                     mask_scores(ts, pos - base, a.window > 0 ? pos - a.window - base : -1, a.sinks - base,
                                 flags & 1 ? s_kbad + slot * 4 : nullptr);
@@ -688,7 +701,7 @@ __global__ void __launch_bounds__(Shape<DP, FMT, LOAD, TREE>::kThreads, 1) k_att
             const int64_t blk = block_of(c, a.b, p.u.s, t, place);
             if (blk < 0) {
                 f.bad = true;
-                report(c.status, kEInval);
+                if constexpr (!TREE) report(c.status, kEInval);  // (mask_tree does)
                 return f;
             }
             f.off = blk * c.sb + place * c.st + p.u.h * c.sh;
@@ -853,7 +866,7 @@ __global__ void __launch_bounds__(Shape<DP, FMT, LOAD, TREE>::kThreads, 1) k_att
                 const int blk = (int)block_of(c, a.b, cu.u.s, t, place);
                 if (blk < 0) {
                     bad = true;
-                    report(c.status, kEInval);
+                    if constexpr (!TREE) report(c.status, kEInval);  // (mask_tree does)
                 }
                 return blk;
             };

@@ -151,6 +151,10 @@ __device__ __noinline__ void join_parts(const AttendLaunch &a, int c0, int parts
     }
 }
 
+// (a.tree: records what a token's block out of range is to a row that sees it)
+__device__ __noinline__ void report_tree(const AttendLaunch &a, int q0, int row0, int rows, int ql, int kv, int t) {
+    if (tree_rows_see(a, q0, row0, rows, ql, kv, t)) report(a.c.status, kEInval);
+}
 // Whether token t of a unit has a block out of range.
 __device__ __forceinline__ bool no_block(const AttendLaunch &a, const Unit &u, int t) {
     int place;
@@ -219,7 +223,9 @@ __global__ void __launch_bounds__(kThreads, Solo<DP, FMT, NR>::kCtas) k_attend_s
         const unsigned have = __ballot_sync(0xffffffffu, there);  // a bit a token
         if (__any_sync(0xffffffffu, mine && !there)) {
             if constexpr (FMT == kFmt16) bad_tiles |= 1u << (tile & 31);
-            report(c.status, kEInval);
+            if constexpr (!TREE) report(c.status, kEInval);
+            else if (mine && !there) report_tree(a, lk.u.q0, lk.u.qt * kRows, lk.u.rows, lk.u.ql, lk.u.kv, t0 + lane);
+            if constexpr (TREE) __syncwarp();
         }
         if (even) {
 #pragma unroll

@@ -10,8 +10,8 @@ import pytest
 torch = pytest.importorskip("torch")
 
 import test_gpu_cache as base  # noqa: E402
-from test_gpu_cache import R, SEQS, _built  # noqa: E402,F401
-from test_gpu_cache_tokens import expected, weights_of  # noqa: E402
+from test_gpu_cache import C, R, SEQS, _built  # noqa: E402,F401
+from test_gpu_cache_tokens import Tree, expected, weights_of  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -95,3 +95,54 @@ def test_rows_of_infinite_lse_add_nothing(fmt, G, D):
         mixed = lse.clone()
         mixed[::2], mixed[1::4] = math.inf, -math.inf
         weighed(c, 0.5, lse=mixed)
+
+
+# ---------------------------------------------------------------------------------------------
+# trees under a window: blocks that no row reads any more
+
+def gone(c, window, sinks):
+    """A block table without the blocks whose tokens no row of a chain or tree that names itself sees: those at or below context - window."""
+    table = c.table.clone()
+    for s, (ql, kv) in enumerate(c.seqs):
+        lowest = kv - ql - window + 1  # the root's first token
+        for i in range(max(0, lowest) // c.b):
+            if i * c.b >= sinks:
+                table[s, i] = -1
+    return table
+
+
+@pytest.mark.parametrize("fmt,b", [("16", 16), ("16", 5), ("16", 1), ("e4m3", 16), ("int8", 7)])
+@pytest.mark.parametrize("sinks", [0, 4])
+def test_tree_blocks_behind_the_window_may_be_gone(fmt, b, sinks):
+    # contexts whose last hidden token ends a block, and others; few rows, many, and a unit of several CTAs
+    for seqs, G in (([(4, 4 + 96), (1, 1 + 111), (2, 2 + 64), (3, 200)], 2), ([(40, 40 + 320), (64, 64 + 35), (7, 7 + 175)], 4),
+                    ([(16, 16 + 40000)], 4)):
+        for window in (32, 35):
+            c = Tree(seqs, G=G, b=b, fmt=fmt, seed=84)
+            want, wl = c.cache.attend(c.q, c.batch, window=window, sinks=sinks, lse=True, tree=c.tree)
+            assert c.cache.status() == R().LR_OK
+            batch = C().CacheBatch(c.q_start, c.kv_len, gone(c, window, sinks), max(q for q, _ in seqs))
+            out, lse = c.cache.attend(c.q, batch, window=window, sinks=sinks, lse=True, tree=c.tree)
+            assert c.cache.status() == R().LR_OK, window
+            assert torch.isfinite(want).all() and torch.equal(out, want) and torch.equal(lse, wl)
+
+
+@pytest.mark.parametrize("fmt,b", [("16", 16), ("16", 5), ("e4m3", 16), ("int8", 7)])
+@pytest.mark.parametrize("q,G", [(4, 2), (40, 4)])
+def test_tree_rows_that_read_a_block_that_is_gone(fmt, b, q, G):
+    # a row that names nothing stands at the context's last position and sees one token more than the others: where its block is gone,
+    # that row alone is NaN, and the error recorded
+    window = 32
+    c = Tree([(q, q + window + 3 * b - 1), (q, q + 200)], G=G, b=b, fmt=fmt, seed=85)
+    table = c.table.clone()
+    table[0, :3] = c.nb  # tokens below context - window + 1
+    batch = C().CacheBatch(c.q_start, c.kv_len, table, q)
+    want, _ = c.cache.attend(c.q, c.batch, window=window, tree=c.tree)
+    out, _ = c.cache.attend(c.q, batch, window=window, tree=c.tree)
+    assert c.cache.status() == R().LR_OK and torch.equal(out, want)
+    masks = c.tree.clone()
+    masks[1] = 0
+    out, _ = c.cache.attend(c.q, batch, window=window, tree=masks)
+    assert c.cache.status() == R().LR_EINVAL and c.cache.status() == R().LR_OK
+    assert torch.isnan(out[1]).all()
+    assert torch.equal(torch.cat([out[:1], out[2:]]), torch.cat([want[:1], want[2:]]))
