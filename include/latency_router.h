@@ -550,7 +550,7 @@ LR_API int lr_cache_weigh(lr_cache *c, const lr_cache_batch *b, int32_t T, const
  * last `recent`, and of the rest those with the largest weights, ties to the lowest position.  (A budget below sinks + recent
  * takes the first of those.)  NaN counts as larger than all numbers.
  * kept: [num_seqs][num_kv_heads][cap], positions in ascending order, -1 from count[s] on; count: [num_seqs].
- * budget: [num_seqs], each in [0, cap], or NULL: cap.  sinks, recent >= 0, together at most cap.  q_start is not used.
+ * budget: [num_seqs], each in [0, cap], or NULL: cap.  sinks, recent >= 0, together at most cap.  q_start is not used, and may be NULL.
  * num_seqs * num_kv_heads is at most 2^26.
  * Device errors, each LR_EINVAL: a sequence whose kv_len or budget is out of range keeps nothing (count 0); a token
  * whose block is out of range has the lowest weight. */
@@ -563,7 +563,7 @@ LR_API int lr_cache_select(lr_cache *c, const lr_cache_batch *b, const float *we
  * sequence has count tokens; after a tree was verified, the accepted path moves up behind its context (start).
  * kept: [num_seqs][kept_heads][cap], kept_heads num_kv_heads or 1 (one list for all heads); each list ascends from
  * start on: start <= kept[0] < kept[1] < ... < kv_len.  Entries from count on are not read.  start: [num_seqs], or NULL: 0.
- * q_start is not used.  Places from start + count on keep what they hold.  No block that is written to may be another
+ * q_start is not used, and may be NULL.  Places from start + count on keep what they hold.  No block that is written to may be another
  * sequence's of the batch, or the same sequence's twice.
  * Device errors, each LR_EINVAL: a sequence whose kv_len, count (over cap) or start (start + count over kv_len) is out of range is left as it is;
  * an entry that does not ascend, lies below its place or past kv_len, or whose block or whose place's block is out of

@@ -45,12 +45,12 @@ inline bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 1
 // Strides (elements of `size` bytes) that keep every vector 16-byte aligned.
 inline bool good_stride(int64_t s, int size) { return s >= 0 && s < (1ll << 56) && s * size % 16 == 0; }
 
-// The checks that the calls share; 0 if the batch may be launched.
-inline const char *bad_batch(const lr_cache_batch *b, int32_t T) {
+// The checks that the calls share; 0 if the batch may be launched.  (rows: the call uses q_start)
+inline const char *bad_batch(const lr_cache_batch *b, int32_t T, bool rows = true) {
     if (!b) return "null batch";
     if (T < 0) return "T < 0";
     if (b->num_seqs < 0) return "num_seqs < 0";
-    if (b->num_seqs > 0 && (!b->q_start || !b->kv_len || !b->block_table)) return "null batch array";
+    if (b->num_seqs > 0 && ((rows && !b->q_start) || !b->kv_len || !b->block_table)) return "null batch array";
     if (b->max_q < 1) return "max_q < 1";
     if (b->max_blocks < 0 || b->table_stride < b->max_blocks) return "table_stride below max_blocks";
     return nullptr;

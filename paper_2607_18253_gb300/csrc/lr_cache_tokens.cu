@@ -74,7 +74,7 @@ int lr_cache_select(lr_cache *c, const lr_cache_batch *b, const float *weights, 
                     int32_t *count, void *stream) {
     if (!c) return LR_EINVAL;
     c->err.clear();
-    if (const char *m = bad_batch(b, 0)) return fail(c, LR_EINVAL, m);
+    if (const char *m = bad_batch(b, 0, false)) return fail(c, LR_EINVAL, m);
     if (b->num_seqs > c->cfg.max_seqs) return fail(c, LR_ECAPACITY, "num_seqs exceeds max_seqs");
     if (const char *m = bad_lists(c, b, cap)) return fail(c, LR_EINVAL, m);
     if (sinks < 0 || recent < 0 || (long long)sinks + recent > cap) return fail(c, LR_EINVAL, "sinks and recent must not be negative, and fit into cap");
@@ -103,7 +103,7 @@ int lr_cache_keep(lr_cache *c, const lr_cache_batch *b, int32_t cap, const int32
                   const int32_t *start, float *weights, int64_t block_stride, int64_t token_stride, int64_t head_stride, void *stream) {
     if (!c) return LR_EINVAL;
     c->err.clear();
-    if (const char *m = bad_batch(b, 0)) return fail(c, LR_EINVAL, m);
+    if (const char *m = bad_batch(b, 0, false)) return fail(c, LR_EINVAL, m);
     if (b->num_seqs > c->cfg.max_seqs) return fail(c, LR_ECAPACITY, "num_seqs exceeds max_seqs");
     if (const char *m = bad_lists(c, b, cap)) return fail(c, LR_EINVAL, m);
     if (kept_heads != 1 && kept_heads != c->cfg.num_kv_heads) return fail(c, LR_EINVAL, "kept_heads must be 1 or num_kv_heads");

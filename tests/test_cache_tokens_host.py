@@ -121,3 +121,15 @@ def test_more_drafted_tokens_than_mask_bits(lib, cache):
     assert call(lib, cache, "tree", batch(max_q=65)) != 0
     assert b"tree_words" in lib.lr_cache_last_error(cache)
     assert call(lib, cache, "tree", batch(max_q=65), words=3) == 0
+
+
+@pytest.mark.parametrize("name", list(FN))
+def test_a_batch_without_q_start(lib, cache, name):
+    # the choice and the move do not use it
+    from paper_2607_18253_gb300 import router as R
+    b = ctypes.byref(R._CacheBatch(1, 64, None, 16, 16, 4, 4))
+    before = lib.fake_launched()
+    assert call(lib, cache, name, b) == (R.LR_OK if name in ("select", "keep") else R.LR_EINVAL)
+    assert lib.fake_launched() == before + (name in ("select", "keep"))
+    for bad in (R._CacheBatch(1, 64, None, None, 16, 4, 4), R._CacheBatch(1, 64, None, 16, None, 4, 4)):
+        assert call(lib, cache, name, ctypes.byref(bad)) == R.LR_EINVAL
