@@ -1,6 +1,7 @@
 // Host side of the calls on which tokens a paged cache keeps: the weight that they have received, the choice, the move.
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 
 #include "lr_cache_host.cuh"
 
@@ -14,6 +15,13 @@ const char *bad_weights(const void *w, int64_t block, int64_t token, int64_t hea
     auto good = [](int64_t s) { return s >= 0 && s < (1ll << 56); };
     if (!good(block) || !good(token) || !good(head)) return "strides of weights must be non-negative";
     return nullptr;
+}
+
+// (lists of int32; null where there is none)
+bool aligned4(std::initializer_list<const void *> lists) {
+    for (const void *p : lists)
+        if (reinterpret_cast<uintptr_t>(p) % 4) return false;
+    return true;
 }
 
 const char *bad_lists(const lr_cache *c, const lr_cache_batch *b, int32_t cap) {
@@ -81,6 +89,7 @@ int lr_cache_select(lr_cache *c, const lr_cache_batch *b, const float *weights, 
     if (b->num_seqs == 0) return LR_OK;
     if (const char *m = bad_weights(weights, block_stride, token_stride, head_stride)) return fail(c, LR_EINVAL, m);
     if (!count || (cap > 0 && !kept)) return fail(c, LR_EINVAL, "null kept or count");
+    if (!aligned4({kept, count, budget})) return fail(c, LR_EINVAL, "kept, count and budget must be 4-byte aligned");
     SelectLaunch a;
     std::memset(&a, 0, sizeof(a));
     a.c = c->dev;
@@ -111,6 +120,7 @@ int lr_cache_keep(lr_cache *c, const lr_cache_batch *b, int32_t cap, const int32
         if (const char *m = bad_weights(weights, block_stride, token_stride, head_stride)) return fail(c, LR_EINVAL, m);
     if (b->num_seqs == 0 || cap == 0) return LR_OK;
     if (!kept || !count) return fail(c, LR_EINVAL, "null kept or count");
+    if (!aligned4({kept, count, start})) return fail(c, LR_EINVAL, "kept, count and start must be 4-byte aligned");
     KeepLaunch a;
     std::memset(&a, 0, sizeof(a));
     a.c = c->dev;

@@ -133,3 +133,13 @@ def test_a_batch_without_q_start(lib, cache, name):
     assert lib.fake_launched() == before + (name in ("select", "keep"))
     for bad in (R._CacheBatch(1, 64, None, None, 16, 4, 4), R._CacheBatch(1, 64, None, 16, None, 4, 4)):
         assert call(lib, cache, name, ctypes.byref(bad)) == R.LR_EINVAL
+
+
+@pytest.mark.parametrize("name,kw", [("select", dict(kept=18)), ("select", dict(count=17)), ("select", dict(budget=6)), ("keep", dict(kept=18)),
+                                     ("keep", dict(count=17)), ("keep", dict(start=6))])
+def test_lists_that_are_not_aligned_are_refused(lib, cache, name, kw):
+    # (a kernel that read them would fault)
+    from paper_2607_18253_gb300 import router as R
+    before = lib.fake_launched()
+    assert call(lib, cache, name, **kw) == R.LR_EINVAL
+    assert b"aligned" in lib.lr_cache_last_error(cache) and lib.fake_launched() == before
