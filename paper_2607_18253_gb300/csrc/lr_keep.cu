@@ -4,13 +4,15 @@
 // So a batch of tokens may be written once it and all before it are read, and a later batch is read from places that no
 // earlier one writes.  The order holds within a (sequence, KV head) and for each part of a token by itself: K, V, pieces of
 // vectors.  A list, or each such part of it where lists are few, is moved by a cluster of CTAs that read a batch, meet,
-// and write it, with no other wait.
+// and write it, with no other wait.  The meeting orders memory: what is read before it is read before what is written behind it.
 //
 // What bounds it is the bytes moved, and for short lists the chain list -> block table -> vectors.  Of a long list the chain
 // is taken for 512 tokens at once and left in shared memory, with their scales and weights; the vectors then
-// follow batch after batch, the next one's read before the last one's is written.
-// Measured: 512 lists of 2,048 tokens (int8, heads of 128, with scales and weights: 480 MB moved) 100 us, 4.8 TB/s; four lists of 20,000
-// tokens in 16 bits 26 us, 3.1 TB/s; 2,048 lists of up to 16 tokens 9 us (13 with cold caches).
+// follow batch after batch.  A CTA by itself reads the next one before it writes the last one.  A cluster's meeting also waits for the
+// writes of the batch before, so it takes batches of twice as much, and the next one's reads run beside those writes (two vectors a thread,
+// read ahead as a CTA does: 38 us where four take 34; a meeting that orders no memory, and leaves it to the use of what was read: 32).
+// Measured, caches cold: 512 lists of 2,048 tokens (int8, heads of 128, with scales and weights: 480 MB moved) 112 us, 4.3 TB/s; four
+// lists of 20,000 tokens in 16 bits 34 us; 2,048 lists of up to 16 tokens 13 us.
 #include <algorithm>
 
 #include "lr_cache.cuh"
@@ -19,12 +21,15 @@ namespace lr {
 
 namespace {
 
-constexpr int kThreads = 256, kItems = 2, kMaxCluster = 16;
+constexpr int kThreads = 256, kMaxCluster = 16;
 constexpr int kAhead = 2, kRun = kThreads * kAhead;  // tokens of a CTA that are looked up together
+
+// Vectors of a batch that a thread moves, where a CTA has both of K and V, or a cluster one of them.
+__host__ __device__ constexpr int items(bool both) { return both ? 2 : 4; }
 
 template <int LANES, bool BOTH>
 __global__ void __launch_bounds__(kThreads, 4) k_keep(const __grid_constant__ KeepLaunch a) {
-    constexpr int kLanes = LANES * (BOTH ? 2 : 1);
+    constexpr int kLanes = LANES * (BOTH ? 2 : 1), kItems = items(BOTH), kHeld = BOTH ? 2 : 1;
     __shared__ int4 s_move[kRun];  // block and place of a token, and of where it goes; -1: not moved
     const CacheDev &c = a.c;
     const int tid = threadIdx.x, lane = tid % LANES, cl = a.cluster;
@@ -52,15 +57,10 @@ __global__ void __launch_bounds__(kThreads, 4) k_keep(const __grid_constant__ Ke
     auto scale_at = [&](int blk, int place) { return (int64_t)blk * c.ssb + place * c.sst + h * c.ssh; };
     auto weight_at = [&](int blk, int place) { return (int64_t)blk * a.wb + place * a.wt + h * a.wh; };
     // The cluster has read what it was to read before it writes.  (Later reads need not wait for these writes: nothing
-    // that is read later is written before.)  `seen`: of a value read; it has come when it goes into the CTA's barrier, so that the
-    // cluster's need not order memory, which would wait for the last batch's writes.
-    auto meet = [&](uint32_t seen) {
-        if (cl > 1) {
-            __syncthreads_or(seen == 0x5bd1e995u);
-            asm volatile("barrier.cluster.arrive.relaxed.aligned;\n barrier.cluster.wait.aligned;" ::: "memory");
-        } else {
-            __syncthreads();
-        }
+    // that is read later is written before.)
+    auto meet = [&]() {
+        if (cl > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        else __syncthreads();
     };
     const int run = min(kRun, threads * kAhead) / batch * batch;  // of this CTA; the cluster's CTAs take batches in turn
     for (int64_t r0 = 0; r0 < count; r0 += (int64_t)cl * run) {
@@ -101,14 +101,7 @@ __global__ void __launch_bounds__(kThreads, 4) k_keep(const __grid_constant__ Ke
             if (m[u].x >= 0 && c.ks && v_too) vs[u] = c.vs[scale_at(m[u].x, m[u].y)];
             if (m[u].x >= 0 && a.w && k_too) w[u] = a.w[weight_at(m[u].x, m[u].y)];
         }
-        uint32_t seen = 0;
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            if (m[u].x >= 0 && c.ks && k_too) seen |= __float_as_uint(ks[u]);
-            if (m[u].x >= 0 && c.ks && v_too) seen |= __float_as_uint(vs[u]);
-            if (m[u].x >= 0 && a.w && k_too) seen |= __float_as_uint(w[u]);
-        }
-        meet(seen);
+        meet();
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             if (m[u].x >= 0 && c.ks && k_too) c.ks[scale_at(m[u].z, m[u].w)] = ks[u];
@@ -117,8 +110,8 @@ __global__ void __launch_bounds__(kThreads, 4) k_keep(const __grid_constant__ Ke
         }
         // the cluster's batches of the run: as many for each of its CTAs, though the last may have none of their tokens
         const int batches = (int)min((int64_t)(run / batch), (count - r0 + (int64_t)cl * batch - 1) / ((int64_t)cl * batch));
-        uint4 v[2][kItems];
-        char *to[2][kItems];
+        uint4 v[kHeld][kItems];
+        char *to[kHeld][kItems];
         auto read = [&](int n, uint4 (&v)[kItems], char *(&to)[kItems]) {
 #pragma unroll
             for (int u = 0; u < kItems; ++u) {
@@ -132,23 +125,24 @@ __global__ void __launch_bounds__(kThreads, 4) k_keep(const __grid_constant__ Ke
             for (int u = 0; u < kItems; ++u)
                 if (to[u]) *reinterpret_cast<uint4 *>(to[u]) = v[u];
         };
-        auto all = [&](uint4 (&v)[kItems], char *(&to)[kItems]) {
-            uint32_t x = 0;
-#pragma unroll
-            for (int u = 0; u < kItems; ++u)
-                if (to[u]) x |= v[u].x;
-            return x;
-        };
-        // (a batch is written after a meeting that all CTAs come to when they have read the batch behind it)
-        read(0, v[0], to[0]);
-        for (int n = 0; n < batches; n += 2) {
-            if (n + 1 < batches) read(n + 1, v[1], to[1]);
-            meet(all(v[0], to[0]));
-            write(v[0], to[0]);
-            if (n + 1 >= batches) break;
-            if (n + 2 < batches) read(n + 2, v[0], to[0]);
-            meet(all(v[1], to[1]));
-            write(v[1], to[1]);
+        if constexpr (BOTH) {
+            // (a batch is written after a meeting that all threads come to when they have read the batch behind it)
+            read(0, v[0], to[0]);
+            for (int n = 0; n < batches; n += 2) {
+                if (n + 1 < batches) read(n + 1, v[1], to[1]);
+                meet();
+                write(v[0], to[0]);
+                if (n + 1 >= batches) break;
+                if (n + 2 < batches) read(n + 2, v[0], to[0]);
+                meet();
+                write(v[1], to[1]);
+            }
+        } else {
+            for (int n = 0; n < batches; ++n) {
+                read(n, v[0], to[0]);
+                meet();
+                write(v[0], to[0]);
+            }
         }
         if (r0 + (int64_t)cl * run < count) __syncthreads();
     }
@@ -178,7 +172,7 @@ cudaError_t launch_keep(const KeepLaunch &a, int fmt, int sms, cudaStream_t st) 
     const int threads = (int)std::min<long long>(kThreads, std::max<long long>(32, ((long long)a.cap * kl / 4 + 31) / 32 * 32));
     l.cluster = 1;
     if (!both) {
-        auto batch = [&](int ln) { return (long long)threads / ln * kItems; };
+        auto batch = [&](int ln) { return (long long)threads / ln * items(false); };
         auto pieces = [&](int ln) { return (l.vector + ln * 16 - 1) / (ln * 16); };
         while (l.cluster < kMaxCluster && lists * 4 * l.cluster <= room && a.cap > batch(lanes) * l.cluster) l.cluster *= 2;
         while (lanes > 4 && lists * 2 * l.cluster * pieces(lanes / 2) <= room && a.cap > batch(lanes) * l.cluster) lanes /= 2;
