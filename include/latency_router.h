@@ -538,6 +538,8 @@ LR_API int lr_cache_attend_tree(lr_cache *c, const lr_cache_batch *b, int32_t T,
  * else all of the sequence's tokens are written, so that all its blocks must be its own.  A sequence that brings no
  * tokens is left as it is; a row whose lse is -inf (it saw nothing) or +inf adds nothing.
  * A token whose block several sequences of the batch share (a common prefix) has no defined weight.
+ * Rows are causal.  Of a verified tree, the rows of the accepted path are, once lr_cache_keep has moved it up: their queries
+ * and the lse that lr_cache_attend_tree gave them, gathered in the path's order, weigh the sequence as its last tokens.
  * Sums are fp32, in an order that the call's sizes alone decide: the same call gives the same bits.  Over 8-bit
  * caches scores are formed as in lr_cache_attend.  lse: [T][num_q_heads] fp32.
  * Device errors, each LR_EINVAL: a sequence that lr_cache_attend leaves out is left out; a token that a row sees and whose block

@@ -10,7 +10,9 @@
 // blocks are looked up while these are multiplied; their reads are other warps' to hide.
 // Measured (64 single tokens over 128 to 8,192, 32 query heads on 8 KV heads of 128, e4m3): 50 us, 2.75 TB/s.  DRAM is a third busy and
 // the issue slots 40%: what bounds it is a warp's own chain of conversions and dependent steps.  Vectors asked for a tile ahead (to
-// the L2 cache) 54 us, five CTAs an SM, which spill, 68, heads in turn instead of tiles (queries loaded anew each) 83.
+// the L2 cache) 54 us, five CTAs an SM, which spill, 68, heads in turn instead of tiles (queries loaded anew each) 83.  Over 16 bits, with
+// nothing to convert, five CTAs do not spill (caches cold: 69 us, 3.8 TB/s, where four take 75; 256 sequences 139 and 157; one token over
+// 60,000 42 and 46).
 #include <algorithm>
 
 #include "lr_attend.cuh"

@@ -1,10 +1,12 @@
-"""Weights of cached tokens where the kernels' tiles have columns of no row, in a comparison that a NaN fails.
+"""Trees and weights of cached tokens where their kernels can go wrong: tiles with columns of no row, infinities in lse and K, blocks
+behind a window that are gone, groups of more heads than a tile has rows, an accepted path that is weighed.
 
-The reference and the bound are those of test_gpu_cache_tokens.py: |w - want| <= tol in 64 bits, and places that no call
+A weight's comparison fails for a NaN.  The reference and the bound are those of test_gpu_cache_tokens.py: |w - want| <= tol in 64 bits, and places that no call
 writes equal to the last bit (their bound is zero).
 """
 import math
 
+import numpy as np
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -146,3 +148,64 @@ def test_tree_rows_that_read_a_block_that_is_gone(fmt, b, q, G):
     assert c.cache.status() == R().LR_EINVAL and c.cache.status() == R().LR_OK
     assert torch.isnan(out[1]).all()
     assert torch.equal(torch.cat([out[:1], out[2:]]), torch.cat([want[:1], want[2:]]))
+
+
+# ---------------------------------------------------------------------------------------------
+# calls together, and the widest groups
+
+@pytest.mark.parametrize("fmt", ["16", "e4m3", "int8"])
+@pytest.mark.parametrize("G,D", [(65, 64), (130, 16), (256, 64), (1024, 16)])
+def test_groups_of_more_heads_than_a_tile_has_rows(fmt, G, D):
+    for seqs in ([(1, 300), (2, 40)], [(5, 290), (1, 1), (3, 3)]):
+        c = Tree(seqs, H=1, G=G, D=D, fmt=fmt, seed=86)
+        c.check()
+        c.check(window=33, sinks=2)
+        for decay, window in ((1.0, 0), (0.5, 40)):
+            weighed(base.Case(seqs, H=1, G=G, D=D, fmt=fmt, seed=87), decay, window, 2)
+
+
+@pytest.mark.parametrize("fmt", ["16", "e4m3", "int8"])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (37, 3)])
+def test_a_chain_is_the_causal_call(fmt, window, sinks):
+    # within the causal reference's own bounds, over 8 bits as well
+    for seqs in ([(4, 40), (16, 16), (1, 33)], [(70, 900), (33, 161)]):
+        c = Tree(seqs, fmt=fmt, seed=88)
+        rows = [np.packbits(np.tril(np.ones((q, c.words * 32), bool)), axis=1, bitorder="little").view(np.int32) for q, _ in seqs]
+        chain = torch.from_numpy(np.concatenate(rows)).cuda()
+        want, wl, tol, ltol = base.Case.reference(c, None, window, sinks)
+        out, lse = c.cache.attend(c.q, c.batch, window=window, sinks=sinks, lse=True, tree=chain)
+        assert c.cache.status() == R().LR_OK
+        assert bool(((out.double() - want).abs() <= tol).all()) and bool(((lse.double() - wl).abs() <= ltol).all())
+
+
+@pytest.mark.parametrize("fmt", ["16", "int8"])
+@pytest.mark.parametrize("seqs,G", [([(8, 100), (5, 37), (16, 16)], 2), ([(64, 300), (40, 90)], 3)])
+def test_an_accepted_path_is_weighed(fmt, seqs, G):
+    # a tree is verified and its deepest path moved up; the path's rows, gathered with the lse that the tree's attention gave, are
+    # then the sequence's last causal ones
+    c = Tree(seqs, H=2, G=G, D=64, fmt=fmt, seed=89)
+    _, lse = c.check()
+    lse = lse.float()
+    rows, counts, starts = [], [], []
+    kept = torch.full((len(seqs), max(q for q, _ in seqs)), -1, dtype=torch.int32, device="cuda")
+    for s, (q, kv) in enumerate(seqs):
+        path = torch.nonzero(c.paths[s][int(c.paths[s].sum(1).argmax())]).flatten()
+        kept[s, :len(path)] = (kv - q + path).to(torch.int32)
+        rows.append(int(c.q_start[s]) + path)
+        counts.append(len(path))
+        starts.append(kv - q)
+    rows = torch.cat(rows)
+    w0 = weights_of(c)
+    c.cache.keep(kept, torch.tensor(counts, dtype=torch.int32, device="cuda"), c.batch, weights=w0,
+                 start=torch.tensor(starts, dtype=torch.int32, device="cuda"))
+    d = base.Case.__new__(base.Case)
+    d.__dict__.update({k: v for k, v in c.__dict__.items()})
+    d.seqs, d.T, d.q = [(n, a + n) for n, a in zip(counts, starts)], len(rows), c.q[rows].contiguous()
+    d.q_start = torch.tensor([0] + list(np.cumsum(counts)), dtype=torch.int32, device="cuda")
+    d.kv_len = torch.tensor([a + n for n, a in zip(counts, starts)], dtype=torch.int32, device="cuda")
+    d.batch = C().CacheBatch(d.q_start, d.kv_len, d.table, max(counts))
+    w = d.cache.weigh(d.q, lse[rows].contiguous(), d.batch, w0.clone(), decay=0.5)
+    assert d.cache.status() == R().LR_OK
+    want, tol = expected(d, lse[rows], w0, 0.5)
+    assert bool(((w.double() - want).abs() <= tol).all())
+    d.check()
