@@ -262,20 +262,25 @@ __global__ void __launch_bounds__(kThreads, 1) k_weigh_chunk(const __grid_consta
         const int half = warp / 4, t = tid % kTok;
         const uint32_t ts = tm + half * 256 + ((uint32_t)(warp % 4) << 21);
         uint32_t n_s = 0;  // the half's scores so far
+        bool skipped = false;  // the last unit had none of the half's tokens
         for (;; l.next(a, sh)) {
             const int halves = l.halves(), p = l.base() + half * kTok + t;
             const bool on = half < halves, whole = l.whole();
             float f = 0.0f, old = 0.0f;
             int64_t to = -1;
             if (on) {
+                // A half that skipped units waited for their rows alone, and may have come here two phases ahead of this stage's barrier, whose
+                // parity does not tell them apart.  Its scores of the unit come after their K, and all K before it.
+                if (skipped) ok = bar_wait(s_full + 16 * half + 8 * (n_s & 1), n_s >> 1 & 1, dead);
                 const uint32_t st = (key + half) % S::kKeys;
-                ok = bar_wait(k_full + 8 * st, (key + half) / S::kKeys & 1, dead);
+                ok = ok && bar_wait(k_full + 8 * st, (key + half) / S::kKeys & 1, dead);
                 if (!ok) break;
                 f = s_scale[st * kTok + t];
                 to = s_to[st * kTok + t];
                 bar_arrive_warp(k_free + 8 * st);
                 if (whole && to >= 0 && a.decay != 0.0f && p < l.lo) old = a.decay * a.w[to];
             }
+            skipped = !on;
             key += halves;
             // the rows that see the token: from the first of its position on, and where a window hides it up to a last
             const int first = p > l.lo ? (int)min((long long)l.rows, (long long)(p - l.lo) * c.G) : 0;

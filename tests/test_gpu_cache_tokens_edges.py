@@ -99,6 +99,20 @@ def test_rows_of_infinite_lse_add_nothing(fmt, G, D):
         weighed(c, 0.5, lse=mixed)
 
 
+@pytest.mark.parametrize("fmt", ["16", "e4m3", "int8"])
+@pytest.mark.parametrize("G,D,b", [(20, 112, 3), (4, 128, 16), (6, 64, 16), (12, 80, 8)])
+def test_weigh_short_sequences_before_long_ones(fmt, G, D, b):
+    # runs of units of at most 128 tokens, which half of a CTA's warps skip, before units of 256, many of each a CTA
+    seqs = [s for i in range(40) for s in [(12, 12 + (7 * i + j) % 110) for j in range(1 + i % 9)] + [(11 + i % 90, 2000 + 331 * i)]]
+    c = base.Case(seqs, H=2, G=G, D=D, b=b, fmt=fmt, seed=90)
+    for decay, window, sinks in ((0.5, 0, 0), (0.5, 1, 16), (1.0, 700, 4)):
+        a = weighed(c, decay, window, sinks)
+        assert torch.equal(a, weighed(c, decay, window, sinks))
+    d = base.Case([(2, 2), (11, 19649), (101, 31713), (2, 16)], H=3, G=G, D=D, b=b, fmt=fmt, seed=91)
+    for decay, window, sinks in ((0.5, 1, 16), (0.0, 0, 0)):
+        weighed(d, decay, window, sinks)
+
+
 # ---------------------------------------------------------------------------------------------
 # trees under a window: blocks that no row reads any more
 
