@@ -9,7 +9,7 @@
 // The batch is one line of (unit, tile of rows), cut into equal shares for the CTAs; a unit that is cut is joined by
 // the last of its CTAs, in their order.  Of few rows (128 or less a KV head) a unit is one tile, and K's bytes bound it.
 //
-// Measured (32 query heads on 8 KV heads of 128, 16 bits): 4,096 rows at the end of 32,768 tokens 880 us, 1,170 TFLOP/s.  A tile (256
+// Measured (32 query heads on 8 KV heads of 128, 16 bits): 4,096 rows at the end of 32,768 tokens 872 us, 1,180 TFLOP/s.  A tile (256
 // tokens x 128 rows) takes 2,140 cycles, of which the products 1,600, where the tensor cores need 1,024: both operands come from shared
 // memory, which also takes Q and gives the rows' lse.  The exponentials are 1,170 cycles beside them.  Slower were K in tensor
 // memory with tiles of 96 rows (965 us), 16 warps of exponentials (939; with K in tensor memory 1,033), and three of eight
